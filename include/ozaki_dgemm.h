@@ -92,7 +92,9 @@ enum {
     OZAKI_STATUS_HIP_ERROR = 4,    /* a HIP runtime call failed; see ozaki_last_hip_error                  */
     OZAKI_STATUS_NONFINITE = 5,    /* reported by ozaki_last_device_status: A or B held an Inf or NaN      */
     OZAKI_STATUS_STATIC_LIMIT = 6, /* ozaki_dgemm_static: the problem needs more than OZAKI_STATIC_SCRATCH_BYTES */
-    OZAKI_STATUS_SLICE_COUNT = 7   /* num_slices is larger than OZAKI_MAX_SLICES                           */
+    OZAKI_STATUS_SLICE_COUNT = 7,  /* num_slices is larger than OZAKI_MAX_SLICES                           */
+    OZAKI_STATUS_TARGET = 8        /* reported by ozaki_last_device_status: a target of ozaki_linear_loss or    */
+                                   /* ozaki_linear_loss_grad was neither a word of the vocabulary nor `ignore`  */
 };
 
 #define OZAKI_MAX_SLICES 32
@@ -333,6 +335,67 @@ int ozaki_pair_products(int64_t m, int64_t n, int64_t k,
  * numbers; out may alias a or b).
  */
 int ozaki_fp64_add_emulated(const double* a, const double* b, double* out, int64_t n);
+
+/* ------------------------------------------------------------------------------------------------
+ * Low-precision operators for training and serving: FP8 with a scale for each block of 128, the product of
+ * matrices in that form, and the cross entropy of a linear layer.
+ *
+ * A matrix of `rows` vectors is given by its first element, the distance ld between the starts of neighbouring vectors
+ * (in elements) and its type; element e of vector i is X[i * ld + e].  (A row-major matrix's rows, or a column-major
+ * one's columns.)  Vectors start at multiples of 16 bytes: pointers and ld * (bytes per element) are multiples of 16,
+ * and the 16 bytes in which a vector ends may be read whole (what lies behind its end has no influence and is not written).
+ * Results D, dH, dW may lie anywhere.  No size is above OZAKI_MAX_EXTENT, no vector longer than that many bytes or further from
+ * its neighbour.  All pointers are DEVICE.
+ * ---------------------------------------------------------------------------------------------- */
+enum { OZAKI_TYPE_F32 = 0, OZAKI_TYPE_BF16 = 1, OZAKI_TYPE_F16 = 2 };
+
+/* Which elements share a scale. */
+enum {
+    OZAKI_SCALE_VECTORS = 0, /* 128 neighbouring elements of a vector (activations, gradients)                   */
+    OZAKI_SCALE_BLOCKS = 1   /* the same 128 elements of 128 neighbouring vectors (weights)                      */
+};
+#define OZAKI_SCALE_BLOCK 128
+#define OZAKI_MAX_EXTENT (1 << 22)
+
+/* Quantises X (rows vectors of k elements of `type`) to OCP E4M3.  For each block, a being the largest finite magnitude in it
+ * and at least 2^-100:
+ *     scale = a / 448        code = E4M3(x * (448 / a)), to nearest, ties to even; NaN where x is not finite.
+ *   Q, ldq    codes of X's vectors, one byte each; may be null (then so is S)
+ *   S, lds    scales, S[(e / 128) * lds + i] for vector i, with OZAKI_SCALE_BLOCKS S[(e / 128) * lds + i / 128]; lds is at least
+ *             the number of vectors or of blocks of vectors
+ *   Qt, St    the same of the transpose of X, whose k vectors have `rows` elements; may be null
+ * One of Q and Qt is there.  One read of X serves both. */
+int ozaki_quantise_fp8(int64_t rows, int64_t k, const void* X, int64_t ldx, int type, int scaling, void* Q, int64_t ldq, float* S,
+                       int64_t lds, void* Qt, int64_t ldqt, float* St, int64_t ldst);
+
+/* D[i * ldd + j] = sum over b of Sa[b * ldsa + i] * Sb[..] * (sum over e of block b of A[i * lda + e] * B[j * ldb + e]), i < m, j < n:
+ * A's vectors with OZAKI_SCALE_VECTORS, B's with `scaling_b`, as ozaki_quantise_fp8 leaves them.  Products and sums in FP32, D of
+ * `type_d`, rounded once; with `accumulate` the sum is added to what D holds.  k == 0 gives zeros.
+ * Where few results leave compute units without work the inner dimension is cut and the shares meet in the context's
+ * workspace: ozaki_gemm_fp8_workspace_bytes, 0 where none is needed.  The cut depends on m, n and k only. */
+int ozaki_gemm_fp8(int64_t m, int64_t n, int64_t k, const void* A, int64_t lda, const float* Sa, int64_t ldsa, const void* B, int64_t ldb,
+                   const float* Sb, int64_t ldsb, int scaling_b, void* D, int64_t ldd, int type_d, int accumulate);
+size_t ozaki_gemm_fp8_workspace_bytes(int64_t m, int64_t n, int64_t k);
+
+/* Softmax cross entropy of the outputs z = H W^T of a linear layer over a vocabulary, which are not kept:
+ *     lse[t] = log(sum over v of exp(z[t][v]))          loss[t] = lse[t] - z[t][targets[t]], 0 where targets[t] == ignore
+ * H: tokens vectors, W: vocab vectors of k elements, both of `type` (BF16 or F16); sums in FP32.  A target that is neither in
+ * 0 .. vocab - 1 nor `ignore` gives a loss of NaN and raises OZAKI_STATUS_TARGET (ozaki_last_device_status).
+ * Needs the context's workspace, ozaki_linear_loss_workspace_bytes(tokens, vocab, k, 0, 0). */
+int ozaki_linear_loss(int64_t tokens, int64_t vocab, int64_t k, const void* H, int64_t ldh, const void* W, int64_t ldw, int type,
+                      const int64_t* targets, int64_t ignore, float* loss, float* lse);
+
+/* Its gradient, from the lse that the call above left and the gradient dloss[t] of whatever was made of the losses:
+ *     g[t][v] = (exp(z[t][v] - lse[t]) - [v == targets[t]]) * dloss[t]      dH = g W      dW = g^T H
+ * in the type of H and W; either result may be null.  Tokens with targets[t] == ignore (or an invalid target, which raises
+ * OZAKI_STATUS_TARGET) have no share: their rows of dH are zeros, and what their rows of H hold does not matter.  g is formed a
+ * piece of the vocabulary at a time, in 16 bits; the piece follows from the workspace, of
+ * ozaki_linear_loss_workspace_bytes(tokens, vocab, k, 1, minimum) bytes: minimum != 0 the least, 0 what is recommended.  With the
+ * recommended size or more the result does not depend on the workspace. */
+int ozaki_linear_loss_grad(int64_t tokens, int64_t vocab, int64_t k, const void* H, int64_t ldh, const void* W, int64_t ldw, int type,
+                           const int64_t* targets, int64_t ignore, const float* lse, const float* dloss, void* dH, int64_t lddh, void* dW,
+                           int64_t lddw);
+size_t ozaki_linear_loss_workspace_bytes(int64_t tokens, int64_t vocab, int64_t k, int grad, int minimum);
 
 #ifdef __cplusplus
 }

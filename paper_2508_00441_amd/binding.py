@@ -25,12 +25,18 @@ ACCUM_EXACT_FIXED = 2
 PAIRS_TRIANGLE, PAIRS_ALL = 0, 1
 SUM_RUNS, SUM_PLAIN = 0, 1
 STATUS_OK, STATUS_INFEASIBLE, STATUS_WORKSPACE, STATUS_HIP_ERROR, STATUS_NONFINITE, STATUS_STATIC_LIMIT, STATUS_SLICE_COUNT = 0, 1, 3, 4, 5, 6, 7
+STATUS_TARGET = 8
 STATIC_SCRATCH_BYTES = 64 << 20
 MAX_SLICES = 32
+TYPE_F32, TYPE_BF16, TYPE_F16 = 0, 1, 2
+SCALE_VECTORS, SCALE_BLOCKS = 0, 1
+SCALE_BLOCK = 128
+MAX_EXTENT = 1 << 22
 
 SLICE_FORMATS = {"fp8": SLICE_FP8_E4M3, "fp16": SLICE_FP16, "fp6": SLICE_FP6_E2M3, "fp6_e3m2": SLICE_FP6_E3M2, "int8": SLICE_INT8}
 ACCUM_MODES = {"hw": ACCUM_FP64_HW, "emu": ACCUM_FP64_INT_EMU, "exact": ACCUM_EXACT_FIXED}
 PAIR_SETS = {"triangle": PAIRS_TRIANGLE, "full": PAIRS_ALL}
+TYPES = {"f32": TYPE_F32, "bf16": TYPE_BF16, "f16": TYPE_F16}
 SUM_RULES = {"runs": SUM_RUNS, "plain": SUM_PLAIN}
 
 #: every symbol include/ozaki_dgemm.h declares: name -> (restype, argtypes)
@@ -61,6 +67,12 @@ SIGNATURES = {
     "ozaki_split": (_int, [_int, _i64, _i64, _vp, _i64, _int, _int, _i64, _vp, _vp]),
     "ozaki_pair_products": (_int, [_i64, _i64, _i64, _vp, _i64, _vp, _i64, _int, _int, _i64, _int, _int, _vp, _vp]),
     "ozaki_fp64_add_emulated": (_int, [_vp, _vp, _vp, _i64]),
+    "ozaki_quantise_fp8": (_int, [_i64, _i64, _vp, _i64, _int, _int, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64]),
+    "ozaki_gemm_fp8": (_int, [_i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _int, _vp, _i64, _int, _int]),
+    "ozaki_gemm_fp8_workspace_bytes": (_sz, [_i64, _i64, _i64]),
+    "ozaki_linear_loss": (_int, [_i64, _i64, _i64, _vp, _i64, _vp, _i64, _int, _vp, _i64, _vp, _vp]),
+    "ozaki_linear_loss_grad": (_int, [_i64, _i64, _i64, _vp, _i64, _vp, _i64, _int, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _i64]),
+    "ozaki_linear_loss_workspace_bytes": (_sz, [_i64, _i64, _i64, _int, _int]),
 }
 
 _lib = None
@@ -224,3 +236,32 @@ def ozaki_pair_products(m, n, k, A, lda, B, ldb, slice_format, num_slices, k_blo
 
 def ozaki_fp64_add_emulated(a, b, out, n) -> None:
     _check(load().ozaki_fp64_add_emulated(_ptr(a), _ptr(b), _ptr(out), n), "ozaki_fp64_add_emulated")
+
+
+def ozaki_quantise_fp8(rows, k, X, ldx, type, scaling, Q, ldq, S, lds, Qt=None, ldqt=0, St=None, ldst=0, check: bool = True) -> int:
+    st = load().ozaki_quantise_fp8(rows, k, _ptr(X), ldx, type, scaling, _ptr(Q), ldq, _ptr(S), lds, _ptr(Qt), ldqt, _ptr(St), ldst)
+    return _check(st, "ozaki_quantise_fp8") if check else st
+
+
+def ozaki_gemm_fp8_workspace_bytes(m, n, k) -> int:
+    return int(load().ozaki_gemm_fp8_workspace_bytes(m, n, k))
+
+
+def ozaki_gemm_fp8(m, n, k, A, lda, Sa, ldsa, B, ldb, Sb, ldsb, scaling_b, D, ldd, type_d, accumulate=0, check: bool = True) -> int:
+    st = load().ozaki_gemm_fp8(m, n, k, _ptr(A), lda, _ptr(Sa), ldsa, _ptr(B), ldb, _ptr(Sb), ldsb, scaling_b, _ptr(D), ldd, type_d, accumulate)
+    return _check(st, "ozaki_gemm_fp8") if check else st
+
+
+def ozaki_linear_loss_workspace_bytes(tokens, vocab, k, grad, minimum) -> int:
+    return int(load().ozaki_linear_loss_workspace_bytes(tokens, vocab, k, 1 if grad else 0, 1 if minimum else 0))
+
+
+def ozaki_linear_loss(tokens, vocab, k, H, ldh, W, ldw, type, targets, ignore, loss, lse, check: bool = True) -> int:
+    st = load().ozaki_linear_loss(tokens, vocab, k, _ptr(H), ldh, _ptr(W), ldw, type, _ptr(targets), ignore, _ptr(loss), _ptr(lse))
+    return _check(st, "ozaki_linear_loss") if check else st
+
+
+def ozaki_linear_loss_grad(tokens, vocab, k, H, ldh, W, ldw, type, targets, ignore, lse, dloss, dH, lddh, dW, lddw, check: bool = True) -> int:
+    st = load().ozaki_linear_loss_grad(tokens, vocab, k, _ptr(H), ldh, _ptr(W), ldw, type, _ptr(targets), ignore, _ptr(lse), _ptr(dloss),
+                                       _ptr(dH), lddh, _ptr(dW), lddw)
+    return _check(st, "ozaki_linear_loss_grad") if check else st

@@ -5,12 +5,15 @@
 #include <new>
 #include <vector>
 
+#include "low_precision.hpp"
 #include "plan.hpp"
 
 using namespace ozaki;
 
 static_assert(OZAKI_MAX_SLICES == MAX_SLICES, "header and implementation disagree");
 static_assert(OZAKI_SLICE_INT8 == FMT_INT8 && OZAKI_ACCUM_EXACT_FIXED == ACC_EXACT && OZAKI_SUM_PLAIN == SUM_PLAIN,
+              "header and implementation disagree");
+static_assert(OZAKI_TYPE_F16 == TYPE_F16 && OZAKI_SCALE_BLOCKS == SCALE_BLOCKS && OZAKI_SCALE_BLOCK == SCALE_BLOCK && OZAKI_MAX_EXTENT == MAX_VECTOR_BYTES,
               "header and implementation disagree");
 
 // A context: everything a call needs beyond its arguments.
@@ -221,6 +224,29 @@ int dgemm_panels(const Plan& whole, const double* A, int64_t lda, const double* 
 
 WorkMem context_workspace() { return WorkMem{ctx().ws, ctx().ws_bytes}; }
 
+// ---- low-precision operators: what their arguments have in common --------------------------------------------------
+bool extent_ok(int64_t n) { return n >= 0 && n <= OZAKI_MAX_EXTENT; }
+// vectors of k elements: starts at multiples of 16 bytes, and 255 of them stay inside a 32-bit offset
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+bool stride_ok(int64_t ld, int64_t k, int bytes) {
+    return ld >= (k > 1 ? k : 1) && ld <= OZAKI_MAX_EXTENT / bytes && ld * bytes % 16 == 0;
+}
+
+// the loss and its gradient: the arguments that they share, by position
+int check_loss_args(int64_t tokens, int64_t vocab, int64_t k, const void* H, int64_t ldh, const void* W, int64_t ldw, int type, const int64_t* targets) {
+    if (!extent_ok(tokens)) return -1;
+    if (vocab < 1 || !extent_ok(vocab)) return -2;
+    if (k < 1 || !extent_ok(k * 2)) return -3;
+    if (type != OZAKI_TYPE_BF16 && type != OZAKI_TYPE_F16) return -8;
+    if (tokens == 0) return 0;
+    if (!H || !aligned16(H)) return -4;
+    if (!stride_ok(ldh, k, 2)) return -5;
+    if (!W || !aligned16(W)) return -6;
+    if (!stride_ok(ldw, k, 2)) return -7;
+    if (!targets) return -9;
+    return 0;
+}
+
 int plan_for_query(int64_t m, int64_t n, int64_t k, int fmt, int s, int64_t k_block, int pair_set, Plan& pl) {
     if (pair_set != OZAKI_PAIRS_TRIANGLE && pair_set != OZAKI_PAIRS_ALL) return -14;
     return make_plan(m, n, k, fmt, s, k_block, pair_set == OZAKI_PAIRS_ALL, pl);
@@ -311,7 +337,8 @@ int ozaki_last_device_status(void) {
     HIP_TRY(hipStreamSynchronize(c.stream));
     for (int i = 0; i < 2; ++i)
         if (flags[i]) HIP_TRY(hipMemsetAsync(places[i], 0, FLAG_BYTES, c.stream));
-    return ((flags[0] | flags[1]) & 1) ? OZAKI_STATUS_NONFINITE : 0;
+    const int found = flags[0] | flags[1];
+    return (found & 1) ? OZAKI_STATUS_NONFINITE : (found & TARGET_FLAG) ? OZAKI_STATUS_TARGET : 0;
 }
 
 int ozaki_last_hip_error(void) { return ctx().last_hip_error; }
@@ -325,6 +352,7 @@ const char* ozaki_status_string(int status) {
         case OZAKI_STATUS_NONFINITE: return "non-finite input";
         case OZAKI_STATUS_STATIC_LIMIT: return "problem needs more work memory than the static scratch of ozaki_dgemm_static holds";
         case OZAKI_STATUS_SLICE_COUNT: return "num_slices exceeds OZAKI_MAX_SLICES";
+        case OZAKI_STATUS_TARGET: return "a target is neither a word of the vocabulary nor the one to ignore";
         default: return status < 0 ? "invalid argument (the negated value is its 1-based position)" : "unknown status";
     }
 }
@@ -531,6 +559,120 @@ int ozaki_fp64_add_emulated(const double* a, const double* b, double* out, int64
     if (!b) return -2;
     if (!out) return -3;
     HIP_TRY(launch_add_emulated(a, b, out, n, ctx().stream));
+    return 0;
+}
+
+int ozaki_quantise_fp8(int64_t rows, int64_t k, const void* X, int64_t ldx, int type, int scaling, void* Q, int64_t ldq, float* S,
+                       int64_t lds, void* Qt, int64_t ldqt, float* St, int64_t ldst) {
+    if (!extent_ok(rows)) return -1;
+    if (!extent_ok(k)) return -2;
+    if (!type_ok(type)) return -5;
+    if (scaling != OZAKI_SCALE_VECTORS && scaling != OZAKI_SCALE_BLOCKS) return -6;
+    if (rows == 0 || k == 0) return 0;
+    const int64_t shared = scaling == OZAKI_SCALE_BLOCKS ? SCALE_BLOCK : 1;
+    if (!X || !aligned16(X)) return -3;
+    if (ldx < k || ldx * type_bytes(type) % 16 != 0) return -4;
+    if ((!Q && !Qt) || !aligned16(Q)) return -7;
+    if (Q && !stride_ok(ldq, k, 1)) return -8;
+    if ((Q != nullptr) != (S != nullptr)) return -9;
+    if (S && lds < div_up(rows, shared)) return -10;
+    if (!aligned16(Qt)) return -11;
+    if (Qt && !stride_ok(ldqt, rows, 1)) return -12;
+    if ((Qt != nullptr) != (St != nullptr)) return -13;
+    if (St && ldst < div_up(k, shared)) return -14;
+    const QuantiseArgs a{X, rows, k, ldx, static_cast<uint8_t*>(Q), ldq, S, lds, static_cast<uint8_t*>(Qt), ldqt, St, ldst};
+    HIP_TRY(launch_quantise_fp8(a, type, scaling, ctx().stream));
+    return 0;
+}
+
+size_t ozaki_gemm_fp8_workspace_bytes(int64_t m, int64_t n, int64_t k) {
+    if (!extent_ok(m) || !extent_ok(n) || !extent_ok(k)) return 0;
+    const int splits = gemm_fp8_splits(m, n, k);
+    return splits > 1 ? FLAG_BYTES + align_up((size_t)splits * m * n * sizeof(float)) : 0;
+}
+
+int ozaki_gemm_fp8(int64_t m, int64_t n, int64_t k, const void* A, int64_t lda, const float* Sa, int64_t ldsa, const void* B, int64_t ldb,
+                   const float* Sb, int64_t ldsb, int scaling_b, void* D, int64_t ldd, int type_d, int accumulate) {
+    if (!extent_ok(m)) return -1;
+    if (!extent_ok(n)) return -2;
+    if (!extent_ok(k)) return -3;
+    if (scaling_b != OZAKI_SCALE_VECTORS && scaling_b != OZAKI_SCALE_BLOCKS) return -12;
+    if (!type_ok(type_d)) return -15;
+    if (accumulate != 0 && accumulate != 1) return -16;
+    if (m == 0 || n == 0) return 0;
+    if (k > 0) {
+        if (!A || !aligned16(A)) return -4;
+        if (!stride_ok(lda, k, 1)) return -5;
+        if (!Sa) return -6;
+        if (ldsa < m) return -7;
+        if (!B || !aligned16(B)) return -8;
+        if (!stride_ok(ldb, k, 1)) return -9;
+        if (!Sb) return -10;
+        if (ldsb < (scaling_b == OZAKI_SCALE_BLOCKS ? div_up(n, SCALE_BLOCK) : n)) return -11;
+    }
+    if (!D || reinterpret_cast<uintptr_t>(D) % type_bytes(type_d) != 0) return -13;
+    if (ldd < n) return -14;
+    const int splits = gemm_fp8_splits(m, n, k);
+    float* partial = nullptr;
+    if (splits > 1) {
+        if (!ctx().ws || ctx().ws_bytes < ozaki_gemm_fp8_workspace_bytes(m, n, k)) return OZAKI_STATUS_WORKSPACE;
+        partial = reinterpret_cast<float*>(ctx().ws + FLAG_BYTES);
+    }
+    const GemmFp8Args a{static_cast<const uint8_t*>(A), static_cast<const uint8_t*>(B), Sa, Sb, D, partial, m, n, k, lda, ldb, ldsa, ldsb, ldd, accumulate};
+    HIP_TRY(launch_gemm_fp8(a, scaling_b, type_d, splits, ctx().stream));
+    return 0;
+}
+
+size_t ozaki_linear_loss_workspace_bytes(int64_t tokens, int64_t vocab, int64_t k, int grad, int minimum) {
+    if (tokens < 1 || !extent_ok(tokens) || vocab < 1 || !extent_ok(vocab) || k < 1 || !extent_ok(k * 2)) return 0;
+    if (!grad) return loss_bytes(tokens, vocab);
+    return loss_grad_bytes(tokens, vocab, k, minimum ? LOSS_PIECE : loss_grad_piece(tokens, vocab, k));
+}
+
+int ozaki_linear_loss(int64_t tokens, int64_t vocab, int64_t k, const void* H, int64_t ldh, const void* W, int64_t ldw, int type,
+                      const int64_t* targets, int64_t ignore, float* loss, float* lse) {
+    const int st = check_loss_args(tokens, vocab, k, H, ldh, W, ldw, type, targets);
+    if (st != 0 || tokens == 0) return st;
+    if (!loss) return -11;
+    if (!lse) return -12;
+    Context& c = ctx();
+    if (!c.ws || c.ws_bytes < loss_bytes(tokens, vocab)) return OZAKI_STATUS_WORKSPACE;
+    LossArgs a = {};
+    a.H = H; a.W = W; a.targets = targets;
+    a.tokens = tokens; a.vocab = vocab; a.k = k; a.ldh = ldh; a.ldw = ldw; a.ignore = ignore;
+    a.loss = loss; a.lse = lse;
+    a.flags = reinterpret_cast<int*>(c.ws);
+    HIP_TRY(launch_linear_loss(a, type, c.ws, c.stream));
+    return 0;
+}
+
+int ozaki_linear_loss_grad(int64_t tokens, int64_t vocab, int64_t k, const void* H, int64_t ldh, const void* W, int64_t ldw, int type,
+                           const int64_t* targets, int64_t ignore, const float* lse, const float* dloss, void* dH, int64_t lddh, void* dW,
+                           int64_t lddw) {
+    int st = check_loss_args(tokens, vocab, k, H, ldh, W, ldw, type, targets);
+    if (st != 0) return st;
+    if (tokens > 0 && !lse) return -11;
+    if (tokens > 0 && !dloss) return -12;
+    if ((!dH && !dW) || reinterpret_cast<uintptr_t>(dH) % 2 != 0) return -13;
+    if (dH && lddh < k) return -14;
+    if (reinterpret_cast<uintptr_t>(dW) % 2 != 0) return -15;
+    if (dW && lddw < k) return -16;
+    Context& c = ctx();
+    if (tokens == 0) {
+        if (dW) HIP_TRY(launch_zero_rows(dW, vocab, k, lddw, c.stream));
+        return 0;
+    }
+    // the recommended piece of the vocabulary, or the largest that the work memory holds
+    int64_t piece = loss_grad_piece(tokens, vocab, k);
+    while (piece > LOSS_PIECE && c.ws_bytes < loss_grad_bytes(tokens, vocab, k, piece)) piece -= LOSS_PIECE;
+    if (!c.ws || c.ws_bytes < loss_grad_bytes(tokens, vocab, k, piece)) return OZAKI_STATUS_WORKSPACE;
+    LossArgs a = {};
+    a.H = H; a.W = W; a.targets = targets;
+    a.tokens = tokens; a.vocab = vocab; a.k = k; a.ldh = ldh; a.ldw = ldw; a.ignore = ignore;
+    a.lse_in = lse; a.dloss = dloss;
+    a.dH = dH; a.dW = dW; a.lddh = lddh; a.lddw = lddw;
+    a.flags = reinterpret_cast<int*>(c.ws);
+    HIP_TRY(launch_linear_loss_grad(a, type, piece, c.ws, c.stream));
     return 0;
 }
 

@@ -1,0 +1,555 @@
+// Softmax cross entropy of a linear layer's outputs over a vocabulary, and its gradient, without keeping the outputs:
+//     z[t][v] = H[t] . W[v],   lse[t] = log sum_v exp(z[t][v]),   loss[t] = lse[t] - z[t][target[t]]
+//     g[t][v] = (exp(z[t][v] - lse[t]) - [v == target[t]]) * dloss[t],   dH = g W,   dW = g^T H.
+//
+// Forward: a workgroup forms a tile of z in registers and leaves each token's largest value and sum of exponentials over the tile's
+// words, 8 bytes per token and tile; a second launch joins them and takes the target's z, which the lane that held it has written.
+// Gradient: the vocabulary is taken in pieces.  A piece's z are formed again and become g in the 16-bit type of H and W (its rounding is of the
+// size of the result's own), stored as [token][word] and as [word][token]; the two products read it from there.  All products are
+// sums over 16-bit elements in FP32 on the matrix unit (tile_product.hpp) and want both operands contiguous along the inner
+// dimension, hence also a transposed H and a transposed piece of W.
+//
+// FP16's smallest normal number is 2^-14, and g of a word that is unlikely lies far below: g is held times a power of two that takes the
+// largest |dloss| to 2^11 .. 2^12, and the products are scaled back in FP32.
+#include "layout.hpp"
+#include "tile_product.hpp"
+
+namespace ozaki {
+namespace {
+
+constexpr float LOG2_E = 1.44269504088896340736f, LN_2 = 0.69314718055994530942f;
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * LOG2_E); }
+__device__ __forceinline__ float log_of(float x) { return __builtin_amdgcn_logf(x) * LN_2; }
+
+// per token, what a tile of z needs
+struct TokenState {
+    const float* lse;
+    const float* factor;     // dloss times the power of two, 0 where the token does not count
+    const int* target;       // -1 where it does not count
+};
+
+struct LogitWork {
+    const uint8_t* H;
+    const uint8_t* W;        // of the piece
+    int64_t ldh, ldw, bytes; // in bytes
+    int64_t tokens, words, first_word;    // words: of the piece
+    int tiles_m, tiles_n, steps;
+    WorkOrder order;
+    // forward
+    const int64_t* targets;
+    float2* part;            // [tile of words][token]
+    float* target_z;
+    // gradient
+    TokenState token;
+    uint8_t* G;              // [token][ldg], null: not wanted
+    uint8_t* Gt;             // [word][ldgt]
+    int64_t ldg, ldgt;       // elements
+};
+
+template <typename P>
+__device__ __forceinline__ void logits(const LogitWork& w, uint8_t* lds, int64_t& m0, int64_t& n0, v4f32 (&acc)[P::FN][P::FM]) {
+    const WorkItem item = work_item(blockIdx.x, gridDim.x, w.order, w.tiles_m, w.tiles_n);
+    m0 = (int64_t)item.bm * P::TM;
+    n0 = (int64_t)item.bn * P::TN;
+    const int64_t left_m = w.tokens - m0, left_n = w.words - n0;
+    const TileOperand X{w.W + n0 * w.ldw, w.ldw, (int)(left_n < P::TN ? left_n : P::TN), nullptr, 0};
+    const TileOperand Y{w.H + m0 * w.ldh, w.ldh, (int)(left_m < P::TM ? left_m : P::TM), nullptr, 0};
+    P::multiply(lds, X, Y, w.bytes, 0, w.steps, acc);
+}
+
+template <typename P>
+__device__ __forceinline__ void loss_forward_body(const LogitWork& w) {
+    __shared__ __attribute__((aligned(16))) uint8_t lds[P::LDS_BYTES];
+    int64_t m0, n0;
+    v4f32 acc[P::FN][P::FM] = {};
+    logits<P>(w, lds, m0, n0, acc);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wn = wave / P::WM, wm = wave % P::WM, g = lane >> 4;
+    float2* const joined = reinterpret_cast<float2*>(lds);            // [wn][token]
+    const int first = wn * P::FN * 16 + 4 * g;                        // this lane's first word in the tile
+    const int words = (int)(w.words - n0 < P::TN ? w.words - n0 : P::TN);
+#pragma unroll
+    for (int j = 0; j < P::FM; ++j) {
+        const int t = (wm * P::FM + j) * 16 + (lane & 15);
+        const int64_t target = m0 + t < w.tokens ? w.targets[m0 + t] - n0 : -1;
+        float most = -__builtin_inff();
+#pragma unroll
+        for (int i = 0; i < P::FN; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int v = first + 16 * i + r;
+                if (v >= words) acc[i][j][r] = -__builtin_inff();
+                most = fmaxf(most, acc[i][j][r]);
+                if (v < words && v == target) w.target_z[m0 + t] = acc[i][j][r];
+            }
+        most = fmaxf(most, __shfl_xor(most, 16));
+        most = fmaxf(most, __shfl_xor(most, 32));
+        const float base = most == -__builtin_inff() ? 0.0f : most;   // nothing but minus infinity: a sum of zero
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < P::FN; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sum += exp_of(acc[i][j][r] - base);
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        if (g == 0) joined[wn * P::TM + t] = make_float2(most, sum);
+    }
+    __syncthreads();
+    for (int t = threadIdx.x; t < P::TM; t += P::THREADS) {
+        if (m0 + t >= w.tokens) break;
+        float most = -__builtin_inff(), sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < P::WN; ++i) most = fmaxf(most, joined[i * P::TM + t].x);
+        const float base = most == -__builtin_inff() ? 0.0f : most;
+#pragma unroll
+        for (int i = 0; i < P::WN; ++i) sum += joined[i * P::TM + t].y * exp_of(joined[i * P::TM + t].x - base);
+        w.part[(n0 / P::TN) * w.tokens + m0 + t] = make_float2(most, sum);
+    }
+}
+
+// Sixteen tokens, sixteen shares of the tiles of words.
+__global__ void __launch_bounds__(256) loss_join_kernel(const float2* part, const float* target_z, const int64_t* targets, int64_t tokens,
+                                                        int64_t vocab, int64_t ignore, int tiles, float* loss, float* lse, int* flags) {
+    __shared__ float2 share[16][17];
+    const int tl = threadIdx.x & 15, s = threadIdx.x >> 4;
+    const int64_t t = (int64_t)blockIdx.x * 16 + tl, at = t < tokens ? t : tokens - 1;
+    float most = -__builtin_inff(), sum = 0.0f;
+    for (int i = s; i < tiles; i += 16) {
+        const float2 p = part[(int64_t)i * tokens + at];
+        const float higher = fmaxf(most, p.x), base = higher == -__builtin_inff() ? 0.0f : higher;
+        sum = sum * exp_of(most - base) + p.y * exp_of(p.x - base);
+        most = higher;
+    }
+    share[tl][s] = make_float2(most, sum);
+    __syncthreads();
+    if (s != 0 || t >= tokens) return;
+    float all = -__builtin_inff(), total = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) all = fmaxf(all, share[tl][i].x);
+    const float base = all == -__builtin_inff() ? 0.0f : all;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) total += share[tl][i].y * exp_of(share[tl][i].x - base);
+    const float l = base + log_of(total);
+    const int64_t target = targets[t];
+    const bool counts = target != ignore, real = target >= 0 && target < vocab;
+    lse[t] = l;
+    loss[t] = !counts ? 0.0f : real ? l - target_z[t] : __builtin_nanf("");
+    if (counts && !real) atomicOr(flags, TARGET_FLAG);
+}
+
+// Gradient, in front of everything: what counts of every token, and the power of two that g is held times (scale[0], its inverse scale[1]).
+template <int TYPE>
+__global__ void __launch_bounds__(1024) loss_tokens_kernel(const int64_t* targets, const float* dloss, int64_t tokens, int64_t vocab,
+                                                           int64_t ignore, float* factor, int* target_out, float* scale, int* flags) {
+    __shared__ float shared_most[16];
+    float up = 1.0f;
+    if constexpr (TYPE == TYPE_F16) {
+        float most = 0.0f;
+        for (int64_t t = threadIdx.x; t < tokens; t += 1024)
+            if (targets[t] != ignore) {
+                const float d = fabsf(dloss[t]);
+                most = d < __builtin_inff() ? fmaxf(most, d) : most;
+            }
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) most = fmaxf(most, __shfl_xor(most, s));
+        if ((threadIdx.x & 63) == 0) shared_most[threadIdx.x >> 6] = most;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) most = fmaxf(most, shared_most[i]);
+        int e = 12;
+        if (most > 0.0f) {
+            e = 12 - (((__float_as_int(most) >> 23) & 0xFF) - 126);   // most < 2^(its exponent + 1)
+            e = e < -100 ? -100 : e > 100 ? 100 : e;
+        }
+        up = __int_as_float((e + 127) << 23);
+    }
+    for (int64_t t = threadIdx.x; t < tokens; t += 1024) {
+        const int64_t target = targets[t];
+        const bool counts = target != ignore, real = target >= 0 && target < vocab;
+        if (counts && !real) atomicOr(flags, TARGET_FLAG);
+        factor[t] = counts && real ? dloss[t] * up : 0.0f;
+        target_out[t] = counts && real ? (int)target : -1;
+    }
+    if (threadIdx.x == 0) {
+        scale[0] = up;
+        scale[1] = 1.0f / up;
+    }
+}
+
+// A tile of g: through LDS, [token][word], so that both results are written in pieces of 16 bytes.
+template <typename P, typename T>
+__device__ __forceinline__ void loss_g_body(const LogitWork& w) {
+    constexpr int STRIDE = P::TN * 2 + 16;            // bytes between tokens
+    __shared__ __attribute__((aligned(16))) uint8_t lds[P::LDS_BYTES > P::TM * STRIDE ? P::LDS_BYTES : P::TM * STRIDE];
+    int64_t m0, n0;
+    v4f32 acc[P::FN][P::FM] = {};
+    logits<P>(w, lds, m0, n0, acc);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wn = wave / P::WM, wm = wave % P::WM, g = lane >> 4;
+    const int first = wn * P::FN * 16 + 4 * g;
+    const int words = (int)(w.words - n0 < P::TN ? w.words - n0 : P::TN);
+    typedef T four __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int j = 0; j < P::FM; ++j) {
+        const int t = (wm * P::FM + j) * 16 + (lane & 15);
+        const bool real = m0 + t < w.tokens;
+        const int target = real ? w.token.target[m0 + t] : -1;
+        const float factor = target >= 0 ? w.token.factor[m0 + t] : 0.0f, lse = target >= 0 ? w.token.lse[m0 + t] : 0.0f;
+        const int at = target >= 0 ? (int)(target - w.first_word - n0) : -1;
+#pragma unroll
+        for (int i = 0; i < P::FN; ++i) {
+            four v;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int word = first + 16 * i + r;
+                const float p = exp_of(acc[i][j][r] - lse) - (word == at ? 1.0f : 0.0f);
+                v[r] = (T)(target >= 0 && word < words ? p * factor : 0.0f);
+            }
+            *reinterpret_cast<four*>(lds + t * STRIDE + (first + 16 * i) * 2) = v;
+        }
+    }
+    __syncthreads();
+    if (w.G != nullptr) {
+        for (int c = threadIdx.x; c < P::TM * P::TN / 8; c += P::THREADS) {
+            const int t = c / (P::TN / 8), p = c % (P::TN / 8);
+            if (m0 + t >= w.tokens) break;
+            *reinterpret_cast<v4i32*>(w.G + ((m0 + t) * w.ldg + n0 + p * 8) * 2) = *reinterpret_cast<const v4i32*>(lds + t * STRIDE + p * 16);
+        }
+    }
+    if (w.Gt != nullptr) {
+        for (int c = threadIdx.x; c < P::TM * P::TN / 8; c += P::THREADS) {
+            const int word = c % P::TN, p = c / P::TN;
+            if (word >= words) continue;
+            v4i32 v;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const unsigned lo = *reinterpret_cast<const uint16_t*>(lds + (p * 8 + 2 * q) * STRIDE + word * 2);
+                const unsigned hi = *reinterpret_cast<const uint16_t*>(lds + (p * 8 + 2 * q + 1) * STRIDE + word * 2);
+                v[q] = (int)(lo | hi << 16);
+            }
+            *reinterpret_cast<v4i32*>(w.Gt + ((n0 + word) * w.ldgt + m0 + p * 8) * 2) = v;
+        }
+    }
+}
+
+// [row][column] -> [column][row] of 16-bit elements, 64 x 64 at a time; rows beyond the matrix, and rows that `counts` marks with -1, are zeros.
+__global__ void __launch_bounds__(256) loss_transpose_kernel(const uint16_t* from, int64_t ld, int64_t rows, int64_t columns, const int* counts,
+                                                             uint16_t* to, int64_t ldt) {
+    __shared__ uint16_t tile[64][66];
+    const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 64;
+    const int in = threadIdx.x & 63;
+    for (int i = threadIdx.x >> 6; i < 64; i += 4) {
+        const bool real = r0 + i < rows && c0 + in < columns && (counts == nullptr || counts[r0 + i] >= 0);
+        tile[i][in] = real ? from[(r0 + i) * ld + c0 + in] : (uint16_t)0;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x >> 6; i < 64; i += 4)
+        if (c0 + i < columns) to[(c0 + i) * ldt + r0 + in] = tile[in][i];
+}
+
+// D = X Y^T of 16-bit operands that lie in work memory or are the caller's: rows of Y are D's rows
+struct ProductWork {
+    const uint8_t* X;
+    const uint8_t* Y;
+    int64_t ldx, ldy, bytes;
+    int64_t m, n;
+    int tiles_m, tiles_n, steps, splits;
+    WorkOrder order;
+    void* D;
+    int64_t ldd;
+    const float* scale;      // what the sums are multiplied by
+    float* partial;          // not null: unscaled sums go there, [split][m][n]
+};
+
+__device__ __forceinline__ int split_begin(int steps, int splits, int s) { return (int)((int64_t)steps * s / splits); }
+
+template <typename P, typename T>
+__device__ __forceinline__ void loss_product_body(const ProductWork& w) {
+    __shared__ __attribute__((aligned(16))) uint8_t lds[P::LDS_BYTES];
+    const WorkItem item = work_item(blockIdx.x, gridDim.x, w.order, w.tiles_m, w.tiles_n);
+    const int64_t m0 = (int64_t)item.bm * P::TM, n0 = (int64_t)item.bn * P::TN, left_m = w.m - m0, left_n = w.n - n0;
+    const TileOperand X{w.X + n0 * w.ldx, w.ldx, (int)(left_n < P::TN ? left_n : P::TN), nullptr, 0};
+    const TileOperand Y{w.Y + m0 * w.ldy, w.ldy, (int)(left_m < P::TM ? left_m : P::TM), nullptr, 0};
+    v4f32 acc[P::FN][P::FM] = {};
+    const int split = item.gi;
+    P::multiply(lds, X, Y, w.bytes, split_begin(w.steps, w.splits, split), split_begin(w.steps, w.splits, split + 1), acc);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wn = wave / P::WM, wm = wave % P::WM;
+    if (w.partial != nullptr) {
+        const bool wide = w.n % 4 == 0;
+#pragma unroll
+        for (int j = 0; j < P::FM; ++j) {
+            const int64_t m = m0 + (wm * P::FM + j) * 16 + (lane & 15);
+            if (m >= w.m) continue;
+#pragma unroll
+            for (int i = 0; i < P::FN; ++i) {
+                const int64_t n = n0 + (wn * P::FN + i) * 16 + 4 * (lane >> 4);
+                put_four(w.partial + ((int64_t)split * w.m + m) * w.n + n, acc[i][j], w.n - n, wide, false);
+            }
+        }
+        return;
+    }
+    const float scale = *w.scale;
+    T* const D = static_cast<T*>(w.D);
+    const bool wide = w.ldd % 4 == 0 && reinterpret_cast<uintptr_t>(D) % 8 == 0;
+#pragma unroll
+    for (int j = 0; j < P::FM; ++j) {
+        const int64_t m = m0 + (wm * P::FM + j) * 16 + (lane & 15);
+        if (m >= w.m) continue;
+#pragma unroll
+        for (int i = 0; i < P::FN; ++i) {
+            const int64_t n = n0 + (wn * P::FN + i) * 16 + 4 * (lane >> 4);
+            put_four(D + m * w.ldd + n, acc[i][j] * scale, w.n - n, wide, false);
+        }
+    }
+}
+
+// The sums of a piece's shares of the inner dimension, on top of the pieces' before it (`sum`, unless it is the first); the last piece's go to D.
+template <typename T>
+__device__ __forceinline__ void join_body(const float* partial, int splits, int64_t m, int64_t n, float* sum, bool first, bool last,
+                                          const float* scale, T* D, int64_t ldd) {
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < m * n; at += (int64_t)gridDim.x * 256) {
+        float s = first ? 0.0f : sum[at];
+        for (int i = 0; i < splits; ++i) s += partial[(int64_t)i * m * n + at];
+        if (last) D[at / n * ldd + at % n] = (T)(s * *scale);
+        else sum[at] = s;
+    }
+}
+
+__global__ void __launch_bounds__(256) zero_rows_kernel(uint16_t* D, int64_t rows, int64_t k, int64_t ldd) {
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < rows * k; at += (int64_t)gridDim.x * 256) D[at / k * ldd + at % k] = 0;
+}
+
+constexpr int kind_of(int type) { return type == TYPE_F16 ? KIND_F16 : KIND_BF16; }
+template <int TYPE> using LargeTile = Tile<kind_of(TYPE), 2, 4, 8, 4, 2>;      // 256 words or columns, 256 tokens or rows
+template <int TYPE> using MiddleTile = Tile<kind_of(TYPE), 2, 2, 4, 2, 3>;     // 128, 64
+template <int TYPE> using FewTile = Tile<kind_of(TYPE), 4, 1, 2, 1, 4>;        // 128, 16
+
+template <int TYPE>
+__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) loss_forward_large_kernel(const LogitWork w) { loss_forward_body<LargeTile<TYPE>>(w); }
+template <int TYPE>
+__global__ void __launch_bounds__(256) loss_forward_middle_kernel(const LogitWork w) { loss_forward_body<MiddleTile<TYPE>>(w); }
+template <int TYPE>
+__global__ void __launch_bounds__(256) loss_forward_few_kernel(const LogitWork w) { loss_forward_body<FewTile<TYPE>>(w); }
+template <int TYPE>
+__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) loss_g_large_kernel(const LogitWork w) { loss_g_body<LargeTile<TYPE>, typename Element<TYPE>::type>(w); }
+template <int TYPE>
+__global__ void __launch_bounds__(256) loss_g_middle_kernel(const LogitWork w) { loss_g_body<MiddleTile<TYPE>, typename Element<TYPE>::type>(w); }
+template <int TYPE>
+__global__ void __launch_bounds__(256) loss_g_few_kernel(const LogitWork w) { loss_g_body<FewTile<TYPE>, typename Element<TYPE>::type>(w); }
+template <int TYPE>
+__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) loss_product_large_kernel(const ProductWork w) { loss_product_body<LargeTile<TYPE>, typename Element<TYPE>::type>(w); }
+template <int TYPE>
+__global__ void __launch_bounds__(256) loss_product_middle_kernel(const ProductWork w) { loss_product_body<MiddleTile<TYPE>, typename Element<TYPE>::type>(w); }
+template <int TYPE>
+__global__ void __launch_bounds__(256) loss_product_few_kernel(const ProductWork w) { loss_product_body<FewTile<TYPE>, typename Element<TYPE>::type>(w); }
+template <int TYPE>
+__global__ void __launch_bounds__(256) loss_product_join_kernel(const float* partial, int splits, int64_t m, int64_t n, float* sum, bool first, bool last,
+                                                                const float* scale, void* D, int64_t ldd) {
+    join_body(partial, splits, m, n, sum, first, last, scale, static_cast<typename Element<TYPE>::type*>(D), ldd);
+}
+
+// ---- shapes and work memory ------------------------------------------------------------------------------------
+enum { FEW, MIDDLE, LARGE };
+int shape_for(int64_t m, int64_t n) { return m <= 16 ? FEW : div_up(m, 256) * div_up(n, 256) < 128 || m <= 64 ? MIDDLE : LARGE; }
+int tile_m(int shape) { return shape == FEW ? 16 : shape == MIDDLE ? 64 : 256; }
+int tile_n(int shape) { return shape == LARGE ? 256 : 128; }
+WorkOrder order_for(int shape, int64_t tiles_m, int64_t items) {
+    return shape == LARGE && items >= 512 ? WorkOrder{32, tiles_m > 8 ? 4 : 8} : WorkOrder{0, 0};
+}
+// shares of an inner dimension of `steps` steps, so that there are workgroups for every compute unit
+int product_splits(int64_t m, int64_t n, int64_t steps) {
+    const int shape = shape_for(m, n);
+    const int64_t tiles = div_up(m, tile_m(shape)) * div_up(n, tile_n(shape)), want = (shape == LARGE ? 256 : 512) / tiles, most = steps / 8;
+    const int64_t s = want < most ? want : most;
+    return (int)(s < 1 ? 1 : s > 32 ? 32 : s);
+}
+
+size_t up(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
+constexpr int64_t EDGE = 256;            // what g is padded to, with zeros
+int64_t padded(int64_t n) { return div_up(n, EDGE) * EDGE; }
+
+struct GradPlaces {
+    float* scale;
+    float* factor;
+    int* target;
+    uint8_t* Ht;
+    uint8_t* Wt;
+    uint8_t* G;
+    uint8_t* Gt;
+    float* partial;
+    float* sum;
+    size_t total;
+};
+GradPlaces grad_places(uint8_t* ws, int64_t tokens, int64_t vocab, int64_t k, int64_t piece) {
+    GradPlaces p;
+    size_t at = 256;                     // the flag words
+    auto take = [&](size_t bytes) { uint8_t* const here = ws + at; at += up(bytes); return here; };
+    const int64_t words = piece < vocab ? piece : vocab;
+    const int splits = product_splits(tokens, k, div_up(words * 2, STEP_BYTES));
+    p.scale = reinterpret_cast<float*>(take(8));
+    p.factor = reinterpret_cast<float*>(take((size_t)tokens * 4));
+    p.target = reinterpret_cast<int*>(take((size_t)tokens * 4));
+    p.Ht = take((size_t)k * padded(tokens) * 2);
+    p.Wt = take((size_t)k * padded(words) * 2);
+    p.G = take((size_t)tokens * padded(words) * 2);
+    p.Gt = take((size_t)words * padded(tokens) * 2);
+    const bool joined = splits > 1 || piece < vocab;
+    p.partial = reinterpret_cast<float*>(take(joined ? (size_t)splits * tokens * k * 4 : 0));
+    p.sum = reinterpret_cast<float*>(take(piece < vocab ? (size_t)tokens * k * 4 : 0));
+    p.total = at;
+    return p;
+}
+
+template <int TYPE>
+hipError_t launch_product(ProductWork w, int shape, hipStream_t st) {
+    w.tiles_m = (int)div_up(w.m, tile_m(shape));
+    w.tiles_n = (int)div_up(w.n, tile_n(shape));
+    const int64_t items = (int64_t)w.tiles_m * w.tiles_n * w.splits;
+    w.order = order_for(shape, w.tiles_m, items);
+    if (shape == FEW) hipLaunchKernelGGL((loss_product_few_kernel<TYPE>), dim3((unsigned)items), dim3(256), 0, st, w);
+    else if (shape == MIDDLE) hipLaunchKernelGGL((loss_product_middle_kernel<TYPE>), dim3((unsigned)items), dim3(256), 0, st, w);
+    else hipLaunchKernelGGL((loss_product_large_kernel<TYPE>), dim3((unsigned)items), dim3(512), 0, st, w);
+    return hipGetLastError();
+}
+
+void set_tiles(LogitWork& w, int shape) {
+    w.tiles_m = (int)div_up(w.tokens, tile_m(shape));
+    w.tiles_n = (int)div_up(w.words, tile_n(shape));
+    w.order = order_for(shape, w.tiles_m, (int64_t)w.tiles_m * w.tiles_n);
+    w.steps = (int)div_up(w.bytes, STEP_BYTES);
+}
+
+template <int TYPE>
+hipError_t forward_typed(const LossArgs& a, uint8_t* ws, hipStream_t st) {
+    const int shape = shape_for(a.tokens, a.vocab);
+    const int64_t tiles = div_up(a.vocab, tile_n(shape));
+    LogitWork w = {};
+    w.H = static_cast<const uint8_t*>(a.H);
+    w.W = static_cast<const uint8_t*>(a.W);
+    w.ldh = a.ldh * 2;
+    w.ldw = a.ldw * 2;
+    w.bytes = a.k * 2;
+    w.tokens = a.tokens;
+    w.words = a.vocab;
+    set_tiles(w, shape);
+    w.targets = a.targets;
+    w.target_z = reinterpret_cast<float*>(ws + 256);
+    w.part = reinterpret_cast<float2*>(ws + 256 + up((size_t)a.tokens * 4));
+    const unsigned blocks = (unsigned)(w.tiles_m * (int64_t)w.tiles_n);
+    if (shape == FEW) hipLaunchKernelGGL((loss_forward_few_kernel<TYPE>), dim3(blocks), dim3(256), 0, st, w);
+    else if (shape == MIDDLE) hipLaunchKernelGGL((loss_forward_middle_kernel<TYPE>), dim3(blocks), dim3(256), 0, st, w);
+    else hipLaunchKernelGGL((loss_forward_large_kernel<TYPE>), dim3(blocks), dim3(512), 0, st, w);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(loss_join_kernel, dim3((unsigned)div_up(a.tokens, 16)), dim3(256), 0, st, w.part, w.target_z, a.targets, a.tokens, a.vocab,
+                       a.ignore, (int)tiles, a.loss, a.lse, a.flags);
+    return hipGetLastError();
+}
+
+#define OZAKI_LOSS_TRY(expr) do { const hipError_t e_ = (expr); if (e_ != hipSuccess) return e_; } while (0)
+
+hipError_t transpose(const void* from, int64_t ld, int64_t rows, int64_t columns, const int* counts, uint8_t* to, hipStream_t st) {
+    hipLaunchKernelGGL(loss_transpose_kernel, dim3((unsigned)(padded(rows) / 64), (unsigned)div_up(columns, 64)), dim3(256), 0, st,
+                       static_cast<const uint16_t*>(from), ld, rows, columns, counts, reinterpret_cast<uint16_t*>(to), padded(rows));
+    return hipGetLastError();
+}
+
+template <int TYPE>
+hipError_t grad_typed(const LossArgs& a, int64_t piece, uint8_t* ws, hipStream_t st) {
+    const GradPlaces p = grad_places(ws, a.tokens, a.vocab, a.k, piece);
+    hipLaunchKernelGGL((loss_tokens_kernel<TYPE>), dim3(1), dim3(1024), 0, st, a.targets, a.dloss, a.tokens, a.vocab, a.ignore, p.factor, p.target,
+                       p.scale, a.flags);
+    OZAKI_LOSS_TRY(hipGetLastError());
+    if (a.dW != nullptr) OZAKI_LOSS_TRY(transpose(a.H, a.ldh, a.tokens, a.k, p.target, p.Ht, st));
+    const bool joined = piece < a.vocab;
+    for (int64_t first = 0; first < a.vocab; first += piece) {
+        const int64_t words = a.vocab - first < piece ? a.vocab - first : piece;
+        const uint8_t* const W = static_cast<const uint8_t*>(a.W) + first * a.ldw * 2;
+        LogitWork w = {};
+        w.H = static_cast<const uint8_t*>(a.H);
+        w.W = W;
+        w.ldh = a.ldh * 2;
+        w.ldw = a.ldw * 2;
+        w.bytes = a.k * 2;
+        w.tokens = a.tokens;
+        w.words = words;
+        w.first_word = first;
+        const int shape = shape_for(a.tokens, words);
+        set_tiles(w, shape);
+        w.token = TokenState{a.lse_in, p.factor, p.target};
+        w.G = a.dH != nullptr ? p.G : nullptr;
+        w.Gt = a.dW != nullptr ? p.Gt : nullptr;
+        w.ldg = padded(words);
+        w.ldgt = padded(a.tokens);
+        const unsigned blocks = (unsigned)(w.tiles_m * (int64_t)w.tiles_n);
+        if (shape == FEW) hipLaunchKernelGGL((loss_g_few_kernel<TYPE>), dim3(blocks), dim3(256), 0, st, w);
+        else if (shape == MIDDLE) hipLaunchKernelGGL((loss_g_middle_kernel<TYPE>), dim3(blocks), dim3(256), 0, st, w);
+        else hipLaunchKernelGGL((loss_g_large_kernel<TYPE>), dim3(blocks), dim3(512), 0, st, w);
+        OZAKI_LOSS_TRY(hipGetLastError());
+        if (a.dH != nullptr) {
+            OZAKI_LOSS_TRY(transpose(W, a.ldw, words, a.k, nullptr, p.Wt, st));
+            ProductWork d = {};
+            d.X = p.Wt;
+            d.Y = p.G;
+            d.ldx = d.ldy = padded(words) * 2;
+            d.bytes = words * 2;
+            d.m = a.tokens;
+            d.n = a.k;
+            d.steps = (int)div_up(d.bytes, STEP_BYTES);
+            d.splits = product_splits(d.m, d.n, d.steps);
+            d.D = a.dH;
+            d.ldd = a.lddh;
+            d.scale = p.scale + 1;
+            d.partial = joined || d.splits > 1 ? p.partial : nullptr;
+            OZAKI_LOSS_TRY((launch_product<TYPE>(d, shape_for(d.m, d.n), st)));
+            if (d.partial != nullptr) {
+                const int64_t blocks_j = div_up(d.m * d.n, 256);
+                hipLaunchKernelGGL((loss_product_join_kernel<TYPE>), dim3((unsigned)(blocks_j < 4096 ? blocks_j : 4096)), dim3(256), 0, st, p.partial, d.splits,
+                                   d.m, d.n, p.sum, first == 0, first + piece >= a.vocab, d.scale, a.dH, a.lddh);
+                OZAKI_LOSS_TRY(hipGetLastError());
+            }
+        }
+        if (a.dW != nullptr) {
+            ProductWork d = {};
+            d.X = p.Ht;
+            d.Y = p.Gt;
+            d.ldx = d.ldy = padded(a.tokens) * 2;
+            d.bytes = a.tokens * 2;
+            d.m = words;
+            d.n = a.k;
+            d.steps = (int)div_up(d.bytes, STEP_BYTES);
+            d.splits = 1;
+            d.D = static_cast<uint8_t*>(a.dW) + first * a.lddw * 2;
+            d.ldd = a.lddw;
+            d.scale = p.scale + 1;
+            OZAKI_LOSS_TRY((launch_product<TYPE>(d, shape_for(d.m, d.n), st)));
+        }
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+size_t loss_bytes(int64_t tokens, int64_t vocab) {
+    return 256 + up((size_t)tokens * 4) + up((size_t)div_up(vocab, tile_n(shape_for(tokens, vocab))) * tokens * sizeof(float2));
+}
+size_t loss_grad_bytes(int64_t tokens, int64_t vocab, int64_t k, int64_t piece) { return grad_places(nullptr, tokens, vocab, k, piece).total; }
+
+// As few pieces as keep one piece's g, [token][word] and [word][token], and its transposed weights within 1 GiB, all of a length.
+int64_t loss_grad_piece(int64_t tokens, int64_t vocab, int64_t k) {
+    const int64_t per_word = 2 * (2 * padded(tokens) + k), fits = ((int64_t)1 << 30) / per_word, most = fits < LOSS_PIECE ? LOSS_PIECE : fits;
+    const int64_t piece = padded(div_up(vocab, div_up(vocab, most)));
+    return piece < LOSS_PIECE ? LOSS_PIECE : piece;
+}
+
+hipError_t launch_zero_rows(void* D, int64_t rows, int64_t k, int64_t ldd, hipStream_t st) {
+    const int64_t blocks = div_up(rows * k, 256);
+    hipLaunchKernelGGL(zero_rows_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, st, static_cast<uint16_t*>(D), rows, k, ldd);
+    return hipGetLastError();
+}
+hipError_t launch_linear_loss(const LossArgs& a, int type, uint8_t* ws, hipStream_t st) {
+    return type == TYPE_F16 ? forward_typed<TYPE_F16>(a, ws, st) : forward_typed<TYPE_BF16>(a, ws, st);
+}
+hipError_t launch_linear_loss_grad(const LossArgs& a, int type, int64_t piece, uint8_t* ws, hipStream_t st) {
+    return type == TYPE_F16 ? grad_typed<TYPE_F16>(a, piece, ws, st) : grad_typed<TYPE_BF16>(a, piece, ws, st);
+}
+
+}  // namespace ozaki

@@ -1,0 +1,279 @@
+"""ozaki_linear_loss and ozaki_linear_loss_grad against their definitions in 64 bits, within bounds of their 32-bit sums and of the 16 bits of g."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import low_precision as plain  # noqa: E402
+from paper_2508_00441_amd import binding as lib, device  # noqa: E402
+
+SHAPES = [(1, 1, 1), (1, 1000, 64), (3, 5, 8), (7, 513, 100), (16, 2000, 257), (17, 300, 72), (33, 129, 640), (64, 4099, 128), (65, 1000, 33), (200, 3001, 200),
+          (257, 255, 1000), (300, 511, 64)]
+EXP = 2.0 ** -20                                                    # relative, of an exponential, a logarithm and the sums around them
+
+
+class Problem:
+    def __init__(self, tokens, vocab, k, type, seed, ignored=0.2, spread=2.0, ignore=-100):
+        gen = torch.Generator().manual_seed(seed)
+        dtype = plain.DTYPES[type]
+        self.tokens, self.vocab, self.k, self.type, self.ignore = tokens, vocab, k, type, ignore
+        self.h = torch.randn((tokens, k), generator=gen).to(dtype)
+        self.w = (torch.randn((vocab, k), generator=gen) * spread / k ** 0.5).to(dtype)
+        self.targets = torch.randint(0, vocab, (tokens,), generator=gen)
+        self.targets[torch.rand((tokens,), generator=gen) < ignored] = ignore
+        self.dloss = torch.randn((tokens,), generator=gen)
+        self.upload()
+
+    def upload(self):
+        self.H, self.W = plain.padded(self.h, 8, float("nan")).cuda(), plain.padded(self.w, 8, float("nan")).cuda()
+        self.T = self.targets.cuda()
+
+    def arguments(self):
+        return (self.tokens, self.vocab, self.k, self.H, self.H.shape[1], self.W, self.W.shape[1], lib.TYPES[self.type], self.T, self.ignore)
+
+    def forward(self):
+        loss, lse = (torch.full((self.tokens,), float("nan"), device="cuda") for _ in range(2))
+        lib.ozaki_linear_loss(*self.arguments(), loss, lse)
+        return loss, lse
+
+    def gradient(self, lse, ldh=None, ldw=None, want=("dh", "dw")):
+        dtype = plain.DTYPES[self.type]
+        dh = torch.full((self.tokens, ldh or self.k), float("nan"), dtype=dtype, device="cuda") if "dh" in want else None
+        dw = torch.full((self.vocab, ldw or self.k), float("nan"), dtype=dtype, device="cuda") if "dw" in want else None
+        lib.ozaki_linear_loss_grad(*self.arguments(), lse, self.dloss.cuda(), dh, ldh or self.k, dw, ldw or self.k)
+        return dh, dw
+
+    def gradient_bounds(self, lse):
+        """(the gradient, what the result may be off) of H, and of W."""
+        want_h, want_w, g, p, h = plain.loss_gradient(self.h, self.w, self.targets, self.ignore, lse.cpu(), self.dloss)
+        u, tiny = plain.ROUNDING[self.type]
+        # of g: its rounding (FP16: also where it runs out of normal numbers, half of 2^-24 where the largest |dloss| is 2^11), z's and the exponential's errors
+        dg = u * g.abs() + p * ((plain.logit_error(h, self.w) + EXP).unsqueeze(1) * (1 + u))
+        if self.type == "f16":
+            dg = dg + 2.0 ** -36 * float(torch.where(self.targets == self.ignore, 0.0, self.dloss).abs().max())
+        w, h = self.w.double().abs(), h.abs()
+        out = []
+        for want, by, other, terms in ((want_h, dg, w, self.vocab + 40), (want_w, dg.t(), h, self.tokens + 4)):
+            size = g.abs() if by is dg else g.abs().t()
+            bound = by @ other + 2 * terms * 2.0 ** -24 * ((size + by) @ other)
+            out.append((want, bound + u * (want.abs() + bound) + tiny))
+        return out
+
+    def check_gradient(self, dh, dw, lse):
+        for got, (want, bound) in zip((dh, dw), self.gradient_bounds(lse)):
+            if got is not None:
+                assert bool(torch.all((got[:, : self.k].cpu().double() - want).abs() <= bound))
+
+
+@pytest.fixture()
+def workspace():
+    ws = device.Workspace(256 << 20)
+    yield ws
+    ws.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("type", ["bf16", "f16"])
+@pytest.mark.parametrize("tokens,vocab,k", SHAPES + [(2500, 3000, 136)])
+def test_loss(tokens, vocab, k, type, workspace):
+    x = Problem(tokens, vocab, k, type, tokens + vocab + k)
+    loss, lse = x.forward()
+    assert lib.ozaki_last_device_status() == 0
+    want, want_lse, _ = plain.loss_forward(x.h, x.w, x.targets, x.ignore)
+    bound = plain.logit_error(x.h, x.w) + EXP * (1 + want_lse.abs())
+    assert bool(torch.all((lse.cpu().double() - want_lse).abs() <= bound))
+    assert bool(torch.all((loss.cpu().double() - want).abs() <= 2 * bound + 2.0 ** -23 * want.abs()))
+    assert bool(torch.all(loss.cpu()[x.targets == x.ignore] == 0.0))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("type", ["bf16", "f16"])
+@pytest.mark.parametrize("tokens,vocab,k", SHAPES + [(1500, 6000, 136)])
+def test_gradient(tokens, vocab, k, type, workspace):
+    x = Problem(tokens, vocab, k, type, tokens + vocab + k)
+    _, lse = x.forward()
+    dh, dw = x.gradient(lse)
+    x.check_gradient(dh, dw, lse)
+    assert bool(torch.all(dh[(x.T == x.ignore)] == 0.0))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("type", ["bf16", "f16"])
+def test_gradient_in_pieces_and_one_result_at_a_time(type):
+    x = Problem(150, 2900, 200, type, 1)
+    least, best = (lib.ozaki_linear_loss_workspace_bytes(x.tokens, x.vocab, x.k, True, m) for m in (True, False))
+    assert 0 < least < best
+    for size in (best, (least + best) // 2, least):
+        ws = device.Workspace(size)
+        _, lse = x.forward()
+        dh, dw = x.gradient(lse)
+        x.check_gradient(dh, dw, lse)
+        only_h, only_w = x.gradient(lse, want=("dh",))[0], x.gradient(lse, want=("dw",))[1]
+        assert torch.equal(only_h, dh) and torch.equal(only_w, dw)
+        ws.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("type", ["bf16", "f16"])
+def test_results_inside_larger_ones(type, workspace):
+    x = Problem(70, 400, 99, type, 2)
+    _, lse = x.forward()
+    dh, dw = x.gradient(lse, ldh=103, ldw=117)
+    x.check_gradient(dh, dw, lse)
+    assert bool(torch.isnan(dh[:, 99:]).all()) and bool(torch.isnan(dw[:, 99:]).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("type", ["bf16", "f16"])
+@pytest.mark.parametrize("tokens", [20, 300])
+def test_what_ignored_tokens_hold_does_not_matter(tokens, type, workspace):
+    x = Problem(tokens, 700, 128, type, 3, ignored=0.5)
+    gone = x.targets == x.ignore
+    x.h[gone] = float("nan")
+    x.h[gone.nonzero()[0, 0]] = float("inf")
+    x.dloss[gone] = float("nan")
+    x.upload()
+    loss, lse = x.forward()
+    assert bool(torch.all(loss[gone.cuda()] == 0.0)) and bool(torch.isfinite(loss).all())
+    dh, dw = x.gradient(lse)
+    x.check_gradient(dh, dw, torch.where(gone, 0.0, lse.cpu()))
+    assert lib.ozaki_last_device_status() == 0
+
+
+@pytest.mark.gpu
+def test_all_tokens_ignored_and_none_at_all(workspace):
+    x = Problem(40, 300, 64, "bf16", 4, ignored=1.1)
+    loss, lse = x.forward()
+    dh, dw = x.gradient(lse)
+    assert bool(torch.all(loss == 0.0)) and bool(torch.all(dh == 0.0)) and bool(torch.all(dw == 0.0))
+    dw.fill_(3.0)
+    lib.ozaki_linear_loss(0, 300, 64, None, 64, None, 64, lib.TYPE_BF16, None, -100, None, None)
+    lib.ozaki_linear_loss_grad(0, 300, 64, None, 64, None, 64, lib.TYPE_BF16, None, -100, None, None, None, 0, dw, 64)
+    assert bool(torch.all(dw == 0.0))
+
+
+@pytest.mark.gpu
+def test_targets_outside_the_vocabulary(workspace):
+    x = Problem(50, 300, 64, "bf16", 5, ignored=0.0)
+    good, lse = x.forward()
+    bad = torch.tensor([3, 17, 49])
+    x.targets[bad] = torch.tensor([300, -1, 1 << 40])
+    x.upload()
+    loss, lse = x.forward()
+    assert lib.ozaki_last_device_status() == lib.STATUS_TARGET and lib.ozaki_last_device_status() == 0
+    fine = torch.ones(50, dtype=torch.bool)
+    fine[bad] = False
+    assert bool(torch.isnan(loss.cpu()[bad]).all()) and torch.equal(loss.cpu()[fine], good.cpu()[fine])
+    dh, dw = x.gradient(lse)
+    assert lib.ozaki_last_device_status() == lib.STATUS_TARGET
+    x.targets[bad] = x.ignore
+    x.check_gradient(dh, dw, lse)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens", [5, 400])
+def test_outputs_far_apart_and_at_infinity(tokens, workspace):
+    """Words whose output is minus infinity have no share; a token whose outputs are hundreds apart has a loss of its target's distance."""
+    x = Problem(tokens, 900, 64, "bf16", 6, spread=200.0, ignored=0.0)
+    x.h[:, 0] = 1.0
+    x.w[10:800, 0] = -float("inf")
+    x.targets[x.targets >= 10] = 3
+    x.upload()
+    loss, lse = x.forward()
+    want, want_lse, _ = plain.loss_forward(x.h, x.w, x.targets, x.ignore)
+    finite = x.w.clone()
+    finite[10:800, 0] = 0.0
+    bound = plain.logit_error(x.h, finite) + EXP * (1 + want_lse.abs())
+    assert bool(torch.all((lse.cpu().double() - want_lse).abs() <= bound))
+    assert bool(torch.all((loss.cpu().double() - want).abs() <= 2 * bound + 2.0 ** -23 * want.abs()))
+
+
+@pytest.mark.gpu
+def test_small_upstream_gradients_in_16_bit_floats(workspace):
+    """A mean over very many tokens: dloss alone would take g below FP16's smallest number; the result itself is what may underflow."""
+    x = Problem(130, 2000, 256, "f16", 7, ignored=0.0)
+    x.dloss = torch.full((130,), 1e-5)
+    _, lse = x.forward()
+    dh, dw = x.gradient(lse)
+    x.check_gradient(dh, dw, lse)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("type", ["bf16", "f16"])
+def test_gradient_against_differences(type, workspace):
+    """Central differences of the 64-bit loss along random directions, whose own error is of the third derivative's size times the step squared."""
+    x = Problem(40, 500, 96, type, 8)
+    _, lse = x.forward()
+    dh, dw = x.gradient(lse)
+    gen = torch.Generator().manual_seed(80)
+
+    def total(h, w):
+        return float((plain.loss_forward(h, w, x.targets, x.ignore)[0] * torch.where(x.targets == x.ignore, 0.0, x.dloss.double())).sum())
+
+    for which, got, (_, bound) in zip("hw", (dh, dw), x.gradient_bounds(lse)):
+        at = {"h": x.h.double(), "w": x.w.double()}
+        for _ in range(3):
+            d = torch.randn(at[which].shape, generator=gen, dtype=torch.float64)
+            e = 1e-5
+            difference = (total(**{**at, which: at[which] + e * d}) - total(**{**at, which: at[which] - e * d})) / (2 * e)
+            along = float((got.cpu().double() * d).sum())
+            # (the step's own errors: 1e-10 of third derivatives, 1e-16 of a sum of some hundred over 1e-5)
+            assert abs(along - difference) <= float((bound * d.abs()).sum()) + 1e-6
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens,vocab,k", [(1, 3000, 512), (100, 3000, 512), (1500, 5000, 64)])
+def test_the_same_bits_every_time_and_in_graphs(tokens, vocab, k, workspace):
+    x = Problem(tokens, vocab, k, "bf16", 9)
+    dloss = x.dloss.cuda()
+    loss, lse = x.forward()
+    dh, dw = x.gradient(lse)
+    out = [torch.empty_like(t) for t in (loss, lse, dh, dw)]
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        lib.ozaki_set_stream(torch.cuda.current_stream().cuda_stream)
+        lib.ozaki_linear_loss(*x.arguments(), out[0], out[1])
+        lib.ozaki_linear_loss_grad(*x.arguments(), out[1], dloss, out[2], k, out[3], k)
+    lib.ozaki_set_stream(torch.cuda.current_stream().cuda_stream)
+    for i in range(3):
+        for t in out:
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, want in zip(out, (loss, lse, dh, dw)):
+            assert torch.equal(got, want)
+        x.H[:, :k].mul_(0.5)                                        # new inputs for the next replay
+        loss, lse = x.forward()
+        dh, dw = x.gradient(lse)
+
+
+P = 1 << 20
+FORWARD = dict(tokens=100, vocab=200, k=30, H=P, ldh=32, W=P, ldw=32, type=lib.TYPE_BF16, targets=P, ignore=-100, loss=P, lse=P)
+SHARED = [(1, dict(tokens=-1)), (1, dict(tokens=lib.MAX_EXTENT + 1)), (2, dict(vocab=0)), (2, dict(vocab=lib.MAX_EXTENT + 1)), (3, dict(k=0)),
+          (3, dict(k=lib.MAX_EXTENT)), (4, dict(H=None)), (4, dict(H=P + 8)), (5, dict(ldh=24)), (5, dict(ldh=36)), (6, dict(W=None)), (6, dict(W=P + 2)),
+          (7, dict(ldw=24)), (7, dict(ldw=33)), (8, dict(type=lib.TYPE_F32)), (8, dict(type=3)), (9, dict(targets=None))]
+
+
+@pytest.mark.parametrize("position,arguments", SHARED + [(11, dict(loss=None)), (12, dict(lse=None))])
+def test_refusals_of_the_loss(position, arguments):
+    assert lib.ozaki_linear_loss(**{**FORWARD, **arguments}, check=False) == -position
+
+
+@pytest.mark.parametrize("position,arguments", SHARED + [(11, dict(lse=None)), (12, dict(dloss=None)), (13, dict(dH=None, dW=None)), (13, dict(dH=P + 1)),
+                                                         (14, dict(lddh=29)), (15, dict(dW=P + 1)), (16, dict(lddw=29))])
+def test_refusals_of_the_gradient(position, arguments):
+    a = {n: v for n, v in FORWARD.items() if n != "loss"} | dict(dloss=P, dH=P, lddh=30, dW=P, lddw=30)
+    assert lib.ozaki_linear_loss_grad(**{**a, **arguments}, check=False) == -position
+
+
+def test_without_work_memory():
+    assert lib.ozaki_linear_loss_workspace_bytes(0, 200, 30, False, False) == 0 and lib.ozaki_linear_loss_workspace_bytes(100, 200, 30, False, False) > 0
+    context = lib.ozaki_context_create()
+    lib.ozaki_context_use(context)
+    try:
+        assert lib.ozaki_linear_loss(**FORWARD, check=False) == lib.STATUS_WORKSPACE
+        a = {n: v for n, v in FORWARD.items() if n != "loss"} | dict(dloss=P, dH=P, lddh=30, dW=P, lddw=30)
+        assert lib.ozaki_linear_loss_grad(**a, check=False) == lib.STATUS_WORKSPACE
+    finally:
+        lib.ozaki_context_use(None)
+        lib.ozaki_context_destroy(context)
