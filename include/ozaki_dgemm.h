@@ -359,7 +359,7 @@ enum {
 
 /* Quantises X (rows vectors of k elements of `type`) to OCP E4M3.  For each block, a being the largest finite magnitude in it
  * and at least 2^-100:
- *     scale = a / 448        code = E4M3(x * (448 / a)), to nearest, ties to even; NaN where x is not finite.
+ *     scale = a / 448        code = E4M3(x * 448 / a), rounded once, to nearest, ties to even; NaN where x is not finite.
  *   Q, ldq    codes of X's vectors, one byte each; may be null (then so is S)
  *   S, lds    scales, S[(e / 128) * lds + i] for vector i, with OZAKI_SCALE_BLOCKS S[(e / 128) * lds + i / 128]; lds is at least
  *             the number of vectors or of blocks of vectors

@@ -9,8 +9,10 @@
 // sums over 16-bit elements in FP32 on the matrix unit (tile_product.hpp) and want both operands contiguous along the inner
 // dimension, hence also a transposed H and a transposed piece of W.
 //
-// FP16's smallest normal number is 2^-14, and g of a word that is unlikely lies far below: g is held times a power of two that takes the
-// largest |dloss| to 2^11 .. 2^12, and the products are scaled back in FP32.
+// What is held of g is (exp(z - lse) - [v == target]) * 2^12, without dloss.  Its largest entries, the targets', are then near a power of two
+// and lose nothing to 16 bits; times dloss they all lose alike, which does not average out (1.7 times the error of the result's own
+// rounding in FP16).  2^12 keeps the words down to a probability of 2^-26 among FP16's normal numbers.  dloss comes in where it costs no
+// rounding: as a factor of the rows of dH, and for dW with the transposed H, times dloss over the largest |dloss|, which is one for a mean.
 #include "layout.hpp"
 #include "tile_product.hpp"
 
@@ -24,9 +26,9 @@ __device__ __forceinline__ float log_of(float x) { return __builtin_amdgcn_logf(
 // per token, what a tile of z needs
 struct TokenState {
     const float* lse;
-    const float* factor;     // dloss times the power of two, 0 where the token does not count
     const int* target;       // -1 where it does not count
 };
+constexpr float HELD = 4096.0f;          // what g is held times
 
 struct LogitWork {
     const uint8_t* H;
@@ -136,43 +138,32 @@ __global__ void __launch_bounds__(256) loss_join_kernel(const float2* part, cons
     if (counts && !real) atomicOr(flags, TARGET_FLAG);
 }
 
-// Gradient, in front of everything: what counts of every token, and the power of two that g is held times (scale[0], its inverse scale[1]).
-template <int TYPE>
+// Gradient, in front of everything: every token's target, its factor of dH's row, its share of dW relative to the largest, and the factor of dW.
 __global__ void __launch_bounds__(1024) loss_tokens_kernel(const int64_t* targets, const float* dloss, int64_t tokens, int64_t vocab,
-                                                           int64_t ignore, float* factor, int* target_out, float* scale, int* flags) {
+                                                           int64_t ignore, int* target_out, float* row_factor, float* share, float* dw_factor, int* flags) {
     __shared__ float shared_most[16];
-    float up = 1.0f;
-    if constexpr (TYPE == TYPE_F16) {
-        float most = 0.0f;
-        for (int64_t t = threadIdx.x; t < tokens; t += 1024)
-            if (targets[t] != ignore) {
-                const float d = fabsf(dloss[t]);
-                most = d < __builtin_inff() ? fmaxf(most, d) : most;
-            }
-#pragma unroll
-        for (int s = 1; s < 64; s <<= 1) most = fmaxf(most, __shfl_xor(most, s));
-        if ((threadIdx.x & 63) == 0) shared_most[threadIdx.x >> 6] = most;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 16; ++i) most = fmaxf(most, shared_most[i]);
-        int e = 12;
-        if (most > 0.0f) {
-            e = 12 - (((__float_as_int(most) >> 23) & 0xFF) - 126);   // most < 2^(its exponent + 1)
-            e = e < -100 ? -100 : e > 100 ? 100 : e;
+    float most = 0.0f;
+    for (int64_t t = threadIdx.x; t < tokens; t += 1024)
+        if (targets[t] != ignore) {
+            const float d = fabsf(dloss[t]);
+            most = d < __builtin_inff() ? fmaxf(most, d) : most;
         }
-        up = __int_as_float((e + 127) << 23);
-    }
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) most = fmaxf(most, __shfl_xor(most, s));
+    if ((threadIdx.x & 63) == 0) shared_most[threadIdx.x >> 6] = most;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) most = fmaxf(most, shared_most[i]);
+    if (most == 0.0f) most = 1.0f;
     for (int64_t t = threadIdx.x; t < tokens; t += 1024) {
         const int64_t target = targets[t];
-        const bool counts = target != ignore, real = target >= 0 && target < vocab;
-        if (counts && !real) atomicOr(flags, TARGET_FLAG);
-        factor[t] = counts && real ? dloss[t] * up : 0.0f;
-        target_out[t] = counts && real ? (int)target : -1;
+        const bool wanted = target != ignore, counts = wanted && target >= 0 && target < vocab;
+        if (wanted && !counts) atomicOr(flags, TARGET_FLAG);
+        target_out[t] = counts ? (int)target : -1;
+        row_factor[t] = counts ? dloss[t] * (1.0f / HELD) : 0.0f;
+        share[t] = counts ? dloss[t] / most : 0.0f;
     }
-    if (threadIdx.x == 0) {
-        scale[0] = up;
-        scale[1] = 1.0f / up;
-    }
+    if (threadIdx.x == 0) *dw_factor = most * (1.0f / HELD);
 }
 
 // A tile of g: through LDS, [token][word], so that both results are written in pieces of 16 bytes.
@@ -192,7 +183,7 @@ __device__ __forceinline__ void loss_g_body(const LogitWork& w) {
         const int t = (wm * P::FM + j) * 16 + (lane & 15);
         const bool real = m0 + t < w.tokens;
         const int target = real ? w.token.target[m0 + t] : -1;
-        const float factor = target >= 0 ? w.token.factor[m0 + t] : 0.0f, lse = target >= 0 ? w.token.lse[m0 + t] : 0.0f;
+        const float lse = target >= 0 ? w.token.lse[m0 + t] : 0.0f;
         const int at = target >= 0 ? (int)(target - w.first_word - n0) : -1;
 #pragma unroll
         for (int i = 0; i < P::FN; ++i) {
@@ -201,7 +192,7 @@ __device__ __forceinline__ void loss_g_body(const LogitWork& w) {
             for (int r = 0; r < 4; ++r) {
                 const int word = first + 16 * i + r;
                 const float p = exp_of(acc[i][j][r] - lse) - (word == at ? 1.0f : 0.0f);
-                v[r] = (T)(target >= 0 && word < words ? p * factor : 0.0f);
+                v[r] = (T)(target >= 0 && word < words ? p * HELD : 0.0f);
             }
             *reinterpret_cast<four*>(lds + t * STRIDE + (first + 16 * i) * 2) = v;
         }
@@ -230,15 +221,19 @@ __device__ __forceinline__ void loss_g_body(const LogitWork& w) {
     }
 }
 
-// [row][column] -> [column][row] of 16-bit elements, 64 x 64 at a time; rows beyond the matrix, and rows that `counts` marks with -1, are zeros.
-__global__ void __launch_bounds__(256) loss_transpose_kernel(const uint16_t* from, int64_t ld, int64_t rows, int64_t columns, const int* counts,
-                                                             uint16_t* to, int64_t ldt) {
-    __shared__ uint16_t tile[64][66];
+// [row][column] -> [column][row], 64 x 64 at a time, zeros for rows beyond the matrix; rows times `share` if there is one, where those
+// of tokens that do not count (counts[row] < 0) are zeros whatever they hold.
+template <typename T>
+__device__ __forceinline__ void transpose_body(const T* from, int64_t ld, int64_t rows, int64_t columns, const int* counts, const float* share, T* to,
+                                               int64_t ldt) {
+    __shared__ T tile[64][66];
     const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 64;
     const int in = threadIdx.x & 63;
     for (int i = threadIdx.x >> 6; i < 64; i += 4) {
         const bool real = r0 + i < rows && c0 + in < columns && (counts == nullptr || counts[r0 + i] >= 0);
-        tile[i][in] = real ? from[(r0 + i) * ld + c0 + in] : (uint16_t)0;
+        T x = real ? from[(r0 + i) * ld + c0 + in] : (T)0.0f;
+        if (real && share != nullptr) x = (T)((float)x * share[r0 + i]);
+        tile[i][in] = x;
     }
     __syncthreads();
     for (int i = threadIdx.x >> 6; i < 64; i += 4)
@@ -255,7 +250,8 @@ struct ProductWork {
     WorkOrder order;
     void* D;
     int64_t ldd;
-    const float* scale;      // what the sums are multiplied by
+    const float* row_factor; // what the sums are multiplied by: one for every row of D, or
+    const float* factor;     // the same for all
     float* partial;          // not null: unscaled sums go there, [split][m][n]
 };
 
@@ -286,13 +282,13 @@ __device__ __forceinline__ void loss_product_body(const ProductWork& w) {
         }
         return;
     }
-    const float scale = *w.scale;
     T* const D = static_cast<T*>(w.D);
     const bool wide = w.ldd % 4 == 0 && reinterpret_cast<uintptr_t>(D) % 8 == 0;
 #pragma unroll
     for (int j = 0; j < P::FM; ++j) {
         const int64_t m = m0 + (wm * P::FM + j) * 16 + (lane & 15);
         if (m >= w.m) continue;
+        const float scale = w.row_factor != nullptr ? w.row_factor[m] : *w.factor;
 #pragma unroll
         for (int i = 0; i < P::FN; ++i) {
             const int64_t n = n0 + (wn * P::FN + i) * 16 + 4 * (lane >> 4);
@@ -304,11 +300,11 @@ __device__ __forceinline__ void loss_product_body(const ProductWork& w) {
 // The sums of a piece's shares of the inner dimension, on top of the pieces' before it (`sum`, unless it is the first); the last piece's go to D.
 template <typename T>
 __device__ __forceinline__ void join_body(const float* partial, int splits, int64_t m, int64_t n, float* sum, bool first, bool last,
-                                          const float* scale, T* D, int64_t ldd) {
+                                          const float* row_factor, T* D, int64_t ldd) {
     for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < m * n; at += (int64_t)gridDim.x * 256) {
         float s = first ? 0.0f : sum[at];
         for (int i = 0; i < splits; ++i) s += partial[(int64_t)i * m * n + at];
-        if (last) D[at / n * ldd + at % n] = (T)(s * *scale);
+        if (last) D[at / n * ldd + at % n] = (T)(s * row_factor[at / n]);
         else sum[at] = s;
     }
 }
@@ -342,8 +338,15 @@ template <int TYPE>
 __global__ void __launch_bounds__(256) loss_product_few_kernel(const ProductWork w) { loss_product_body<FewTile<TYPE>, typename Element<TYPE>::type>(w); }
 template <int TYPE>
 __global__ void __launch_bounds__(256) loss_product_join_kernel(const float* partial, int splits, int64_t m, int64_t n, float* sum, bool first, bool last,
-                                                                const float* scale, void* D, int64_t ldd) {
-    join_body(partial, splits, m, n, sum, first, last, scale, static_cast<typename Element<TYPE>::type*>(D), ldd);
+                                                                const float* row_factor, void* D, int64_t ldd) {
+    join_body(partial, splits, m, n, sum, first, last, row_factor, static_cast<typename Element<TYPE>::type*>(D), ldd);
+}
+
+template <int TYPE>
+__global__ void __launch_bounds__(256) loss_transpose_kernel(const void* from, int64_t ld, int64_t rows, int64_t columns, const int* counts, const float* share,
+                                                             void* to, int64_t ldt) {
+    typedef typename Element<TYPE>::type T;
+    transpose_body(static_cast<const T*>(from), ld, rows, columns, counts, share, static_cast<T*>(to), ldt);
 }
 
 // ---- shapes and work memory ------------------------------------------------------------------------------------
@@ -367,8 +370,9 @@ constexpr int64_t EDGE = 256;            // what g is padded to, with zeros
 int64_t padded(int64_t n) { return div_up(n, EDGE) * EDGE; }
 
 struct GradPlaces {
-    float* scale;
-    float* factor;
+    float* dw_factor;
+    float* row_factor;
+    float* share;
     int* target;
     uint8_t* Ht;
     uint8_t* Wt;
@@ -384,8 +388,9 @@ GradPlaces grad_places(uint8_t* ws, int64_t tokens, int64_t vocab, int64_t k, in
     auto take = [&](size_t bytes) { uint8_t* const here = ws + at; at += up(bytes); return here; };
     const int64_t words = piece < vocab ? piece : vocab;
     const int splits = product_splits(tokens, k, div_up(words * 2, STEP_BYTES));
-    p.scale = reinterpret_cast<float*>(take(8));
-    p.factor = reinterpret_cast<float*>(take((size_t)tokens * 4));
+    p.dw_factor = reinterpret_cast<float*>(take(4));
+    p.row_factor = reinterpret_cast<float*>(take((size_t)tokens * 4));
+    p.share = reinterpret_cast<float*>(take((size_t)tokens * 4));
     p.target = reinterpret_cast<int*>(take((size_t)tokens * 4));
     p.Ht = take((size_t)k * padded(tokens) * 2);
     p.Wt = take((size_t)k * padded(words) * 2);
@@ -446,19 +451,20 @@ hipError_t forward_typed(const LossArgs& a, uint8_t* ws, hipStream_t st) {
 
 #define OZAKI_LOSS_TRY(expr) do { const hipError_t e_ = (expr); if (e_ != hipSuccess) return e_; } while (0)
 
-hipError_t transpose(const void* from, int64_t ld, int64_t rows, int64_t columns, const int* counts, uint8_t* to, hipStream_t st) {
-    hipLaunchKernelGGL(loss_transpose_kernel, dim3((unsigned)(padded(rows) / 64), (unsigned)div_up(columns, 64)), dim3(256), 0, st,
-                       static_cast<const uint16_t*>(from), ld, rows, columns, counts, reinterpret_cast<uint16_t*>(to), padded(rows));
+template <int TYPE>
+hipError_t transpose(const void* from, int64_t ld, int64_t rows, int64_t columns, const int* counts, const float* share, uint8_t* to, hipStream_t st) {
+    hipLaunchKernelGGL((loss_transpose_kernel<TYPE>), dim3((unsigned)(padded(rows) / 64), (unsigned)div_up(columns, 64)), dim3(256), 0, st, from, ld, rows,
+                       columns, counts, share, to, padded(rows));
     return hipGetLastError();
 }
 
 template <int TYPE>
 hipError_t grad_typed(const LossArgs& a, int64_t piece, uint8_t* ws, hipStream_t st) {
     const GradPlaces p = grad_places(ws, a.tokens, a.vocab, a.k, piece);
-    hipLaunchKernelGGL((loss_tokens_kernel<TYPE>), dim3(1), dim3(1024), 0, st, a.targets, a.dloss, a.tokens, a.vocab, a.ignore, p.factor, p.target,
-                       p.scale, a.flags);
+    hipLaunchKernelGGL(loss_tokens_kernel, dim3(1), dim3(1024), 0, st, a.targets, a.dloss, a.tokens, a.vocab, a.ignore, p.target, p.row_factor, p.share,
+                       p.dw_factor, a.flags);
     OZAKI_LOSS_TRY(hipGetLastError());
-    if (a.dW != nullptr) OZAKI_LOSS_TRY(transpose(a.H, a.ldh, a.tokens, a.k, p.target, p.Ht, st));
+    if (a.dW != nullptr) OZAKI_LOSS_TRY(transpose<TYPE>(a.H, a.ldh, a.tokens, a.k, p.target, p.share, p.Ht, st));
     const bool joined = piece < a.vocab;
     for (int64_t first = 0; first < a.vocab; first += piece) {
         const int64_t words = a.vocab - first < piece ? a.vocab - first : piece;
@@ -474,7 +480,7 @@ hipError_t grad_typed(const LossArgs& a, int64_t piece, uint8_t* ws, hipStream_t
         w.first_word = first;
         const int shape = shape_for(a.tokens, words);
         set_tiles(w, shape);
-        w.token = TokenState{a.lse_in, p.factor, p.target};
+        w.token = TokenState{a.lse_in, p.target};
         w.G = a.dH != nullptr ? p.G : nullptr;
         w.Gt = a.dW != nullptr ? p.Gt : nullptr;
         w.ldg = padded(words);
@@ -485,7 +491,7 @@ hipError_t grad_typed(const LossArgs& a, int64_t piece, uint8_t* ws, hipStream_t
         else hipLaunchKernelGGL((loss_g_large_kernel<TYPE>), dim3(blocks), dim3(512), 0, st, w);
         OZAKI_LOSS_TRY(hipGetLastError());
         if (a.dH != nullptr) {
-            OZAKI_LOSS_TRY(transpose(W, a.ldw, words, a.k, nullptr, p.Wt, st));
+            OZAKI_LOSS_TRY(transpose<TYPE>(W, a.ldw, words, a.k, nullptr, nullptr, p.Wt, st));
             ProductWork d = {};
             d.X = p.Wt;
             d.Y = p.G;
@@ -497,13 +503,13 @@ hipError_t grad_typed(const LossArgs& a, int64_t piece, uint8_t* ws, hipStream_t
             d.splits = product_splits(d.m, d.n, d.steps);
             d.D = a.dH;
             d.ldd = a.lddh;
-            d.scale = p.scale + 1;
+            d.row_factor = p.row_factor;
             d.partial = joined || d.splits > 1 ? p.partial : nullptr;
             OZAKI_LOSS_TRY((launch_product<TYPE>(d, shape_for(d.m, d.n), st)));
             if (d.partial != nullptr) {
                 const int64_t blocks_j = div_up(d.m * d.n, 256);
                 hipLaunchKernelGGL((loss_product_join_kernel<TYPE>), dim3((unsigned)(blocks_j < 4096 ? blocks_j : 4096)), dim3(256), 0, st, p.partial, d.splits,
-                                   d.m, d.n, p.sum, first == 0, first + piece >= a.vocab, d.scale, a.dH, a.lddh);
+                                   d.m, d.n, p.sum, first == 0, first + piece >= a.vocab, d.row_factor, a.dH, a.lddh);
                 OZAKI_LOSS_TRY(hipGetLastError());
             }
         }
@@ -519,7 +525,7 @@ hipError_t grad_typed(const LossArgs& a, int64_t piece, uint8_t* ws, hipStream_t
             d.splits = 1;
             d.D = static_cast<uint8_t*>(a.dW) + first * a.lddw * 2;
             d.ldd = a.lddw;
-            d.scale = p.scale + 1;
+            d.factor = p.dw_factor;
             OZAKI_LOSS_TRY((launch_product<TYPE>(d, shape_for(d.m, d.n), st)));
         }
     }

@@ -1,9 +1,10 @@
 // Quantisation to OCP E4M3 with a 32-bit scale for each block of 128 elements of a vector, or for each 128 x 128 square.
 //
-// For a block with the largest finite magnitude a (at least 2^-100, so that neither factor below leaves the normal range):
-//     scale = a / 448,     code = E4M3(x * (448 / a)),  rounded to nearest, ties to even.
-// 448 is the largest value of E4M3; the two roundings in front of the conversion leave x * (448 / a) at most 2^-22 above it, which still
-// rounds to it.  An element that is not finite gets the code NaN and does not count for the scale, so one of them spoils only itself.
+// For a block with the largest finite magnitude a (at least 2^-100):
+//     scale = a / 448, rounded to 32 bits,     code = E4M3(x * 448 / a), rounded once, to nearest, ties to even.
+// 448 is the largest value of E4M3.  The quotient is rounded once (of_block): a tie between two codes is common with 16-bit elements
+// (a and x have 8 or 11 significant bits), and x times a rounded 448 / a would decide it by that factor's error.  An element that is not
+// finite gets the code NaN and does not count for the scale, so one of them spoils only itself.
 //
 // The scales lie [block of the inner dimension][vector]: a product's step over 128 elements then reads the scales of neighbouring
 // vectors as one contiguous piece.
@@ -25,17 +26,46 @@ __device__ __forceinline__ float finite_magnitude(T x) {
     return a < __builtin_inff() ? a : 0.0f;                  // (false for NaN too)
 }
 
-// codes of eight values, the first in the lowest byte
-__device__ __forceinline__ v2i32 codes_of(const float (&x)[8], float factor) {
+// x * 448 / a, in a form that rounds to E4M3 as the exact quotient does: as 0.875 x over 2^-9 a, which cannot overflow.  Division by the
+// correctly rounded reciprocal with one correction gives the nearest 32-bit number.  With 16-bit elements 0.875 x is exact and no quotient
+// comes so near a tie between two codes without being it; with 32-bit ones it may, and the quotient is then made odd (in its last
+// bit) on the side of the exact one, which is never a tie.
+struct Divisor {
+    float a, inverse;
+    __device__ __forceinline__ explicit Divisor(float amax) : a(amax * 0.001953125f), inverse(1.0f / (amax * 0.001953125f)) {}
+};
+template <typename T>
+__device__ __forceinline__ float of_block(float x, const Divisor& d) {
+    const float y = x * 0.875f, p = y * d.inverse;
+    float r = __builtin_fmaf(-p, d.a, y);
+    if constexpr (sizeof(T) == 2) return __builtin_fmaf(r, d.inverse, p);
+    const float lost = __builtin_fmaf(x, 0.875f, -y);
+    float q = __builtin_fmaf(r + lost, d.inverse, p);
+    r = __builtin_fmaf(-q, d.a, y) + lost;
+    const int bits = __float_as_int(q);
+    if (r != 0.0f && (bits & 1) == 0 && q != 0.0f) q = __int_as_float(bits + ((__float_as_int(r) ^ bits) < 0 ? -1 : 1));
+    return q;
+}
+
+// codes of eight quotients, the first in the lowest byte
+__device__ __forceinline__ v2i32 codes_of(const float (&x)[8]) {
     v2i32 q;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         int w = 0;
-        w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * h] * factor, x[4 * h + 1] * factor, w, false);
-        w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * h + 2] * factor, x[4 * h + 3] * factor, w, true);
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * h], x[4 * h + 1], w, false);
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * h + 2], x[4 * h + 3], w, true);
         q[h] = w;
     }
     return q;
+}
+template <typename T>
+__device__ __forceinline__ v2i32 quantised(const float (&x)[8], float amax) {
+    const Divisor d(amax);
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = of_block<T>(x[i], d);
+    return codes_of(y);
 }
 
 // eight elements from `at`, which is 16-byte aligned; zeros from element `left` on
@@ -84,7 +114,7 @@ __global__ void __launch_bounds__(256) quantise_vectors_kernel(const QuantiseArg
     for (int i = 0; i < 8; ++i) most = fmaxf(most, finite_magnitude(x[i]));
     most = fmaxf(row_max(most), SMALLEST_AMAX);
     if (!real) return;
-    store_eight(a.Q + row * a.ldq + e, a.k - e, codes_of(x, E4M3_MAX / most));
+    store_eight(a.Q + row * a.ldq + e, a.k - e, quantised<T>(x, most));
     if (part == 0) a.S[kb * a.lds + row] = most / E4M3_MAX;
 }
 
@@ -138,7 +168,7 @@ __global__ void __launch_bounds__(256) quantise_tile_kernel(const QuantiseArgs a
             const int64_t row = row0 + g * 8 + i;
             const float most = SCALING == SCALE_BLOCKS ? of_square : fmaxf(row_max(in_row[i]), SMALLEST_AMAX);
             if (row >= a.rows) continue;
-            store_eight(a.Q + row * a.ldq + e, left, codes_of(x[i], E4M3_MAX / most));
+            store_eight(a.Q + row * a.ldq + e, left, quantised<T>(x[i], most));
             if (SCALING == SCALE_VECTORS && part == 0) a.S[blockIdx.y * a.lds + row] = most / E4M3_MAX;
         }
         if (SCALING == SCALE_BLOCKS && threadIdx.x == 0) a.S[blockIdx.y * a.lds + blockIdx.x] = of_square / E4M3_MAX;
@@ -148,7 +178,7 @@ __global__ void __launch_bounds__(256) quantise_tile_kernel(const QuantiseArgs a
         for (int j = 0; j < 8; ++j) {
             const float most = SCALING == SCALE_BLOCKS ? of_square : in_column[j];
             const float column[8] = {x[0][j], x[1][j], x[2][j], x[3][j], x[4][j], x[5][j], x[6][j], x[7][j]};
-            *reinterpret_cast<v2i32*>(turned + (part * 8 + j) * TURNED + g * 8) = codes_of(column, E4M3_MAX / most);
+            *reinterpret_cast<v2i32*>(turned + (part * 8 + j) * TURNED + g * 8) = quantised<T>(column, most);
             if (SCALING == SCALE_VECTORS && g == 0 && j < left) a.St[blockIdx.x * a.ldst + e + j] = most / E4M3_MAX;
         }
         if (SCALING == SCALE_BLOCKS && threadIdx.x == 0) a.St[blockIdx.x * a.ldst + blockIdx.y] = of_square / E4M3_MAX;

@@ -37,13 +37,17 @@ def spread(s, rows, k, blocks):
     return s.repeat_interleave(BLOCK, 1)[:, :k]
 
 
+def to_e4m3(y):
+    """The nearest E4M3 value of 64-bit numbers up to 448 in magnitude, ties to even: steps of 2^-3 of the binade, of 2^-9 below 2^-6."""
+    step = torch.exp2(torch.floor(torch.log2(y.abs().clamp(min=2.0 ** -6))) - 3)
+    return (torch.round(y / step) * step).float().to(torch.float8_e4m3fn)
+
+
 def quantised(x, blocks):
-    """Codes (float8_e4m3fn) and scales of a CPU float32 tensor, each step rounded to 32 bits as the operator's definition says."""
+    """Codes (float8_e4m3fn) and scales of a CPU float32 tensor: the quotient in 64 bits (its numerator is exact, so that ties are ties)."""
     amax = block_amax(x, blocks)
-    factor = torch.full_like(amax, 448.0) / amax                    # (448.0 / amax would be 448 times the rounded reciprocal)
-    y = x * spread(factor, x.shape[0], x.shape[1], blocks)
-    y = torch.where(torch.isfinite(x), y, torch.full_like(y, float("nan")))
-    return y.to(torch.float8_e4m3fn), amax / 448.0
+    y = x.double() * 448.0 / spread(amax.double(), x.shape[0], x.shape[1], blocks)
+    return to_e4m3(torch.where(torch.isfinite(y), y, torch.full_like(y, float("nan")))), amax / torch.full_like(amax, 448.0)
 
 
 def dequantised(q, s, blocks):

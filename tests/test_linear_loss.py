@@ -46,15 +46,23 @@ class Problem:
         """(the gradient, what the result may be off) of H, and of W."""
         want_h, want_w, g, p, h = plain.loss_gradient(self.h, self.w, self.targets, self.ignore, lse.cpu(), self.dloss)
         u, tiny = plain.ROUNDING[self.type]
-        # of g: its rounding (FP16: also where it runs out of normal numbers, half of 2^-24 where the largest |dloss| is 2^11), z's and the exponential's errors
-        dg = u * g.abs() + p * ((plain.logit_error(h, self.w) + EXP).unsqueeze(1) * (1 + u))
+        # of g without dloss: its rounding (FP16: also where it runs out of normal numbers, half of 2^-24 below 2^-12), z's and the exponential's errors;
+        # dW's other operand is H times the token's share of the largest |dloss|, rounded where the shares differ
+        factor = torch.where(self.targets == self.ignore, 0.0, self.dloss.double()).abs().unsqueeze(1)
+        dg = u * g.abs() + p * ((plain.logit_error(h, self.w) + EXP).unsqueeze(1) * (1 + u)) + 2.0 ** -22 * g.abs()
         if self.type == "f16":
-            dg = dg + 2.0 ** -36 * float(torch.where(self.targets == self.ignore, 0.0, self.dloss).abs().max())
+            dg = dg + 2.0 ** -37 * factor
+        shares = torch.unique(factor[factor > 0])
+        dgw, least = dg, 0.0
+        if len(shares) > 1:
+            dgw = dg + u * (1 + u) * g.abs()
+            if self.type == "f16":                                  # (half the smallest step of the product of H and the share)
+                least = 2.0 ** -25 * float(factor.max()) * torch.where(factor > 0, g.abs() / factor, 0.0).sum(0).unsqueeze(1)
         w, h = self.w.double().abs(), h.abs()
         out = []
-        for want, by, other, terms in ((want_h, dg, w, self.vocab + 40), (want_w, dg.t(), h, self.tokens + 4)):
+        for want, by, other, terms in ((want_h, dg, w, self.vocab + 40), (want_w, dgw.t(), h, self.tokens + 4)):
             size = g.abs() if by is dg else g.abs().t()
-            bound = by @ other + 2 * terms * 2.0 ** -24 * ((size + by) @ other)
+            bound = by @ other + 2 * terms * 2.0 ** -24 * ((size + by) @ other) + (0.0 if by is dg else least)
             out.append((want, bound + u * (want.abs() + bound) + tiny))
         return out
 

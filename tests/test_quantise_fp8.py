@@ -1,4 +1,4 @@
-"""ozaki_quantise_fp8: codes and scales equal to the definition's, bit for bit."""
+"""ozaki_quantise_fp8: codes and scales equal to the definition's, every one of them."""
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -37,11 +37,9 @@ def _call(x, type, blocks, straight=True, transposed=False, stream=None):
 
 def _same(Q, S, x, blocks):
     q, s = plain.quantised(x.float(), blocks)
-    got, want = Q.cpu(), q.view(torch.uint8)
-    codes = got[:, : x.shape[1]]
-    nan = torch.isnan(q.float())
-    assert torch.equal(codes[~nan], want[~nan])
-    assert bool(torch.all((codes[nan] & 0x7F) == 0x7F))
+    got = Q.cpu()
+    values, want = got[:, : x.shape[1]].contiguous().view(torch.float8_e4m3fn).float(), q.float()       # (zeros are equal whatever their sign)
+    assert torch.equal(torch.isnan(values), torch.isnan(want)) and torch.equal(values.nan_to_num(0.0), want.nan_to_num(0.0))
     assert bool(torch.all(got[:, x.shape[1]:] == 0x55)), "wrote behind a vector's end"
     sc = S.cpu()
     assert torch.equal(sc[:, : s.shape[1]], s)
@@ -89,6 +87,26 @@ def test_every_value_and_every_tie_of_the_format():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("type", ["bf16", "f16", "f32"])
+def test_quotients_on_and_next_to_ties(type):
+    """Elements a fraction of the block's largest that lies half-way between two codes, and (32 bits) its neighbours."""
+    codes = torch.arange(0, 127, dtype=torch.uint8).view(torch.float8_e4m3fn).double()
+    ties = ((codes[1:] + codes[:-1]) / 2)
+    gen = torch.Generator().manual_seed(11)
+    amax = torch.cat([torch.tensor([448.0, 1.75, 7.0, 1.0, 1.5, 3.0 * 2.0 ** -30 if type != "f16" else 3.0]), torch.rand((60,), generator=gen) + 1.0])
+    amax = amax.to(plain.DTYPES[type]).double().unsqueeze(1)
+    x = (ties * amax / 448.0).to(plain.DTYPES[type])
+    if type == "f32":
+        x = torch.cat([x, torch.nextafter(x, torch.zeros_like(x)), torch.nextafter(x, torch.full_like(x, 9.0))])
+        amax = amax.repeat(3, 1)
+    x = torch.cat([x, amax.to(x.dtype), -amax.to(x.dtype)], 1)      # 128: a block each
+    for blocks in (False, True):
+        Q, S, Qt, St = _call(x, type, blocks, True, True)
+        _same(Q, S, x, blocks)
+        _same(Qt, St, x.t().contiguous(), blocks)
+
+
+@pytest.mark.gpu
 def test_more_than_2_31_elements():
     rows, k = 1 << 15, (1 << 16) + 128
     X = torch.zeros((rows, k), dtype=torch.bfloat16, device="cuda")
@@ -101,7 +119,7 @@ def test_more_than_2_31_elements():
     torch.cuda.synchronize()
     for r in (0, 1, 2, rows // 2, rows - 2, rows - 1):
         q, s = plain.quantised(X[r: r + 1].float().cpu(), False)
-        assert torch.equal(Q[r: r + 1].cpu(), q.view(torch.uint8)) and torch.equal(S[:, r: r + 1].cpu(), s)
+        assert torch.equal(Q[r: r + 1].view(torch.float8_e4m3fn).float().cpu(), q.float()) and torch.equal(S[:, r: r + 1].cpu(), s)
 
 
 @pytest.mark.gpu
