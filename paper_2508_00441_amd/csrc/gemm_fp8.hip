@@ -32,33 +32,11 @@ __device__ __forceinline__ void gemm_fp8_body(const GemmFp8Work& w) {
     v4f32 acc[P::FN][P::FM] = {};
     P::multiply(lds, X, Y, a.k, split_begin(w.steps, w.splits, split), split_begin(w.steps, w.splits, split + 1), acc);
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wn = wave / P::WM, wm = wave % P::WM;
-    if (w.splits > 1) {
-        const bool wide = a.n % 4 == 0;
-#pragma unroll
-        for (int j = 0; j < P::FM; ++j) {
-            const int64_t i_m = m0 + (wm * P::FM + j) * 16 + (lane & 15);
-            if (i_m >= a.m) continue;
-#pragma unroll
-            for (int i = 0; i < P::FN; ++i) {
-                const int64_t i_n = n0 + (wn * P::FN + i) * 16 + 4 * (lane >> 4);
-                put_four(a.partial + ((int64_t)split * a.m + i_m) * a.n + i_n, acc[i][j], a.n - i_n, wide, false);
-            }
-        }
-        return;
-    }
-    T* const D = static_cast<T*>(a.D);
-    const bool wide = a.ldd % 4 == 0 && reinterpret_cast<uintptr_t>(D) % (4 * sizeof(T)) == 0;
-#pragma unroll
-    for (int j = 0; j < P::FM; ++j) {
-        const int64_t i_m = m0 + (wm * P::FM + j) * 16 + (lane & 15);
-        if (i_m >= a.m) continue;
-#pragma unroll
-        for (int i = 0; i < P::FN; ++i) {
-            const int64_t i_n = n0 + (wn * P::FN + i) * 16 + 4 * (lane >> 4);
-            put_four(D + i_m * a.ldd + i_n, acc[i][j], a.n - i_n, wide, a.accumulate != 0);
-        }
-    }
+    const auto one = [](int64_t) { return 1.0f; };
+    if (w.splits > 1)
+        store_tile<P, false>(lds, acc, a.partial + ((int64_t)split * a.m + m0) * a.n + n0, a.n, left_m, left_n, false, one);
+    else
+        store_tile<P, (P::THREADS > 256)>(lds, acc, static_cast<T*>(a.D) + m0 * a.ldd + n0, a.ldd, left_m, left_n, a.accumulate != 0, one);
 }
 
 template <int TYPE, int SCALING> constexpr int kind_of() {
@@ -67,7 +45,7 @@ template <int TYPE, int SCALING> constexpr int kind_of() {
 
 template <int SCALING, int TYPE>
 __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) gemm_fp8_large_kernel(const GemmFp8Work w) {
-    gemm_fp8_body<Tile<kind_of<TYPE, SCALING>(), 2, 4, 8, 4, 2>, TYPE>(w);
+    gemm_fp8_body<PairedTile<kind_of<TYPE, SCALING>()>, TYPE>(w);
 }
 // 256 x 128 for 32-bit results: the widened fragments of 256 x 256 do not fit beside its accumulators
 template <int SCALING>
@@ -129,7 +107,7 @@ hipError_t launch_kind(const GemmFp8Args& a, int splits, hipStream_t st) {
     w.tiles_m = (int)div_up(a.m, tm);
     w.tiles_n = (int)div_up(a.n, s.tn);
     const int64_t tiles = (int64_t)w.tiles_m * w.tiles_n;
-    w.order = tiles * splits >= 512 ? WorkOrder{32, w.tiles_m > 8 ? 4 : 8} : WorkOrder{0, 0};
+        w.order = tiles * splits >= 512 ? WorkOrder{32, w.tiles_m > 8 ? 4 : 8} : WorkOrder{0, 0};
     const unsigned blocks = (unsigned)(tiles * splits);
     if (s.tm == 16) hipLaunchKernelGGL((gemm_fp8_few_kernel<SCALING, TYPE>), dim3(blocks), dim3(256), 0, st, w);
     else if (s.tm == 128) hipLaunchKernelGGL((gemm_fp8_middle_kernel<SCALING, TYPE>), dim3(blocks), dim3(256), 0, st, w);

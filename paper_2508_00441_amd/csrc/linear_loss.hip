@@ -267,34 +267,12 @@ __device__ __forceinline__ void loss_product_body(const ProductWork& w) {
     v4f32 acc[P::FN][P::FM] = {};
     const int split = item.gi;
     P::multiply(lds, X, Y, w.bytes, split_begin(w.steps, w.splits, split), split_begin(w.steps, w.splits, split + 1), acc);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wn = wave / P::WM, wm = wave % P::WM;
     if (w.partial != nullptr) {
-        const bool wide = w.n % 4 == 0;
-#pragma unroll
-        for (int j = 0; j < P::FM; ++j) {
-            const int64_t m = m0 + (wm * P::FM + j) * 16 + (lane & 15);
-            if (m >= w.m) continue;
-#pragma unroll
-            for (int i = 0; i < P::FN; ++i) {
-                const int64_t n = n0 + (wn * P::FN + i) * 16 + 4 * (lane >> 4);
-                put_four(w.partial + ((int64_t)split * w.m + m) * w.n + n, acc[i][j], w.n - n, wide, false);
-            }
-        }
+        store_tile<P, false>(lds, acc, w.partial + ((int64_t)split * w.m + m0) * w.n + n0, w.n, left_m, left_n, false, [](int64_t) { return 1.0f; });
         return;
     }
-    T* const D = static_cast<T*>(w.D);
-    const bool wide = w.ldd % 4 == 0 && reinterpret_cast<uintptr_t>(D) % 8 == 0;
-#pragma unroll
-    for (int j = 0; j < P::FM; ++j) {
-        const int64_t m = m0 + (wm * P::FM + j) * 16 + (lane & 15);
-        if (m >= w.m) continue;
-        const float scale = w.row_factor != nullptr ? w.row_factor[m] : *w.factor;
-#pragma unroll
-        for (int i = 0; i < P::FN; ++i) {
-            const int64_t n = n0 + (wn * P::FN + i) * 16 + 4 * (lane >> 4);
-            put_four(D + m * w.ldd + n, acc[i][j] * scale, w.n - n, wide, false);
-        }
-    }
+    store_tile<P, (P::THREADS > 256)>(lds, acc, static_cast<T*>(w.D) + m0 * w.ldd + n0, w.ldd, left_m, left_n, false,
+                  [&](int64_t m) { return w.row_factor != nullptr ? w.row_factor[m0 + m] : *w.factor; });
 }
 
 // The sums of a piece's shares of the inner dimension, on top of the pieces' before it (`sum`, unless it is the first); the last piece's go to D.
@@ -314,7 +292,7 @@ __global__ void __launch_bounds__(256) zero_rows_kernel(uint16_t* D, int64_t row
 }
 
 constexpr int kind_of(int type) { return type == TYPE_F16 ? KIND_F16 : KIND_BF16; }
-template <int TYPE> using LargeTile = Tile<kind_of(TYPE), 2, 4, 8, 4, 2>;      // 256 words or columns, 256 tokens or rows
+template <int TYPE> using LargeTile = PairedTile<kind_of(TYPE)>;      // 256 words or columns, 256 tokens or rows
 template <int TYPE> using MiddleTile = Tile<kind_of(TYPE), 2, 2, 4, 2, 3>;     // 128, 64
 template <int TYPE> using FewTile = Tile<kind_of(TYPE), 4, 1, 2, 1, 4>;        // 128, 16
 

@@ -15,6 +15,8 @@
 // sixteen zero bytes, and where the end lies inside a piece the bytes behind it are cleared in LDS, in both operands: what the
 // caller's memory holds there may be a NaN.
 #pragma once
+#include <type_traits>
+
 #include "low_precision.hpp"
 
 namespace ozaki {
@@ -87,6 +89,16 @@ __device__ __forceinline__ void put_four(T* at, v4f32 v, int64_t left, bool wide
         for (int r = 0; r < 4; ++r)
             if (r < left) at[r] = (T)(accumulate ? v[r] + (float)at[r] : v[r]);
     }
+}
+
+// the first `keep` of sixteen bytes, zeros behind them
+__device__ __forceinline__ v4i32 first_bytes(v4i32 v, int keep) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int bytes = keep - 4 * q;
+        v[q] = bytes >= 4 ? v[q] : bytes <= 0 ? 0 : v[q] & (int)((1u << (8 * bytes)) - 1);
+    }
+    return v;
 }
 
 // Waits until at most N vector-memory operations of this wave are outstanding and its LDS operations are done, then meets the others.
@@ -206,54 +218,78 @@ struct Tile {
             const v4i32 lo = *reinterpret_cast<const v4i32*>(at + piece0), hi = *reinterpret_cast<const v4i32*>(at + piece1);
             return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         };
+        // A step's products.  The order is fixed: a product's fused multiply-adds come behind the next products, which cover the matrix
+        // unit's latency, and a row's fragment is read while the row two before it is multiplied.
         auto compute = [&]() {
             const uint8_t* const stage = lds + read_buf * STAGE_BYTES;
             typedef typename Fragment<WIDE>::type operand;
-            operand y[FM];
-#pragma unroll
-            for (int j = 0; j < FM; ++j) y[j] = Fragment<WIDE>::of(fragment(stage + ybase + j * 16 * STEP_BYTES));
+            constexpr int AHEAD = FN > 1 ? 2 : 1;                     // rows whose fragments are read in front
+            operand y[FM], x[AHEAD + 1];
+            auto row = [&](int i) { return Fragment<WIDE>::of(fragment(stage + xbase + i * 16 * STEP_BYTES)); };
+            __builtin_amdgcn_sched_barrier(0);
             if constexpr (FP8) {
                 const float* const scales = reinterpret_cast<const float*>(stage + ROWS * STEP_BYTES);
-                float sy[FM];
+                constexpr int MOST = BLOCKS ? 3 : 2, LAG = FM * FN > MOST ? MOST : FM * FN - 1, T = LAG + 1;
+                float sy[FM], sx_all = 0.0f;
+                v4f32 t[T], sx[2] = {};
+#pragma unroll
+                for (int j = 0; j < FM; ++j) {
+                    y[j] = Fragment<WIDE>::of(fragment(stage + ybase + j * 16 * STEP_BYTES));
+                    if (j < AHEAD && j < FN) x[j] = row(j);
+                }
+                if (AHEAD > FM) x[1] = row(1);
 #pragma unroll
                 for (int j = 0; j < FM; ++j) sy[j] = scales[TN + (wm * FM + j) * 16 + frow];
-                if constexpr (BLOCKS) {
-                    // the wave's rows lie in one block of 128 vectors
-                    static_assert(SCALE_BLOCK % (FN * 16) == 0, "");
-                    const float sx = scales[wn * FN * 16];
+                // (the wave's rows lie in one block of 128 vectors)
+                static_assert(!BLOCKS || SCALE_BLOCK % (FN * 16) == 0, "");
+                if constexpr (BLOCKS) sx_all = scales[wn * FN * 16];
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int j = 0; j < FM; ++j) sy[j] *= sx;
-                }
-#pragma unroll
-                for (int i = 0; i < FN; ++i) {
-                    const operand x = Fragment<WIDE>::of(fragment(stage + xbase + i * 16 * STEP_BYTES));
-                    v4f32 sx = {};
-                    if constexpr (!BLOCKS) sx = *reinterpret_cast<const v4f32*>(scales + (wn * FN + i) * 16 + 4 * g);
-#pragma unroll
-                    for (int j = 0; j < FM; ++j) {
-                        const v4f32 t = Fragment<WIDE>::product(x, y[j]);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) acc[i][j][r] = __builtin_fmaf(t[r], BLOCKS ? sy[j] : sx[r] * sy[j], acc[i][j][r]);
+                for (int n = 0; n < FN * FM + LAG; ++n) {
+                    if (n < FN * FM) {
+                        const int i = n / FM, j = n % FM;
+                        if (j == 0 && i + AHEAD < FN) x[(i + AHEAD) % (AHEAD + 1)] = row(i + AHEAD);
+                        if (!BLOCKS && j == 0) sx[i & 1] = *reinterpret_cast<const v4f32*>(scales + (wn * FN + i) * 16 + 4 * g);
+                        t[n % T] = Fragment<WIDE>::product(x[i % (AHEAD + 1)], y[j]);
                     }
-                    if constexpr (WIDE) __builtin_amdgcn_sched_barrier(0);              // no second row's fragment beside this one: registers
+                    if (BLOCKS && n == LAG) {
+#pragma unroll
+                        for (int j = 0; j < FM; ++j) sy[j] *= sx_all;
+                    }
+                    if (n >= LAG) {
+                        const int d = n - LAG, i = d / FM, j = d % FM;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            acc[i][j][r] = __builtin_fmaf(t[d % T][r], BLOCKS ? sy[j] : sx[i & 1][r] * sy[j], acc[i][j][r]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             } else {
 #pragma unroll
+                for (int j = 0; j < FM; ++j) {
+                    y[j] = Fragment<WIDE>::of(fragment(stage + ybase + j * 16 * STEP_BYTES));
+                    if (j < AHEAD && j < FN) x[j] = row(j);
+                }
+                if (AHEAD > FM) x[1] = row(1);
+#pragma unroll
                 for (int i = 0; i < FN; ++i) {
-                    const v8i32 x = fragment(stage + xbase + i * 16 * STEP_BYTES);
+                    if (i + AHEAD < FN) x[(i + AHEAD) % (AHEAD + 1)] = row(i + AHEAD);
+                    const v8i32 xi = x[i % (AHEAD + 1)];
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
                         for (int j = 0; j < FM; ++j) {
-                            const v4i32 xh = h ? __builtin_shufflevector(x, x, 4, 5, 6, 7) : __builtin_shufflevector(x, x, 0, 1, 2, 3);
+                            const v4i32 xh = h ? __builtin_shufflevector(xi, xi, 4, 5, 6, 7) : __builtin_shufflevector(xi, xi, 0, 1, 2, 3);
                             const v4i32 yh = h ? __builtin_shufflevector(y[j], y[j], 4, 5, 6, 7) : __builtin_shufflevector(y[j], y[j], 0, 1, 2, 3);
                             if constexpr (KIND == KIND_BF16)
                                 acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf16, xh), __builtin_bit_cast(v8bf16, yh), acc[i][j], 0, 0, 0);
                             else
                                 acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8f16, xh), __builtin_bit_cast(v8f16, yh), acc[i][j], 0, 0, 0);
                         }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
+            __builtin_amdgcn_sched_barrier(0);
             read_buf = read_buf + 1 == NST ? 0 : read_buf + 1;
         };
 
@@ -277,8 +313,8 @@ struct Tile {
             if (s + 1 == steps && (last_bytes & 15) != 0) {
                 // the end lies inside a piece
                 for (int row = tid; row < ROWS; row += THREADS) {
-                    uint8_t* const at = lds + read_buf * STAGE_BYTES + row * STEP_BYTES + (((last_bytes >> 4) ^ ((row >> 1) & 7)) << 4);
-                    for (int b = last_bytes & 15; b < 16; ++b) at[b] = 0;
+                    v4i32* const at = reinterpret_cast<v4i32*>(lds + read_buf * STAGE_BYTES + row * STEP_BYTES + (((last_bytes >> 4) ^ ((row >> 1) & 7)) << 4));
+                    *at = first_bytes(*at, last_bytes & 15);
                 }
                 tile_wait<(NST - 1) * (LPW + SPW)>();
             }
@@ -287,6 +323,238 @@ struct Tile {
         tile_wait<0>();
     }
 };
+
+// The product of 256 X with 256 Y in eight waves, two to a SIMD, for large results: Tile's layout and arithmetic with another pipeline.
+//
+// Two steps' vectors fit into LDS (128 of its 160 KiB), and with one meeting per step a step's loads get no more than a step's time to arrive
+// and all waves start a step together, with LDS reads and nothing to multiply.  Here a step's loads come in two parts, each asked for as
+// soon as the part it replaces has been read and met one and a half steps later:
+//     part 1: all of Y and rows 0 - 63 of each 128 of X (what rows 0 - 3 of a wave's tiles need), and the scales
+//     part 2: rows 64 - 127 of each 128 of X.
+// Rows of products 0 .. 7 of step s (each of FM tiles):
+//     head of row 3: part 2 of step s has arrived; part 1 of s has been read: part 1 of s + 2 is asked for
+//     head of row 7: part 1 of step s + 1 has arrived; part 2 of s has been read: part 2 of s + 2 is asked for
+// X's fragments are read a row in front, across the end of the step; Y's fragment j of the next step in row 7, where the last product
+// that reads it has been issued.  So no wave waits for LDS at a step's head.
+// Whole steps are loaded with buffer instructions, whose addresses are 32-bit offsets of a lane and of the step: 256 accumulators of two waves
+// leave no registers for 64-bit ones.
+template <int KIND>
+struct PairedTile {
+    typedef Tile<KIND, 2, 4, 8, 4, 2> Base;
+    static constexpr bool FP8 = Base::FP8, BLOCKS = Base::BLOCKS;
+    static_assert(!Base::WIDE, "registers");
+    static constexpr int WN = 2, WM = 4, FN = 8, FM = 4, WAVES = 8, THREADS = 512, TN = 256, TM = 256, ROWS = 512;
+    static constexpr int STAGE_BYTES = ROWS * STEP_BYTES, SCALE_BYTES = FP8 ? ROWS * 4 : 0, SCALE_RING = 3;
+    static constexpr int LDS_BYTES = 2 * STAGE_BYTES + SCALE_RING * SCALE_BYTES;
+    static_assert(LDS_BYTES >= Base::LDS_BYTES, "");
+    static constexpr int P1 = 6, P2 = 2, S = FP8 ? 1 : 0;            // loads of a wave
+
+    // Vectors that end inside a piece: their last step on its own, by Tile.  (Clearing the piece in the pipeline costs it a hundred registers.)
+    __device__ static void multiply(uint8_t* lds, const TileOperand& X, const TileOperand& Y, int64_t bytes, int step0, int step1,
+                                    v4f32 (&acc)[FN][FM]) {
+        const bool inside = (bytes & 15) != 0 && bytes < (int64_t)step1 * STEP_BYTES;
+        const int whole = step1 - (inside ? 1 : 0);
+        if (whole > step0) pipeline(lds, X, Y, bytes, step0, whole, acc);
+        if (inside) Base::multiply(lds, offset(X, whole), offset(Y, whole), bytes - (int64_t)whole * STEP_BYTES, 0, 1, acc);
+    }
+
+    __device__ static TileOperand offset(const TileOperand& o, int step) {
+        return TileOperand{o.vectors + (int64_t)step * STEP_BYTES, o.stride, o.rows, o.scales + (int64_t)step * o.scale_stride, o.scale_stride};
+    }
+
+    __device__ static void pipeline(uint8_t* lds, const TileOperand& X, const TileOperand& Y, int64_t bytes, int step0, int step1,
+                                    v4f32 (&acc)[FN][FM]) {
+        const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const int wn = wave / WM, wm = wave % WM;
+        const int steps = step1 - step0;
+        const int64_t rest = bytes - (int64_t)(step1 - 1) * STEP_BYTES;
+        const int last_bytes = rest < STEP_BYTES ? (int)rest : STEP_BYTES;
+        const bool ragged = last_bytes < STEP_BYTES;
+
+        // Load i of a wave brings eight rows of the stage (X's 256, then Y's): Y for i < 4, X's of part 1 for i = 4, 5, of part 2 for i = 6, 7.
+        const int y_first = TN + wave * 32, x_first = (wave >> 2) * 128 + (wave & 3) * 16;
+        auto row_of = [&](int i) { return i < 4 ? y_first + 8 * i : x_first + (i < P1 ? 8 * (i - 4) : 64 + 8 * (i - P1)); };
+        // (beyond `RECORDS` bytes these resources give zeros)
+        constexpr unsigned RECORDS = 0x7FFFFFFFu;
+        const __amdgpu_buffer_rsrc_t in_x = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(X.vectors), 0, RECORDS, 0x00027000);
+        const __amdgpu_buffer_rsrc_t in_y = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(Y.vectors), 0, RECORDS, 0x00027000);
+        unsigned voff[P1 + P2];
+#pragma unroll
+        for (int i = 0; i < P1 + P2; ++i) {
+            const int row = row_of(i) + (lane >> 3), mine = i < 4 ? row - TN : row, rows = i < 4 ? Y.rows : X.rows;
+            voff[i] = (unsigned)(mine < rows ? mine : rows - 1) * (unsigned)(i < 4 ? Y.stride : X.stride) + (((lane & 7) ^ ((row >> 1) & 7)) << 4);
+        }
+        // the scales of a wave's 64 rows of the stage
+        const bool x_scales = wave < 4;
+        unsigned soff = 0;
+        if constexpr (FP8) {
+            const int row = (wave & 3) * 64 + lane, rows = x_scales ? X.rows : Y.rows, real = row < rows ? row : rows - 1;
+            soff = 4 * (unsigned)(x_scales && BLOCKS ? real / SCALE_BLOCK : real);
+        }
+        // load i of step `s`; `plain`: a whole step is there to be read; otherwise zeros come from behind the vectors' end
+        auto load = [&](int i, int s, bool plain) {
+            unsigned at = voff[i];
+            if (!plain) {
+                const int limit = s + 1 < steps ? STEP_BYTES : s + 1 == steps ? last_bytes : 0;
+                if ((int)((lane & 7) ^ (((row_of(i) + (lane >> 3)) >> 1) & 7)) * 16 >= limit) at = RECORDS;
+            }
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(i < 4 ? in_y : in_x, OZAKI_TILE_LPTR(lds + (s & 1) * STAGE_BYTES + row_of(i) * STEP_BYTES), 16, at,
+                                                     (step0 + s) * STEP_BYTES, 0, 0);
+        };
+        int scale_to = 0, scale_at = 0;                               // places in the ring of scales
+        auto load_scales = [&](int s, bool plain) {
+            if constexpr (FP8) {
+                const float* const block = x_scales ? X.scales + (int64_t)(step0 + s) * X.scale_stride : Y.scales + (int64_t)(step0 + s) * Y.scale_stride;
+                const __amdgpu_buffer_rsrc_t in = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(block), 0, plain || s < steps ? RECORDS : 0, 0x00027000);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(in, OZAKI_TILE_LPTR(lds + 2 * STAGE_BYTES + scale_to * SCALE_BYTES + wave * 256), 4, soff, 0, 0, 0);
+                scale_to = scale_to + 1 == SCALE_RING ? 0 : scale_to + 1;
+            }
+        };
+        const int frow = lane & 15, g = lane >> 4, fsw = (frow >> 1) & 7;
+        const int piece0 = (g ^ fsw) << 4, piece1 = ((g + 4) ^ fsw) << 4;
+        const int xbase = (wn * FN * 16 + frow) * STEP_BYTES, ybase = (TN + wm * FM * 16 + frow) * STEP_BYTES;
+        auto fragment = [&](int at, int s) -> v8i32 {
+            const uint8_t* const p = lds + (s & 1) * STAGE_BYTES + at;
+            const v4i32 lo = *reinterpret_cast<const v4i32*>(p + piece0), hi = *reinterpret_cast<const v4i32*>(p + piece1);
+            return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        };
+        auto half = [](const v8i32& v, int h) {
+            return h ? __builtin_shufflevector(v, v, 4, 5, 6, 7) : __builtin_shufflevector(v, v, 0, 1, 2, 3);
+        };
+        v8i32 y[FM], x[2];
+
+        // in front of step 0: all four parts of two steps
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const bool plain = s + 1 < steps || (s + 1 == steps && !ragged);
+#pragma unroll
+            for (int i = 0; i < P1; ++i) load(i, s, plain);
+            load_scales(s, plain);
+#pragma unroll
+            for (int i = P1; i < P1 + P2; ++i) load(i, s, plain);
+        }
+        tile_wait<P2 + P1 + S + P2>();
+#pragma unroll
+        for (int j = 0; j < FM; ++j) y[j] = fragment(ybase + j * 16 * STEP_BYTES, 0);
+        x[0] = fragment(xbase, 0);
+
+        // one step; `plain`: the loads that it asks for are of whole steps, and there is a next one
+        auto step = [&](int s, auto plain_c) {
+            constexpr bool PLAIN = decltype(plain_c)::value;
+            const bool full = PLAIN || s + 3 < steps || (s + 3 == steps && !ragged);
+            const float* const scales = reinterpret_cast<const float*>(lds + 2 * STAGE_BYTES + scale_at * SCALE_BYTES);
+            scale_at = scale_at + 1 == SCALE_RING ? 0 : scale_at + 1;
+            constexpr int LAG = !FP8 ? 0 : BLOCKS ? 3 : 2;
+            float sy[FM], sx_all = 0.0f;
+            v4f32 t[LAG + 1], sx[2] = {};
+            if constexpr (FP8) {
+#pragma unroll
+                for (int j = 0; j < FM; ++j) sy[j] = scales[TN + (wm * FM + j) * 16 + frow];
+                if constexpr (BLOCKS) sx_all = scales[wn * FN * 16];
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int n = 0; n < FN * FM + LAG; ++n) {
+                const int i = n / FM, j = n % FM;
+                if (n < FN * FM) {
+                    if (j == 0 && i == 3) tile_wait<P1 + S + P2>();
+                    if (j == 0 && i == 7) tile_wait<P2 + P1 + S>();
+                    // (behind the last step these read what is there and nobody uses)
+                    if (j == 0) x[(i + 1) & 1] = fragment(xbase + (i + 1) % FN * 16 * STEP_BYTES, i + 1 < FN ? s : s + 1);
+                    if (FP8 && !BLOCKS && j == 0) sx[i & 1] = *reinterpret_cast<const v4f32*>(scales + (wn * FN + i) * 16 + 4 * g);
+                    const v8i32 xi = x[i & 1];
+                    if constexpr (FP8) {
+                        t[n % (LAG + 1)] = Fragment<false>::product(xi, y[j]);
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            if constexpr (KIND == KIND_BF16)
+                                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf16, half(xi, h)), __builtin_bit_cast(v8bf16, half(y[j], h)), acc[i][j], 0, 0, 0);
+                            else
+                                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8f16, half(xi, h)), __builtin_bit_cast(v8f16, half(y[j], h)), acc[i][j], 0, 0, 0);
+                        }
+                    }
+                    if (i == FN - 1) y[j] = fragment(ybase + j * 16 * STEP_BYTES, s + 1);
+                    // the loads, one behind a product
+                    const int l = n - 3 * FM;
+                    if (l >= 0 && l < P1) load(l, s + 2, PLAIN || full);
+                    if (l == P1) load_scales(s + 2, PLAIN || full);
+                    if (n >= 7 * FM && n < 7 * FM + P2) load(P1 + n - 7 * FM, s + 2, PLAIN || full);
+                }
+                if (BLOCKS && n == LAG) {
+#pragma unroll
+                    for (int q = 0; q < FM; ++q) sy[q] *= sx_all;
+                }
+                if (FP8 && n >= LAG) {
+                    const int d = n - LAG, di = d / FM, dj = d % FM;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        acc[di][dj][r] = __builtin_fmaf(t[d % (LAG + 1)][r], BLOCKS ? sy[dj] : sx[di & 1][r] * sy[dj], acc[di][dj][r]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        const std::integral_constant<bool, true> plain;
+        const std::integral_constant<bool, false> checked;
+        int s = 0;
+        for (; s + 4 < steps; s += 2) {
+            step(s, plain);
+            step(s + 1, plain);
+        }
+        for (; s < steps; ++s) step(s, checked);
+        tile_wait<0>();
+    }
+};
+
+// Stores the tile that P::multiply has left, times factor(row of D) and (accumulate) on top of what D holds, D being its first element: `left_m` rows
+// and `left_n` columns of it are there.  A lane has four neighbouring columns of sixteen rows; through LDS, 16 rows of every wave at a time
+// in 32 bits, D's rows are written in whole 16-byte pieces of neighbouring lanes.  Rows of D that are not aligned to that are written by element.
+// STREAMED: results of the large shapes, more than the L2 caches hold (FP8, 4096 x 4096 x 256 19.3 -> 17.0 us, 8192 x 8192 x 4096 252 -> 244).
+template <typename P, bool STREAMED, typename T, typename F>
+__device__ __forceinline__ void store_tile(uint8_t* lds, const v4f32 (&acc)[P::FN][P::FM], T* D, int64_t ldd, int64_t left_m, int64_t left_n,
+                                           bool accumulate, F factor) {
+    constexpr int STRIDE = P::TN * 4 + 16, PER = 16 / sizeof(T), PIECES = P::TN / PER, ROWS = P::WM * 16;
+    static_assert(ROWS * STRIDE <= P::LDS_BYTES && P::THREADS % PIECES == 0, "");
+    typedef T piece __attribute__((ext_vector_type(PER)));
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wn = wave / P::WM, wm = wave % P::WM;
+    const int columns = left_n < P::TN ? (int)left_n : P::TN;
+    const bool wide = ldd % PER == 0 && reinterpret_cast<uintptr_t>(D) % 16 == 0;
+    const int whole = wide ? columns / PER * PER : 0, loose = columns - whole;
+#pragma unroll
+    for (int j = 0; j < P::FM; ++j) {
+        uint8_t* const mine = lds + (wm * 16 + (lane & 15)) * STRIDE + (wn * P::FN * 16 + 4 * (lane >> 4)) * 4;
+#pragma unroll
+        for (int i = 0; i < P::FN; ++i) *reinterpret_cast<v4f32*>(mine + i * 64) = acc[i][j];
+        __syncthreads();
+        const int column = threadIdx.x % PIECES * PER;
+        if (column < whole) {
+#pragma unroll 1
+            for (int r = threadIdx.x / PIECES; r < ROWS; r += P::THREADS / PIECES) {
+                const int64_t m = ((r >> 4) * P::FM + j) * 16 + (r & 15);
+                if (m >= left_m) continue;
+                const float* const from = reinterpret_cast<const float*>(lds + r * STRIDE) + column;
+                piece* const to = reinterpret_cast<piece*>(D + m * ldd + column);
+                const float f = factor(m);
+                piece v = {};
+                if (accumulate) v = *to;
+#pragma unroll
+                for (int q = 0; q < PER; ++q) v[q] = (T)(accumulate ? (float)v[q] + from[q] * f : from[q] * f);
+                if constexpr (STREAMED) __builtin_nontemporal_store(v, to);
+                else *to = v;
+            }
+        }
+#pragma unroll 1
+        for (int i = threadIdx.x; i < ROWS * loose; i += P::THREADS) {
+            const int r = i / loose, c = whole + i % loose;
+            const int64_t m = ((r >> 4) * P::FM + j) * 16 + (r & 15);
+            if (m >= left_m) continue;
+            const float v = reinterpret_cast<const float*>(lds + r * STRIDE)[c] * factor(m);
+            T* const to = D + m * ldd + c;
+            *to = (T)(accumulate ? (float)*to + v : v);
+        }
+        __syncthreads();
+    }
+}
 
 }  // namespace
 }  // namespace ozaki

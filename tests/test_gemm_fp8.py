@@ -73,6 +73,18 @@ def test_large_products(m, n, k, blocks, workspace):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("type_d", ["bf16", "f32", "f16"])
+@pytest.mark.parametrize("blocks", [True, False])
+@pytest.mark.parametrize("m,n,k", [(3600, 3501, 520), (4100, 3329, 257), (3585, 3584, 1301), (3600, 3600, 100), (3601, 3590, 127), (3600, 3600, 128),
+                                   (3584, 3600, 2176), (3600, 3700, 656)])
+def test_products_of_many_tiles(m, n, k, blocks, type_d, workspace):
+    o = Operands(m, n, k, blocks, 12)
+    D = torch.full((m, n), float("nan"), dtype=plain.DTYPES[type_d], device="cuda")
+    o.multiply(D, n, type_d)
+    _check(o, D, type_d)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("m,n,k", [(1, 200, 2000), (40, 200, 700), (2400, 2400, 300)])
 def test_scales_far_apart(m, n, k, workspace):
     o = Operands(m, n, k, True, 2, wide=True)

@@ -81,7 +81,7 @@ def workspace():
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("type", ["bf16", "f16"])
-@pytest.mark.parametrize("tokens,vocab,k", SHAPES + [(2500, 3000, 136)])
+@pytest.mark.parametrize("tokens,vocab,k", SHAPES + [(2500, 3000, 136), (3000, 4001, 600), (2900, 4000, 1001)])
 def test_loss(tokens, vocab, k, type, workspace):
     x = Problem(tokens, vocab, k, type, tokens + vocab + k)
     loss, lse = x.forward()
@@ -95,7 +95,7 @@ def test_loss(tokens, vocab, k, type, workspace):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("type", ["bf16", "f16"])
-@pytest.mark.parametrize("tokens,vocab,k", SHAPES + [(1500, 6000, 136)])
+@pytest.mark.parametrize("tokens,vocab,k", SHAPES + [(1500, 6000, 136), (3000, 4001, 600), (2900, 4000, 1001)])
 def test_gradient(tokens, vocab, k, type, workspace):
     x = Problem(tokens, vocab, k, type, tokens + vocab + k)
     _, lse = x.forward()
