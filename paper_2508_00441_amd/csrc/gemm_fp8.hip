@@ -57,10 +57,86 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
     gemm_fp8_body<Tile<kind_of<TYPE, SCALING>(), 2, 2, 4, 4, 2>, TYPE>(w);
 }
 template <int SCALING, int TYPE>
-__global__ void __launch_bounds__(256) gemm_fp8_few_kernel(const GemmFp8Work w) {
-    gemm_fp8_body<Tile<kind_of<TYPE, SCALING>(), 4, 1, 1, 1, 6>, TYPE>(w);
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) gemm_fp8_small_kernel(const GemmFp8Work w) {
+    gemm_fp8_body<Tile<kind_of<TYPE, SCALING>(), 2, 2, 2, 2, 4>, TYPE>(w);
 }
 
+// Up to sixteen vectors of A: a workgroup forms sixteen columns of D, its waves taking every WAVES-th block of the inner dimension straight
+// from memory into registers, and adds its waves' sums in LDS, in their order.  B is read once and bounds it; with nothing staged a wave has AHEAD
+// blocks of it (2 KiB each) in flight at once.
+constexpr int FEW_WAVES = 8, AHEAD = 4;
+
+template <int SCALING, int TYPE>
+__global__ void __launch_bounds__(FEW_WAVES * 64) gemm_fp8_few_kernel(const GemmFp8Args a) {
+    constexpr int WAVES = FEW_WAVES;
+    typedef typename Element<TYPE>::type T;
+    typedef Fragment<TYPE == TYPE_F32> F;
+    __shared__ __attribute__((aligned(16))) v4f32 sums[WAVES][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 15, g = lane >> 4;
+    const int64_t n0 = (int64_t)blockIdx.x * 16;
+    const int my_n = n0 + row < a.n ? row : (int)(a.n - 1 - n0), my_m = row < a.m ? row : (int)a.m - 1;
+    const uint8_t* const x_at = a.B + (n0 + my_n) * a.ldb + g * 16;
+    const uint8_t* const y_at = a.A + my_m * a.lda + g * 16;
+    const float* const sx_at = SCALING == SCALE_BLOCKS ? a.Sb + n0 / SCALE_BLOCK : a.Sb + n0;
+    const int steps = (int)div_up(a.k, SCALE_BLOCK);
+    int four[4];                                     // this lane's four columns of the result
+#pragma unroll
+    for (int r = 0; r < 4; ++r) four[r] = n0 + 4 * g + r < a.n ? 4 * g + r : (int)(a.n - 1 - n0);
+    v4i32 x[AHEAD][2], y[AHEAD][2];
+    v4f32 sx[AHEAD];
+    float sy[AHEAD];
+    // (behind the end of the vectors, and of the blocks, something that is there is read and not used)
+    auto load = [&](int u, int s) {
+        s = s < steps ? s : steps - 1;
+        const int64_t at = (int64_t)s * SCALE_BLOCK;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t from = at + g * 16 + h * 64 < a.k ? at + h * 64 : -(int64_t)g * 16;
+            x[u][h] = *reinterpret_cast<const v4i32*>(x_at + from);
+            y[u][h] = *reinterpret_cast<const v4i32*>(y_at + from);
+        }
+        sy[u] = a.Sa[s * a.ldsa + my_m];
+        if constexpr (SCALING == SCALE_BLOCKS) {
+            sx[u][0] = sx_at[s * a.ldsb];
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sx[u][r] = sx_at[s * a.ldsb + four[r]];
+        }
+    };
+    v4f32 acc = {};
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) load(u, wave + u * WAVES);
+    for (int first = wave; first < steps; first += WAVES * AHEAD) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int s = first + u * WAVES;
+            if (s >= steps) break;
+            if ((int64_t)(s + 1) * SCALE_BLOCK > a.k) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int left = (int)(a.k - (int64_t)s * SCALE_BLOCK) - g * 16 - h * 64, keep = left < 0 ? 0 : left;
+                    x[u][h] = first_bytes(x[u][h], keep);
+                    y[u][h] = first_bytes(y[u][h], keep);
+                }
+            }
+            const v4f32 t = F::product(F::of(__builtin_shufflevector(x[u][0], x[u][1], 0, 1, 2, 3, 4, 5, 6, 7)),
+                                       F::of(__builtin_shufflevector(y[u][0], y[u][1], 0, 1, 2, 3, 4, 5, 6, 7)));
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[r] = __builtin_fmaf(t[r], sx[u][SCALING == SCALE_BLOCKS ? 0 : r] * sy[u], acc[r]);
+            if (first + WAVES * AHEAD < steps) load(u, s + WAVES * AHEAD);
+        }
+    }
+    sums[wave][lane] = acc;
+    __syncthreads();
+    // thread (m, n) of sixteen by sixteen: the neighbours write neighbouring columns
+    const int n = threadIdx.x & 15, m = threadIdx.x >> 4;
+    if (threadIdx.x >= 256 || m >= a.m || n0 + n >= a.n) return;
+    float sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) sum += reinterpret_cast<const float*>(&sums[w][(n >> 2) * 16 + m])[n & 3];
+    T* const to = static_cast<T*>(a.D) + m * a.ldd + n0 + n;
+    *to = (T)(a.accumulate ? (float)*to + sum : sum);
+}
 // sums the pieces of the inner dimension in their order
 template <int TYPE>
 __global__ void __launch_bounds__(256) gemm_fp8_join_kernel(const GemmFp8Args a, const int splits) {
@@ -81,16 +157,16 @@ __global__ void __launch_bounds__(256) gemm_fp8_join_kernel(const GemmFp8Args a,
     put_four(D + i * a.ldd + j, sum, a.n - j, wide, a.accumulate != 0);
 }
 
-constexpr int FEW = 16;                   // vectors of A up to which the kernel for few of them runs
-struct Shape { int tm, tn, splits; };
+enum { FEW, SMALL, MIDDLE, LARGE };
+struct Shape { int kind, tm, tn, splits; };
 Shape shape_of(int64_t m, int64_t n, int64_t k) {
-    const int64_t steps = div_up(k, SCALE_BLOCK);
-    Shape s{256, 256, 1};
-    if (m <= FEW) s = {16, 64, 1};
-    else if (div_up(m, 256) * div_up(n, 256) < 192) s = {128, 128, 1};
-    if (s.tm < 256) {
-        const int64_t tiles = div_up(m, s.tm) * div_up(n, s.tn), want = 512 / tiles;
-        int64_t splits = want < steps / 4 ? want : steps / 4;
+    if (m <= 16) return Shape{FEW, 16, 16, 1};
+    Shape s{LARGE, 256, 256, 1};
+    if (m <= 512) s = Shape{SMALL, 64, 64, 1};
+    else if (div_up(m, 256) * div_up(n, 256) < 192) s = Shape{MIDDLE, 128, 128, 1};
+    if (s.kind != LARGE) {
+        const int64_t steps = div_up(k, SCALE_BLOCK), tiles = div_up(m, s.tm) * div_up(n, s.tn), want = 256 / tiles;
+        const int64_t splits = want < steps / 4 ? want : steps / 4;
         s.splits = (int)(splits < 1 ? 1 : splits > 16 ? 16 : splits);
     }
     return s;
@@ -99,22 +175,27 @@ Shape shape_of(int64_t m, int64_t n, int64_t k) {
 template <int SCALING, int TYPE>
 hipError_t launch_kind(const GemmFp8Args& a, int splits, hipStream_t st) {
     const Shape s = shape_of(a.m, a.n, a.k);
+    if (s.kind == FEW) {
+        const unsigned blocks = (unsigned)div_up(a.n, 16);
+        hipLaunchKernelGGL((gemm_fp8_few_kernel<SCALING, TYPE>), dim3(blocks), dim3(FEW_WAVES * 64), 0, st, a);
+        return hipGetLastError();
+    }
     GemmFp8Work w;
     w.g = a;
     w.steps = (int)div_up(a.k, SCALE_BLOCK);
     w.splits = splits;
-    const int tm = TYPE == TYPE_F32 && s.tm == 256 ? 128 : s.tm;
+    const int tm = TYPE == TYPE_F32 && s.kind == LARGE ? 128 : s.tm;
     w.tiles_m = (int)div_up(a.m, tm);
     w.tiles_n = (int)div_up(a.n, s.tn);
     const int64_t tiles = (int64_t)w.tiles_m * w.tiles_n;
-        w.order = tiles * splits >= 512 ? WorkOrder{32, w.tiles_m > 8 ? 4 : 8} : WorkOrder{0, 0};
+    w.order = WorkOrder{s.kind == LARGE ? 32 : 64, w.tiles_m > 8 ? 4 : 8};
     const unsigned blocks = (unsigned)(tiles * splits);
-    if (s.tm == 16) hipLaunchKernelGGL((gemm_fp8_few_kernel<SCALING, TYPE>), dim3(blocks), dim3(256), 0, st, w);
-    else if (s.tm == 128) hipLaunchKernelGGL((gemm_fp8_middle_kernel<SCALING, TYPE>), dim3(blocks), dim3(256), 0, st, w);
+    if (s.kind == SMALL) hipLaunchKernelGGL((gemm_fp8_small_kernel<SCALING, TYPE>), dim3(blocks), dim3(256), 0, st, w);
+    else if (s.kind == MIDDLE) hipLaunchKernelGGL((gemm_fp8_middle_kernel<SCALING, TYPE>), dim3(blocks), dim3(256), 0, st, w);
     else if constexpr (TYPE == TYPE_F32) hipLaunchKernelGGL((gemm_fp8_wide_kernel<SCALING>), dim3(blocks), dim3(512), 0, st, w);
     else hipLaunchKernelGGL((gemm_fp8_large_kernel<SCALING, TYPE>), dim3(blocks), dim3(512), 0, st, w);
     if (splits > 1) {
-        hipError_t e = hipGetLastError();
+        const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         hipLaunchKernelGGL((gemm_fp8_join_kernel<TYPE>), dim3((unsigned)div_up(a.n, 1024), (unsigned)a.m), dim3(256), 0, st, a, splits);
     }

@@ -332,9 +332,7 @@ enum { FEW, MIDDLE, LARGE };
 int shape_for(int64_t m, int64_t n) { return m <= 16 ? FEW : div_up(m, 256) * div_up(n, 256) < 128 || m <= 64 ? MIDDLE : LARGE; }
 int tile_m(int shape) { return shape == FEW ? 16 : shape == MIDDLE ? 64 : 256; }
 int tile_n(int shape) { return shape == LARGE ? 256 : 128; }
-WorkOrder order_for(int shape, int64_t tiles_m, int64_t items) {
-    return shape == LARGE && items >= 512 ? WorkOrder{32, tiles_m > 8 ? 4 : 8} : WorkOrder{0, 0};
-}
+WorkOrder order_for(int shape, int64_t tiles_m) { return WorkOrder{shape == LARGE ? 32 : 64, tiles_m > 8 ? 4 : 8}; }
 // shares of an inner dimension of `steps` steps, so that there are workgroups for every compute unit
 int product_splits(int64_t m, int64_t n, int64_t steps) {
     const int shape = shape_for(m, n);
@@ -386,7 +384,7 @@ hipError_t launch_product(ProductWork w, int shape, hipStream_t st) {
     w.tiles_m = (int)div_up(w.m, tile_m(shape));
     w.tiles_n = (int)div_up(w.n, tile_n(shape));
     const int64_t items = (int64_t)w.tiles_m * w.tiles_n * w.splits;
-    w.order = order_for(shape, w.tiles_m, items);
+    w.order = order_for(shape, w.tiles_m);
     if (shape == FEW) hipLaunchKernelGGL((loss_product_few_kernel<TYPE>), dim3((unsigned)items), dim3(256), 0, st, w);
     else if (shape == MIDDLE) hipLaunchKernelGGL((loss_product_middle_kernel<TYPE>), dim3((unsigned)items), dim3(256), 0, st, w);
     else hipLaunchKernelGGL((loss_product_large_kernel<TYPE>), dim3((unsigned)items), dim3(512), 0, st, w);
@@ -396,7 +394,7 @@ hipError_t launch_product(ProductWork w, int shape, hipStream_t st) {
 void set_tiles(LogitWork& w, int shape) {
     w.tiles_m = (int)div_up(w.tokens, tile_m(shape));
     w.tiles_n = (int)div_up(w.words, tile_n(shape));
-    w.order = order_for(shape, w.tiles_m, (int64_t)w.tiles_m * w.tiles_n);
+    w.order = order_for(shape, w.tiles_m);
     w.steps = (int)div_up(w.bytes, STEP_BYTES);
 }
 
