@@ -5,14 +5,14 @@
 // Forward: a workgroup forms a tile of z in registers and leaves each token's largest value and sum of exponentials over the tile's
 // words, 8 bytes per token and tile; a second launch joins them and takes the target's z, which the lane that held it has written.
 // Gradient: the vocabulary is taken in pieces.  A piece's z are formed again and become g in the 16-bit type of H and W (its rounding is of the
-// size of the result's own), stored as [token][word] and as [word][token]; the two products read it from there.  All products are
-// sums over 16-bit elements in FP32 on the matrix unit (tile_product.hpp) and want both operands contiguous along the inner
-// dimension, hence also a transposed H and a transposed piece of W.
+// size of the result's own), stored as [token][word]; the two products read it from there.  All products are sums over 16-bit elements in
+// FP32 on the matrix unit (tile_product.hpp).  W in dH, and g and H in dW, lie across the inner dimension; they are turned on the way from LDS
+// to registers (with copies turned in memory the gradient of 4096 x 65536 x 4096 took 5.3 ms, of 16 x 65536 x 2048 0.44 ms).
 //
 // What is held of g is (exp(z - lse) - [v == target]) * 2^12, without dloss.  Its largest entries, the targets', are then near a power of two
 // and lose nothing to 16 bits; times dloss they all lose alike, which does not average out (1.7 times the error of the result's own
 // rounding in FP16).  2^12 keeps the words down to a probability of 2^-26 among FP16's normal numbers.  dloss comes in where it costs no
-// rounding: as a factor of the rows of dH, and for dW with the transposed H, times dloss over the largest |dloss|, which is one for a mean.
+// rounding: as a factor of the rows of dH, and for dW with a copy of H times dloss over the largest |dloss|, which is one for a mean.
 #include "layout.hpp"
 #include "tile_product.hpp"
 
@@ -43,9 +43,8 @@ struct LogitWork {
     float* target_z;
     // gradient
     TokenState token;
-    uint8_t* G;              // [token][ldg], null: not wanted
-    uint8_t* Gt;             // [word][ldgt]
-    int64_t ldg, ldgt;       // elements
+    uint8_t* G;              // [token][ldg]; zeros behind the piece's words, up to a whole tile
+    int64_t ldg;             // elements
 };
 
 template <typename P>
@@ -166,7 +165,7 @@ __global__ void __launch_bounds__(1024) loss_tokens_kernel(const int64_t* target
     if (threadIdx.x == 0) *dw_factor = most * (1.0f / HELD);
 }
 
-// A tile of g: through LDS, [token][word], so that both results are written in pieces of 16 bytes.
+// A tile of g, through LDS so that it is written in rows of 16-byte pieces.
 template <typename P, typename T>
 __device__ __forceinline__ void loss_g_body(const LogitWork& w) {
     constexpr int STRIDE = P::TN * 2 + 16;            // bytes between tokens
@@ -198,53 +197,37 @@ __device__ __forceinline__ void loss_g_body(const LogitWork& w) {
         }
     }
     __syncthreads();
-    if (w.G != nullptr) {
-        for (int c = threadIdx.x; c < P::TM * P::TN / 8; c += P::THREADS) {
-            const int t = c / (P::TN / 8), p = c % (P::TN / 8);
-            if (m0 + t >= w.tokens) break;
-            *reinterpret_cast<v4i32*>(w.G + ((m0 + t) * w.ldg + n0 + p * 8) * 2) = *reinterpret_cast<const v4i32*>(lds + t * STRIDE + p * 16);
-        }
-    }
-    if (w.Gt != nullptr) {
-        for (int c = threadIdx.x; c < P::TM * P::TN / 8; c += P::THREADS) {
-            const int word = c % P::TN, p = c / P::TN;
-            if (word >= words) continue;
-            v4i32 v;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const unsigned lo = *reinterpret_cast<const uint16_t*>(lds + (p * 8 + 2 * q) * STRIDE + word * 2);
-                const unsigned hi = *reinterpret_cast<const uint16_t*>(lds + (p * 8 + 2 * q + 1) * STRIDE + word * 2);
-                v[q] = (int)(lo | hi << 16);
-            }
-            *reinterpret_cast<v4i32*>(w.Gt + ((n0 + word) * w.ldgt + m0 + p * 8) * 2) = v;
-        }
+    for (int c = threadIdx.x; c < P::TM * P::TN / 8; c += P::THREADS) {
+        const int t = c / (P::TN / 8), p = c % (P::TN / 8);
+        if (m0 + t >= w.tokens) break;
+        *reinterpret_cast<v4i32*>(w.G + ((m0 + t) * w.ldg + n0 + p * 8) * 2) = *reinterpret_cast<const v4i32*>(lds + t * STRIDE + p * 16);
     }
 }
 
-// [row][column] -> [column][row], 64 x 64 at a time, zeros for rows beyond the matrix; rows times `share` if there is one, where those
-// of tokens that do not count (counts[row] < 0) are zeros whatever they hold.
+// H for dW: times the token's share, zeros where the token does not count, whatever it holds
 template <typename T>
-__device__ __forceinline__ void transpose_body(const T* from, int64_t ld, int64_t rows, int64_t columns, const int* counts, const float* share, T* to,
-                                               int64_t ldt) {
-    __shared__ T tile[64][66];
-    const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 64;
-    const int in = threadIdx.x & 63;
-    for (int i = threadIdx.x >> 6; i < 64; i += 4) {
-        const bool real = r0 + i < rows && c0 + in < columns && (counts == nullptr || counts[r0 + i] >= 0);
-        T x = real ? from[(r0 + i) * ld + c0 + in] : (T)0.0f;
-        if (real && share != nullptr) x = (T)((float)x * share[r0 + i]);
-        tile[i][in] = x;
+__device__ __forceinline__ void shares_body(const T* H, int64_t ldh, int64_t tokens, int64_t k, const int* target, const float* share, T* to, int64_t ld) {
+    typedef T eight __attribute__((ext_vector_type(8)));
+    const int64_t pieces = ld / 8;
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < tokens * pieces; at += (int64_t)gridDim.x * 256) {
+        const int64_t t = at / pieces, e = at % pieces * 8;
+        eight x = {};
+        if (target[t] >= 0) {
+            const float f = share[t];
+            x = *reinterpret_cast<const eight*>(H + t * ldh + e);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = (T)((float)x[i] * f);
+        }
+        *reinterpret_cast<eight*>(to + t * ld + e) = x;
     }
-    __syncthreads();
-    for (int i = threadIdx.x >> 6; i < 64; i += 4)
-        if (c0 + i < columns) to[(c0 + i) * ldt + r0 + in] = tile[in][i];
 }
 
-// D = X Y^T of 16-bit operands that lie in work memory or are the caller's: rows of Y are D's rows
+// D = X Y^T of 16-bit operands; rows of Y are D's rows
 struct ProductWork {
     const uint8_t* X;
     const uint8_t* Y;
-    int64_t ldx, ldy, bytes;
+    int64_t ldx, ldy, bytes; // ldx, ldy: in bytes
+    int64_t elements;        // of the inner dimension (turned operands)
     int64_t m, n;
     int tiles_m, tiles_n, steps, splits;
     WorkOrder order;
@@ -257,13 +240,13 @@ struct ProductWork {
 
 __device__ __forceinline__ int split_begin(int steps, int splits, int s) { return (int)((int64_t)steps * s / splits); }
 
-template <typename P, typename T>
+template <typename P, typename T, bool XT, bool YT>
 __device__ __forceinline__ void loss_product_body(const ProductWork& w) {
     __shared__ __attribute__((aligned(16))) uint8_t lds[P::LDS_BYTES];
     const WorkItem item = work_item(blockIdx.x, gridDim.x, w.order, w.tiles_m, w.tiles_n);
     const int64_t m0 = (int64_t)item.bm * P::TM, n0 = (int64_t)item.bn * P::TN, left_m = w.m - m0, left_n = w.n - n0;
-    const TileOperand X{w.X + n0 * w.ldx, w.ldx, (int)(left_n < P::TN ? left_n : P::TN), nullptr, 0};
-    const TileOperand Y{w.Y + m0 * w.ldy, w.ldy, (int)(left_m < P::TM ? left_m : P::TM), nullptr, 0};
+    const TileOperand X{w.X + n0 * (XT ? 2 : w.ldx), w.ldx, (int)(left_n < P::TN ? left_n : P::TN), nullptr, 0, w.elements};
+    const TileOperand Y{w.Y + m0 * (YT ? 2 : w.ldy), w.ldy, (int)(left_m < P::TM ? left_m : P::TM), nullptr, 0, w.elements};
     v4f32 acc[P::FN][P::FM] = {};
     const int split = item.gi;
     P::multiply(lds, X, Y, w.bytes, split_begin(w.steps, w.splits, split), split_begin(w.steps, w.splits, split + 1), acc);
@@ -308,12 +291,27 @@ template <int TYPE>
 __global__ void __launch_bounds__(256) loss_g_middle_kernel(const LogitWork w) { loss_g_body<MiddleTile<TYPE>, typename Element<TYPE>::type>(w); }
 template <int TYPE>
 __global__ void __launch_bounds__(256) loss_g_few_kernel(const LogitWork w) { loss_g_body<FewTile<TYPE>, typename Element<TYPE>::type>(w); }
+// dH = g W, and dW = g^T H
 template <int TYPE>
-__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) loss_product_large_kernel(const ProductWork w) { loss_product_body<LargeTile<TYPE>, typename Element<TYPE>::type>(w); }
+__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) loss_dh_large_kernel(const ProductWork w) {
+    loss_product_body<PairedTile<kind_of(TYPE), true, false>, typename Element<TYPE>::type, true, false>(w);
+}
 template <int TYPE>
-__global__ void __launch_bounds__(256) loss_product_middle_kernel(const ProductWork w) { loss_product_body<MiddleTile<TYPE>, typename Element<TYPE>::type>(w); }
+__global__ void __launch_bounds__(256) loss_dh_middle_kernel(const ProductWork w) {
+    loss_product_body<Tile<kind_of(TYPE), 2, 2, 4, 2, 3, true, false>, typename Element<TYPE>::type, true, false>(w);
+}
 template <int TYPE>
-__global__ void __launch_bounds__(256) loss_product_few_kernel(const ProductWork w) { loss_product_body<FewTile<TYPE>, typename Element<TYPE>::type>(w); }
+__global__ void __launch_bounds__(256) loss_dh_few_kernel(const ProductWork w) {
+    loss_product_body<Tile<kind_of(TYPE), 4, 1, 2, 1, 4, true, false>, typename Element<TYPE>::type, true, false>(w);
+}
+template <int TYPE>
+__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) loss_dw_large_kernel(const ProductWork w) {
+    loss_product_body<PairedTile<kind_of(TYPE), true, true>, typename Element<TYPE>::type, true, true>(w);
+}
+template <int TYPE>
+__global__ void __launch_bounds__(256) loss_dw_middle_kernel(const ProductWork w) {
+    loss_product_body<Tile<kind_of(TYPE), 2, 2, 4, 4, 2, true, true>, typename Element<TYPE>::type, true, true>(w);
+}
 template <int TYPE>
 __global__ void __launch_bounds__(256) loss_product_join_kernel(const float* partial, int splits, int64_t m, int64_t n, float* sum, bool first, bool last,
                                                                 const float* row_factor, void* D, int64_t ldd) {
@@ -321,10 +319,10 @@ __global__ void __launch_bounds__(256) loss_product_join_kernel(const float* par
 }
 
 template <int TYPE>
-__global__ void __launch_bounds__(256) loss_transpose_kernel(const void* from, int64_t ld, int64_t rows, int64_t columns, const int* counts, const float* share,
-                                                             void* to, int64_t ldt) {
+__global__ void __launch_bounds__(256) loss_shares_kernel(const void* H, int64_t ldh, int64_t tokens, int64_t k, const int* target, const float* share, void* to,
+                                                          int64_t ld) {
     typedef typename Element<TYPE>::type T;
-    transpose_body(static_cast<const T*>(from), ld, rows, columns, counts, share, static_cast<T*>(to), ldt);
+    shares_body(static_cast<const T*>(H), ldh, tokens, k, target, share, static_cast<T*>(to), ld);
 }
 
 // ---- shapes and work memory ------------------------------------------------------------------------------------
@@ -333,27 +331,29 @@ int shape_for(int64_t m, int64_t n) { return m <= 16 ? FEW : div_up(m, 256) * di
 int tile_m(int shape) { return shape == FEW ? 16 : shape == MIDDLE ? 64 : 256; }
 int tile_n(int shape) { return shape == LARGE ? 256 : 128; }
 WorkOrder order_for(int shape, int64_t tiles_m) { return WorkOrder{shape == LARGE ? 32 : 64, tiles_m > 8 ? 4 : 8}; }
-// shares of an inner dimension of `steps` steps, so that there are workgroups for every compute unit
-int product_splits(int64_t m, int64_t n, int64_t steps) {
-    const int shape = shape_for(m, n);
+// dH, whose inner dimension is the vocabulary: large tiles also where they are few, if that leaves every compute unit a share of it of
+// some length (1003 x 1024 over 50001 words: 16 tiles in 16 shares)
+struct ProductShape { int shape, splits; };
+ProductShape dh_shape(int64_t m, int64_t n, int64_t steps) {
+    int shape = shape_for(m, n);
+    if (shape == MIDDLE && m > 64 && div_up(m, 256) * div_up(n, 256) * (steps / 16) >= 128) shape = LARGE;
     const int64_t tiles = div_up(m, tile_m(shape)) * div_up(n, tile_n(shape)), want = (shape == LARGE ? 256 : 512) / tiles, most = steps / 8;
     const int64_t s = want < most ? want : most;
-    return (int)(s < 1 ? 1 : s > 32 ? 32 : s);
+    return ProductShape{shape, (int)(s < 1 ? 1 : s > 32 ? 32 : s)};
 }
 
 size_t up(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 constexpr int64_t EDGE = 256;            // what g is padded to, with zeros
 int64_t padded(int64_t n) { return div_up(n, EDGE) * EDGE; }
+int64_t in_eights(int64_t n) { return div_up(n, 8) * 8; }
 
 struct GradPlaces {
     float* dw_factor;
     float* row_factor;
     float* share;
     int* target;
-    uint8_t* Ht;
-    uint8_t* Wt;
+    uint8_t* Hs;
     uint8_t* G;
-    uint8_t* Gt;
     float* partial;
     float* sum;
     size_t total;
@@ -363,15 +363,13 @@ GradPlaces grad_places(uint8_t* ws, int64_t tokens, int64_t vocab, int64_t k, in
     size_t at = 256;                     // the flag words
     auto take = [&](size_t bytes) { uint8_t* const here = ws + at; at += up(bytes); return here; };
     const int64_t words = piece < vocab ? piece : vocab;
-    const int splits = product_splits(tokens, k, div_up(words * 2, STEP_BYTES));
+    const int splits = dh_shape(tokens, k, div_up(words * 2, STEP_BYTES)).splits;
     p.dw_factor = reinterpret_cast<float*>(take(4));
     p.row_factor = reinterpret_cast<float*>(take((size_t)tokens * 4));
     p.share = reinterpret_cast<float*>(take((size_t)tokens * 4));
     p.target = reinterpret_cast<int*>(take((size_t)tokens * 4));
-    p.Ht = take((size_t)k * padded(tokens) * 2);
-    p.Wt = take((size_t)k * padded(words) * 2);
+    p.Hs = take((size_t)tokens * in_eights(k) * 2);
     p.G = take((size_t)tokens * padded(words) * 2);
-    p.Gt = take((size_t)words * padded(tokens) * 2);
     const bool joined = splits > 1 || piece < vocab;
     p.partial = reinterpret_cast<float*>(take(joined ? (size_t)splits * tokens * k * 4 : 0));
     p.sum = reinterpret_cast<float*>(take(piece < vocab ? (size_t)tokens * k * 4 : 0));
@@ -380,14 +378,26 @@ GradPlaces grad_places(uint8_t* ws, int64_t tokens, int64_t vocab, int64_t k, in
 }
 
 template <int TYPE>
-hipError_t launch_product(ProductWork w, int shape, hipStream_t st) {
+hipError_t launch_dh(ProductWork w, int shape, hipStream_t st) {
     w.tiles_m = (int)div_up(w.m, tile_m(shape));
     w.tiles_n = (int)div_up(w.n, tile_n(shape));
-    const int64_t items = (int64_t)w.tiles_m * w.tiles_n * w.splits;
     w.order = order_for(shape, w.tiles_m);
-    if (shape == FEW) hipLaunchKernelGGL((loss_product_few_kernel<TYPE>), dim3((unsigned)items), dim3(256), 0, st, w);
-    else if (shape == MIDDLE) hipLaunchKernelGGL((loss_product_middle_kernel<TYPE>), dim3((unsigned)items), dim3(256), 0, st, w);
-    else hipLaunchKernelGGL((loss_product_large_kernel<TYPE>), dim3((unsigned)items), dim3(512), 0, st, w);
+    const dim3 blocks((unsigned)((int64_t)w.tiles_m * w.tiles_n * w.splits));
+    if (shape == FEW) hipLaunchKernelGGL((loss_dh_few_kernel<TYPE>), blocks, dim3(256), 0, st, w);
+    else if (shape == MIDDLE) hipLaunchKernelGGL((loss_dh_middle_kernel<TYPE>), blocks, dim3(256), 0, st, w);
+    else hipLaunchKernelGGL((loss_dh_large_kernel<TYPE>), blocks, dim3(512), 0, st, w);
+    return hipGetLastError();
+}
+template <int TYPE>
+hipError_t launch_dw(ProductWork w, hipStream_t st) {
+    const bool large = shape_for(w.m, w.n) == LARGE;
+    const int edge = large ? 256 : 128;
+    w.tiles_m = (int)div_up(w.m, edge);
+    w.tiles_n = (int)div_up(w.n, edge);
+    w.order = order_for(large ? LARGE : MIDDLE, w.tiles_m);
+    const dim3 blocks((unsigned)((int64_t)w.tiles_m * w.tiles_n));
+    if (large) hipLaunchKernelGGL((loss_dw_large_kernel<TYPE>), blocks, dim3(512), 0, st, w);
+    else hipLaunchKernelGGL((loss_dw_middle_kernel<TYPE>), blocks, dim3(256), 0, st, w);
     return hipGetLastError();
 }
 
@@ -428,19 +438,17 @@ hipError_t forward_typed(const LossArgs& a, uint8_t* ws, hipStream_t st) {
 #define OZAKI_LOSS_TRY(expr) do { const hipError_t e_ = (expr); if (e_ != hipSuccess) return e_; } while (0)
 
 template <int TYPE>
-hipError_t transpose(const void* from, int64_t ld, int64_t rows, int64_t columns, const int* counts, const float* share, uint8_t* to, hipStream_t st) {
-    hipLaunchKernelGGL((loss_transpose_kernel<TYPE>), dim3((unsigned)(padded(rows) / 64), (unsigned)div_up(columns, 64)), dim3(256), 0, st, from, ld, rows,
-                       columns, counts, share, to, padded(rows));
-    return hipGetLastError();
-}
-
-template <int TYPE>
 hipError_t grad_typed(const LossArgs& a, int64_t piece, uint8_t* ws, hipStream_t st) {
     const GradPlaces p = grad_places(ws, a.tokens, a.vocab, a.k, piece);
     hipLaunchKernelGGL(loss_tokens_kernel, dim3(1), dim3(1024), 0, st, a.targets, a.dloss, a.tokens, a.vocab, a.ignore, p.target, p.row_factor, p.share,
                        p.dw_factor, a.flags);
     OZAKI_LOSS_TRY(hipGetLastError());
-    if (a.dW != nullptr) OZAKI_LOSS_TRY(transpose<TYPE>(a.H, a.ldh, a.tokens, a.k, p.target, p.share, p.Ht, st));
+    if (a.dW != nullptr) {
+        const int64_t ld = in_eights(a.k), blocks = div_up(a.tokens * (ld / 8), 256);
+        hipLaunchKernelGGL((loss_shares_kernel<TYPE>), dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, st, a.H, a.ldh, a.tokens, a.k, p.target,
+                           p.share, p.Hs, ld);
+        OZAKI_LOSS_TRY(hipGetLastError());
+    }
     const bool joined = piece < a.vocab;
     for (int64_t first = 0; first < a.vocab; first += piece) {
         const int64_t words = a.vocab - first < piece ? a.vocab - first : piece;
@@ -457,31 +465,31 @@ hipError_t grad_typed(const LossArgs& a, int64_t piece, uint8_t* ws, hipStream_t
         const int shape = shape_for(a.tokens, words);
         set_tiles(w, shape);
         w.token = TokenState{a.lse_in, p.target};
-        w.G = a.dH != nullptr ? p.G : nullptr;
-        w.Gt = a.dW != nullptr ? p.Gt : nullptr;
+        w.G = p.G;
         w.ldg = padded(words);
-        w.ldgt = padded(a.tokens);
         const unsigned blocks = (unsigned)(w.tiles_m * (int64_t)w.tiles_n);
         if (shape == FEW) hipLaunchKernelGGL((loss_g_few_kernel<TYPE>), dim3(blocks), dim3(256), 0, st, w);
         else if (shape == MIDDLE) hipLaunchKernelGGL((loss_g_middle_kernel<TYPE>), dim3(blocks), dim3(256), 0, st, w);
         else hipLaunchKernelGGL((loss_g_large_kernel<TYPE>), dim3(blocks), dim3(512), 0, st, w);
         OZAKI_LOSS_TRY(hipGetLastError());
         if (a.dH != nullptr) {
-            OZAKI_LOSS_TRY(transpose<TYPE>(W, a.ldw, words, a.k, nullptr, nullptr, p.Wt, st));
             ProductWork d = {};
-            d.X = p.Wt;
+            d.X = W;
             d.Y = p.G;
-            d.ldx = d.ldy = padded(words) * 2;
-            d.bytes = words * 2;
+            d.ldx = a.ldw * 2;
+            d.ldy = padded(words) * 2;
+            d.bytes = words * 2;                     // (behind them g has zeros to the end of the piece)
+            d.elements = words;
             d.m = a.tokens;
             d.n = a.k;
             d.steps = (int)div_up(d.bytes, STEP_BYTES);
-            d.splits = product_splits(d.m, d.n, d.steps);
+            const ProductShape ps = dh_shape(d.m, d.n, d.steps);
+            d.splits = ps.splits;
             d.D = a.dH;
             d.ldd = a.lddh;
             d.row_factor = p.row_factor;
             d.partial = joined || d.splits > 1 ? p.partial : nullptr;
-            OZAKI_LOSS_TRY((launch_product<TYPE>(d, shape_for(d.m, d.n), st)));
+            OZAKI_LOSS_TRY(launch_dh<TYPE>(d, ps.shape, st));
             if (d.partial != nullptr) {
                 const int64_t blocks_j = div_up(d.m * d.n, 256);
                 hipLaunchKernelGGL((loss_product_join_kernel<TYPE>), dim3((unsigned)(blocks_j < 4096 ? blocks_j : 4096)), dim3(256), 0, st, p.partial, d.splits,
@@ -491,10 +499,12 @@ hipError_t grad_typed(const LossArgs& a, int64_t piece, uint8_t* ws, hipStream_t
         }
         if (a.dW != nullptr) {
             ProductWork d = {};
-            d.X = p.Ht;
-            d.Y = p.Gt;
-            d.ldx = d.ldy = padded(a.tokens) * 2;
+            d.X = p.Hs;
+            d.Y = p.G;
+            d.ldx = in_eights(a.k) * 2;
+            d.ldy = padded(words) * 2;
             d.bytes = a.tokens * 2;
+            d.elements = a.tokens;
             d.m = words;
             d.n = a.k;
             d.steps = (int)div_up(d.bytes, STEP_BYTES);
@@ -502,7 +512,7 @@ hipError_t grad_typed(const LossArgs& a, int64_t piece, uint8_t* ws, hipStream_t
             d.D = static_cast<uint8_t*>(a.dW) + first * a.lddw * 2;
             d.ldd = a.lddw;
             d.factor = p.dw_factor;
-            OZAKI_LOSS_TRY((launch_product<TYPE>(d, shape_for(d.m, d.n), st)));
+            OZAKI_LOSS_TRY(launch_dw<TYPE>(d, st));
         }
     }
     return hipSuccess;
@@ -515,9 +525,9 @@ size_t loss_bytes(int64_t tokens, int64_t vocab) {
 }
 size_t loss_grad_bytes(int64_t tokens, int64_t vocab, int64_t k, int64_t piece) { return grad_places(nullptr, tokens, vocab, k, piece).total; }
 
-// As few pieces as keep one piece's g, [token][word] and [word][token], and its transposed weights within 1 GiB, all of a length.
+// As few pieces as keep one piece's g within 1 GiB, all of a length.
 int64_t loss_grad_piece(int64_t tokens, int64_t vocab, int64_t k) {
-    const int64_t per_word = 2 * (2 * padded(tokens) + k), fits = ((int64_t)1 << 30) / per_word, most = fits < LOSS_PIECE ? LOSS_PIECE : fits;
+    const int64_t fits = ((int64_t)1 << 30) / (2 * tokens), most = fits < LOSS_PIECE ? LOSS_PIECE : fits;
     const int64_t piece = padded(div_up(vocab, div_up(vocab, most)));
     return piece < LOSS_PIECE ? LOSS_PIECE : piece;
 }

@@ -71,7 +71,53 @@ struct TileOperand {
     int rows;                    // vectors from there to the matrix's last, at least 1
     const float* scales;         // FP8: of the tile's first vector (or block of vectors) in inner block 0
     int64_t scale_stride;        // between inner blocks
+    // Turned operands (16 bits): the matrix lies the other way, element e of all vectors in a row; `vectors` is element 0 of the tile's first
+    // vector, `stride` the distance between rows, and `rows` the vectors from there on; there are `elements` rows.
+    int64_t elements = 0;
 };
+
+// A turned operand in LDS: 64 rows of 128 vectors, 256 bytes each, to a panel.  A fragment is read with ds_read_b64_tr_b16, which gives a lane four
+// elements of one vector: the sixteen lanes of a group address four rows of 32 bytes, row (lane % 16) / 4, and get vector lane % 16 of them.
+// Lanes that are served together read rows 0 - 3 of each eight at the same 32 bytes; piece p (32 bytes) of row r lies at p ^ turned_place(r),
+// which spreads them over the banks.
+constexpr int PANEL_BYTES = 64 * 256;
+__device__ __forceinline__ int turned_place(int row) { return (row & 3) | ((row >> 3) & 1) << 2; }
+// Direct loads beside ds_read_b64_tr_b16: the compiler takes every such read to depend on every direct load under way and waits for all of
+// them, which the pipelines here are built not to do, so the loads are written out.  (They have no register to return to; who reads what
+// they bring waits for them in tile_wait.  The pause is for m0, and for scalar registers that a vector instruction may have written just before.)
+__device__ __forceinline__ unsigned lds_place(const uint8_t* lds) { return __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)OZAKI_TILE_LPTR(lds)); }
+__device__ __forceinline__ void direct_load(const uint8_t* from, const uint8_t* lds) {
+    int m0;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0"
+                 : "=&s"(m0) : "s"(lds_place(lds)), "v"(from) : "memory");
+}
+__device__ __forceinline__ void direct_load(v4i32 resource, unsigned offset, int step, const uint8_t* lds) {
+    int m0;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 4\n\tbuffer_load_dwordx4 %2, %3, %4 offen lds\n\ts_mov_b32 m0, %0"
+                 : "=&s"(m0) : "s"(lds_place(lds)), "v"(offset), "s"(resource), "s"(step) : "memory");
+}
+// the words of a raw buffer resource
+__device__ __forceinline__ v4i32 resource_of(const uint8_t* base, unsigned records) {
+    const uint64_t at = reinterpret_cast<uint64_t>(base);
+    return v4i32{__builtin_amdgcn_readfirstlane((int)(unsigned)at), __builtin_amdgcn_readfirstlane((int)(unsigned)(at >> 32) & 0xFFFF), (int)records, 0x00027000};
+}
+
+// the lane's share of 16 vectors (piece `p` of a panel) and 64 elements, in the order in which a lane reads pieces g and g + 4 of an ordinary row
+__device__ __forceinline__ v8i32 turned_fragment(const uint8_t* panel, int p, int lane) {
+    typedef short v4i16 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) v4i16* place;
+    const int g = lane >> 4, in = (lane >> 2) & 3, at = (8 * g + in) * 256 + ((p ^ (in | (g & 1) << 2)) << 5) + (lane & 3) * 8;
+    v8i32 out;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const v2i32 two = __builtin_bit_cast(v2i32, __builtin_amdgcn_ds_read_tr16_b64_v4i16((place)OZAKI_TILE_LPTR(panel + at + (32 * h + 4 * t) * 256)));
+            out[4 * h + 2 * t] = two[0];
+            out[4 * h + 2 * t + 1] = two[1];
+        }
+    return out;
+}
 
 // four neighbouring elements of a row of D, the first `left` of them; `wide`: D's rows start at multiples of four elements
 template <typename T>
@@ -111,8 +157,8 @@ __device__ __forceinline__ void tile_wait() {
     asm volatile("" ::: "memory");
 }
 
-// WN x WM waves, each FN x FM tiles of 16 x 16
-template <int KIND, int WN_, int WM_, int FN_, int FM_, int NST_>
+// WN x WM waves, each FN x FM tiles of 16 x 16; XT, YT: the operand is turned
+template <int KIND, int WN_, int WM_, int FN_, int FM_, int NST_, bool XT = false, bool YT = false>
 struct Tile {
     static constexpr bool FP8 = KIND < KIND_BF16, WIDE = KIND == KIND_WIDE_BLOCKS || KIND == KIND_WIDE_VECTORS;
     static constexpr bool BLOCKS = KIND == KIND_FP8_BLOCKS || KIND == KIND_WIDE_BLOCKS;
@@ -123,10 +169,11 @@ struct Tile {
     static constexpr int LDS_BYTES = NST * STAGE_BYTES;
     static constexpr int PIECE_LOADS = ROWS / 8, SCALE_LOADS = SCALE_BYTES / 256;                  // wave instructions of a stage
     static constexpr int LPW = (PIECE_LOADS + WAVES - 1) / WAVES, SPW = (SCALE_LOADS + WAVES - 1) / WAVES;
-    static_assert((WN * FN * 16) % 8 == 0, "");
+    static_assert(!FP8 || (!XT && !YT), "");
+    static_assert((!XT || TN % 128 == 0) && (!YT || TM % 128 == 0), "");
 
     // acc[i][j][r] += X row wn * FN * 16 + 16 i + 4 (lane / 16) + r  times  Y row wm * FM * 16 + 16 j + lane % 16, over the steps
-    // [step0, step1) of vectors of `bytes` bytes.  Ends with nothing in flight and all waves past their last LDS read.
+    // [step0, step1) of vectors of `bytes` bytes (if only one operand is turned, the other has zeros behind them to the end of the 16 bytes).  Ends with nothing in flight and all waves past their last LDS read.
     __device__ static void multiply(uint8_t* lds, const TileOperand& X, const TileOperand& Y, int64_t bytes, int step0, int step1,
                                     v4f32 (&acc)[FN][FM]) {
         const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -152,6 +199,13 @@ struct Tile {
                 voff[i] = (unsigned)(mine < rows ? mine : rows - 1) * (unsigned)(x ? X.stride : Y.stride) + piece * 16;
                 from[i] = (x ? X.vectors : Y.vectors) + (int64_t)step0 * STEP_BYTES;
                 to[i] = at * 1024;
+                if ((x && XT) || (!x && YT)) {
+                    // four rows of a panel
+                    const int q = x ? at : at - TN / 8, e = (q & 15) * 4 + (lane >> 4);
+                    const int v = (q >> 4) * 128 + (((lane & 15) >> 1) ^ turned_place(e)) * 16 + (lane & 1) * 8;
+                    voff[i] = (unsigned)e * (unsigned)(x ? X.stride : Y.stride) + 2 * (unsigned)(v < rows ? v : 0);
+                    from[i] = (x ? X.vectors : Y.vectors) + (int64_t)step0 * 64 * (x ? X.stride : Y.stride);
+                }
             }
         }
         const float* sfrom[SPW > 0 ? SPW : 1];
@@ -171,6 +225,14 @@ struct Tile {
                 sto[i] = ROWS * STEP_BYTES + at * 256;
             }
         }
+        auto is_x = [&](int i) {
+            const int at = wave * LPW + i;
+            return (at < PIECE_LOADS ? at : PIECE_LOADS - 1) * 8 < TN;
+        };
+        auto step_of = [&](int i) -> int64_t {
+            if (XT || YT) return is_x(i) ? (XT ? 64 * X.stride : STEP_BYTES) : (YT ? 64 * Y.stride : STEP_BYTES);
+            return STEP_BYTES;
+        };
         int issue_buf = 0;
         auto issue_scales = [&]() {
             if constexpr (FP8) {
@@ -184,8 +246,9 @@ struct Tile {
         auto issue_full = [&]() {
 #pragma unroll
             for (int i = 0; i < LPW; ++i) {
-                __builtin_amdgcn_global_load_lds(OZAKI_TILE_GPTR(from[i] + voff[i]), OZAKI_TILE_LPTR(lds + issue_buf * STAGE_BYTES + to[i]), 16, 0, 0);
-                from[i] += STEP_BYTES;
+                if constexpr (XT || YT) direct_load(from[i] + voff[i], lds + issue_buf * STAGE_BYTES + to[i]);
+                else __builtin_amdgcn_global_load_lds(OZAKI_TILE_GPTR(from[i] + voff[i]), OZAKI_TILE_LPTR(lds + issue_buf * STAGE_BYTES + to[i]), 16, 0, 0);
+                from[i] += step_of(i);
             }
             issue_scales();
             issue_buf = issue_buf + 1 == NST ? 0 : issue_buf + 1;
@@ -197,8 +260,15 @@ struct Tile {
                 int at = wave * LPW + i;
                 at = at < PIECE_LOADS ? at : PIECE_LOADS - 1;
                 const int piece = (lane & 7) ^ (((at * 8 + (lane >> 3)) >> 1) & 7);
-                const uint8_t* src = none || piece * 16 >= last_bytes ? no_elements : from[i] + voff[i];
-                __builtin_amdgcn_global_load_lds(OZAKI_TILE_GPTR(src), OZAKI_TILE_LPTR(lds + issue_buf * STAGE_BYTES + to[i]), 16, 0, 0);
+                bool there = !none && piece * 16 < last_bytes;
+                if (XT || YT) {
+                    const bool x = at * 8 < TN;
+                    const int e = ((x ? at : at - TN / 8) & 15) * 4 + (lane >> 4);
+                    if (x ? XT : YT) there = !none && (int64_t)(step1 - 1) * 64 + e < (x ? X.elements : Y.elements);
+                }
+                const uint8_t* src = there ? from[i] + voff[i] : no_elements;
+                if constexpr (XT || YT) direct_load(src, lds + issue_buf * STAGE_BYTES + to[i]);
+                else __builtin_amdgcn_global_load_lds(OZAKI_TILE_GPTR(src), OZAKI_TILE_LPTR(lds + issue_buf * STAGE_BYTES + to[i]), 16, 0, 0);
             }
             if constexpr (FP8) {
 #pragma unroll
@@ -225,7 +295,22 @@ struct Tile {
             typedef typename Fragment<WIDE>::type operand;
             constexpr int AHEAD = FN > 1 ? 2 : 1;                     // rows whose fragments are read in front
             operand y[FM], x[AHEAD + 1];
-            auto row = [&](int i) { return Fragment<WIDE>::of(fragment(stage + xbase + i * 16 * STEP_BYTES)); };
+            auto row = [&](int i) {
+                if constexpr (XT) {
+                    const int t = wn * FN + i;
+                    return turned_fragment(stage + (t >> 3) * PANEL_BYTES, t & 7, lane);
+                } else {
+                    return Fragment<WIDE>::of(fragment(stage + xbase + i * 16 * STEP_BYTES));
+                }
+            };
+            auto column = [&](int j) {
+                if constexpr (YT) {
+                    const int t = wm * FM + j;
+                    return turned_fragment(stage + TN * STEP_BYTES + (t >> 3) * PANEL_BYTES, t & 7, lane);
+                } else {
+                    return Fragment<WIDE>::of(fragment(stage + ybase + j * 16 * STEP_BYTES));
+                }
+            };
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (FP8) {
                 const float* const scales = reinterpret_cast<const float*>(stage + ROWS * STEP_BYTES);
@@ -234,7 +319,7 @@ struct Tile {
                 v4f32 t[T], sx[2] = {};
 #pragma unroll
                 for (int j = 0; j < FM; ++j) {
-                    y[j] = Fragment<WIDE>::of(fragment(stage + ybase + j * 16 * STEP_BYTES));
+                    y[j] = column(j);
                     if (j < AHEAD && j < FN) x[j] = row(j);
                 }
                 if (AHEAD > FM) x[1] = row(1);
@@ -267,7 +352,7 @@ struct Tile {
             } else {
 #pragma unroll
                 for (int j = 0; j < FM; ++j) {
-                    y[j] = Fragment<WIDE>::of(fragment(stage + ybase + j * 16 * STEP_BYTES));
+                    y[j] = column(j);
                     if (j < AHEAD && j < FN) x[j] = row(j);
                 }
                 if (AHEAD > FM) x[1] = row(1);
@@ -310,7 +395,7 @@ struct Tile {
             const int next = s + NST - 1;
             if (next + 1 == steps && !ragged) issue_full();
             else issue_last(next >= steps);
-            if (s + 1 == steps && (last_bytes & 15) != 0) {
+            if (!XT && !YT && s + 1 == steps && (last_bytes & 15) != 0) {
                 // the end lies inside a piece
                 for (int row = tid; row < ROWS; row += THREADS) {
                     v4i32* const at = reinterpret_cast<v4i32*>(lds + read_buf * STAGE_BYTES + row * STEP_BYTES + (((last_bytes >> 4) ^ ((row >> 1) & 7)) << 4));
@@ -338,7 +423,7 @@ struct Tile {
 // that reads it has been issued.  So no wave waits for LDS at a step's head.
 // Whole steps are loaded with buffer instructions, whose addresses are 32-bit offsets of a lane and of the step: 256 accumulators of two waves
 // leave no registers for 64-bit ones.
-template <int KIND>
+template <int KIND, bool XT = false, bool YT = false>
 struct PairedTile {
     typedef Tile<KIND, 2, 4, 8, 4, 2> Base;
     static constexpr bool FP8 = Base::FP8, BLOCKS = Base::BLOCKS;
@@ -352,6 +437,10 @@ struct PairedTile {
     // Vectors that end inside a piece: their last step on its own, by Tile.  (Clearing the piece in the pipeline costs it a hundred registers.)
     __device__ static void multiply(uint8_t* lds, const TileOperand& X, const TileOperand& Y, int64_t bytes, int step0, int step1,
                                     v4f32 (&acc)[FN][FM]) {
+        if constexpr (XT || YT) {                    // (a turned operand ends at a row)
+            pipeline(lds, X, Y, bytes, step0, step1, acc);
+            return;
+        }
         const bool inside = (bytes & 15) != 0 && bytes < (int64_t)step1 * STEP_BYTES;
         const int whole = step1 - (inside ? 1 : 0);
         if (whole > step0) pipeline(lds, X, Y, bytes, step0, whole, acc);
@@ -359,7 +448,7 @@ struct PairedTile {
     }
 
     __device__ static TileOperand offset(const TileOperand& o, int step) {
-        return TileOperand{o.vectors + (int64_t)step * STEP_BYTES, o.stride, o.rows, o.scales + (int64_t)step * o.scale_stride, o.scale_stride};
+        return TileOperand{o.vectors + (int64_t)step * STEP_BYTES, o.stride, o.rows, o.scales + (int64_t)step * o.scale_stride, o.scale_stride, 0};
     }
 
     __device__ static void pipeline(uint8_t* lds, const TileOperand& X, const TileOperand& Y, int64_t bytes, int step0, int step1,
@@ -378,11 +467,20 @@ struct PairedTile {
         constexpr unsigned RECORDS = 0x7FFFFFFFu;
         const __amdgpu_buffer_rsrc_t in_x = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(X.vectors), 0, RECORDS, 0x00027000);
         const __amdgpu_buffer_rsrc_t in_y = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(Y.vectors), 0, RECORDS, 0x00027000);
+        // A turned operand's loads bring four rows of a panel of 128 vectors: of X, panel 0 is part 1 and panel 1 part 2.
+        auto panel_load = [&](int i) { return i < 4 ? wave * 4 + i : (i < P1 ? wave * 2 + i - 4 : 16 + wave * 2 + i - P1); };
+        auto element_of = [&](int i) { return (panel_load(i) & 15) * 4 + (lane >> 4); };
         unsigned voff[P1 + P2];
 #pragma unroll
         for (int i = 0; i < P1 + P2; ++i) {
-            const int row = row_of(i) + (lane >> 3), mine = i < 4 ? row - TN : row, rows = i < 4 ? Y.rows : X.rows;
-            voff[i] = (unsigned)(mine < rows ? mine : rows - 1) * (unsigned)(i < 4 ? Y.stride : X.stride) + (((lane & 7) ^ ((row >> 1) & 7)) << 4);
+            const TileOperand& o = i < 4 ? Y : X;
+            const int row = row_of(i) + (lane >> 3), mine = i < 4 ? row - TN : row;
+            voff[i] = (unsigned)(mine < o.rows ? mine : o.rows - 1) * (unsigned)o.stride + (((lane & 7) ^ ((row >> 1) & 7)) << 4);
+            if (i < 4 ? YT : XT) {
+                const int e = element_of(i), panel = panel_load(i) >> 4, c = (((lane & 15) >> 1) ^ turned_place(e)) * 16 + (lane & 1) * 8;
+                const int v = i < 4 ? panel * 128 + c : (c >> 6) * 128 + panel * 64 + (c & 63);
+                voff[i] = (unsigned)e * (unsigned)o.stride + 2 * (unsigned)(v < o.rows ? v : 0);
+            }
         }
         // the scales of a wave's 64 rows of the stage
         const bool x_scales = wave < 4;
@@ -394,12 +492,23 @@ struct PairedTile {
         // load i of step `s`; `plain`: a whole step is there to be read; otherwise zeros come from behind the vectors' end
         auto load = [&](int i, int s, bool plain) {
             unsigned at = voff[i];
+            const bool turned = i < 4 ? YT : XT;
+            const TileOperand& o = i < 4 ? Y : X;
             if (!plain) {
                 const int limit = s + 1 < steps ? STEP_BYTES : s + 1 == steps ? last_bytes : 0;
-                if ((int)((lane & 7) ^ (((row_of(i) + (lane >> 3)) >> 1) & 7)) * 16 >= limit) at = RECORDS;
+                const bool there = turned ? s < steps && (int64_t)(step0 + s) * 64 + element_of(i) < o.elements
+                                          : (int)((lane & 7) ^ (((row_of(i) + (lane >> 3)) >> 1) & 7)) * 16 < limit;
+                if (!there) at = RECORDS;
             }
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(i < 4 ? in_y : in_x, OZAKI_TILE_LPTR(lds + (s & 1) * STAGE_BYTES + row_of(i) * STEP_BYTES), 16, at,
-                                                     (step0 + s) * STEP_BYTES, 0, 0);
+            uint8_t* const to = lds + (s & 1) * STAGE_BYTES + (turned ? (i < 4 ? TN * STEP_BYTES : 0) + panel_load(i) * 1024 : row_of(i) * STEP_BYTES);
+            if (turned) {
+                // (a step is 64 rows on, which may pass 32 bits)
+                direct_load(resource_of(o.vectors + (int64_t)(step0 + s) * 64 * o.stride, RECORDS), at, 0, to);
+            } else if (XT || YT) {
+                direct_load(resource_of(o.vectors, RECORDS), at, (step0 + s) * STEP_BYTES, to);
+            } else {
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(i < 4 ? in_y : in_x, OZAKI_TILE_LPTR(to), 16, at, (step0 + s) * STEP_BYTES, 0, 0);
+            }
         };
         int scale_to = 0, scale_at = 0;                               // places in the ring of scales
         auto load_scales = [&](int s, bool plain) {
@@ -421,6 +530,15 @@ struct PairedTile {
         auto half = [](const v8i32& v, int h) {
             return h ? __builtin_shufflevector(v, v, 4, 5, 6, 7) : __builtin_shufflevector(v, v, 0, 1, 2, 3);
         };
+        // fragment i of this wave's rows of X, j of its rows of Y, in step s
+        auto x_fragment = [&](int i, int s) -> v8i32 {
+            if constexpr (XT) return turned_fragment(lds + (s & 1) * STAGE_BYTES + (i >> 2) * PANEL_BYTES, wn * 4 + (i & 3), lane);
+            else return fragment(xbase + i * 16 * STEP_BYTES, s);
+        };
+        auto y_fragment = [&](int j, int s) -> v8i32 {
+            if constexpr (YT) return turned_fragment(lds + (s & 1) * STAGE_BYTES + TN * STEP_BYTES + (wm >> 1) * PANEL_BYTES, (wm & 1) * 4 + j, lane);
+            else return fragment(ybase + j * 16 * STEP_BYTES, s);
+        };
         v8i32 y[FM], x[2];
 
         // in front of step 0: all four parts of two steps
@@ -435,8 +553,8 @@ struct PairedTile {
         }
         tile_wait<P2 + P1 + S + P2>();
 #pragma unroll
-        for (int j = 0; j < FM; ++j) y[j] = fragment(ybase + j * 16 * STEP_BYTES, 0);
-        x[0] = fragment(xbase, 0);
+        for (int j = 0; j < FM; ++j) y[j] = y_fragment(j, 0);
+        x[0] = x_fragment(0, 0);
 
         // one step; `plain`: the loads that it asks for are of whole steps, and there is a next one
         auto step = [&](int s, auto plain_c) {
@@ -460,7 +578,7 @@ struct PairedTile {
                     if (j == 0 && i == 3) tile_wait<P1 + S + P2>();
                     if (j == 0 && i == 7) tile_wait<P2 + P1 + S>();
                     // (behind the last step these read what is there and nobody uses)
-                    if (j == 0) x[(i + 1) & 1] = fragment(xbase + (i + 1) % FN * 16 * STEP_BYTES, i + 1 < FN ? s : s + 1);
+                    if (j == 0) x[(i + 1) & 1] = x_fragment((i + 1) % FN, i + 1 < FN ? s : s + 1);
                     if (FP8 && !BLOCKS && j == 0) sx[i & 1] = *reinterpret_cast<const v4f32*>(scales + (wn * FN + i) * 16 + 4 * g);
                     const v8i32 xi = x[i & 1];
                     if constexpr (FP8) {
@@ -474,7 +592,7 @@ struct PairedTile {
                                 acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8f16, half(xi, h)), __builtin_bit_cast(v8f16, half(y[j], h)), acc[i][j], 0, 0, 0);
                         }
                     }
-                    if (i == FN - 1) y[j] = fragment(ybase + j * 16 * STEP_BYTES, s + 1);
+                    if (i == FN - 1) y[j] = y_fragment(j, s + 1);
                     // the loads, one behind a product
                     const int l = n - 3 * FM;
                     if (l >= 0 && l < P1) load(l, s + 2, PLAIN || full);
