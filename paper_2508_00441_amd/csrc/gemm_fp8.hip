@@ -61,41 +61,76 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
     gemm_fp8_body<Tile<kind_of<TYPE, SCALING>(), 2, 2, 2, 2, 4>, TYPE>(w);
 }
 
-// Up to sixteen vectors of A: a workgroup forms sixteen columns of D, its waves taking every WAVES-th block of the inner dimension straight
-// from memory into registers, and adds its waves' sums in LDS, in their order.  B is read once and bounds it; with nothing staged a wave has AHEAD
-// blocks of it (2 KiB each) in flight at once.
-constexpr int FEW_WAVES = 8, AHEAD = 4;
+// Up to sixteen vectors of A: no tile in LDS.  A workgroup of FEW_WAVES waves takes sixteen vectors of B, a wave every FEW_WAVES-th step, straight
+// from memory into registers; the waves' sums are added in LDS, in their order.  B is read once and bounds it.  A wave has AHEAD steps (2 KiB of B
+// each) under way.  1 x 8192 x 4096: 8.0 us; by 16 x 64 tiles with the inner dimension in shares that meet in memory 11.6 us.  1 x 16384 x 16384: 53 us,
+// 5.1 TB/s.
+constexpr int FEW = 16, FEW_WAVES = 8, AHEAD = 4;
 
-template <int SCALING, int TYPE>
-__global__ void __launch_bounds__(FEW_WAVES * 64) gemm_fp8_few_kernel(const GemmFp8Args a) {
-    constexpr int WAVES = FEW_WAVES;
-    typedef typename Element<TYPE>::type T;
-    typedef Fragment<TYPE == TYPE_F32> F;
-    __shared__ __attribute__((aligned(16))) v4f32 sums[WAVES][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 15, g = lane >> 4;
-    const int64_t n0 = (int64_t)blockIdx.x * 16;
-    const int my_n = n0 + row < a.n ? row : (int)(a.n - 1 - n0), my_m = row < a.m ? row : (int)a.m - 1;
-    const uint8_t* const x_at = a.B + (n0 + my_n) * a.ldb + g * 16;
-    const uint8_t* const y_at = a.A + my_m * a.lda + g * 16;
-    const float* const sx_at = SCALING == SCALE_BLOCKS ? a.Sb + n0 / SCALE_BLOCK : a.Sb + n0;
-    const int steps = (int)div_up(a.k, SCALE_BLOCK);
-    int four[4];                                     // this lane's four columns of the result
-#pragma unroll
-    for (int r = 0; r < 4; ++r) four[r] = n0 + 4 * g + r < a.n ? 4 * g + r : (int)(a.n - 1 - n0);
+struct FewPieces {
     v4i32 x[AHEAD][2], y[AHEAD][2];
-    v4f32 sx[AHEAD];
-    float sy[AHEAD];
-    // (behind the end of the vectors, and of the blocks, something that is there is read and not used)
-    auto load = [&](int u, int s) {
-        s = s < steps ? s : steps - 1;
-        const int64_t at = (int64_t)s * SCALE_BLOCK;
+    const uint8_t* x_at;         // this lane's vector, from piece lane / 16 on
+    const uint8_t* y_at;
+    int64_t bytes;
+    int g, steps;
+    __device__ __forceinline__ FewPieces(const TileOperand& X, const TileOperand& Y, int64_t bytes_, int lane)
+        : bytes(bytes_), g(lane >> 4), steps((int)div_up(bytes_, STEP_BYTES)) {
+        const int row = lane & 15;
+        x_at = X.vectors + (int64_t)(row < X.rows ? row : X.rows - 1) * X.stride + g * 16;
+        y_at = Y.vectors + (int64_t)(row < Y.rows ? row : Y.rows - 1) * Y.stride + g * 16;
+    }
+    // (behind the end of the vectors something that is there is read and not used)
+    __device__ __forceinline__ void load(int u, int s) {
+        const int64_t at = (int64_t)s * STEP_BYTES;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int64_t from = at + g * 16 + h * 64 < a.k ? at + h * 64 : -(int64_t)g * 16;
+            const int64_t from = at + g * 16 + h * 64 < bytes ? at + h * 64 : -(int64_t)g * 16;
             x[u][h] = *reinterpret_cast<const v4i32*>(x_at + from);
             y[u][h] = *reinterpret_cast<const v4i32*>(y_at + from);
         }
-        sy[u] = a.Sa[s * a.ldsa + my_m];
+    }
+    __device__ __forceinline__ void clear_end(int u, int s) {
+        if ((int64_t)(s + 1) * STEP_BYTES <= bytes) return;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int left = (int)(bytes - (int64_t)s * STEP_BYTES) - g * 16 - h * 64, keep = left < 0 ? 0 : left;
+            x[u][h] = first_bytes(x[u][h], keep);
+            y[u][h] = first_bytes(y[u][h], keep);
+        }
+    }
+};
+
+// the sum over a workgroup's waves of element (vector m of Y, n of X) of their products, for thread 16 m + n < 256
+__device__ __forceinline__ float few_sum(v4f32 (&sums)[FEW_WAVES][64], v4f32 mine) {
+    sums[threadIdx.x >> 6][threadIdx.x & 63] = mine;
+    __syncthreads();
+    const int n = threadIdx.x & 15, m = (threadIdx.x >> 4) & 15;
+    float sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < FEW_WAVES; ++w) sum += reinterpret_cast<const float*>(&sums[w][(n >> 2) * 16 + m])[n & 3];
+    return sum;
+}
+
+template <int SCALING, int TYPE>
+__global__ void __launch_bounds__(FEW_WAVES * 64) gemm_fp8_few_kernel(const GemmFp8Args a) {
+    typedef typename Element<TYPE>::type T;
+    typedef Fragment<TYPE == TYPE_F32> F;
+    __shared__ __attribute__((aligned(16))) v4f32 sums[FEW_WAVES][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
+    const int64_t n0 = (int64_t)blockIdx.x * 16;
+    const int left_n = a.n - n0 < 16 ? (int)(a.n - n0) : 16;
+    FewPieces p(TileOperand{a.B + n0 * a.ldb, a.ldb, left_n, nullptr, 0}, TileOperand{a.A, a.lda, (int)a.m, nullptr, 0}, a.k, lane);
+    const float* const sx_at = SCALING == SCALE_BLOCKS ? a.Sb + n0 / SCALE_BLOCK : a.Sb + n0;
+    const float* const sy_at = a.Sa + ((lane & 15) < a.m ? lane & 15 : a.m - 1);
+    int four[4];                                     // this lane's four columns of the result
+#pragma unroll
+    for (int r = 0; r < 4; ++r) four[r] = 4 * g + r < left_n ? 4 * g + r : left_n - 1;
+    v4f32 sx[AHEAD];
+    float sy[AHEAD];
+    auto load = [&](int u, int s) {
+        s = s < p.steps ? s : p.steps - 1;
+        p.load(u, s);
+        sy[u] = sy_at[s * a.ldsa];
         if constexpr (SCALING == SCALE_BLOCKS) {
             sx[u][0] = sx_at[s * a.ldsb];
         } else {
@@ -105,38 +140,27 @@ __global__ void __launch_bounds__(FEW_WAVES * 64) gemm_fp8_few_kernel(const Gemm
     };
     v4f32 acc = {};
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) load(u, wave + u * WAVES);
-    for (int first = wave; first < steps; first += WAVES * AHEAD) {
+    for (int u = 0; u < AHEAD; ++u) load(u, wave + u * FEW_WAVES);
+    for (int first = wave; first < p.steps; first += FEW_WAVES * AHEAD) {
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
-            const int s = first + u * WAVES;
-            if (s >= steps) break;
-            if ((int64_t)(s + 1) * SCALE_BLOCK > a.k) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int left = (int)(a.k - (int64_t)s * SCALE_BLOCK) - g * 16 - h * 64, keep = left < 0 ? 0 : left;
-                    x[u][h] = first_bytes(x[u][h], keep);
-                    y[u][h] = first_bytes(y[u][h], keep);
-                }
-            }
-            const v4f32 t = F::product(F::of(__builtin_shufflevector(x[u][0], x[u][1], 0, 1, 2, 3, 4, 5, 6, 7)),
-                                       F::of(__builtin_shufflevector(y[u][0], y[u][1], 0, 1, 2, 3, 4, 5, 6, 7)));
+            const int s = first + u * FEW_WAVES;
+            if (s >= p.steps) break;
+            p.clear_end(u, s);
+            const v4f32 t = F::product(F::of(__builtin_shufflevector(p.x[u][0], p.x[u][1], 0, 1, 2, 3, 4, 5, 6, 7)),
+                                       F::of(__builtin_shufflevector(p.y[u][0], p.y[u][1], 0, 1, 2, 3, 4, 5, 6, 7)));
 #pragma unroll
             for (int r = 0; r < 4; ++r) acc[r] = __builtin_fmaf(t[r], sx[u][SCALING == SCALE_BLOCKS ? 0 : r] * sy[u], acc[r]);
-            if (first + WAVES * AHEAD < steps) load(u, s + WAVES * AHEAD);
+            if (first + FEW_WAVES * AHEAD < p.steps) load(u, s + FEW_WAVES * AHEAD);
         }
     }
-    sums[wave][lane] = acc;
-    __syncthreads();
-    // thread (m, n) of sixteen by sixteen: the neighbours write neighbouring columns
+    const float sum = few_sum(sums, acc);
     const int n = threadIdx.x & 15, m = threadIdx.x >> 4;
-    if (threadIdx.x >= 256 || m >= a.m || n0 + n >= a.n) return;
-    float sum = 0.0f;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) sum += reinterpret_cast<const float*>(&sums[w][(n >> 2) * 16 + m])[n & 3];
+    if (threadIdx.x >= 256 || m >= a.m || n >= left_n) return;
     T* const to = static_cast<T*>(a.D) + m * a.ldd + n0 + n;
     *to = (T)(a.accumulate ? (float)*to + sum : sum);
 }
+
 // sums the pieces of the inner dimension in their order
 template <int TYPE>
 __global__ void __launch_bounds__(256) gemm_fp8_join_kernel(const GemmFp8Args a, const int splits) {
@@ -157,10 +181,10 @@ __global__ void __launch_bounds__(256) gemm_fp8_join_kernel(const GemmFp8Args a,
     put_four(D + i * a.ldd + j, sum, a.n - j, wide, a.accumulate != 0);
 }
 
-enum { FEW, SMALL, MIDDLE, LARGE };
+enum { VECTORS, SMALL, MIDDLE, LARGE };
 struct Shape { int kind, tm, tn, splits; };
 Shape shape_of(int64_t m, int64_t n, int64_t k) {
-    if (m <= 16) return Shape{FEW, 16, 16, 1};
+    if (m <= FEW) return Shape{VECTORS, FEW, 16, 1};
     Shape s{LARGE, 256, 256, 1};
     if (m <= 512) s = Shape{SMALL, 64, 64, 1};
     else if (div_up(m, 256) * div_up(n, 256) < 192) s = Shape{MIDDLE, 128, 128, 1};
@@ -175,7 +199,7 @@ Shape shape_of(int64_t m, int64_t n, int64_t k) {
 template <int SCALING, int TYPE>
 hipError_t launch_kind(const GemmFp8Args& a, int splits, hipStream_t st) {
     const Shape s = shape_of(a.m, a.n, a.k);
-    if (s.kind == FEW) {
+    if (s.kind == VECTORS) {
         const unsigned blocks = (unsigned)div_up(a.n, 16);
         hipLaunchKernelGGL((gemm_fp8_few_kernel<SCALING, TYPE>), dim3(blocks), dim3(FEW_WAVES * 64), 0, st, a);
         return hipGetLastError();

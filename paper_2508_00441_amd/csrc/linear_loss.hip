@@ -107,29 +107,39 @@ __device__ __forceinline__ void loss_forward_body(const LogitWork& w) {
     }
 }
 
-// Sixteen tokens, sixteen shares of the tiles of words.
+// TOKENS tokens a workgroup, 256 / TOKENS shares of the tiles of words for each.
+template <int TOKENS>
 __global__ void __launch_bounds__(256) loss_join_kernel(const float2* part, const float* target_z, const int64_t* targets, int64_t tokens,
                                                         int64_t vocab, int64_t ignore, int tiles, float* loss, float* lse, int* flags) {
-    __shared__ float2 share[16][17];
-    const int tl = threadIdx.x & 15, s = threadIdx.x >> 4;
-    const int64_t t = (int64_t)blockIdx.x * 16 + tl, at = t < tokens ? t : tokens - 1;
+    constexpr int SHARES = 256 / TOKENS, AT_ONCE = 4;
+    __shared__ float2 share[4][TOKENS];
+    const int tl = threadIdx.x % TOKENS, s = threadIdx.x / TOKENS;
+    const int64_t t = (int64_t)blockIdx.x * TOKENS + tl, at = t < tokens ? t : tokens - 1;
     float most = -__builtin_inff(), sum = 0.0f;
-    for (int i = s; i < tiles; i += 16) {
-        const float2 p = part[(int64_t)i * tokens + at];
-        const float higher = fmaxf(most, p.x), base = higher == -__builtin_inff() ? 0.0f : higher;
-        sum = sum * exp_of(most - base) + p.y * exp_of(p.x - base);
+    const auto add = [&](float m, float v) {
+        const float higher = fmaxf(most, m), base = higher == -__builtin_inff() ? 0.0f : higher;
+        sum = sum * exp_of(most - base) + v * exp_of(m - base);
         most = higher;
+    };
+    for (int i = s; i < tiles; i += SHARES * AT_ONCE) {
+        float2 p[AT_ONCE];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) p[u] = i + u * SHARES < tiles ? part[(int64_t)(i + u * SHARES) * tokens + at] : make_float2(-__builtin_inff(), 0.0f);
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) add(p[u].x, p[u].y);
     }
-    share[tl][s] = make_float2(most, sum);
+    // the shares of a token lie TOKENS lanes apart in a wave, and in four waves
+#pragma unroll
+    for (int d = TOKENS; d < 64; d <<= 1) {
+        const float m = __shfl_xor(most, d), v = __shfl_xor(sum, d);
+        add(m, v);
+    }
+    if ((threadIdx.x & 63) < TOKENS) share[threadIdx.x >> 6][tl] = make_float2(most, sum);
     __syncthreads();
-    if (s != 0 || t >= tokens) return;
-    float all = -__builtin_inff(), total = 0.0f;
+    if (threadIdx.x >= TOKENS || t >= tokens) return;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) all = fmaxf(all, share[tl][i].x);
-    const float base = all == -__builtin_inff() ? 0.0f : all;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) total += share[tl][i].y * exp_of(share[tl][i].x - base);
-    const float l = base + log_of(total);
+    for (int w = 1; w < 4; ++w) add(share[w][tl].x, share[w][tl].y);
+    const float l = (most == -__builtin_inff() ? 0.0f : most) + log_of(sum);
     const int64_t target = targets[t];
     const bool counts = target != ignore, real = target >= 0 && target < vocab;
     lse[t] = l;
@@ -277,7 +287,9 @@ __global__ void __launch_bounds__(256) zero_rows_kernel(uint16_t* D, int64_t row
 constexpr int kind_of(int type) { return type == TYPE_F16 ? KIND_F16 : KIND_BF16; }
 template <int TYPE> using LargeTile = PairedTile<kind_of(TYPE)>;      // 256 words or columns, 256 tokens or rows
 template <int TYPE> using MiddleTile = Tile<kind_of(TYPE), 2, 2, 4, 2, 3>;     // 128, 64
-template <int TYPE> using FewTile = Tile<kind_of(TYPE), 4, 1, 2, 1, 4>;        // 128, 16
+// 64, 16: 16 tokens, 65536 words of 2048 in 57 us; 128 words a workgroup 62, straight from memory into registers 75 (there the tokens are read as
+// often as the words).  One token, 131072 words of 4096: 190, 203, 180.
+template <int TYPE> using FewTile = Tile<kind_of(TYPE), 4, 1, 1, 1, 4>;
 
 template <int TYPE>
 __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) loss_forward_large_kernel(const LogitWork w) { loss_forward_body<LargeTile<TYPE>>(w); }
@@ -330,6 +342,7 @@ enum { FEW, MIDDLE, LARGE };
 int shape_for(int64_t m, int64_t n) { return m <= 16 ? FEW : div_up(m, 256) * div_up(n, 256) < 128 || m <= 64 ? MIDDLE : LARGE; }
 int tile_m(int shape) { return shape == FEW ? 16 : shape == MIDDLE ? 64 : 256; }
 int tile_n(int shape) { return shape == LARGE ? 256 : 128; }
+int tile_words(int shape) { return shape == FEW ? 64 : tile_n(shape); }      // of the kernels that form z
 WorkOrder order_for(int shape, int64_t tiles_m) { return WorkOrder{shape == LARGE ? 32 : 64, tiles_m > 8 ? 4 : 8}; }
 // dH, whose inner dimension is the vocabulary: large tiles also where they are few, if that leaves every compute unit a share of it of
 // some length (1003 x 1024 over 50001 words: 16 tiles in 16 shares)
@@ -403,7 +416,7 @@ hipError_t launch_dw(ProductWork w, hipStream_t st) {
 
 void set_tiles(LogitWork& w, int shape) {
     w.tiles_m = (int)div_up(w.tokens, tile_m(shape));
-    w.tiles_n = (int)div_up(w.words, tile_n(shape));
+    w.tiles_n = (int)div_up(w.words, tile_words(shape));
     w.order = order_for(shape, w.tiles_m);
     w.steps = (int)div_up(w.bytes, STEP_BYTES);
 }
@@ -411,7 +424,7 @@ void set_tiles(LogitWork& w, int shape) {
 template <int TYPE>
 hipError_t forward_typed(const LossArgs& a, uint8_t* ws, hipStream_t st) {
     const int shape = shape_for(a.tokens, a.vocab);
-    const int64_t tiles = div_up(a.vocab, tile_n(shape));
+    const int64_t tiles = div_up(a.vocab, tile_words(shape));
     LogitWork w = {};
     w.H = static_cast<const uint8_t*>(a.H);
     w.W = static_cast<const uint8_t*>(a.W);
@@ -430,8 +443,12 @@ hipError_t forward_typed(const LossArgs& a, uint8_t* ws, hipStream_t st) {
     else hipLaunchKernelGGL((loss_forward_large_kernel<TYPE>), dim3(blocks), dim3(512), 0, st, w);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(loss_join_kernel, dim3((unsigned)div_up(a.tokens, 16)), dim3(256), 0, st, w.part, w.target_z, a.targets, a.tokens, a.vocab,
-                       a.ignore, (int)tiles, a.loss, a.lse, a.flags);
+    const auto join = [&](auto kernel, int tokens) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)div_up(a.tokens, tokens)), dim3(256), 0, st, w.part, w.target_z, a.targets, a.tokens, a.vocab, a.ignore,
+                           (int)tiles, a.loss, a.lse, a.flags);
+    };
+    if (a.tokens <= 64) join(loss_join_kernel<1>, 1);
+    else join(loss_join_kernel<4>, 4);
     return hipGetLastError();
 }
 
@@ -521,7 +538,7 @@ hipError_t grad_typed(const LossArgs& a, int64_t piece, uint8_t* ws, hipStream_t
 }  // namespace
 
 size_t loss_bytes(int64_t tokens, int64_t vocab) {
-    return 256 + up((size_t)tokens * 4) + up((size_t)div_up(vocab, tile_n(shape_for(tokens, vocab))) * tokens * sizeof(float2));
+    return 256 + up((size_t)tokens * 4) + up((size_t)div_up(vocab, tile_words(shape_for(tokens, vocab))) * tokens * sizeof(float2));
 }
 size_t loss_grad_bytes(int64_t tokens, int64_t vocab, int64_t k, int64_t piece) { return grad_places(nullptr, tokens, vocab, k, piece).total; }
 
