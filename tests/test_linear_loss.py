@@ -95,7 +95,8 @@ def test_loss(tokens, vocab, k, type, workspace):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("type", ["bf16", "f16"])
-@pytest.mark.parametrize("tokens,vocab,k", SHAPES + [(1500, 6000, 136), (3000, 4001, 600), (2900, 4000, 1001)])
+@pytest.mark.parametrize("tokens,vocab,k", SHAPES + [(1500, 6000, 136), (3000, 4001, 600), (2900, 4000, 1001), (700, 9001, 1000),
+                                                     (130, 9001, 1000), (65, 33000, 264), (1, 33000, 300), (17, 40001, 72)])
 def test_gradient(tokens, vocab, k, type, workspace):
     x = Problem(tokens, vocab, k, type, tokens + vocab + k)
     _, lse = x.forward()
@@ -253,6 +254,24 @@ def test_the_same_bits_every_time_and_in_graphs(tokens, vocab, k, workspace):
         x.H[:, :k].mul_(0.5)                                        # new inputs for the next replay
         loss, lse = x.forward()
         dh, dw = x.gradient(lse)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens", [9, 70, 300])
+def test_offsets_beyond_2_32(tokens, workspace):
+    """Weights, and their gradient, whose last words lie beyond 4 GiB."""
+    vocab, k, ld = 40000, 100, 1 << 16
+    x = Problem(tokens, vocab, k, "bf16", 10)
+    wide = torch.full((vocab, ld), float("nan"), dtype=torch.bfloat16, device="cuda")
+    wide[:, :k] = x.w.cuda()
+    x.W = wide
+    loss, lse = x.forward()
+    want, want_lse, _ = plain.loss_forward(x.h, x.w, x.targets, x.ignore)
+    bound = plain.logit_error(x.h, x.w) + EXP * (1 + want_lse.abs())
+    assert bool(torch.all((loss.cpu().double() - want).abs() <= 2 * bound + 2.0 ** -23 * want.abs()))
+    dh, dw = x.gradient(lse, ldw=ld)
+    x.check_gradient(dh, dw, lse)
+    assert bool(torch.isnan(dw[:, k:]).all())
 
 
 P = 1 << 20
