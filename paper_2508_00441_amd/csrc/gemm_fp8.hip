@@ -47,11 +47,6 @@ template <int SCALING, int TYPE>
 __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) gemm_fp8_large_kernel(const GemmFp8Work w) {
     gemm_fp8_body<PairedTile<kind_of<TYPE, SCALING>()>, TYPE>(w);
 }
-// 256 x 128 for 32-bit results: the widened fragments of 256 x 256 do not fit beside its accumulators
-template <int SCALING>
-__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) gemm_fp8_wide_kernel(const GemmFp8Work w) {
-    gemm_fp8_body<Tile<kind_of<TYPE_F32, SCALING>(), 4, 2, 4, 4, 3>, TYPE_F32>(w);
-}
 template <int SCALING, int TYPE>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) gemm_fp8_middle_kernel(const GemmFp8Work w) {
     gemm_fp8_body<Tile<kind_of<TYPE, SCALING>(), 2, 2, 4, 4, 2>, TYPE>(w);
@@ -198,7 +193,10 @@ Shape shape_of(int64_t m, int64_t n, int64_t k) {
 
 template <int SCALING, int TYPE>
 hipError_t launch_kind(const GemmFp8Args& a, int splits, hipStream_t st) {
-    const Shape s = shape_of(a.m, a.n, a.k);
+    Shape s = shape_of(a.m, a.n, a.k);
+    // 32-bit results: the widened fragments of a 256 x 256 tile do not fit beside its accumulators, and two workgroups of 128 x 128, which pause at
+    // different times, do better than one of 256 x 128 (16384 x 4096 x 8192: 1030 and 1080 us)
+    if (TYPE == TYPE_F32 && s.kind == LARGE) s = Shape{MIDDLE, 128, 128, 1};
     if (s.kind == VECTORS) {
         const unsigned blocks = (unsigned)div_up(a.n, 16);
         hipLaunchKernelGGL((gemm_fp8_few_kernel<SCALING, TYPE>), dim3(blocks), dim3(FEW_WAVES * 64), 0, st, a);
@@ -208,16 +206,14 @@ hipError_t launch_kind(const GemmFp8Args& a, int splits, hipStream_t st) {
     w.g = a;
     w.steps = (int)div_up(a.k, SCALE_BLOCK);
     w.splits = splits;
-    const int tm = TYPE == TYPE_F32 && s.kind == LARGE ? 128 : s.tm;
-    w.tiles_m = (int)div_up(a.m, tm);
+    w.tiles_m = (int)div_up(a.m, s.tm);
     w.tiles_n = (int)div_up(a.n, s.tn);
     const int64_t tiles = (int64_t)w.tiles_m * w.tiles_n;
     w.order = WorkOrder{s.kind == LARGE ? 32 : 64, w.tiles_m > 8 ? 4 : 8};
     const unsigned blocks = (unsigned)(tiles * splits);
     if (s.kind == SMALL) hipLaunchKernelGGL((gemm_fp8_small_kernel<SCALING, TYPE>), dim3(blocks), dim3(256), 0, st, w);
     else if (s.kind == MIDDLE) hipLaunchKernelGGL((gemm_fp8_middle_kernel<SCALING, TYPE>), dim3(blocks), dim3(256), 0, st, w);
-    else if constexpr (TYPE == TYPE_F32) hipLaunchKernelGGL((gemm_fp8_wide_kernel<SCALING>), dim3(blocks), dim3(512), 0, st, w);
-    else hipLaunchKernelGGL((gemm_fp8_large_kernel<SCALING, TYPE>), dim3(blocks), dim3(512), 0, st, w);
+    else if constexpr (TYPE != TYPE_F32) hipLaunchKernelGGL((gemm_fp8_large_kernel<SCALING, TYPE>), dim3(blocks), dim3(512), 0, st, w);
     if (splits > 1) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
