@@ -588,7 +588,7 @@ int ozaki_quantise_fp8(int64_t rows, int64_t k, const void* X, int64_t ldx, int 
 size_t ozaki_gemm_fp8_workspace_bytes(int64_t m, int64_t n, int64_t k) {
     if (!extent_ok(m) || !extent_ok(n) || !extent_ok(k)) return 0;
     const int splits = gemm_fp8_splits(m, n, k);
-    return splits > 1 ? FLAG_BYTES + align_up((size_t)splits * m * n * sizeof(float)) : 0;
+    return splits > 1 ? FLAG_BYTES + align_up((size_t)splits * m * in_fours(n) * sizeof(float)) : 0;
 }
 
 int ozaki_gemm_fp8(int64_t m, int64_t n, int64_t k, const void* A, int64_t lda, const float* Sa, int64_t ldsa, const void* B, int64_t ldb,

@@ -34,7 +34,7 @@ __device__ __forceinline__ void gemm_fp8_body(const GemmFp8Work& w) {
 
     const auto one = [](int64_t) { return 1.0f; };
     if (w.splits > 1)
-        store_tile<P, false>(lds, acc, a.partial + ((int64_t)split * a.m + m0) * a.n + n0, a.n, left_m, left_n, false, one);
+        store_tile<P, false>(lds, acc, a.partial + ((int64_t)split * a.m + m0) * in_fours(a.n) + n0, in_fours(a.n), left_m, in_fours(left_n), false, one);
     else
         store_tile<P, (P::THREADS > 256)>(lds, acc, static_cast<T*>(a.D) + m0 * a.ldd + n0, a.ldd, left_m, left_n, a.accumulate != 0, one);
 }
@@ -160,17 +160,11 @@ __global__ void __launch_bounds__(FEW_WAVES * 64) gemm_fp8_few_kernel(const Gemm
 template <int TYPE>
 __global__ void __launch_bounds__(256) gemm_fp8_join_kernel(const GemmFp8Args a, const int splits) {
     typedef typename Element<TYPE>::type T;
-    const int64_t j = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, i = blockIdx.y;
+    const int64_t j = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, i = blockIdx.y, ld = in_fours(a.n);
     if (j >= a.n) return;
     v4f32 sum = {};
-    if (a.n % 4 == 0) {
-        for (int s = 0; s < splits; ++s) sum += *reinterpret_cast<const v4f32*>(a.partial + ((int64_t)s * a.m + i) * a.n + j);
-    } else {
-        for (int s = 0; s < splits; ++s)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (j + r < a.n) sum[r] += a.partial[((int64_t)s * a.m + i) * a.n + j + r];
-    }
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) sum += *reinterpret_cast<const v4f32*>(a.partial + ((int64_t)s * a.m + i) * ld + j);
     T* const D = static_cast<T*>(a.D);
     const bool wide = a.ldd % 4 == 0 && reinterpret_cast<uintptr_t>(D) % (4 * sizeof(T)) == 0;
     put_four(D + i * a.ldd + j, sum, a.n - j, wide, a.accumulate != 0);

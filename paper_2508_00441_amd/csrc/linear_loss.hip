@@ -245,7 +245,7 @@ struct ProductWork {
     int64_t ldd;
     const float* row_factor; // what the sums are multiplied by: one for every row of D, or
     const float* factor;     // the same for all
-    float* partial;          // not null: unscaled sums go there, [split][m][n]
+    float* partial;          // not null: unscaled sums go there, [split][m][n in fours]
 };
 
 __device__ __forceinline__ int split_begin(int steps, int splits, int s) { return (int)((int64_t)steps * s / splits); }
@@ -261,7 +261,8 @@ __device__ __forceinline__ void loss_product_body(const ProductWork& w) {
     const int split = item.gi;
     P::multiply(lds, X, Y, w.bytes, split_begin(w.steps, w.splits, split), split_begin(w.steps, w.splits, split + 1), acc);
     if (w.partial != nullptr) {
-        store_tile<P, false>(lds, acc, w.partial + ((int64_t)split * w.m + m0) * w.n + n0, w.n, left_m, left_n, false, [](int64_t) { return 1.0f; });
+        store_tile<P, false>(lds, acc, w.partial + ((int64_t)split * w.m + m0) * in_fours(w.n) + n0, in_fours(w.n), left_m, in_fours(left_n), false,
+                             [](int64_t) { return 1.0f; });
         return;
     }
     store_tile<P, (P::THREADS > 256)>(lds, acc, static_cast<T*>(w.D) + m0 * w.ldd + n0, w.ldd, left_m, left_n, false,
@@ -269,15 +270,20 @@ __device__ __forceinline__ void loss_product_body(const ProductWork& w) {
 }
 
 // The sums of a piece's shares of the inner dimension, on top of the pieces' before it (`sum`, unless it is the first); the last piece's go to D.
+// A workgroup a row.
 template <typename T>
 __device__ __forceinline__ void join_body(const float* partial, int splits, int64_t m, int64_t n, float* sum, bool first, bool last,
                                           const float* row_factor, T* D, int64_t ldd) {
-    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < m * n; at += (int64_t)gridDim.x * 256) {
-        float s = first ? 0.0f : sum[at];
-        for (int i = 0; i < splits; ++i) s += partial[(int64_t)i * m * n + at];
-        if (last) D[at / n * ldd + at % n] = (T)(s * row_factor[at / n]);
-        else sum[at] = s;
-    }
+    const int64_t ld = in_fours(n);
+    for (int64_t i = blockIdx.x; i < m; i += gridDim.x)
+        for (int64_t j = threadIdx.x * 4; j < n; j += 1024) {
+            v4f32 s = {};
+            if (!first) s = *reinterpret_cast<const v4f32*>(sum + i * ld + j);
+#pragma unroll 4
+            for (int p = 0; p < splits; ++p) s += *reinterpret_cast<const v4f32*>(partial + ((int64_t)p * m + i) * ld + j);
+            if (last) put_four(D + i * ldd + j, s * row_factor[i], n - j, ldd % 4 == 0 && reinterpret_cast<uintptr_t>(D) % (4 * sizeof(T)) == 0, false);
+            else *reinterpret_cast<v4f32*>(sum + i * ld + j) = s;
+        }
 }
 
 __global__ void __launch_bounds__(256) zero_rows_kernel(uint16_t* D, int64_t rows, int64_t k, int64_t ldd) {
@@ -287,6 +293,7 @@ __global__ void __launch_bounds__(256) zero_rows_kernel(uint16_t* D, int64_t row
 constexpr int kind_of(int type) { return type == TYPE_F16 ? KIND_F16 : KIND_BF16; }
 template <int TYPE> using LargeTile = PairedTile<kind_of(TYPE)>;      // 256 words or columns, 256 tokens or rows
 template <int TYPE> using MiddleTile = Tile<kind_of(TYPE), 2, 2, 4, 2, 3>;     // 128, 64
+template <int TYPE> using SmallTile = Tile<kind_of(TYPE), 2, 2, 2, 2, 4>;      // 64, 64
 // 64, 16: 16 tokens, 65536 words of 2048 in 57 us; 128 words a workgroup 62, straight from memory into registers 75 (there the tokens are read as
 // often as the words).  One token, 131072 words of 4096: 190, 203, 180.
 template <int TYPE> using FewTile = Tile<kind_of(TYPE), 4, 1, 1, 1, 4>;
@@ -296,11 +303,15 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
 template <int TYPE>
 __global__ void __launch_bounds__(256) loss_forward_middle_kernel(const LogitWork w) { loss_forward_body<MiddleTile<TYPE>>(w); }
 template <int TYPE>
+__global__ void __launch_bounds__(256) loss_forward_small_kernel(const LogitWork w) { loss_forward_body<SmallTile<TYPE>>(w); }
+template <int TYPE>
 __global__ void __launch_bounds__(256) loss_forward_few_kernel(const LogitWork w) { loss_forward_body<FewTile<TYPE>>(w); }
 template <int TYPE>
 __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) loss_g_large_kernel(const LogitWork w) { loss_g_body<LargeTile<TYPE>, typename Element<TYPE>::type>(w); }
 template <int TYPE>
 __global__ void __launch_bounds__(256) loss_g_middle_kernel(const LogitWork w) { loss_g_body<MiddleTile<TYPE>, typename Element<TYPE>::type>(w); }
+template <int TYPE>
+__global__ void __launch_bounds__(256) loss_g_small_kernel(const LogitWork w) { loss_g_body<SmallTile<TYPE>, typename Element<TYPE>::type>(w); }
 template <int TYPE>
 __global__ void __launch_bounds__(256) loss_g_few_kernel(const LogitWork w) { loss_g_body<FewTile<TYPE>, typename Element<TYPE>::type>(w); }
 // dH = g W, and dW = g^T H
@@ -338,11 +349,17 @@ __global__ void __launch_bounds__(256) loss_shares_kernel(const void* H, int64_t
 }
 
 // ---- shapes and work memory ------------------------------------------------------------------------------------
-enum { FEW, MIDDLE, LARGE };
+enum { FEW, SMALL, MIDDLE, LARGE };
 int shape_for(int64_t m, int64_t n) { return m <= 16 ? FEW : div_up(m, 256) * div_up(n, 256) < 128 || m <= 64 ? MIDDLE : LARGE; }
-int tile_m(int shape) { return shape == FEW ? 16 : shape == MIDDLE ? 64 : 256; }
+// Of the kernels that form z: where tiles of 128 words and 64 tokens leave compute units without work, tiles of 64 words
+// (81 tokens, 7855 words of 3136: 19.7 us against 26.2; 400, 3053 of 1296: 15.4 against 16.0).
+int logit_shape(int64_t tokens, int64_t words) {
+    const int shape = shape_for(tokens, words);
+    return shape == MIDDLE && div_up(tokens, 64) * div_up(words, 128) < 256 ? SMALL : shape;
+}
+int tile_m(int shape) { return shape == FEW ? 16 : shape == LARGE ? 256 : 64; }
 int tile_n(int shape) { return shape == LARGE ? 256 : 128; }
-int tile_words(int shape) { return shape == FEW ? 64 : tile_n(shape); }      // of the kernels that form z
+int tile_words(int shape) { return shape == FEW || shape == SMALL ? 64 : tile_n(shape); }      // of the kernels that form z
 WorkOrder order_for(int shape, int64_t tiles_m) { return WorkOrder{shape == LARGE ? 32 : 64, tiles_m > 8 ? 4 : 8}; }
 // dH, whose inner dimension is the vocabulary: large tiles also where they are few, if that leaves every compute unit a share of it of
 // some length (1003 x 1024 over 50001 words: 16 tiles in 16 shares)
@@ -384,8 +401,8 @@ GradPlaces grad_places(uint8_t* ws, int64_t tokens, int64_t vocab, int64_t k, in
     p.Hs = take((size_t)tokens * in_eights(k) * 2);
     p.G = take((size_t)tokens * padded(words) * 2);
     const bool joined = splits > 1 || piece < vocab;
-    p.partial = reinterpret_cast<float*>(take(joined ? (size_t)splits * tokens * k * 4 : 0));
-    p.sum = reinterpret_cast<float*>(take(piece < vocab ? (size_t)tokens * k * 4 : 0));
+    p.partial = reinterpret_cast<float*>(take(joined ? (size_t)splits * tokens * in_fours(k) * 4 : 0));
+    p.sum = reinterpret_cast<float*>(take(piece < vocab ? (size_t)tokens * in_fours(k) * 4 : 0));
     p.total = at;
     return p;
 }
@@ -423,7 +440,7 @@ void set_tiles(LogitWork& w, int shape) {
 
 template <int TYPE>
 hipError_t forward_typed(const LossArgs& a, uint8_t* ws, hipStream_t st) {
-    const int shape = shape_for(a.tokens, a.vocab);
+    const int shape = logit_shape(a.tokens, a.vocab);
     const int64_t tiles = div_up(a.vocab, tile_words(shape));
     LogitWork w = {};
     w.H = static_cast<const uint8_t*>(a.H);
@@ -439,6 +456,7 @@ hipError_t forward_typed(const LossArgs& a, uint8_t* ws, hipStream_t st) {
     w.part = reinterpret_cast<float2*>(ws + 256 + up((size_t)a.tokens * 4));
     const unsigned blocks = (unsigned)(w.tiles_m * (int64_t)w.tiles_n);
     if (shape == FEW) hipLaunchKernelGGL((loss_forward_few_kernel<TYPE>), dim3(blocks), dim3(256), 0, st, w);
+    else if (shape == SMALL) hipLaunchKernelGGL((loss_forward_small_kernel<TYPE>), dim3(blocks), dim3(256), 0, st, w);
     else if (shape == MIDDLE) hipLaunchKernelGGL((loss_forward_middle_kernel<TYPE>), dim3(blocks), dim3(256), 0, st, w);
     else hipLaunchKernelGGL((loss_forward_large_kernel<TYPE>), dim3(blocks), dim3(512), 0, st, w);
     const hipError_t e = hipGetLastError();
@@ -479,13 +497,14 @@ hipError_t grad_typed(const LossArgs& a, int64_t piece, uint8_t* ws, hipStream_t
         w.tokens = a.tokens;
         w.words = words;
         w.first_word = first;
-        const int shape = shape_for(a.tokens, words);
+        const int shape = logit_shape(a.tokens, words);
         set_tiles(w, shape);
         w.token = TokenState{a.lse_in, p.target};
         w.G = p.G;
         w.ldg = padded(words);
         const unsigned blocks = (unsigned)(w.tiles_m * (int64_t)w.tiles_n);
         if (shape == FEW) hipLaunchKernelGGL((loss_g_few_kernel<TYPE>), dim3(blocks), dim3(256), 0, st, w);
+        else if (shape == SMALL) hipLaunchKernelGGL((loss_g_small_kernel<TYPE>), dim3(blocks), dim3(256), 0, st, w);
         else if (shape == MIDDLE) hipLaunchKernelGGL((loss_g_middle_kernel<TYPE>), dim3(blocks), dim3(256), 0, st, w);
         else hipLaunchKernelGGL((loss_g_large_kernel<TYPE>), dim3(blocks), dim3(512), 0, st, w);
         OZAKI_LOSS_TRY(hipGetLastError());
@@ -508,8 +527,7 @@ hipError_t grad_typed(const LossArgs& a, int64_t piece, uint8_t* ws, hipStream_t
             d.partial = joined || d.splits > 1 ? p.partial : nullptr;
             OZAKI_LOSS_TRY(launch_dh<TYPE>(d, ps.shape, st));
             if (d.partial != nullptr) {
-                const int64_t blocks_j = div_up(d.m * d.n, 256);
-                hipLaunchKernelGGL((loss_product_join_kernel<TYPE>), dim3((unsigned)(blocks_j < 4096 ? blocks_j : 4096)), dim3(256), 0, st, p.partial, d.splits,
+                hipLaunchKernelGGL((loss_product_join_kernel<TYPE>), dim3((unsigned)(d.m < 65536 ? d.m : 65536)), dim3(256), 0, st, p.partial, d.splits,
                                    d.m, d.n, p.sum, first == 0, first + piece >= a.vocab, d.row_factor, a.dH, a.lddh);
                 OZAKI_LOSS_TRY(hipGetLastError());
             }
@@ -538,7 +556,7 @@ hipError_t grad_typed(const LossArgs& a, int64_t piece, uint8_t* ws, hipStream_t
 }  // namespace
 
 size_t loss_bytes(int64_t tokens, int64_t vocab) {
-    return 256 + up((size_t)tokens * 4) + up((size_t)div_up(vocab, tile_words(shape_for(tokens, vocab))) * tokens * sizeof(float2));
+    return 256 + up((size_t)tokens * 4) + up((size_t)div_up(vocab, tile_words(logit_shape(tokens, vocab))) * tokens * sizeof(float2));
 }
 size_t loss_grad_bytes(int64_t tokens, int64_t vocab, int64_t k, int64_t piece) { return grad_places(nullptr, tokens, vocab, k, piece).total; }
 

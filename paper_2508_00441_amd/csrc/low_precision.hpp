@@ -15,6 +15,7 @@ constexpr int64_t MAX_VECTOR_BYTES = (int64_t)1 << 22;      // between vectors, 
 inline bool type_ok(int type) { return type >= TYPE_F32 && type <= TYPE_F16; }
 inline int type_bytes(int type) { return type == TYPE_F32 ? 4 : 2; }
 __host__ __device__ inline int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+__host__ __device__ inline int64_t in_fours(int64_t n) { return (n + 3) & ~(int64_t)3; }
 
 // ---- quantise_fp8.hip ----------------------------------------------------------------------------------------
 struct QuantiseArgs {
@@ -38,7 +39,7 @@ struct GemmFp8Args {
     const float* Sa;         // [k block][m]
     const float* Sb;         // [k block][n], or [k block][n / 128]
     void* D;                 // m x n, rows ldd apart
-    float* partial;          // splits > 1: [split][m][n]
+    float* partial;          // splits > 1: [split][m][n in fours]
     int64_t m, n, k, lda, ldb, ldsa, ldsb, ldd;
     int accumulate;
 };

@@ -632,7 +632,7 @@ template <typename P, bool STREAMED, typename T, typename F>
 __device__ __forceinline__ void store_tile(uint8_t* lds, const v4f32 (&acc)[P::FN][P::FM], T* D, int64_t ldd, int64_t left_m, int64_t left_n,
                                            bool accumulate, F factor) {
     constexpr int STRIDE = P::TN * 4 + 16, PER = 16 / sizeof(T), PIECES = P::TN / PER, ROWS = P::WM * 16;
-    static_assert(ROWS * STRIDE <= P::LDS_BYTES && P::THREADS % PIECES == 0, "");
+    static_assert(ROWS * STRIDE <= P::LDS_BYTES && P::THREADS % PIECES == 0 && P::THREADS % P::TN == 0, "");
     typedef T piece __attribute__((ext_vector_type(PER)));
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wn = wave / P::WM, wm = wave % P::WM;
     const int columns = left_n < P::TN ? (int)left_n : P::TN;
@@ -661,14 +661,20 @@ __device__ __forceinline__ void store_tile(uint8_t* lds, const v4f32 (&acc)[P::F
                 else *to = v;
             }
         }
+        // what is left, a thread a column (all of them where D's rows are not aligned)
+        if (loose > 0) {
+            constexpr int AT_ONCE = P::THREADS / P::TN;
+            const int c = whole + threadIdx.x % P::TN;
+            if (c < columns) {
 #pragma unroll 1
-        for (int i = threadIdx.x; i < ROWS * loose; i += P::THREADS) {
-            const int r = i / loose, c = whole + i % loose;
-            const int64_t m = ((r >> 4) * P::FM + j) * 16 + (r & 15);
-            if (m >= left_m) continue;
-            const float v = reinterpret_cast<const float*>(lds + r * STRIDE)[c] * factor(m);
-            T* const to = D + m * ldd + c;
-            *to = (T)(accumulate ? (float)*to + v : v);
+                for (int r = threadIdx.x / P::TN; r < ROWS; r += AT_ONCE) {
+                    const int64_t m = ((r >> 4) * P::FM + j) * 16 + (r & 15);
+                    if (m >= left_m) continue;
+                    const float v = reinterpret_cast<const float*>(lds + r * STRIDE)[c] * factor(m);
+                    T* const to = D + m * ldd + c;
+                    *to = (T)(accumulate ? (float)*to + v : v);
+                }
+            }
         }
         __syncthreads();
     }

@@ -122,6 +122,16 @@ def test_gradient_in_pieces_and_one_result_at_a_time(type):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("tokens,vocab,k", [(5, 2600, 203), (77, 2701, 201), (301, 3001, 333)])
+def test_gradient_in_pieces_of_odd_sizes(tokens, vocab, k):
+    x = Problem(tokens, vocab, k, "bf16", 3)
+    least = device.Workspace(lib.ozaki_linear_loss_workspace_bytes(tokens, vocab, k, True, True))
+    _, lse = x.forward()
+    x.check_gradient(*x.gradient(lse), lse)
+    least.close()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("type", ["bf16", "f16"])
 def test_results_inside_larger_ones(type, workspace):
     x = Problem(70, 400, 99, type, 2)
