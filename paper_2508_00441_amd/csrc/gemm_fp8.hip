@@ -185,12 +185,16 @@ Shape shape_of(int64_t m, int64_t n, int64_t k) {
     return s;
 }
 
+// Large tiles run in rounds of one for every compute unit.  Where the last round has few of them, the rows or columns of D that they hold, of the
+// longer dimension, are left to 128 x 128 tiles in a launch of their own, if these run in one round (4608 x 4096 x 4096, 288 tiles: 93 us against 112,
+// x 512 30 against 37; 5500 x 4096 x 4096, 352 tiles: 106 against 118).
+int64_t in_rounds(int64_t length, int64_t across) {
+    const int64_t tiles = across * div_up(length, 256), over = tiles % 256, whole = (tiles - over) / across;
+    return over == 0 || whole == 0 || tiles - whole * across > 128 ? length : whole * 256;
+}
+
 template <int SCALING, int TYPE>
-hipError_t launch_kind(const GemmFp8Args& a, int splits, hipStream_t st) {
-    Shape s = shape_of(a.m, a.n, a.k);
-    // 32-bit results: the widened fragments of a 256 x 256 tile do not fit beside its accumulators, and two workgroups of 128 x 128, which pause at
-    // different times, do better than one of 256 x 128 (16384 x 4096 x 8192: 1030 and 1080 us)
-    if (TYPE == TYPE_F32 && s.kind == LARGE) s = Shape{MIDDLE, 128, 128, 1};
+hipError_t launch_kind(const GemmFp8Args& a, int splits, Shape s, hipStream_t st) {
     if (s.kind == VECTORS) {
         const unsigned blocks = (unsigned)div_up(a.n, 16);
         hipLaunchKernelGGL((gemm_fp8_few_kernel<SCALING, TYPE>), dim3(blocks), dim3(FEW_WAVES * 64), 0, st, a);
@@ -216,6 +220,33 @@ hipError_t launch_kind(const GemmFp8Args& a, int splits, hipStream_t st) {
     return hipGetLastError();
 }
 
+template <int SCALING, int TYPE>
+hipError_t launch_scaled(GemmFp8Args a, int splits, hipStream_t st) {
+    const Shape s = shape_of(a.m, a.n, a.k), middle{MIDDLE, 128, 128, 1};
+    if (s.kind != LARGE) return launch_kind<SCALING, TYPE>(a, splits, s, st);
+    // 32-bit results: the widened fragments of a 256 x 256 tile do not fit beside its accumulators, and two workgroups of 128 x 128, which pause at
+    // different times, do better than one of 256 x 128 (16384 x 4096 x 8192: 1030 and 1080 us)
+    if (TYPE == TYPE_F32) return launch_kind<SCALING, TYPE>(a, splits, middle, st);
+    const int64_t m = a.m, n = a.n;
+    if (m >= n) a.m = in_rounds(m, div_up(n, 256));
+    else a.n = in_rounds(n, div_up(m, 256));
+    const hipError_t e = launch_kind<SCALING, TYPE>(a, splits, s, st);
+    if (e != hipSuccess || (a.m == m && a.n == n)) return e;
+    typedef typename Element<TYPE>::type T;
+    if (a.m < m) {
+        a.A = static_cast<const uint8_t*>(a.A) + a.m * a.lda;
+        a.Sa += a.m;
+        a.D = static_cast<T*>(a.D) + a.m * a.ldd;
+        a.m = m - a.m;
+    } else {
+        a.B = static_cast<const uint8_t*>(a.B) + a.n * a.ldb;
+        a.Sb += SCALING == SCALE_BLOCKS ? a.n / SCALE_BLOCK : a.n;
+        a.D = static_cast<T*>(a.D) + a.n;
+        a.n = n - a.n;
+    }
+    return launch_kind<SCALING, TYPE>(a, splits, middle, st);
+}
+
 template <int TYPE>
 __global__ void __launch_bounds__(256) gemm_fp8_empty_kernel(const GemmFp8Args a) {
     typedef typename Element<TYPE>::type T;
@@ -230,7 +261,7 @@ hipError_t launch_typed(const GemmFp8Args& a, int scaling, int splits, hipStream
         hipLaunchKernelGGL((gemm_fp8_empty_kernel<TYPE>), dim3((unsigned)(a.m * a.n < 1 << 24 ? div_up(a.m * a.n, 256) : 1 << 16)), dim3(256), 0, st, a);
         return hipGetLastError();
     }
-    return scaling == SCALE_BLOCKS ? launch_kind<SCALE_BLOCKS, TYPE>(a, splits, st) : launch_kind<SCALE_VECTORS, TYPE>(a, splits, st);
+    return scaling == SCALE_BLOCKS ? launch_scaled<SCALE_BLOCKS, TYPE>(a, splits, st) : launch_scaled<SCALE_VECTORS, TYPE>(a, splits, st);
 }
 
 }  // namespace

@@ -646,7 +646,7 @@ __device__ __forceinline__ void store_tile(uint8_t* lds, const v4f32 (&acc)[P::F
         __syncthreads();
         const int column = threadIdx.x % PIECES * PER;
         if (column < whole) {
-#pragma unroll 1
+#pragma unroll 2
             for (int r = threadIdx.x / PIECES; r < ROWS; r += P::THREADS / PIECES) {
                 const int64_t m = ((r >> 4) * P::FM + j) * 16 + (r & 15);
                 if (m >= left_m) continue;
@@ -666,7 +666,7 @@ __device__ __forceinline__ void store_tile(uint8_t* lds, const v4f32 (&acc)[P::F
             constexpr int AT_ONCE = P::THREADS / P::TN;
             const int c = whole + threadIdx.x % P::TN;
             if (c < columns) {
-#pragma unroll 1
+#pragma unroll 4
                 for (int r = threadIdx.x / P::TN; r < ROWS; r += AT_ONCE) {
                     const int64_t m = ((r >> 4) * P::FM + j) * 16 + (r & 15);
                     if (m >= left_m) continue;

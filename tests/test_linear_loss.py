@@ -106,6 +106,13 @@ def test_gradient(tokens, vocab, k, type, workspace):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("tokens,vocab,k", [(1030, 13201, 1100), (513, 22017, 136), (1900, 8705, 600)])
+def test_vocabularies_whose_last_tiles_are_few(tokens, vocab, k, workspace):
+    test_loss(tokens, vocab, k, "bf16", workspace)
+    test_gradient(tokens, vocab, k, "bf16", workspace)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("type", ["bf16", "f16"])
 def test_gradient_in_pieces_and_one_result_at_a_time(type):
     x = Problem(150, 2900, 200, type, 1)
