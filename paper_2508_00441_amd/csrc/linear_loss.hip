@@ -147,16 +147,20 @@ __global__ void __launch_bounds__(256) loss_join_kernel(const float2* part, cons
     if (counts && !real) atomicOr(flags, TARGET_FLAG);
 }
 
-// Gradient, in front of everything: every token's target, its factor of dH's row, its share of dW relative to the largest, and the factor of dW.
-__global__ void __launch_bounds__(1024) loss_tokens_kernel(const int64_t* targets, const float* dloss, int64_t tokens, int64_t vocab,
-                                                           int64_t ignore, int* target_out, float* row_factor, float* share, float* dw_factor, int* flags) {
+// Gradient, in front of everything: every token's target, its factor of dH's row and the factor of dW; and H for dW, times the token's share of the
+// largest |dloss|, zeros where the token does not count, whatever it holds.  Every workgroup finds the largest |dloss| by itself (a launch of
+// its own for that took 2.5 us, and 4.6 with 1003 tokens).
+template <typename T>
+__device__ __forceinline__ void tokens_body(const T* H, int64_t ldh, const int64_t* targets, const float* dloss, int64_t tokens, int64_t vocab, int64_t ignore,
+                                            int* target_out, float* row_factor, float* dw_factor, T* to, int64_t ld, int* flags) {
+    typedef T eight __attribute__((ext_vector_type(8)));
     __shared__ float shared_most[16];
     float most = 0.0f;
-    for (int64_t t = threadIdx.x; t < tokens; t += 1024)
-        if (targets[t] != ignore) {
-            const float d = fabsf(dloss[t]);
-            most = d < __builtin_inff() ? fmaxf(most, d) : most;
-        }
+#pragma unroll 4
+    for (int64_t t = threadIdx.x; t < tokens; t += 1024) {
+        const float d = targets[t] != ignore ? fabsf(dloss[t]) : 0.0f;
+        most = d < __builtin_inff() ? fmaxf(most, d) : most;
+    }
 #pragma unroll
     for (int s = 1; s < 64; s <<= 1) most = fmaxf(most, __shfl_xor(most, s));
     if ((threadIdx.x & 63) == 0) shared_most[threadIdx.x >> 6] = most;
@@ -164,15 +168,29 @@ __global__ void __launch_bounds__(1024) loss_tokens_kernel(const int64_t* target
 #pragma unroll
     for (int i = 0; i < 16; ++i) most = fmaxf(most, shared_most[i]);
     if (most == 0.0f) most = 1.0f;
-    for (int64_t t = threadIdx.x; t < tokens; t += 1024) {
-        const int64_t target = targets[t];
-        const bool wanted = target != ignore, counts = wanted && target >= 0 && target < vocab;
-        if (wanted && !counts) atomicOr(flags, TARGET_FLAG);
-        target_out[t] = counts ? (int)target : -1;
-        row_factor[t] = counts ? dloss[t] * (1.0f / HELD) : 0.0f;
-        share[t] = counts ? dloss[t] / most : 0.0f;
+    if (blockIdx.x == 0) {
+        for (int64_t t = threadIdx.x; t < tokens; t += 1024) {
+            const int64_t target = targets[t];
+            const bool wanted = target != ignore, counts = wanted && target >= 0 && target < vocab;
+            if (wanted && !counts) atomicOr(flags, TARGET_FLAG);
+            target_out[t] = counts ? (int)target : -1;
+            row_factor[t] = counts ? dloss[t] * (1.0f / HELD) : 0.0f;
+        }
+        if (threadIdx.x == 0) *dw_factor = most * (1.0f / HELD);
     }
-    if (threadIdx.x == 0) *dw_factor = most * (1.0f / HELD);
+    if (to == nullptr) return;
+    const int64_t pieces = ld / 8;
+    for (int64_t at = (int64_t)blockIdx.x * 1024 + threadIdx.x; at < tokens * pieces; at += (int64_t)gridDim.x * 1024) {
+        const int64_t t = at / pieces, e = at % pieces * 8, target = targets[t];
+        eight x = {};
+        if (target != ignore && target >= 0 && target < vocab) {
+            const float f = dloss[t] / most;
+            x = *reinterpret_cast<const eight*>(H + t * ldh + e);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = (T)((float)x[i] * f);
+        }
+        *reinterpret_cast<eight*>(to + t * ld + e) = x;
+    }
 }
 
 // A tile of g, through LDS so that it is written in rows of 16-byte pieces.
@@ -211,24 +229,6 @@ __device__ __forceinline__ void loss_g_body(const LogitWork& w) {
         const int t = c / (P::TN / 8), p = c % (P::TN / 8);
         if (m0 + t >= w.tokens) break;
         *reinterpret_cast<v4i32*>(w.G + ((m0 + t) * w.ldg + n0 + p * 8) * 2) = *reinterpret_cast<const v4i32*>(lds + t * STRIDE + p * 16);
-    }
-}
-
-// H for dW: times the token's share, zeros where the token does not count, whatever it holds
-template <typename T>
-__device__ __forceinline__ void shares_body(const T* H, int64_t ldh, int64_t tokens, int64_t k, const int* target, const float* share, T* to, int64_t ld) {
-    typedef T eight __attribute__((ext_vector_type(8)));
-    const int64_t pieces = ld / 8;
-    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < tokens * pieces; at += (int64_t)gridDim.x * 256) {
-        const int64_t t = at / pieces, e = at % pieces * 8;
-        eight x = {};
-        if (target[t] >= 0) {
-            const float f = share[t];
-            x = *reinterpret_cast<const eight*>(H + t * ldh + e);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = (T)((float)x[i] * f);
-        }
-        *reinterpret_cast<eight*>(to + t * ld + e) = x;
     }
 }
 
@@ -347,10 +347,10 @@ __global__ void __launch_bounds__(256) loss_product_join_kernel(const float* par
 }
 
 template <int TYPE>
-__global__ void __launch_bounds__(256) loss_shares_kernel(const void* H, int64_t ldh, int64_t tokens, int64_t k, const int* target, const float* share, void* to,
-                                                          int64_t ld) {
+__global__ void __launch_bounds__(1024) loss_tokens_kernel(const void* H, int64_t ldh, const int64_t* targets, const float* dloss, int64_t tokens, int64_t vocab,
+                                                           int64_t ignore, int* target_out, float* row_factor, float* dw_factor, void* to, int64_t ld, int* flags) {
     typedef typename Element<TYPE>::type T;
-    shares_body(static_cast<const T*>(H), ldh, tokens, k, target, share, static_cast<T*>(to), ld);
+    tokens_body(static_cast<const T*>(H), ldh, targets, dloss, tokens, vocab, ignore, target_out, row_factor, dw_factor, static_cast<T*>(to), ld, flags);
 }
 
 // ---- shapes and work memory ------------------------------------------------------------------------------------
@@ -401,7 +401,6 @@ int64_t in_eights(int64_t n) { return div_up(n, 8) * 8; }
 struct GradPlaces {
     float* dw_factor;
     float* row_factor;
-    float* share;
     int* target;
     uint8_t* Hs;
     uint8_t* G;
@@ -417,7 +416,6 @@ GradPlaces grad_places(uint8_t* ws, int64_t tokens, int64_t vocab, int64_t k, in
     const int splits = dh_shape(tokens, k, div_up(words * 2, STEP_BYTES)).splits;
     p.dw_factor = reinterpret_cast<float*>(take(4));
     p.row_factor = reinterpret_cast<float*>(take((size_t)tokens * 4));
-    p.share = reinterpret_cast<float*>(take((size_t)tokens * 4));
     p.target = reinterpret_cast<int*>(take((size_t)tokens * 4));
     p.Hs = take((size_t)tokens * in_eights(k) * 2);
     p.G = take((size_t)tokens * padded(words) * 2);
@@ -507,15 +505,10 @@ hipError_t forward_typed(const LossArgs& a, uint8_t* ws, hipStream_t st) {
 template <int TYPE>
 hipError_t grad_typed(const LossArgs& a, int64_t piece, uint8_t* ws, hipStream_t st) {
     const GradPlaces p = grad_places(ws, a.tokens, a.vocab, a.k, piece);
-    hipLaunchKernelGGL(loss_tokens_kernel, dim3(1), dim3(1024), 0, st, a.targets, a.dloss, a.tokens, a.vocab, a.ignore, p.target, p.row_factor, p.share,
-                       p.dw_factor, a.flags);
+    const int64_t ldhs = in_eights(a.k), blocks_t = a.dW != nullptr ? div_up(a.tokens * (ldhs / 8), 1024) : 1;
+    hipLaunchKernelGGL((loss_tokens_kernel<TYPE>), dim3((unsigned)(blocks_t < 512 ? blocks_t : 512)), dim3(1024), 0, st, a.H, a.ldh, a.targets, a.dloss,
+                       a.tokens, a.vocab, a.ignore, p.target, p.row_factor, p.dw_factor, a.dW != nullptr ? p.Hs : nullptr, ldhs, a.flags);
     OZAKI_LOSS_TRY(hipGetLastError());
-    if (a.dW != nullptr) {
-        const int64_t ld = in_eights(a.k), blocks = div_up(a.tokens * (ld / 8), 256);
-        hipLaunchKernelGGL((loss_shares_kernel<TYPE>), dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, st, a.H, a.ldh, a.tokens, a.k, p.target,
-                           p.share, p.Hs, ld);
-        OZAKI_LOSS_TRY(hipGetLastError());
-    }
     const bool joined = piece < a.vocab;
     for (int64_t first = 0; first < a.vocab; first += piece) {
         const int64_t words = a.vocab - first < piece ? a.vocab - first : piece;
@@ -572,7 +565,7 @@ hipError_t grad_typed(const LossArgs& a, int64_t piece, uint8_t* ws, hipStream_t
             ProductWork d = {};
             d.X = p.Hs;
             d.Y = p.G;
-            d.ldx = in_eights(a.k) * 2;
+            d.ldx = ldhs * 2;
             d.ldy = padded(words) * 2;
             d.bytes = a.tokens * 2;
             d.elements = a.tokens;
