@@ -356,6 +356,8 @@ enum {
 };
 #define OZAKI_SCALE_BLOCK 128
 #define OZAKI_MAX_EXTENT (1 << 22)
+#define OZAKI_MAX_QUANTISED (1LL << 34) /* rows * k of ozaki_quantise_fp8 (a launch has fewer than 2^32 threads)       */
+#define OZAKI_MAX_LOGITS (1LL << 38)    /* tokens * vocab of ozaki_linear_loss and its gradient                       */
 
 /* Quantises X (rows vectors of k elements of `type`) to OCP E4M3.  For each block, a being the largest finite magnitude in it
  * and at least 2^-100:

@@ -32,6 +32,7 @@ TYPE_F32, TYPE_BF16, TYPE_F16 = 0, 1, 2
 SCALE_VECTORS, SCALE_BLOCKS = 0, 1
 SCALE_BLOCK = 128
 MAX_EXTENT = 1 << 22
+MAX_QUANTISED, MAX_LOGITS = 1 << 34, 1 << 38
 
 SLICE_FORMATS = {"fp8": SLICE_FP8_E4M3, "fp16": SLICE_FP16, "fp6": SLICE_FP6_E2M3, "fp6_e3m2": SLICE_FP6_E3M2, "int8": SLICE_INT8}
 ACCUM_MODES = {"hw": ACCUM_FP64_HW, "emu": ACCUM_FP64_INT_EMU, "exact": ACCUM_EXACT_FIXED}

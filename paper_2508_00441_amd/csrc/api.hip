@@ -235,8 +235,8 @@ bool stride_ok(int64_t ld, int64_t k, int bytes) {
 // the loss and its gradient: the arguments that they share, by position
 int check_loss_args(int64_t tokens, int64_t vocab, int64_t k, const void* H, int64_t ldh, const void* W, int64_t ldw, int type, const int64_t* targets) {
     if (!extent_ok(tokens)) return -1;
-    if (vocab < 1 || !extent_ok(vocab)) return -2;
-    if (k < 1 || !extent_ok(k * 2)) return -3;
+    if (vocab < 1 || !extent_ok(vocab) || tokens * vocab > OZAKI_MAX_LOGITS) return -2;
+    if (k < 1 || k > OZAKI_MAX_EXTENT / 2) return -3;
     if (type != OZAKI_TYPE_BF16 && type != OZAKI_TYPE_F16) return -8;
     if (tokens == 0) return 0;
     if (!H || !aligned16(H)) return -4;
@@ -565,7 +565,7 @@ int ozaki_fp64_add_emulated(const double* a, const double* b, double* out, int64
 int ozaki_quantise_fp8(int64_t rows, int64_t k, const void* X, int64_t ldx, int type, int scaling, void* Q, int64_t ldq, float* S,
                        int64_t lds, void* Qt, int64_t ldqt, float* St, int64_t ldst) {
     if (!extent_ok(rows)) return -1;
-    if (!extent_ok(k)) return -2;
+    if (!extent_ok(k) || rows * k > OZAKI_MAX_QUANTISED) return -2;
     if (!type_ok(type)) return -5;
     if (scaling != OZAKI_SCALE_VECTORS && scaling != OZAKI_SCALE_BLOCKS) return -6;
     if (rows == 0 || k == 0) return 0;
@@ -624,7 +624,7 @@ int ozaki_gemm_fp8(int64_t m, int64_t n, int64_t k, const void* A, int64_t lda, 
 }
 
 size_t ozaki_linear_loss_workspace_bytes(int64_t tokens, int64_t vocab, int64_t k, int grad, int minimum) {
-    if (tokens < 1 || !extent_ok(tokens) || vocab < 1 || !extent_ok(vocab) || k < 1 || !extent_ok(k * 2)) return 0;
+    if (tokens < 1 || !extent_ok(tokens) || vocab < 1 || !extent_ok(vocab) || tokens * vocab > OZAKI_MAX_LOGITS || k < 1 || k > OZAKI_MAX_EXTENT / 2) return 0;
     if (!grad) return loss_bytes(tokens, vocab);
     return loss_grad_bytes(tokens, vocab, k, minimum ? LOSS_PIECE : loss_grad_piece(tokens, vocab, k));
 }

@@ -310,6 +310,12 @@ def test_refusals_of_the_gradient(position, arguments):
     assert lib.ozaki_linear_loss_grad(**{**a, **arguments}, check=False) == -position
 
 
+@pytest.mark.parametrize("sizes,position", [(dict(tokens=lib.MAX_EXTENT, vocab=lib.MAX_LOGITS // lib.MAX_EXTENT + 1), 2), (dict(k=1 << 62), 3)])
+def test_refuses_more_than_a_launch_holds(sizes, position):
+    assert lib.ozaki_linear_loss(**{**FORWARD, **sizes}, check=False) == -position
+    assert lib.ozaki_linear_loss_workspace_bytes(**{**dict(tokens=100, vocab=200, k=30), **sizes}, grad=False, minimum=False) == 0
+
+
 def test_without_work_memory():
     assert lib.ozaki_linear_loss_workspace_bytes(0, 200, 30, False, False) == 0 and lib.ozaki_linear_loss_workspace_bytes(100, 200, 30, False, False) > 0
     context = lib.ozaki_context_create()

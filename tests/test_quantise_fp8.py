@@ -164,6 +164,11 @@ def test_refusals(position, arguments):
         lib.ozaki_quantise_fp8(**{**a, **arguments})
 
 
+def test_refuses_more_than_a_launch_holds():
+    a = dict(X=P, ldx=1 << 14, type=lib.TYPE_BF16, scaling=lib.SCALE_VECTORS, Q=P, ldq=1 << 14, S=P, lds=lib.MAX_EXTENT)
+    assert lib.ozaki_quantise_fp8(rows=lib.MAX_QUANTISED // (1 << 14) + 1, k=1 << 14, **a, check=False) == -2
+
+
 def test_nothing_to_do():
     for rows, k in ((0, 100), (100, 0)):
         assert lib.ozaki_quantise_fp8(rows, k, None, 0, lib.TYPE_BF16, lib.SCALE_VECTORS, None, 0, None, 0) == 0
