@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
 }
 template <int SCALING, int TYPE>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) gemm_fp8_small_kernel(const GemmFp8Work w) {
-    gemm_fp8_body<Tile<kind_of<TYPE, SCALING>(), 2, 2, 2, 2, 4>, TYPE>(w);
+    gemm_fp8_body<Tile<kind_of<TYPE, SCALING>(), 2, 2, 2, 2, 3>, TYPE>(w);
 }
 
 // Up to sixteen vectors of A: no tile in LDS.  A workgroup of FEW_WAVES waves takes sixteen vectors of B, a wave every FEW_WAVES-th step, straight
@@ -172,22 +172,26 @@ __global__ void __launch_bounds__(256) gemm_fp8_join_kernel(const GemmFp8Args a,
 
 enum { VECTORS, SMALL, MIDDLE, LARGE };
 struct Shape { int kind, tm, tn, splits; };
+// By how many tiles of 128 x 128 there are for 256 compute units, each of which holds two (times with blocks of scales, 16-bit results, in us):
+//     fewer than 256, or up to 64 rows or columns    64 x 64       512 x 4096 x 4096: 17.7, by 128 x 128 23.8;  1000 x 1000 x 1024 (32 bits) 9.1, 16.9
+//     up to 512, or up to 128 rows or columns        128 x 128     2048 x 4096 x 4096: 40, by 256 x 256 50;  900 x 4000 x 2048: 17.8, by 64 x 64 20.6
+//     more                                           256 x 256     2304 x 4096 x 4096: 51, by 128 x 128 60;  200 x 65536 x 2048: 43, 55
+// 32-bit results: no tiles of 256 x 256.  The widened fragments do not fit beside their accumulators, and two workgroups of 128 x 128, which pause
+// at different times, do better than one of 256 x 128 (16384 x 4096 x 8192: 1030 and 1080).
+// Where 64 x 64 tiles are too few, the inner dimension is cut, into shares of at least four steps (64 x 4096 x 16384: 17.3 for 256 shares in all,
+// 18.4 for 512; shares of eight steps: 64 x 2048 x 2048 9.5 against 8.5).
 Shape shape_of(int64_t m, int64_t n, int64_t k) {
     if (m <= FEW) return Shape{VECTORS, FEW, 16, 1};
-    Shape s{LARGE, 256, 256, 1};
-    if (m <= 512) s = Shape{SMALL, 64, 64, 1};
-    else if (div_up(m, 256) * div_up(n, 256) < 192) s = Shape{MIDDLE, 128, 128, 1};
-    if (s.kind != LARGE) {
-        const int64_t steps = div_up(k, SCALE_BLOCK), tiles = div_up(m, s.tm) * div_up(n, s.tn), want = 256 / tiles;
-        const int64_t splits = want < steps / 4 ? want : steps / 4;
-        s.splits = (int)(splits < 1 ? 1 : splits > 16 ? 16 : splits);
-    }
-    return s;
+    const int64_t middle = div_up(m, 128) * div_up(n, 128), least = m < n ? m : n;
+    if (middle >= 256 && least > 64) return middle <= 512 || least <= 128 ? Shape{MIDDLE, 128, 128, 1} : Shape{LARGE, 256, 256, 1};
+    const int64_t steps = div_up(k, SCALE_BLOCK), tiles = div_up(m, 64) * div_up(n, 64), want = 256 / tiles, most = steps / 4;
+    const int64_t splits = want < most ? want : most;
+    return Shape{SMALL, 64, 64, (int)(splits < 1 ? 1 : splits > 16 ? 16 : splits)};
 }
 
 // Large tiles run in rounds of one for every compute unit.  Where the last round has few of them, the rows or columns of D that they hold, of the
-// longer dimension, are left to 128 x 128 tiles in a launch of their own, if these run in one round (4608 x 4096 x 4096, 288 tiles: 93 us against 112,
-// x 512 30 against 37; 5500 x 4096 x 4096, 352 tiles: 106 against 118).
+// longer dimension, are left to smaller tiles in a launch of their own, if these run in one round (4608 x 4096 x 4096, 288 tiles: 83 us against 112,
+// x 512 27 against 37; 5500 x 4096 x 4096, 352 tiles: 102 against 118).
 int64_t in_rounds(int64_t length, int64_t across) {
     const int64_t tiles = across * div_up(length, 256), over = tiles % 256, whole = (tiles - over) / across;
     return over == 0 || whole == 0 || tiles - whole * across > 128 ? length : whole * 256;
@@ -222,15 +226,13 @@ hipError_t launch_kind(const GemmFp8Args& a, int splits, Shape s, hipStream_t st
 
 template <int SCALING, int TYPE>
 hipError_t launch_scaled(GemmFp8Args a, int splits, hipStream_t st) {
-    const Shape s = shape_of(a.m, a.n, a.k), middle{MIDDLE, 128, 128, 1};
+    const Shape s = shape_of(a.m, a.n, a.k);
     if (s.kind != LARGE) return launch_kind<SCALING, TYPE>(a, splits, s, st);
-    // 32-bit results: the widened fragments of a 256 x 256 tile do not fit beside its accumulators, and two workgroups of 128 x 128, which pause at
-    // different times, do better than one of 256 x 128 (16384 x 4096 x 8192: 1030 and 1080 us)
-    if (TYPE == TYPE_F32) return launch_kind<SCALING, TYPE>(a, splits, middle, st);
+    if (TYPE == TYPE_F32) return launch_kind<SCALING, TYPE>(a, 1, Shape{MIDDLE, 128, 128, 1}, st);
     const int64_t m = a.m, n = a.n;
     if (m >= n) a.m = in_rounds(m, div_up(n, 256));
     else a.n = in_rounds(n, div_up(m, 256));
-    const hipError_t e = launch_kind<SCALING, TYPE>(a, splits, s, st);
+    const hipError_t e = launch_kind<SCALING, TYPE>(a, 1, s, st);
     if (e != hipSuccess || (a.m == m && a.n == n)) return e;
     typedef typename Element<TYPE>::type T;
     if (a.m < m) {
@@ -244,7 +246,7 @@ hipError_t launch_scaled(GemmFp8Args a, int splits, hipStream_t st) {
         a.D = static_cast<T*>(a.D) + a.n;
         a.n = n - a.n;
     }
-    return launch_kind<SCALING, TYPE>(a, splits, middle, st);
+    return launch_kind<SCALING, TYPE>(a, 1, shape_of(a.m, a.n, a.k), st);
 }
 
 template <int TYPE>
