@@ -211,7 +211,7 @@ hipError_t launch_kind(const GemmFp8Args& a, int splits, Shape s, hipStream_t st
     w.tiles_m = (int)div_up(a.m, s.tm);
     w.tiles_n = (int)div_up(a.n, s.tn);
     const int64_t tiles = (int64_t)w.tiles_m * w.tiles_n;
-    w.order = WorkOrder{s.kind == LARGE ? 32 : 64, w.tiles_m > 8 ? 4 : 8};
+    w.order = WorkOrder{s.kind == LARGE ? 32 : 64, 8};             // 4096 x 4096 x 4096: 70 us, in plain order 75
     const unsigned blocks = (unsigned)(tiles * splits);
     if (s.kind == SMALL) hipLaunchKernelGGL((gemm_fp8_small_kernel<SCALING, TYPE>), dim3(blocks), dim3(256), 0, st, w);
     else if (s.kind == MIDDLE) hipLaunchKernelGGL((gemm_fp8_middle_kernel<SCALING, TYPE>), dim3(blocks), dim3(256), 0, st, w);

@@ -355,7 +355,9 @@ __global__ void __launch_bounds__(1024) loss_tokens_kernel(const void* H, int64_
 
 // ---- shapes and work memory ------------------------------------------------------------------------------------
 enum { FEW, SMALL, MIDDLE, LARGE };
-int shape_for(int64_t m, int64_t n) { return m <= 16 ? FEW : div_up(m, 256) * div_up(n, 256) < 128 || m <= 64 ? MIDDLE : LARGE; }
+// Up to 16 rows tiles of that many; of 256 x 256 from 128 of them on, but not for few rows; in between 128 x 64, two to a compute unit (forward, in us:
+// 512 tokens, 8000 words of 1024: 19, by large tiles 31; 1024, 12288 of 2048: 49, by middle ones 69; 100, 32768 of 2048: 42, by large ones 52).
+int shape_for(int64_t m, int64_t n) { return m <= 16 ? FEW : div_up(m, 256) * div_up(n, 256) < 128 || m <= 128 ? MIDDLE : LARGE; }
 // Of the kernels that form z: where tiles of 128 words and 64 tokens leave compute units without work, tiles of 64 words
 // (81 tokens, 7855 words of 3136: 19.7 us against 26.2; 400, 3053 of 1296: 15.4 against 16.0).
 int logit_shape(int64_t tokens, int64_t words) {
@@ -365,9 +367,11 @@ int logit_shape(int64_t tokens, int64_t words) {
 int tile_m(int shape) { return shape == FEW ? 16 : shape == LARGE ? 256 : 64; }
 int tile_n(int shape) { return shape == LARGE ? 256 : 128; }
 int tile_words(int shape) { return shape == FEW || shape == SMALL ? 64 : tile_n(shape); }      // of the kernels that form z
-WorkOrder order_for(int shape, int64_t tiles_m) { return WorkOrder{shape == LARGE ? 32 : 64, tiles_m > 8 ? 4 : 8}; }
+// tiles that run on an XCD at a time share its L2: 4096 tokens, 65536 words of 4096, gradient 4.98 ms, in plain order 5.37
+WorkOrder order_for(int shape) { return WorkOrder{shape == LARGE ? 32 : 64, 8}; }
 // dH, whose inner dimension is the vocabulary: large tiles also where they are few, if that leaves every compute unit a share of it of
-// some length (1003 x 1024 over 50001 words: 16 tiles in 16 shares)
+// some length (1003 x 1024 over 50001 words: 16 tiles in 16 shares; the whole gradient 339 us, with middle tiles 383).  Shares of at least eight steps,
+// as many as run at a time (twice as many: 365).
 // Large tiles run in rounds of one for every compute unit.  Where the last round has few of them, the words that they hold are left to smaller
 // tiles in a launch of their own (1003 tokens and 50001 words, 784 tiles: of 1000 elements 129 us against 144, of 256 58 against 66, the gradient
 // 353 against 376 and 150 against 157; up to 64 tiles, 256 of 128 x 128).
@@ -387,7 +391,7 @@ int64_t logit_tiles(const LogitPlan& p) { return div_up(p.words[0], tile_words(p
 struct ProductShape { int shape, splits; };
 ProductShape dh_shape(int64_t m, int64_t n, int64_t steps) {
     int shape = shape_for(m, n);
-    if (shape == MIDDLE && m > 64 && div_up(m, 256) * div_up(n, 256) * (steps / 16) >= 128) shape = LARGE;
+    if (shape == MIDDLE && m > 128 && div_up(m, 256) * div_up(n, 256) * (steps / 16) >= 128) shape = LARGE;
     const int64_t tiles = div_up(m, tile_m(shape)) * div_up(n, tile_n(shape)), want = (shape == LARGE ? 256 : 512) / tiles, most = steps / 8;
     const int64_t s = want < most ? want : most;
     return ProductShape{shape, (int)(s < 1 ? 1 : s > 32 ? 32 : s)};
@@ -432,7 +436,7 @@ template <int TYPE>
 hipError_t launch_dh(ProductWork w, int shape, hipStream_t st) {
     w.tiles_m = (int)div_up(w.m, tile_m(shape));
     w.tiles_n = (int)div_up(w.n, tile_n(shape));
-    w.order = order_for(shape, w.tiles_m);
+    w.order = order_for(shape);
     const dim3 blocks((unsigned)((int64_t)w.tiles_m * w.tiles_n * w.splits));
     if (shape == FEW) hipLaunchKernelGGL((loss_dh_few_kernel<TYPE>), blocks, dim3(256), 0, st, w);
     else if (shape == MIDDLE) hipLaunchKernelGGL((loss_dh_middle_kernel<TYPE>), blocks, dim3(256), 0, st, w);
@@ -445,7 +449,7 @@ hipError_t launch_dw(ProductWork w, hipStream_t st) {
     const int edge = large ? 256 : 128;
     w.tiles_m = (int)div_up(w.m, edge);
     w.tiles_n = (int)div_up(w.n, edge);
-    w.order = order_for(large ? LARGE : MIDDLE, w.tiles_m);
+    w.order = order_for(large ? LARGE : MIDDLE);
     const dim3 blocks((unsigned)((int64_t)w.tiles_m * w.tiles_n));
     if (large) hipLaunchKernelGGL((loss_dw_large_kernel<TYPE>), blocks, dim3(512), 0, st, w);
     else hipLaunchKernelGGL((loss_dw_middle_kernel<TYPE>), blocks, dim3(256), 0, st, w);
@@ -456,7 +460,7 @@ void set_tiles(LogitWork& w, int shape) {
     w.steps = (int)div_up(w.bytes, STEP_BYTES);
     w.tiles_m = (int)div_up(w.tokens, tile_m(shape));
     w.tiles_n = (int)div_up(w.words, tile_words(shape));
-    w.order = order_for(shape, w.tiles_m);
+    w.order = order_for(shape);
 }
 // the second share of a plan, behind the first
 void second_share(LogitWork& w, const LogitPlan& p) {
