@@ -2,6 +2,8 @@
 //     D[i][j] = sum over blocks b of  Sa[b][i] * Sb[b][j or j / 128] * (sum over e in b of A[i][e] * B[j][e])
 // A block's products are summed by the matrix unit in FP32, the blocks' sums by FP32 fused multiply-adds with the product of their two
 // scales; D is rounded once.  A D of 16 bits takes the FP8 instructions, a D of 32 bits the FP16 ones (Fragment in tile_product.hpp).
+// Few vectors of A are bound by the read of B, many by the matrix unit's issue (4096 x 4096 x 4096: 61 us, 2.2 PFLOP/s), 32-bit results by the vector
+// unit, which widens the codes (16384 x 4096 x 8192: 1.03 ms, 1.07 PFLOP/s).
 #include "layout.hpp"
 #include "tile_product.hpp"
 
@@ -107,14 +109,16 @@ __device__ __forceinline__ float few_sum(v4f32 (&sums)[FEW_WAVES][64], v4f32 min
 }
 
 template <int SCALING, int TYPE>
-__global__ void __launch_bounds__(FEW_WAVES * 64) gemm_fp8_few_kernel(const GemmFp8Args a) {
+__global__ void __launch_bounds__(FEW_WAVES * 64) gemm_fp8_few_kernel(const GemmFp8Args a, const int splits) {
     typedef typename Element<TYPE>::type T;
     typedef Fragment<TYPE == TYPE_F32> F;
     __shared__ __attribute__((aligned(16))) v4f32 sums[FEW_WAVES][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
-    const int64_t n0 = (int64_t)blockIdx.x * 16;
+    const int split = blockIdx.x % splits;
+    const int64_t n0 = (int64_t)(blockIdx.x / splits) * 16;
     const int left_n = a.n - n0 < 16 ? (int)(a.n - n0) : 16;
     FewPieces p(TileOperand{a.B + n0 * a.ldb, a.ldb, left_n, nullptr, 0}, TileOperand{a.A, a.lda, (int)a.m, nullptr, 0}, a.k, lane);
+    const int begin = split_begin(p.steps, splits, split), end = split_begin(p.steps, splits, split + 1);
     const float* const sx_at = SCALING == SCALE_BLOCKS ? a.Sb + n0 / SCALE_BLOCK : a.Sb + n0;
     const float* const sy_at = a.Sa + ((lane & 15) < a.m ? lane & 15 : a.m - 1);
     int four[4];                                     // this lane's four columns of the result
@@ -123,7 +127,7 @@ __global__ void __launch_bounds__(FEW_WAVES * 64) gemm_fp8_few_kernel(const Gemm
     v4f32 sx[AHEAD];
     float sy[AHEAD];
     auto load = [&](int u, int s) {
-        s = s < p.steps ? s : p.steps - 1;
+        s = s < end ? s : end - 1;
         p.load(u, s);
         sy[u] = sy_at[s * a.ldsa];
         if constexpr (SCALING == SCALE_BLOCKS) {
@@ -135,23 +139,27 @@ __global__ void __launch_bounds__(FEW_WAVES * 64) gemm_fp8_few_kernel(const Gemm
     };
     v4f32 acc = {};
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) load(u, wave + u * FEW_WAVES);
-    for (int first = wave; first < p.steps; first += FEW_WAVES * AHEAD) {
+    for (int u = 0; u < AHEAD; ++u) load(u, begin + wave + u * FEW_WAVES);
+    for (int first = begin + wave; first < end; first += FEW_WAVES * AHEAD) {
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const int s = first + u * FEW_WAVES;
-            if (s >= p.steps) break;
+            if (s >= end) break;
             p.clear_end(u, s);
             const v4f32 t = F::product(F::of(__builtin_shufflevector(p.x[u][0], p.x[u][1], 0, 1, 2, 3, 4, 5, 6, 7)),
                                        F::of(__builtin_shufflevector(p.y[u][0], p.y[u][1], 0, 1, 2, 3, 4, 5, 6, 7)));
 #pragma unroll
             for (int r = 0; r < 4; ++r) acc[r] = __builtin_fmaf(t[r], sx[u][SCALING == SCALE_BLOCKS ? 0 : r] * sy[u], acc[r]);
-            if (first + FEW_WAVES * AHEAD < p.steps) load(u, s + FEW_WAVES * AHEAD);
+            if (first + FEW_WAVES * AHEAD < end) load(u, s + FEW_WAVES * AHEAD);
         }
     }
     const float sum = few_sum(sums, acc);
     const int n = threadIdx.x & 15, m = threadIdx.x >> 4;
     if (threadIdx.x >= 256 || m >= a.m || n >= left_n) return;
+    if (splits > 1) {
+        a.partial[((int64_t)split * a.m + m) * in_fours(a.n) + n0 + n] = sum;
+        return;
+    }
     T* const to = static_cast<T*>(a.D) + m * a.ldd + n0 + n;
     *to = (T)(a.accumulate ? (float)*to + sum : sum);
 }
@@ -179,14 +187,18 @@ struct Shape { int kind, tm, tn, splits; };
 // 32-bit results: no tiles of 256 x 256.  The widened fragments do not fit beside their accumulators, and two workgroups of 128 x 128, which pause
 // at different times, do better than one of 256 x 128 (16384 x 4096 x 8192: 1030 and 1080).
 // Where 64 x 64 tiles are too few, the inner dimension is cut, into shares of at least four steps (64 x 4096 x 16384: 17.3 for 256 shares in all,
-// 18.4 for 512; shares of eight steps: 64 x 2048 x 2048 9.5 against 8.5).
+// 18.4 for 512; shares of eight steps: 64 x 2048 x 2048 9.5 against 8.5).  Where few vectors meet few of B: of at least 32 steps, from three shares on
+// (1 x 64 x 65536: 7.5, uncut 37.7; 1 x 1024 x 16384: 8.4, 11.9, in shares of 64 steps 10.0; but 1 x 2048 x 8192, two shares: 8.1, uncut 7.7).
 Shape shape_of(int64_t m, int64_t n, int64_t k) {
-    if (m <= FEW) return Shape{VECTORS, FEW, 16, 1};
+    const int64_t steps = div_up(k, SCALE_BLOCK);
+    const auto shares = [](int64_t want, int64_t most) {
+        const int64_t s = want < most ? want : most;
+        return (int)(s < 1 ? 1 : s > 16 ? 16 : s);
+    };
+    if (m <= FEW) return Shape{VECTORS, FEW, 16, steps < 96 ? 1 : shares(256 / div_up(n, 16), steps / 32)};
     const int64_t middle = div_up(m, 128) * div_up(n, 128), least = m < n ? m : n;
     if (middle >= 256 && least > 64) return middle <= 512 || least <= 128 ? Shape{MIDDLE, 128, 128, 1} : Shape{LARGE, 256, 256, 1};
-    const int64_t steps = div_up(k, SCALE_BLOCK), tiles = div_up(m, 64) * div_up(n, 64), want = 256 / tiles, most = steps / 4;
-    const int64_t splits = want < most ? want : most;
-    return Shape{SMALL, 64, 64, (int)(splits < 1 ? 1 : splits > 16 ? 16 : splits)};
+    return Shape{SMALL, 64, 64, shares(256 / (div_up(m, 64) * div_up(n, 64)), steps / 4)};
 }
 
 // Large tiles run in rounds of one for every compute unit.  Where the last round has few of them, the rows or columns of D that they hold, of the
@@ -199,11 +211,6 @@ int64_t in_rounds(int64_t length, int64_t across) {
 
 template <int SCALING, int TYPE>
 hipError_t launch_kind(const GemmFp8Args& a, int splits, Shape s, hipStream_t st) {
-    if (s.kind == VECTORS) {
-        const unsigned blocks = (unsigned)div_up(a.n, 16);
-        hipLaunchKernelGGL((gemm_fp8_few_kernel<SCALING, TYPE>), dim3(blocks), dim3(FEW_WAVES * 64), 0, st, a);
-        return hipGetLastError();
-    }
     GemmFp8Work w;
     w.g = a;
     w.steps = (int)div_up(a.k, SCALE_BLOCK);
@@ -213,7 +220,8 @@ hipError_t launch_kind(const GemmFp8Args& a, int splits, Shape s, hipStream_t st
     const int64_t tiles = (int64_t)w.tiles_m * w.tiles_n;
     w.order = WorkOrder{s.kind == LARGE ? 32 : 64, 8};             // 4096 x 4096 x 4096: 70 us, in plain order 75
     const unsigned blocks = (unsigned)(tiles * splits);
-    if (s.kind == SMALL) hipLaunchKernelGGL((gemm_fp8_small_kernel<SCALING, TYPE>), dim3(blocks), dim3(256), 0, st, w);
+    if (s.kind == VECTORS) hipLaunchKernelGGL((gemm_fp8_few_kernel<SCALING, TYPE>), dim3(blocks), dim3(FEW_WAVES * 64), 0, st, a, splits);
+    else if (s.kind == SMALL) hipLaunchKernelGGL((gemm_fp8_small_kernel<SCALING, TYPE>), dim3(blocks), dim3(256), 0, st, w);
     else if (s.kind == MIDDLE) hipLaunchKernelGGL((gemm_fp8_middle_kernel<SCALING, TYPE>), dim3(blocks), dim3(256), 0, st, w);
     else if constexpr (TYPE != TYPE_F32) hipLaunchKernelGGL((gemm_fp8_large_kernel<SCALING, TYPE>), dim3(blocks), dim3(512), 0, st, w);
     if (splits > 1) {

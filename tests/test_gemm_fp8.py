@@ -85,6 +85,17 @@ def test_products_of_many_tiles(m, n, k, blocks, type_d, workspace):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("type_d", ["bf16", "f32"])
+@pytest.mark.parametrize("blocks", [True, False])
+@pytest.mark.parametrize("m,n,k", [(1, 64, 65536), (3, 130, 12401), (16, 65, 20000)])
+def test_few_vectors_of_many_elements(m, n, k, blocks, type_d, workspace):
+    o = Operands(m, n, k, blocks, 14)
+    D = torch.full((m, n), float("nan"), dtype=plain.DTYPES[type_d], device="cuda")
+    o.multiply(D, n, type_d)
+    _check(o, D, type_d)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("type_d", ["bf16", "f16"])
 @pytest.mark.parametrize("blocks", [True, False])
 @pytest.mark.parametrize("m,n,k", [(4353, 3841, 264), (3841, 4353, 401), (4609, 3600, 128)])
