@@ -13,6 +13,9 @@
 // and lose nothing to 16 bits; times dloss they all lose alike, which does not average out (1.7 times the error of the result's own
 // rounding in FP16).  2^12 keeps the words down to a probability of 2^-26 among FP16's normal numbers.  dloss comes in where it costs no
 // rounding: as a factor of the rows of dH, and for dW with a copy of H times dloss over the largest |dloss|, which is one for a mean.
+//
+// Few tokens are bound by the read of W (16 x 65536 x 2048: 52 us and 5 for the join, 5.1 TB/s; the gradient reads it twice, 166 us), many by the matrix
+// unit (4096 x 131072 x 4096: 3.07 ms, 1.43 PFLOP/s; gradient of 4096 x 65536 x 4096: 4.83 ms, 1.36 PFLOP/s).
 #include "layout.hpp"
 #include "tile_product.hpp"
 

@@ -173,7 +173,8 @@ struct Tile {
     static_assert((!XT || TN % 128 == 0) && (!YT || TM % 128 == 0), "");
 
     // acc[i][j][r] += X row wn * FN * 16 + 16 i + 4 (lane / 16) + r  times  Y row wm * FM * 16 + 16 j + lane % 16, over the steps
-    // [step0, step1) of vectors of `bytes` bytes (if only one operand is turned, the other has zeros behind them to the end of the 16 bytes).  Ends with nothing in flight and all waves past their last LDS read.
+    // [step0, step1) of vectors of `bytes` bytes (if only one operand is turned, the other has zeros behind them to the end of the 16 bytes).  Ends
+    // with nothing in flight and all waves past their last LDS read.
     __device__ static void multiply(uint8_t* lds, const TileOperand& X, const TileOperand& Y, int64_t bytes, int step0, int step1,
                                     v4f32 (&acc)[FN][FM]) {
         const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -423,6 +424,8 @@ struct Tile {
 // that reads it has been issued.  So no wave waits for LDS at a step's head.
 // Whole steps are loaded with buffer instructions, whose addresses are 32-bit offsets of a lane and of the step: 256 accumulators of two waves
 // leave no registers for 64-bit ones.
+// FP8, 8192 x 8192 x 8192: 460 us, 2.39 PFLOP/s, the matrix unit busy 60 % of the cycles at 1.9 GHz; without loads and LDS reads it would be 3.2 PFLOP/s.
+// BF16, 4096 x 65536 x 4096: 1.43 PFLOP/s, busy 74 %; 2.07 without.  Bound by the two together: LDS reads and scales hold up the issue.
 template <int KIND, bool XT = false, bool YT = false>
 struct PairedTile {
     typedef Tile<KIND, 2, 4, 8, 4, 2> Base;
