@@ -29,7 +29,7 @@ __device__ __forceinline__ float log_of(float x) { return __builtin_amdgcn_logf(
 // per token, what a tile of z needs
 struct TokenState {
     const float* lse;
-    const int* target;       // -1 where it does not count
+    const int* target;
 };
 constexpr float HELD = 4096.0f;          // what g is held times
 
@@ -38,6 +38,7 @@ struct LogitWork {
     const uint8_t* W;        // of the piece
     int64_t ldh, ldw, bytes; // in bytes
     int64_t tokens, words, first_word;    // words: of the piece
+    const int* count;        // not null: how many tokens there really are
     int tiles_m, tiles_n, steps;
     WorkOrder order;
     // forward
@@ -50,15 +51,19 @@ struct LogitWork {
     int64_t ldg;             // elements
 };
 
+// the tile of z that this workgroup has; false where it has none
 template <typename P>
-__device__ __forceinline__ void logits(const LogitWork& w, uint8_t* lds, int64_t& m0, int64_t& n0, v4f32 (&acc)[P::FN][P::FM]) {
-    const WorkItem item = work_item(blockIdx.x, gridDim.x, w.order, w.tiles_m, w.tiles_n);
+__device__ __forceinline__ bool logits(const LogitWork& w, uint8_t* lds, int64_t tokens, int64_t& m0, int64_t& n0, v4f32 (&acc)[P::FN][P::FM]) {
+    const unsigned tiles_m = (unsigned)div_up(tokens, P::TM), total = tiles_m * (unsigned)w.tiles_n;
+    if (blockIdx.x >= total) return false;
+    const WorkItem item = work_item(blockIdx.x, total, w.order, tiles_m, w.tiles_n);
     m0 = (int64_t)item.bm * P::TM;
     n0 = (int64_t)item.bn * P::TN;
-    const int64_t left_m = w.tokens - m0, left_n = w.words - n0;
+    const int64_t left_m = tokens - m0, left_n = w.words - n0;
     const TileOperand X{w.W + n0 * w.ldw, w.ldw, (int)(left_n < P::TN ? left_n : P::TN), nullptr, 0};
     const TileOperand Y{w.H + m0 * w.ldh, w.ldh, (int)(left_m < P::TM ? left_m : P::TM), nullptr, 0};
     P::multiply(lds, X, Y, w.bytes, 0, w.steps, acc);
+    return true;
 }
 
 template <typename P>
@@ -66,7 +71,7 @@ __device__ __forceinline__ void loss_forward_body(const LogitWork& w) {
     __shared__ __attribute__((aligned(16))) uint8_t lds[P::LDS_BYTES];
     int64_t m0, n0;
     v4f32 acc[P::FN][P::FM] = {};
-    logits<P>(w, lds, m0, n0, acc);
+    if (!logits<P>(w, lds, w.tokens, m0, n0, acc)) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wn = wave / P::WM, wm = wave % P::WM, g = lane >> 4;
     float2* const joined = reinterpret_cast<float2*>(lds);            // [wn][token]
     const int first = wn * P::FN * 16 + 4 * g;                        // this lane's first word in the tile
@@ -150,49 +155,120 @@ __global__ void __launch_bounds__(256) loss_join_kernel(const float2* part, cons
     if (counts && !real) atomicOr(flags, TARGET_FLAG);
 }
 
-// Gradient, in front of everything: every token's target, its factor of dH's row and the factor of dW; and H for dW, times the token's share of the
-// largest |dloss|, zeros where the token does not count, whatever it holds.  Every workgroup finds the largest |dloss| by itself (a launch of
-// its own for that took 2.5 us, and 4.6 with 1003 tokens).
+// Gradient, in front of everything.  Tokens that do not count (often more than half: prompts, padding) cost the products nothing: those that do are
+// copied together, in their order, H as it is and (for dW) times the token's share of the largest |dloss|; with them go their targets, lse and
+// factors of dH's rows, and where in dH those lie.  How many there are only the card knows: the kernels behind this one are launched for all tokens,
+// and workgroups without any end at once.  Rows of dH of the other tokens become zeros here.
+// A workgroup has `each` neighbouring tokens; it finds the largest |dloss| and how many count in front of its own by itself (12 bytes a token; a
+// launch of its own for that took 2.5 us, and 4.6 with 1003 tokens).
+struct GradTokens {
+    const int64_t* targets;
+    const float* lse;
+    const float* dloss;
+    int64_t tokens, vocab, ignore, k, each;
+    // of the tokens that count, in their order
+    int* count;
+    int* place;              // in dH
+    int* target_out;
+    float* lse_out;
+    float* row_factor;
+    float* dw_factor;        // one number
+    int* flags;
+};
+constexpr int TOKEN_THREADS = 512;
+
 template <typename T>
-__device__ __forceinline__ void tokens_body(const T* H, int64_t ldh, const int64_t* targets, const float* dloss, int64_t tokens, int64_t vocab, int64_t ignore,
-                                            int* target_out, float* row_factor, float* dw_factor, T* to, int64_t ld, int* flags) {
+__device__ __forceinline__ void tokens_body(const GradTokens& w, const T* H, int64_t ldh, T* Hc, T* Hs, int64_t ld, T* dH, int64_t lddh) {
     typedef T eight __attribute__((ext_vector_type(8)));
-    __shared__ float shared_most[16];
+    constexpr int WAVES = TOKEN_THREADS / 64;
+    __shared__ float most_of[WAVES];
+    __shared__ int before_of[WAVES], all_of[WAVES], at_of[TOKEN_THREADS];
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const int64_t first = (int64_t)blockIdx.x * w.each, end = first + w.each < w.tokens ? first + w.each : w.tokens;
+    const auto counts = [&](int64_t target) { return target != w.ignore && target >= 0 && target < w.vocab; };
     float most = 0.0f;
+    int before = 0, all = 0;
 #pragma unroll 4
-    for (int64_t t = threadIdx.x; t < tokens; t += 1024) {
-        const float d = targets[t] != ignore ? fabsf(dloss[t]) : 0.0f;
+    for (int64_t t = tid; t < w.tokens; t += TOKEN_THREADS) {
+        const bool c = counts(w.targets[t]);
+        const float d = c ? fabsf(w.dloss[t]) : 0.0f;
         most = d < __builtin_inff() ? fmaxf(most, d) : most;
+        all += c;
+        before += c && t < first;
     }
 #pragma unroll
-    for (int s = 1; s < 64; s <<= 1) most = fmaxf(most, __shfl_xor(most, s));
-    if ((threadIdx.x & 63) == 0) shared_most[threadIdx.x >> 6] = most;
+    for (int s = 1; s < 64; s <<= 1) {
+        most = fmaxf(most, __shfl_xor(most, s));
+        before += __shfl_xor(before, s);
+        all += __shfl_xor(all, s);
+    }
+    if (lane == 0) {
+        most_of[wave] = most;
+        before_of[wave] = before;
+        all_of[wave] = all;
+    }
     __syncthreads();
+    before = all = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) most = fmaxf(most, shared_most[i]);
-    if (most == 0.0f) most = 1.0f;
-    if (blockIdx.x == 0) {
-        for (int64_t t = threadIdx.x; t < tokens; t += 1024) {
-            const int64_t target = targets[t];
-            const bool wanted = target != ignore, counts = wanted && target >= 0 && target < vocab;
-            if (wanted && !counts) atomicOr(flags, TARGET_FLAG);
-            target_out[t] = counts ? (int)target : -1;
-            row_factor[t] = counts ? dloss[t] * (1.0f / HELD) : 0.0f;
-        }
-        if (threadIdx.x == 0) *dw_factor = most * (1.0f / HELD);
+    for (int i = 0; i < WAVES; ++i) {
+        most = fmaxf(most, most_of[i]);
+        before += before_of[i];
+        all += all_of[i];
     }
-    if (to == nullptr) return;
+    if (most == 0.0f) most = 1.0f;
+    if (blockIdx.x == 0 && tid == 0) {
+        *w.count = all;
+        *w.dw_factor = most * (1.0f / HELD);
+    }
     const int64_t pieces = ld / 8;
-    for (int64_t at = (int64_t)blockIdx.x * 1024 + threadIdx.x; at < tokens * pieces; at += (int64_t)gridDim.x * 1024) {
-        const int64_t t = at / pieces, e = at % pieces * 8, target = targets[t];
-        eight x = {};
-        if (target != ignore && target >= 0 && target < vocab) {
-            const float f = dloss[t] / most;
-            x = *reinterpret_cast<const eight*>(H + t * ldh + e);
+    const bool wide = lddh % 8 == 0 && reinterpret_cast<uintptr_t>(dH) % 16 == 0;
+    for (int64_t from = first; from < end; from += TOKEN_THREADS) {
+        // the places of the next tokens, one a thread
+        const int64_t t = from + tid;
+        const bool c = t < end && counts(w.targets[t]);
+        const unsigned long long in_wave = __ballot(c);
+        __syncthreads();
+        if (lane == 0) all_of[wave] = __popcll(in_wave);
+        __syncthreads();
+        int at = before + __popcll(in_wave & ((1ull << lane) - 1));
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = (T)((float)x[i] * f);
+        for (int i = 0; i < WAVES; ++i) {
+            at += i < wave ? all_of[i] : 0;
+            before += all_of[i];
         }
-        *reinterpret_cast<eight*>(to + t * ld + e) = x;
+        at_of[tid] = c ? at : -1;
+        if (c) {
+            w.place[at] = (int)t;
+            w.target_out[at] = (int)w.targets[t];
+            w.lse_out[at] = w.lse[t];
+            w.row_factor[at] = w.dloss[t] * (1.0f / HELD);
+        } else if (t < end && w.targets[t] != w.ignore) {
+            atomicOr(w.flags, TARGET_FLAG);
+        }
+        __syncthreads();
+        const int64_t here = end - from < TOKEN_THREADS ? end - from : TOKEN_THREADS;
+        for (int64_t p = tid; p < here * pieces; p += TOKEN_THREADS) {
+            const int64_t i = p / pieces, e = p % pieces * 8;
+            const int to = at_of[i];
+            if (to >= 0) {
+                eight x = *reinterpret_cast<const eight*>(H + (from + i) * ldh + e);
+                *reinterpret_cast<eight*>(Hc + to * ld + e) = x;
+                if (Hs == nullptr) continue;
+                const float f = w.dloss[from + i] / most;
+#pragma unroll
+                for (int q = 0; q < 8; ++q) x[q] = (T)((float)x[q] * f);
+                *reinterpret_cast<eight*>(Hs + to * ld + e) = x;
+            } else if (dH != nullptr) {
+                T* const row = dH + (from + i) * lddh + e;
+                if (wide && e + 8 <= w.k) {
+                    *reinterpret_cast<eight*>(row) = eight{};
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        if (e + q < w.k) row[q] = (T)0.0f;
+                }
+            }
+        }
     }
 }
 
@@ -203,7 +279,8 @@ __device__ __forceinline__ void loss_g_body(const LogitWork& w) {
     __shared__ __attribute__((aligned(16))) uint8_t lds[P::LDS_BYTES > P::TM * STRIDE ? P::LDS_BYTES : P::TM * STRIDE];
     int64_t m0, n0;
     v4f32 acc[P::FN][P::FM] = {};
-    logits<P>(w, lds, m0, n0, acc);
+    const int64_t tokens = *w.count;
+    if (!logits<P>(w, lds, tokens, m0, n0, acc)) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wn = wave / P::WM, wm = wave % P::WM, g = lane >> 4;
     const int first = wn * P::FN * 16 + 4 * g;
     const int words = (int)(w.words - n0 < P::TN ? w.words - n0 : P::TN);
@@ -211,10 +288,9 @@ __device__ __forceinline__ void loss_g_body(const LogitWork& w) {
 #pragma unroll
     for (int j = 0; j < P::FM; ++j) {
         const int t = (wm * P::FM + j) * 16 + (lane & 15);
-        const bool real = m0 + t < w.tokens;
-        const int target = real ? w.token.target[m0 + t] : -1;
-        const float lse = target >= 0 ? w.token.lse[m0 + t] : 0.0f;
-        const int at = target >= 0 ? (int)(target - w.first_word - n0) : -1;
+        const bool real = m0 + t < tokens;
+        const float lse = real ? w.token.lse[m0 + t] : 0.0f;
+        const int at = real ? (int)(w.token.target[m0 + t] - w.first_word - n0) : -1;
 #pragma unroll
         for (int i = 0; i < P::FN; ++i) {
             four v;
@@ -222,7 +298,7 @@ __device__ __forceinline__ void loss_g_body(const LogitWork& w) {
             for (int r = 0; r < 4; ++r) {
                 const int word = first + 16 * i + r;
                 const float p = exp_of(acc[i][j][r] - lse) - (word == at ? 1.0f : 0.0f);
-                v[r] = (T)(target >= 0 && word < words ? p * HELD : 0.0f);
+                v[r] = (T)(word < words ? p * HELD : 0.0f);
             }
             *reinterpret_cast<four*>(lds + t * STRIDE + (first + 16 * i) * 2) = v;
         }
@@ -230,7 +306,7 @@ __device__ __forceinline__ void loss_g_body(const LogitWork& w) {
     __syncthreads();
     for (int c = threadIdx.x; c < P::TM * P::TN / 8; c += P::THREADS) {
         const int t = c / (P::TN / 8), p = c % (P::TN / 8);
-        if (m0 + t >= w.tokens) break;
+        if (m0 + t >= tokens) break;
         *reinterpret_cast<v4i32*>(w.G + ((m0 + t) * w.ldg + n0 + p * 8) * 2) = *reinterpret_cast<const v4i32*>(lds + t * STRIDE + p * 16);
     }
 }
@@ -239,10 +315,12 @@ __device__ __forceinline__ void loss_g_body(const LogitWork& w) {
 struct ProductWork {
     const uint8_t* X;
     const uint8_t* Y;
-    int64_t ldx, ldy, bytes; // ldx, ldy: in bytes
-    int64_t elements;        // of the inner dimension (turned operands)
-    int64_t m, n;
-    int tiles_m, tiles_n, steps, splits;
+    int64_t ldx, ldy;        // in bytes
+    int64_t elements;        // of the inner dimension: the words of dH; of dW the tokens
+    int64_t m, n;            // rows of D (dH: for all tokens) and its columns
+    const int* count;        // how many tokens there really are
+    const int* place;        // dH: which row of D a token's is
+    int tiles_n, splits;
     WorkOrder order;
     void* D;
     int64_t ldd;
@@ -253,27 +331,29 @@ struct ProductWork {
 
 __device__ __forceinline__ int split_begin(int steps, int splits, int s) { return (int)((int64_t)steps * s / splits); }
 
-template <typename P, typename T, bool XT, bool YT>
+template <typename P, typename T, bool DW>
 __device__ __forceinline__ void loss_product_body(const ProductWork& w) {
     __shared__ __attribute__((aligned(16))) uint8_t lds[P::LDS_BYTES];
-    const WorkItem item = work_item(blockIdx.x, gridDim.x, w.order, w.tiles_m, w.tiles_n);
-    const int64_t m0 = (int64_t)item.bm * P::TM, n0 = (int64_t)item.bn * P::TN, left_m = w.m - m0, left_n = w.n - n0;
-    const TileOperand X{w.X + n0 * (XT ? 2 : w.ldx), w.ldx, (int)(left_n < P::TN ? left_n : P::TN), nullptr, 0, w.elements};
-    const TileOperand Y{w.Y + m0 * (YT ? 2 : w.ldy), w.ldy, (int)(left_m < P::TM ? left_m : P::TM), nullptr, 0, w.elements};
+    const int64_t count = *w.count, m = DW ? w.m : count, elements = DW ? count : w.elements;
+    const int steps = (int)div_up(elements * 2, STEP_BYTES);
+    const unsigned tiles_m = (unsigned)div_up(m, P::TM), total = tiles_m * (unsigned)w.tiles_n * (unsigned)w.splits;
+    if (blockIdx.x >= total) return;
+    const WorkItem item = work_item(blockIdx.x, total, w.order, tiles_m, w.tiles_n);
+    const int64_t m0 = (int64_t)item.bm * P::TM, n0 = (int64_t)item.bn * P::TN, left_m = m - m0, left_n = w.n - n0;
+    const TileOperand X{w.X + n0 * 2, w.ldx, (int)(left_n < P::TN ? left_n : P::TN), nullptr, 0, elements};
+    const TileOperand Y{w.Y + m0 * (DW ? 2 : w.ldy), w.ldy, (int)(left_m < P::TM ? left_m : P::TM), nullptr, 0, elements};
     v4f32 acc[P::FN][P::FM] = {};
     const int split = item.gi;
-    P::multiply(lds, X, Y, w.bytes, split_begin(w.steps, w.splits, split), split_begin(w.steps, w.splits, split + 1), acc);
-    if (w.partial != nullptr) {
+    if (steps > 0) P::multiply(lds, X, Y, elements * 2, split_begin(steps, w.splits, split), split_begin(steps, w.splits, split + 1), acc);
+    if constexpr (DW) {
+        const float all = *w.factor;
+        store_tile<P, (P::THREADS > 256)>(lds, acc, static_cast<T*>(w.D) + m0 * w.ldd + n0, w.ldd, left_m, left_n, false, [&](int64_t) { return all; });
+    } else if (w.partial != nullptr) {
         store_tile<P, false>(lds, acc, w.partial + ((int64_t)split * w.m + m0) * in_fours(w.n) + n0, in_fours(w.n), left_m, in_fours(left_n), false,
                              [](int64_t) { return 1.0f; });
-        return;
-    }
-    T* const D = static_cast<T*>(w.D) + m0 * w.ldd + n0;
-    if constexpr (YT) {
-        const float all = *w.factor;
-        store_tile<P, (P::THREADS > 256)>(lds, acc, D, w.ldd, left_m, left_n, false, [&](int64_t) { return all; });
     } else {
-        store_tile<P, (P::THREADS > 256)>(lds, acc, D, w.ldd, left_m, left_n, false, [&](int64_t m) { return w.row_factor[m0 + m]; });
+        store_tile<P, (P::THREADS > 256)>(lds, acc, static_cast<T*>(w.D) + n0, w.ldd, left_m, left_n, false, [&](int64_t r) { return w.row_factor[m0 + r]; },
+                                          [&](int64_t r) { return (int64_t)w.place[m0 + r]; });
     }
 }
 
@@ -281,15 +361,15 @@ __device__ __forceinline__ void loss_product_body(const ProductWork& w) {
 // A workgroup a row.
 template <typename T>
 __device__ __forceinline__ void join_body(const float* partial, int splits, int64_t m, int64_t n, float* sum, bool first, bool last,
-                                          const float* row_factor, T* D, int64_t ldd) {
-    const int64_t ld = in_fours(n);
-    for (int64_t i = blockIdx.x; i < m; i += gridDim.x)
+                                          const int* count, const int* place, const float* row_factor, T* D, int64_t ldd) {
+    const int64_t ld = in_fours(n), rows = *count;
+    for (int64_t i = blockIdx.x; i < rows; i += gridDim.x)
         for (int64_t j = threadIdx.x * 4; j < n; j += 1024) {
             v4f32 s = {};
             if (!first) s = *reinterpret_cast<const v4f32*>(sum + i * ld + j);
 #pragma unroll 4
             for (int p = 0; p < splits; ++p) s += *reinterpret_cast<const v4f32*>(partial + ((int64_t)p * m + i) * ld + j);
-            if (last) put_four(D + i * ldd + j, s * row_factor[i], n - j, ldd % 4 == 0 && reinterpret_cast<uintptr_t>(D) % (4 * sizeof(T)) == 0, false);
+            if (last) put_four(D + place[i] * ldd + j, s * row_factor[i], n - j, ldd % 4 == 0 && reinterpret_cast<uintptr_t>(D) % (4 * sizeof(T)) == 0, false);
             else *reinterpret_cast<v4f32*>(sum + i * ld + j) = s;
         }
 }
@@ -325,35 +405,35 @@ __global__ void __launch_bounds__(256) loss_g_few_kernel(const LogitWork w) { lo
 // dH = g W, and dW = g^T H
 template <int TYPE>
 __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) loss_dh_large_kernel(const ProductWork w) {
-    loss_product_body<PairedTile<kind_of(TYPE), true, false>, typename Element<TYPE>::type, true, false>(w);
+    loss_product_body<PairedTile<kind_of(TYPE), true, false>, typename Element<TYPE>::type, false>(w);
 }
 template <int TYPE>
 __global__ void __launch_bounds__(256) loss_dh_middle_kernel(const ProductWork w) {
-    loss_product_body<Tile<kind_of(TYPE), 2, 2, 4, 2, 3, true, false>, typename Element<TYPE>::type, true, false>(w);
+    loss_product_body<Tile<kind_of(TYPE), 2, 2, 4, 2, 3, true, false>, typename Element<TYPE>::type, false>(w);
 }
 template <int TYPE>
 __global__ void __launch_bounds__(256) loss_dh_few_kernel(const ProductWork w) {
-    loss_product_body<Tile<kind_of(TYPE), 4, 1, 2, 1, 4, true, false>, typename Element<TYPE>::type, true, false>(w);
+    loss_product_body<Tile<kind_of(TYPE), 4, 1, 2, 1, 4, true, false>, typename Element<TYPE>::type, false>(w);
 }
 template <int TYPE>
 __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) loss_dw_large_kernel(const ProductWork w) {
-    loss_product_body<PairedTile<kind_of(TYPE), true, true>, typename Element<TYPE>::type, true, true>(w);
+    loss_product_body<PairedTile<kind_of(TYPE), true, true>, typename Element<TYPE>::type, true>(w);
 }
 template <int TYPE>
 __global__ void __launch_bounds__(256) loss_dw_middle_kernel(const ProductWork w) {
-    loss_product_body<Tile<kind_of(TYPE), 2, 2, 4, 4, 2, true, true>, typename Element<TYPE>::type, true, true>(w);
+    loss_product_body<Tile<kind_of(TYPE), 2, 2, 4, 4, 2, true, true>, typename Element<TYPE>::type, true>(w);
 }
 template <int TYPE>
 __global__ void __launch_bounds__(256) loss_product_join_kernel(const float* partial, int splits, int64_t m, int64_t n, float* sum, bool first, bool last,
-                                                                const float* row_factor, void* D, int64_t ldd) {
-    join_body(partial, splits, m, n, sum, first, last, row_factor, static_cast<typename Element<TYPE>::type*>(D), ldd);
+                                                                const int* count, const int* place, const float* row_factor, void* D, int64_t ldd) {
+    join_body(partial, splits, m, n, sum, first, last, count, place, row_factor, static_cast<typename Element<TYPE>::type*>(D), ldd);
 }
 
 template <int TYPE>
-__global__ void __launch_bounds__(1024) loss_tokens_kernel(const void* H, int64_t ldh, const int64_t* targets, const float* dloss, int64_t tokens, int64_t vocab,
-                                                           int64_t ignore, int* target_out, float* row_factor, float* dw_factor, void* to, int64_t ld, int* flags) {
+__global__ void __launch_bounds__(TOKEN_THREADS) loss_tokens_kernel(const GradTokens w, const void* H, int64_t ldh, void* Hc, void* Hs, int64_t ld, void* dH,
+                                                                    int64_t lddh) {
     typedef typename Element<TYPE>::type T;
-    tokens_body(static_cast<const T*>(H), ldh, targets, dloss, tokens, vocab, ignore, target_out, row_factor, dw_factor, static_cast<T*>(to), ld, flags);
+    tokens_body(w, static_cast<const T*>(H), ldh, static_cast<T*>(Hc), static_cast<T*>(Hs), ld, static_cast<T*>(dH), lddh);
 }
 
 // ---- shapes and work memory ------------------------------------------------------------------------------------
@@ -408,7 +488,11 @@ int64_t in_eights(int64_t n) { return div_up(n, 8) * 8; }
 struct GradPlaces {
     float* dw_factor;
     float* row_factor;
+    float* lse;
     int* target;
+    int* place;
+    int* count;
+    uint8_t* Hc;
     uint8_t* Hs;
     uint8_t* G;
     float* partial;
@@ -423,7 +507,11 @@ GradPlaces grad_places(uint8_t* ws, int64_t tokens, int64_t vocab, int64_t k, in
     const int splits = dh_shape(tokens, k, div_up(words * 2, STEP_BYTES)).splits;
     p.dw_factor = reinterpret_cast<float*>(take(4));
     p.row_factor = reinterpret_cast<float*>(take((size_t)tokens * 4));
+    p.count = reinterpret_cast<int*>(take(4));
+    p.lse = reinterpret_cast<float*>(take((size_t)tokens * 4));
     p.target = reinterpret_cast<int*>(take((size_t)tokens * 4));
+    p.place = reinterpret_cast<int*>(take((size_t)tokens * 4));
+    p.Hc = take((size_t)tokens * in_eights(k) * 2);
     p.Hs = take((size_t)tokens * in_eights(k) * 2);
     p.G = take((size_t)tokens * padded(words) * 2);
     const bool joined = splits > 1 || piece < vocab;
@@ -437,10 +525,9 @@ GradPlaces grad_places(uint8_t* ws, int64_t tokens, int64_t vocab, int64_t k, in
 
 template <int TYPE>
 hipError_t launch_dh(ProductWork w, int shape, hipStream_t st) {
-    w.tiles_m = (int)div_up(w.m, tile_m(shape));
     w.tiles_n = (int)div_up(w.n, tile_n(shape));
     w.order = order_for(shape);
-    const dim3 blocks((unsigned)((int64_t)w.tiles_m * w.tiles_n * w.splits));
+    const dim3 blocks((unsigned)(div_up(w.m, tile_m(shape)) * w.tiles_n * w.splits));
     if (shape == FEW) hipLaunchKernelGGL((loss_dh_few_kernel<TYPE>), blocks, dim3(256), 0, st, w);
     else if (shape == MIDDLE) hipLaunchKernelGGL((loss_dh_middle_kernel<TYPE>), blocks, dim3(256), 0, st, w);
     else hipLaunchKernelGGL((loss_dh_large_kernel<TYPE>), blocks, dim3(512), 0, st, w);
@@ -450,10 +537,9 @@ template <int TYPE>
 hipError_t launch_dw(ProductWork w, hipStream_t st) {
     const bool large = shape_for(w.m, w.n) == LARGE;
     const int edge = large ? 256 : 128;
-    w.tiles_m = (int)div_up(w.m, edge);
     w.tiles_n = (int)div_up(w.n, edge);
     w.order = order_for(large ? LARGE : MIDDLE);
-    const dim3 blocks((unsigned)((int64_t)w.tiles_m * w.tiles_n));
+    const dim3 blocks((unsigned)(div_up(w.m, edge) * w.tiles_n));
     if (large) hipLaunchKernelGGL((loss_dw_large_kernel<TYPE>), blocks, dim3(512), 0, st, w);
     else hipLaunchKernelGGL((loss_dw_middle_kernel<TYPE>), blocks, dim3(256), 0, st, w);
     return hipGetLastError();
@@ -512,23 +598,25 @@ hipError_t forward_typed(const LossArgs& a, uint8_t* ws, hipStream_t st) {
 template <int TYPE>
 hipError_t grad_typed(const LossArgs& a, int64_t piece, uint8_t* ws, hipStream_t st) {
     const GradPlaces p = grad_places(ws, a.tokens, a.vocab, a.k, piece);
-    const int64_t ldhs = in_eights(a.k), blocks_t = a.dW != nullptr ? div_up(a.tokens * (ldhs / 8), 1024) : 1;
-    hipLaunchKernelGGL((loss_tokens_kernel<TYPE>), dim3((unsigned)(blocks_t < 512 ? blocks_t : 512)), dim3(1024), 0, st, a.H, a.ldh, a.targets, a.dloss,
-                       a.tokens, a.vocab, a.ignore, p.target, p.row_factor, p.dw_factor, a.dW != nullptr ? p.Hs : nullptr, ldhs, a.flags);
+    const int64_t ldhs = in_eights(a.k), each = div_up(a.tokens, 512);
+    const GradTokens tokens{a.targets, a.lse_in, a.dloss, a.tokens, a.vocab, a.ignore, a.k, each, p.count, p.place, p.target, p.lse, p.row_factor, p.dw_factor, a.flags};
+    hipLaunchKernelGGL((loss_tokens_kernel<TYPE>), dim3((unsigned)div_up(a.tokens, each)), dim3(TOKEN_THREADS), 0, st, tokens, a.H, a.ldh, p.Hc,
+                       a.dW != nullptr ? p.Hs : nullptr, ldhs, a.dH, a.lddh);
     OZAKI_LOSS_TRY(hipGetLastError());
     const bool joined = piece < a.vocab;
     for (int64_t first = 0; first < a.vocab; first += piece) {
         const int64_t words = a.vocab - first < piece ? a.vocab - first : piece;
         const uint8_t* const W = static_cast<const uint8_t*>(a.W) + first * a.ldw * 2;
         LogitWork w = {};
-        w.H = static_cast<const uint8_t*>(a.H);
+        w.H = p.Hc;
         w.W = W;
-        w.ldh = a.ldh * 2;
+        w.ldh = ldhs * 2;
         w.ldw = a.ldw * 2;
         w.bytes = a.k * 2;
         w.tokens = a.tokens;
         w.first_word = first;
-        w.token = TokenState{a.lse_in, p.target};
+        w.count = p.count;
+        w.token = TokenState{p.lse, p.target};
         w.G = p.G;
         w.ldg = padded(words);
         const LogitPlan plan = logit_plan(a.tokens, words);
@@ -550,12 +638,12 @@ hipError_t grad_typed(const LossArgs& a, int64_t piece, uint8_t* ws, hipStream_t
             d.Y = p.G;
             d.ldx = a.ldw * 2;
             d.ldy = padded(words) * 2;
-            d.bytes = words * 2;                     // (behind them g has zeros to the end of the piece)
-            d.elements = words;
+            d.elements = words;                      // (behind them g has zeros to the end of the piece)
+            d.count = p.count;
+            d.place = p.place;
             d.m = a.tokens;
             d.n = a.k;
-            d.steps = (int)div_up(d.bytes, STEP_BYTES);
-            const ProductShape ps = dh_shape(d.m, d.n, d.steps);
+            const ProductShape ps = dh_shape(d.m, d.n, div_up(words * 2, STEP_BYTES));
             d.splits = ps.splits;
             d.D = a.dH;
             d.ldd = a.lddh;
@@ -564,7 +652,7 @@ hipError_t grad_typed(const LossArgs& a, int64_t piece, uint8_t* ws, hipStream_t
             OZAKI_LOSS_TRY(launch_dh<TYPE>(d, ps.shape, st));
             if (d.partial != nullptr) {
                 hipLaunchKernelGGL((loss_product_join_kernel<TYPE>), dim3((unsigned)(d.m < 65536 ? d.m : 65536)), dim3(256), 0, st, p.partial, d.splits,
-                                   d.m, d.n, p.sum, first == 0, first + piece >= a.vocab, d.row_factor, a.dH, a.lddh);
+                                   d.m, d.n, p.sum, first == 0, first + piece >= a.vocab, p.count, p.place, d.row_factor, a.dH, a.lddh);
                 OZAKI_LOSS_TRY(hipGetLastError());
             }
         }
@@ -574,11 +662,9 @@ hipError_t grad_typed(const LossArgs& a, int64_t piece, uint8_t* ws, hipStream_t
             d.Y = p.G;
             d.ldx = ldhs * 2;
             d.ldy = padded(words) * 2;
-            d.bytes = a.tokens * 2;
-            d.elements = a.tokens;
+            d.count = p.count;
             d.m = words;
             d.n = a.k;
-            d.steps = (int)div_up(d.bytes, STEP_BYTES);
             d.splits = 1;
             d.D = static_cast<uint8_t*>(a.dW) + first * a.lddw * 2;
             d.ldd = a.lddw;

@@ -631,9 +631,13 @@ struct PairedTile {
 // and `left_n` columns of it are there.  A lane has four neighbouring columns of sixteen rows; through LDS, 16 rows of every wave at a time
 // in 32 bits, D's rows are written in whole 16-byte pieces of neighbouring lanes.  Rows of D that are not aligned to that are written by element.
 // STREAMED: results of the large shapes, more than the L2 caches hold (FP8, 4096 x 4096 x 256 19.3 -> 17.0 us, 8192 x 8192 x 4096 252 -> 244).
-template <typename P, bool STREAMED, typename T, typename F>
+// place(row): which row of D it becomes.
+struct SameRow {
+    __device__ __forceinline__ int64_t operator()(int64_t m) const { return m; }
+};
+template <typename P, bool STREAMED, typename T, typename F, typename R = SameRow>
 __device__ __forceinline__ void store_tile(uint8_t* lds, const v4f32 (&acc)[P::FN][P::FM], T* D, int64_t ldd, int64_t left_m, int64_t left_n,
-                                           bool accumulate, F factor) {
+                                           bool accumulate, F factor, R place = R()) {
     constexpr int STRIDE = P::TN * 4 + 16, PER = 16 / sizeof(T), PIECES = P::TN / PER, ROWS = P::WM * 16;
     static_assert(ROWS * STRIDE <= P::LDS_BYTES && P::THREADS % PIECES == 0 && P::THREADS % P::TN == 0, "");
     typedef T piece __attribute__((ext_vector_type(PER)));
@@ -654,7 +658,7 @@ __device__ __forceinline__ void store_tile(uint8_t* lds, const v4f32 (&acc)[P::F
                 const int64_t m = ((r >> 4) * P::FM + j) * 16 + (r & 15);
                 if (m >= left_m) continue;
                 const float* const from = reinterpret_cast<const float*>(lds + r * STRIDE) + column;
-                piece* const to = reinterpret_cast<piece*>(D + m * ldd + column);
+                piece* const to = reinterpret_cast<piece*>(D + place(m) * ldd + column);
                 const float f = factor(m);
                 piece v = {};
                 if (accumulate) v = *to;
@@ -674,7 +678,7 @@ __device__ __forceinline__ void store_tile(uint8_t* lds, const v4f32 (&acc)[P::F
                     const int64_t m = ((r >> 4) * P::FM + j) * 16 + (r & 15);
                     if (m >= left_m) continue;
                     const float v = reinterpret_cast<const float*>(lds + r * STRIDE)[c] * factor(m);
-                    T* const to = D + m * ldd + c;
+                    T* const to = D + place(m) * ldd + c;
                     *to = (T)(accumulate ? (float)*to + v : v);
                 }
             }

@@ -106,6 +106,20 @@ def test_gradient(tokens, vocab, k, type, workspace):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("type", ["bf16", "f16"])
+@pytest.mark.parametrize("ignored", [0.6, 0.97])
+@pytest.mark.parametrize("tokens,vocab,k", [(9, 700, 100), (130, 2000, 201), (700, 9001, 400), (2100, 4500, 264)])
+def test_few_tokens_that_count(tokens, vocab, k, ignored, type, workspace):
+    x = Problem(tokens, vocab, k, type, 7, ignored=ignored)
+    x.H[x.T == x.ignore] = float("nan")
+    _, lse = x.forward()
+    lse = torch.where(x.T == x.ignore, 0.0, lse)
+    dh, dw = x.gradient(lse, ldh=k + 3)
+    x.check_gradient(dh, dw, lse)
+    assert bool(torch.all(dh[x.T == x.ignore][:, :k] == 0.0)) and bool(torch.isnan(dh[:, k:]).all())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("tokens,vocab,k", [(1030, 13201, 1100), (513, 22017, 136), (1900, 8705, 600)])
 def test_vocabularies_whose_last_tiles_are_few(tokens, vocab, k, workspace):
     test_loss(tokens, vocab, k, "bf16", workspace)
