@@ -13,6 +13,7 @@
 // and lose nothing to 16 bits; times dloss they all lose alike, which does not average out (1.7 times the error of the result's own
 // rounding in FP16).  2^12 keeps the words down to a probability of 2^-26 among FP16's normal numbers.  dloss comes in where it costs no
 // rounding: as a factor of the rows of dH, and for dW with a copy of H times dloss over the largest |dloss|, which is one for a mean.
+// Only the tokens that count take part (tokens_body).
 //
 // Few tokens are bound by the read of W (16 x 65536 x 2048: 52 us and 5 for the join, 5.1 TB/s; the gradient reads it twice, 166 us), many by the matrix
 // unit (4096 x 131072 x 4096: 3.07 ms, 1.43 PFLOP/s; gradient of 4096 x 65536 x 4096: 4.83 ms, 1.36 PFLOP/s).
@@ -311,6 +312,16 @@ __device__ __forceinline__ void loss_g_body(const LogitWork& w) {
     }
 }
 
+// In how many shares the inner dimension of dH is cut: as many as the workgroups launched for all tokens' tiles make of the tiles that there are
+// (`tiles` of `rows` rows, over all shares), but no more than `most`.
+struct ProductRoom {
+    int tiles, rows, most;
+    __device__ __forceinline__ int splits(int64_t count) const {
+        const int64_t there = div_up(count, rows), s = there > 0 ? tiles / there : 1;
+        return (int)(s < most ? s : most);
+    }
+};
+
 // D = X Y^T of 16-bit operands; rows of Y are D's rows
 struct ProductWork {
     const uint8_t* X;
@@ -320,13 +331,14 @@ struct ProductWork {
     int64_t m, n;            // rows of D (dH: for all tokens) and its columns
     const int* count;        // how many tokens there really are
     const int* place;        // dH: which row of D a token's is
-    int tiles_n, splits;
+    int tiles_n;
+    ProductRoom room;
     WorkOrder order;
     void* D;
     int64_t ldd;
     const float* row_factor; // what the sums are multiplied by, of dH: one for every row,
     const float* factor;     // of dW: the same for all
-    float* partial;          // not null: unscaled sums go there, [split][m][n in fours]
+    float* partial;          // not null: unscaled sums go there, [split][token that counts][n in fours]
 };
 
 __device__ __forceinline__ int split_begin(int steps, int splits, int s) { return (int)((int64_t)steps * s / splits); }
@@ -335,8 +347,8 @@ template <typename P, typename T, bool DW>
 __device__ __forceinline__ void loss_product_body(const ProductWork& w) {
     __shared__ __attribute__((aligned(16))) uint8_t lds[P::LDS_BYTES];
     const int64_t count = *w.count, m = DW ? w.m : count, elements = DW ? count : w.elements;
-    const int steps = (int)div_up(elements * 2, STEP_BYTES);
-    const unsigned tiles_m = (unsigned)div_up(m, P::TM), total = tiles_m * (unsigned)w.tiles_n * (unsigned)w.splits;
+    const int steps = (int)div_up(elements * 2, STEP_BYTES), splits = DW ? 1 : w.room.splits(count);
+    const unsigned tiles_m = (unsigned)div_up(m, P::TM), total = tiles_m * (unsigned)w.tiles_n * (unsigned)splits;
     if (blockIdx.x >= total) return;
     const WorkItem item = work_item(blockIdx.x, total, w.order, tiles_m, w.tiles_n);
     const int64_t m0 = (int64_t)item.bm * P::TM, n0 = (int64_t)item.bn * P::TN, left_m = m - m0, left_n = w.n - n0;
@@ -344,12 +356,12 @@ __device__ __forceinline__ void loss_product_body(const ProductWork& w) {
     const TileOperand Y{w.Y + m0 * (DW ? 2 : w.ldy), w.ldy, (int)(left_m < P::TM ? left_m : P::TM), nullptr, 0, elements};
     v4f32 acc[P::FN][P::FM] = {};
     const int split = item.gi;
-    if (steps > 0) P::multiply(lds, X, Y, elements * 2, split_begin(steps, w.splits, split), split_begin(steps, w.splits, split + 1), acc);
+    if (steps > 0) P::multiply(lds, X, Y, elements * 2, split_begin(steps, splits, split), split_begin(steps, splits, split + 1), acc);
     if constexpr (DW) {
         const float all = *w.factor;
         store_tile<P, (P::THREADS > 256)>(lds, acc, static_cast<T*>(w.D) + m0 * w.ldd + n0, w.ldd, left_m, left_n, false, [&](int64_t) { return all; });
     } else if (w.partial != nullptr) {
-        store_tile<P, false>(lds, acc, w.partial + ((int64_t)split * w.m + m0) * in_fours(w.n) + n0, in_fours(w.n), left_m, in_fours(left_n), false,
+        store_tile<P, false>(lds, acc, w.partial + ((int64_t)split * m + m0) * in_fours(w.n) + n0, in_fours(w.n), left_m, in_fours(left_n), false,
                              [](int64_t) { return 1.0f; });
     } else {
         store_tile<P, (P::THREADS > 256)>(lds, acc, static_cast<T*>(w.D) + n0, w.ldd, left_m, left_n, false, [&](int64_t r) { return w.row_factor[m0 + r]; },
@@ -360,15 +372,16 @@ __device__ __forceinline__ void loss_product_body(const ProductWork& w) {
 // The sums of a piece's shares of the inner dimension, on top of the pieces' before it (`sum`, unless it is the first); the last piece's go to D.
 // A workgroup a row.
 template <typename T>
-__device__ __forceinline__ void join_body(const float* partial, int splits, int64_t m, int64_t n, float* sum, bool first, bool last,
+__device__ __forceinline__ void join_body(const float* partial, const ProductRoom& room, int64_t n, float* sum, bool first, bool last,
                                           const int* count, const int* place, const float* row_factor, T* D, int64_t ldd) {
     const int64_t ld = in_fours(n), rows = *count;
+    const int splits = room.splits(rows);
     for (int64_t i = blockIdx.x; i < rows; i += gridDim.x)
         for (int64_t j = threadIdx.x * 4; j < n; j += 1024) {
             v4f32 s = {};
             if (!first) s = *reinterpret_cast<const v4f32*>(sum + i * ld + j);
 #pragma unroll 4
-            for (int p = 0; p < splits; ++p) s += *reinterpret_cast<const v4f32*>(partial + ((int64_t)p * m + i) * ld + j);
+            for (int p = 0; p < splits; ++p) s += *reinterpret_cast<const v4f32*>(partial + ((int64_t)p * rows + i) * ld + j);
             if (last) put_four(D + place[i] * ldd + j, s * row_factor[i], n - j, ldd % 4 == 0 && reinterpret_cast<uintptr_t>(D) % (4 * sizeof(T)) == 0, false);
             else *reinterpret_cast<v4f32*>(sum + i * ld + j) = s;
         }
@@ -424,9 +437,9 @@ __global__ void __launch_bounds__(256) loss_dw_middle_kernel(const ProductWork w
     loss_product_body<Tile<kind_of(TYPE), 2, 2, 4, 4, 2, true, true>, typename Element<TYPE>::type, true>(w);
 }
 template <int TYPE>
-__global__ void __launch_bounds__(256) loss_product_join_kernel(const float* partial, int splits, int64_t m, int64_t n, float* sum, bool first, bool last,
+__global__ void __launch_bounds__(256) loss_product_join_kernel(const float* partial, const ProductRoom room, int64_t n, float* sum, bool first, bool last,
                                                                 const int* count, const int* place, const float* row_factor, void* D, int64_t ldd) {
-    join_body(partial, splits, m, n, sum, first, last, count, place, row_factor, static_cast<typename Element<TYPE>::type*>(D), ldd);
+    join_body(partial, room, n, sum, first, last, count, place, row_factor, static_cast<typename Element<TYPE>::type*>(D), ldd);
 }
 
 template <int TYPE>
@@ -471,13 +484,18 @@ LogitPlan logit_plan(int64_t tokens, int64_t words) {
     return p;
 }
 int64_t logit_tiles(const LogitPlan& p) { return div_up(p.words[0], tile_words(p.shape[0])) + div_up(p.words[1], tile_words(p.shape[1])); }
-struct ProductShape { int shape, splits; };
+struct ProductShape {
+    int shape, splits, most;
+    ProductRoom room(int64_t m, bool joined) const {
+        const int tiles = (int)div_up(m, tile_m(shape));
+        return joined || splits > 1 ? ProductRoom{tiles * splits, tile_m(shape), most} : ProductRoom{tiles, tile_m(shape), 1};
+    }
+};
 ProductShape dh_shape(int64_t m, int64_t n, int64_t steps) {
     int shape = shape_for(m, n);
     if (shape == MIDDLE && m > 128 && div_up(m, 256) * div_up(n, 256) * (steps / 16) >= 128) shape = LARGE;
-    const int64_t tiles = div_up(m, tile_m(shape)) * div_up(n, tile_n(shape)), want = (shape == LARGE ? 256 : 512) / tiles, most = steps / 8;
-    const int64_t s = want < most ? want : most;
-    return ProductShape{shape, (int)(s < 1 ? 1 : s > 32 ? 32 : s)};
+    const int64_t tiles = div_up(m, tile_m(shape)) * div_up(n, tile_n(shape)), want = (shape == LARGE ? 256 : 512) / tiles, least = steps / 8, most = least < 1 ? 1 : least > 32 ? 32 : least;
+    return ProductShape{shape, (int)(want < 1 ? 1 : want < most ? want : most), (int)most};
 }
 
 size_t up(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
@@ -504,7 +522,7 @@ GradPlaces grad_places(uint8_t* ws, int64_t tokens, int64_t vocab, int64_t k, in
     size_t at = 256;                     // the flag words
     auto take = [&](size_t bytes) { uint8_t* const here = ws + at; at += up(bytes); return here; };
     const int64_t words = piece < vocab ? piece : vocab;
-    const int splits = dh_shape(tokens, k, div_up(words * 2, STEP_BYTES)).splits;
+    const ProductShape dh = dh_shape(tokens, k, div_up(words * 2, STEP_BYTES));
     p.dw_factor = reinterpret_cast<float*>(take(4));
     p.row_factor = reinterpret_cast<float*>(take((size_t)tokens * 4));
     p.count = reinterpret_cast<int*>(take(4));
@@ -514,8 +532,8 @@ GradPlaces grad_places(uint8_t* ws, int64_t tokens, int64_t vocab, int64_t k, in
     p.Hc = take((size_t)tokens * in_eights(k) * 2);
     p.Hs = take((size_t)tokens * in_eights(k) * 2);
     p.G = take((size_t)tokens * padded(words) * 2);
-    const bool joined = splits > 1 || piece < vocab;
-    p.partial = reinterpret_cast<float*>(take(joined ? (size_t)splits * tokens * in_fours(k) * 4 : 0));
+    const bool joined = dh.splits > 1 || piece < vocab;
+    p.partial = reinterpret_cast<float*>(take(joined ? (size_t)dh.splits * div_up(tokens, tile_m(dh.shape)) * tile_m(dh.shape) * in_fours(k) * 4 : 0));
     p.sum = reinterpret_cast<float*>(take(piece < vocab ? (size_t)tokens * in_fours(k) * 4 : 0));
     p.total = at;
     return p;
@@ -527,7 +545,7 @@ template <int TYPE>
 hipError_t launch_dh(ProductWork w, int shape, hipStream_t st) {
     w.tiles_n = (int)div_up(w.n, tile_n(shape));
     w.order = order_for(shape);
-    const dim3 blocks((unsigned)(div_up(w.m, tile_m(shape)) * w.tiles_n * w.splits));
+    const dim3 blocks((unsigned)((int64_t)w.room.tiles * w.tiles_n));
     if (shape == FEW) hipLaunchKernelGGL((loss_dh_few_kernel<TYPE>), blocks, dim3(256), 0, st, w);
     else if (shape == MIDDLE) hipLaunchKernelGGL((loss_dh_middle_kernel<TYPE>), blocks, dim3(256), 0, st, w);
     else hipLaunchKernelGGL((loss_dh_large_kernel<TYPE>), blocks, dim3(512), 0, st, w);
@@ -644,15 +662,14 @@ hipError_t grad_typed(const LossArgs& a, int64_t piece, uint8_t* ws, hipStream_t
             d.m = a.tokens;
             d.n = a.k;
             const ProductShape ps = dh_shape(d.m, d.n, div_up(words * 2, STEP_BYTES));
-            d.splits = ps.splits;
+            d.room = ps.room(d.m, joined);
             d.D = a.dH;
             d.ldd = a.lddh;
             d.row_factor = p.row_factor;
-            d.partial = joined || d.splits > 1 ? p.partial : nullptr;
+            d.partial = joined || ps.splits > 1 ? p.partial : nullptr;
             OZAKI_LOSS_TRY(launch_dh<TYPE>(d, ps.shape, st));
             if (d.partial != nullptr) {
-                hipLaunchKernelGGL((loss_product_join_kernel<TYPE>), dim3((unsigned)(d.m < 65536 ? d.m : 65536)), dim3(256), 0, st, p.partial, d.splits,
-                                   d.m, d.n, p.sum, first == 0, first + piece >= a.vocab, p.count, p.place, d.row_factor, a.dH, a.lddh);
+                hipLaunchKernelGGL((loss_product_join_kernel<TYPE>), dim3((unsigned)(d.m < 65536 ? d.m : 65536)), dim3(256), 0, st, p.partial, d.room, d.n, p.sum, first == 0, first + piece >= a.vocab, p.count, p.place, d.row_factor, a.dH, a.lddh);
                 OZAKI_LOSS_TRY(hipGetLastError());
             }
         }
@@ -665,7 +682,6 @@ hipError_t grad_typed(const LossArgs& a, int64_t piece, uint8_t* ws, hipStream_t
             d.count = p.count;
             d.m = words;
             d.n = a.k;
-            d.splits = 1;
             d.D = static_cast<uint8_t*>(a.dW) + first * a.lddw * 2;
             d.ldd = a.lddw;
             d.factor = p.dw_factor;

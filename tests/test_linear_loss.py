@@ -106,6 +106,16 @@ def test_gradient(tokens, vocab, k, type, workspace):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("tokens,vocab,k", [(77, 2701, 201), (600, 3001, 333)])
+def test_few_tokens_that_count_in_pieces(tokens, vocab, k):
+    x = Problem(tokens, vocab, k, "bf16", 8, ignored=0.9)
+    least = device.Workspace(lib.ozaki_linear_loss_workspace_bytes(tokens, vocab, k, True, True))
+    _, lse = x.forward()
+    x.check_gradient(*x.gradient(lse), lse)
+    least.close()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("type", ["bf16", "f16"])
 @pytest.mark.parametrize("ignored", [0.6, 0.97])
 @pytest.mark.parametrize("tokens,vocab,k", [(9, 700, 100), (130, 2000, 201), (700, 9001, 400), (2100, 4500, 264)])
