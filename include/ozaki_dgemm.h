@@ -244,7 +244,9 @@ size_t ozaki_workspace_bytes_ex(int64_t m, int64_t n, int64_t k, int slice_forma
 int ozaki_set_workspace(void* dev_ptr, size_t bytes);
 
 /* Waits for the stream, then returns OZAKI_STATUS_NONFINITE if a kernel since the last call of this
- * function met an Inf/NaN input, OZAKI_STATUS_HIP_ERROR on a HIP failure, else 0. */
+ * function met an Inf/NaN input, OZAKI_STATUS_TARGET if one met a target outside the vocabulary (the low-precision
+ * operators below), OZAKI_STATUS_HIP_ERROR on a HIP failure, else 0.  A call reports one cause and clears that one: where both
+ * were met, the next call returns OZAKI_STATUS_TARGET. */
 int ozaki_last_device_status(void);
 /* Numeric hipError_t of the most recent failed HIP call of the current context (0 if none). */
 int ozaki_last_hip_error(void);

@@ -335,10 +335,14 @@ int ozaki_last_device_status(void) {
     for (int i = 0; i < 2; ++i)
         if (places[i]) HIP_TRY(hipMemcpyAsync(&flags[i], places[i], sizeof(int), hipMemcpyDeviceToHost, c.stream));
     HIP_TRY(hipStreamSynchronize(c.stream));
-    for (int i = 0; i < 2; ++i)
-        if (flags[i]) HIP_TRY(hipMemsetAsync(places[i], 0, FLAG_BYTES, c.stream));
-    const int found = flags[0] | flags[1];
-    return (found & 1) ? OZAKI_STATUS_NONFINITE : (found & TARGET_FLAG) ? OZAKI_STATUS_TARGET : 0;
+    const int found = flags[0] | flags[1], reported = (found & NONFINITE_FLAG) ? NONFINITE_FLAG : found & TARGET_FLAG;
+    for (int i = 0; i < 2; ++i) {
+        if (flags[i] == 0) continue;
+        HIP_TRY(hipMemsetAsync(places[i], 0, FLAG_BYTES, c.stream));
+        const int left = flags[i] & TARGET_FLAG & ~reported;           // the next call's
+        if (left != 0) HIP_TRY(hipMemsetD32Async(places[i], left, 1, c.stream));
+    }
+    return reported == NONFINITE_FLAG ? OZAKI_STATUS_NONFINITE : reported == TARGET_FLAG ? OZAKI_STATUS_TARGET : 0;
 }
 
 int ozaki_last_hip_error(void) { return ctx().last_hip_error; }

@@ -71,7 +71,8 @@ hipError_t launch_linear_loss(const LossArgs& a, int type, uint8_t* ws, hipStrea
 hipError_t launch_zero_rows(void* D, int64_t rows, int64_t k, int64_t ldd, hipStream_t st);       // of 16-bit elements
 hipError_t launch_linear_loss_grad(const LossArgs& a, int type, int64_t piece, uint8_t* ws, hipStream_t st);
 
-constexpr int TARGET_FLAG = 2;            // bit of flag word 0: a target was neither a word of the vocabulary nor `ignore`
+// bits of flag word 0: an FP64 product's input was not finite; a target was neither a word of the vocabulary nor `ignore`
+constexpr int NONFINITE_FLAG = 1, TARGET_FLAG = 2;
 
 #if defined(__HIPCC__)
 

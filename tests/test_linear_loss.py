@@ -351,3 +351,23 @@ def test_without_work_memory():
     finally:
         lib.ozaki_context_use(None)
         lib.ozaki_context_destroy(context)
+
+
+@pytest.mark.gpu
+def test_every_cause_is_reported_once(workspace):
+    """A target outside the vocabulary and an FP64 product's infinity between two looks at the status: one after the other."""
+    x = Problem(50, 300, 64, "bf16", 5, ignored=0.0)
+    x.targets[7] = 300
+    x.upload()
+    A = torch.ones((64, 64), dtype=torch.float64, device="cuda")
+    A[3, 5] = float("inf")
+    C = torch.empty_like(A)
+    product = lambda: lib.ozaki_dgemm(64, 64, 64, A, 64, A, 64, C, 64, lib.SLICE_FP8_E4M3, 4, 0, lib.ACCUM_FP64_HW)  # noqa: E731
+    for calls in ((x.forward, product), (product, x.forward)):
+        for call in calls:
+            call()
+        assert [lib.ozaki_last_device_status() for _ in range(3)] == [lib.STATUS_NONFINITE, lib.STATUS_TARGET, lib.STATUS_OK]
+    x.forward()
+    assert [lib.ozaki_last_device_status() for _ in range(2)] == [lib.STATUS_TARGET, lib.STATUS_OK]
+    product()
+    assert [lib.ozaki_last_device_status() for _ in range(2)] == [lib.STATUS_NONFINITE, lib.STATUS_OK]
