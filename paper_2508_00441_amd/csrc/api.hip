@@ -630,7 +630,14 @@ int ozaki_gemm_fp8(int64_t m, int64_t n, int64_t k, const void* A, int64_t lda, 
 size_t ozaki_linear_loss_workspace_bytes(int64_t tokens, int64_t vocab, int64_t k, int grad, int minimum) {
     if (tokens < 1 || !extent_ok(tokens) || vocab < 1 || !extent_ok(vocab) || tokens * vocab > OZAKI_MAX_LOGITS || k < 1 || k > OZAKI_MAX_EXTENT / 2) return 0;
     if (!grad) return loss_bytes(tokens, vocab);
-    return loss_grad_bytes(tokens, vocab, k, minimum ? LOSS_PIECE : loss_grad_piece(tokens, vocab, k));
+    const int64_t recommended = loss_grad_piece(tokens, vocab, k);
+    size_t bytes = loss_grad_bytes(tokens, vocab, k, recommended);
+    // (shares and sums of dH come with pieces: shorter ones are not always less)
+    for (int64_t piece = recommended - LOSS_PIECE; minimum && piece >= LOSS_PIECE; piece -= LOSS_PIECE) {
+        const size_t need = loss_grad_bytes(tokens, vocab, k, piece);
+        if (need < bytes) bytes = need;
+    }
+    return bytes;
 }
 
 int ozaki_linear_loss(int64_t tokens, int64_t vocab, int64_t k, const void* H, int64_t ldh, const void* W, int64_t ldw, int type,

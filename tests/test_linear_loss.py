@@ -371,3 +371,29 @@ def test_every_cause_is_reported_once(workspace):
     assert [lib.ozaki_last_device_status() for _ in range(2)] == [lib.STATUS_TARGET, lib.STATUS_OK]
     product()
     assert [lib.ozaki_last_device_status() for _ in range(2)] == [lib.STATUS_NONFINITE, lib.STATUS_OK]
+
+
+@pytest.mark.parametrize("k", [1, 64, 300, 1000, 4096, 8192])
+def test_the_least_work_memory_is_no_more_than_the_recommended(k):
+    for tokens in (1, 17, 150, 1000, 4096, 8192, 70000):
+        for vocab in (1, 255, 300, 1001, 2900, 8192, 32000, 131072):
+            least, best = (lib.ozaki_linear_loss_workspace_bytes(tokens, vocab, k, True, m) for m in (True, False))
+            assert 0 < least <= best, (tokens, vocab)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens,vocab,k", [(40, 300, 1024), (300, 1200, 520), (70, 2600, 1000)])
+def test_gradient_with_the_least_work_memory(tokens, vocab, k):
+    x = Problem(tokens, vocab, k, "bf16", 21)
+    need = lib.ozaki_linear_loss_workspace_bytes(tokens, vocab, k, True, True)
+    forward = device.Workspace(lib.ozaki_linear_loss_workspace_bytes(tokens, vocab, k, False, False))
+    _, lse = x.forward()
+    forward.close()
+    least = device.Workspace(need)
+    dh, dw = x.gradient(lse)
+    x.check_gradient(dh, dw, lse)
+    least.close()
+    short = torch.empty(need - 256, dtype=torch.uint8, device="cuda")
+    lib.ozaki_set_workspace(short, short.numel())
+    assert lib.ozaki_linear_loss_grad(*x.arguments(), lse, x.dloss.cuda(), dh, k, dw, k, check=False) == lib.STATUS_WORKSPACE
+    lib.ozaki_set_workspace(None, 0)
