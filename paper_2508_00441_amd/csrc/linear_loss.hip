@@ -26,6 +26,9 @@ namespace {
 constexpr float LOG2_E = 1.44269504088896340736f, LN_2 = 0.69314718055994530942f;
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * LOG2_E); }
 __device__ __forceinline__ float log_of(float x) { return __builtin_amdgcn_logf(x) * LN_2; }
+// What exponentials are taken relative to: the largest number.  Where that is infinite, zero: nothing but minus infinity gives a sum of zero,
+// and plus infinity, less itself, would give NaN instead of an infinite sum.
+__device__ __forceinline__ float base_of(float most) { return fabsf(most) == __builtin_inff() ? 0.0f : most; }
 
 // per token, what a tile of z needs
 struct TokenState {
@@ -93,7 +96,7 @@ __device__ __forceinline__ void loss_forward_body(const LogitWork& w) {
             }
         most = fmaxf(most, __shfl_xor(most, 16));
         most = fmaxf(most, __shfl_xor(most, 32));
-        const float base = most == -__builtin_inff() ? 0.0f : most;   // nothing but minus infinity: a sum of zero
+        const float base = base_of(most);
         float sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < P::FN; ++i)
@@ -109,7 +112,7 @@ __device__ __forceinline__ void loss_forward_body(const LogitWork& w) {
         float most = -__builtin_inff(), sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < P::WN; ++i) most = fmaxf(most, joined[i * P::TM + t].x);
-        const float base = most == -__builtin_inff() ? 0.0f : most;
+        const float base = base_of(most);
 #pragma unroll
         for (int i = 0; i < P::WN; ++i) sum += joined[i * P::TM + t].y * exp_of(joined[i * P::TM + t].x - base);
         w.part[(n0 / P::TN) * w.tokens + m0 + t] = make_float2(most, sum);
@@ -126,7 +129,7 @@ __global__ void __launch_bounds__(256) loss_join_kernel(const float2* part, cons
     const int64_t t = (int64_t)blockIdx.x * TOKENS + tl, at = t < tokens ? t : tokens - 1;
     float most = -__builtin_inff(), sum = 0.0f;
     const auto add = [&](float m, float v) {
-        const float higher = fmaxf(most, m), base = higher == -__builtin_inff() ? 0.0f : higher;
+        const float higher = fmaxf(most, m), base = base_of(higher);
         sum = sum * exp_of(most - base) + v * exp_of(m - base);
         most = higher;
     };
@@ -148,7 +151,7 @@ __global__ void __launch_bounds__(256) loss_join_kernel(const float2* part, cons
     if (threadIdx.x >= TOKENS || t >= tokens) return;
 #pragma unroll
     for (int w = 1; w < 4; ++w) add(share[w][tl].x, share[w][tl].y);
-    const float l = (most == -__builtin_inff() ? 0.0f : most) + log_of(sum);
+    const float l = base_of(most) + log_of(sum);
     const int64_t target = targets[t];
     const bool counts = target != ignore, real = target >= 0 && target < vocab;
     lse[t] = l;

@@ -397,3 +397,31 @@ def test_gradient_with_the_least_work_memory(tokens, vocab, k):
     lib.ozaki_set_workspace(short, short.numel())
     assert lib.ozaki_linear_loss_grad(*x.arguments(), lse, x.dloss.cuda(), dh, k, dw, k, check=False) == lib.STATUS_WORKSPACE
     lib.ozaki_set_workspace(None, 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("type", ["bf16", "f16"])
+@pytest.mark.parametrize("tokens,vocab", [(5, 900), (70, 900), (400, 9000), (2900, 4000)])
+def test_outputs_at_plus_infinity(tokens, vocab, type, workspace):
+    """The logarithm of a sum that holds an infinite term is infinite, and so is the loss of any other word; of the word itself it is NaN."""
+    x = Problem(tokens, vocab, 64, type, 22, ignored=0.1)
+    x.h[:, 0] = torch.where(torch.arange(tokens) % 3 == 0, 1.0, -1.0)
+    x.w[:, 0] = 0.0
+    x.w[vocab // 2, 0] = float("inf")
+    x.w[vocab // 3] = 0.0
+    x.w[vocab // 3, 1] = 50.0                                       # large outputs beside it, in other tiles
+    x.targets[x.targets == vocab // 2] = 1
+    x.targets[0] = vocab // 2
+    x.upload()
+    loss, lse = x.forward()
+    want, want_lse, _ = plain.loss_forward(x.h, x.w, x.targets, x.ignore)
+    up = x.h[:, 0] > 0
+    finite = x.w.clone()
+    finite[vocab // 2, 0] = 0.0
+    bound = plain.logit_error(x.h, finite) + EXP * (1 + want_lse.abs())
+    assert bool(torch.all(lse.cpu()[up] == float("inf")))
+    assert bool(torch.all((lse.cpu().double() - want_lse).abs()[~up] <= bound[~up]))
+    counts = x.targets != x.ignore
+    counts[0] = False
+    assert bool(torch.isnan(loss[0])) and bool(torch.all(loss.cpu()[up & counts] == float("inf"))) and bool(torch.all(loss.cpu()[x.targets == x.ignore] == 0.0))
+    assert bool(torch.all((loss.cpu().double() - want).abs()[~up & counts] <= (2 * bound + 2.0 ** -23 * want.abs())[~up & counts]))
