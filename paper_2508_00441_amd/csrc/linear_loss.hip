@@ -13,6 +13,10 @@
 // and lose nothing to 16 bits; times dloss they all lose alike, which does not average out (1.7 times the error of the result's own
 // rounding in FP16).  2^12 keeps the words down to a probability of 2^-26 among FP16's normal numbers.  dloss comes in where it costs no
 // rounding: as a factor of the rows of dH, and for dW with a copy of H times dloss over the largest |dloss|, which is one for a mean.
+// Where the shares differ, that copy is rounded to 16 bits once more (on normally distributed numbers the error of dW's rows of tokens of small
+// shares grows from the result's own rounding to 1.4 times that).  In FP16, whose smallest normal number is 2^-14, H times a share below 2^-10 would
+// run out of bits; there g takes up to 2^8 of the share, a power of two that costs it nothing but the words below a probability of 2^-18 of
+// that token, whose error stays below 2^-29 (share_exponent).  So shares down to 2^-19 are as good as others.
 // Only the tokens that count take part (tokens_body).
 //
 // Few tokens are bound by the read of W (16 x 65536 x 2048: 52 us and 5 for the join, 5.1 TB/s; the gradient reads it twice, 166 us), many by the matrix
@@ -34,8 +38,16 @@ __device__ __forceinline__ float base_of(float most) { return fabsf(most) == __b
 struct TokenState {
     const float* lse;
     const int* target;
+    const float* held;       // what its g is held times
 };
-constexpr float HELD = 4096.0f;          // what g is held times
+// What g is held times, HELD / 2^a, where H is held times dloss / (the largest) * 2^a.
+constexpr float HELD = 4096.0f;
+template <typename T>
+__device__ __forceinline__ int share_exponent(float share) {
+    if constexpr (!std::is_same_v<T, _Float16>) return 0;
+    const int a = 117 - ((__float_as_int(share) >> 23) & 0xFF);       // how far below 2^-10
+    return a < 0 ? 0 : a < 8 ? a : 8;
+}
 
 struct LogitWork {
     const uint8_t* H;
@@ -176,6 +188,7 @@ struct GradTokens {
     int* target_out;
     float* lse_out;
     float* row_factor;
+    float* held_out;
     float* dw_factor;        // one number
     int* flags;
 };
@@ -245,7 +258,10 @@ __device__ __forceinline__ void tokens_body(const GradTokens& w, const T* H, int
             w.place[at] = (int)t;
             w.target_out[at] = (int)w.targets[t];
             w.lse_out[at] = w.lse[t];
-            w.row_factor[at] = w.dloss[t] * (1.0f / HELD);
+            const float d = w.dloss[t];
+            const int a = share_exponent<T>(d / most);
+            w.row_factor[at] = ldexpf(d, a) * (1.0f / HELD);
+            w.held_out[at] = ldexpf(HELD, -a);
         } else if (t < end && w.targets[t] != w.ignore) {
             atomicOr(w.flags, TARGET_FLAG);
         }
@@ -258,7 +274,7 @@ __device__ __forceinline__ void tokens_body(const GradTokens& w, const T* H, int
                 eight x = *reinterpret_cast<const eight*>(H + (from + i) * ldh + e);
                 *reinterpret_cast<eight*>(Hc + to * ld + e) = x;
                 if (Hs == nullptr) continue;
-                const float f = w.dloss[from + i] / most;
+                const float share = w.dloss[from + i] / most, f = ldexpf(share, share_exponent<T>(share));
 #pragma unroll
                 for (int q = 0; q < 8; ++q) x[q] = (T)((float)x[q] * f);
                 *reinterpret_cast<eight*>(Hs + to * ld + e) = x;
@@ -293,7 +309,7 @@ __device__ __forceinline__ void loss_g_body(const LogitWork& w) {
     for (int j = 0; j < P::FM; ++j) {
         const int t = (wm * P::FM + j) * 16 + (lane & 15);
         const bool real = m0 + t < tokens;
-        const float lse = real ? w.token.lse[m0 + t] : 0.0f;
+        const float lse = real ? w.token.lse[m0 + t] : 0.0f, held = real ? w.token.held[m0 + t] : 0.0f;
         const int at = real ? (int)(w.token.target[m0 + t] - w.first_word - n0) : -1;
 #pragma unroll
         for (int i = 0; i < P::FN; ++i) {
@@ -302,7 +318,7 @@ __device__ __forceinline__ void loss_g_body(const LogitWork& w) {
             for (int r = 0; r < 4; ++r) {
                 const int word = first + 16 * i + r;
                 const float p = exp_of(acc[i][j][r] - lse) - (word == at ? 1.0f : 0.0f);
-                v[r] = (T)(word < words ? p * HELD : 0.0f);
+                v[r] = (T)(word < words ? p * held : 0.0f);
             }
             *reinterpret_cast<four*>(lds + t * STRIDE + (first + 16 * i) * 2) = v;
         }
@@ -510,6 +526,7 @@ struct GradPlaces {
     float* dw_factor;
     float* row_factor;
     float* lse;
+    float* held;
     int* target;
     int* place;
     int* count;
@@ -530,6 +547,7 @@ GradPlaces grad_places(uint8_t* ws, int64_t tokens, int64_t vocab, int64_t k, in
     p.row_factor = reinterpret_cast<float*>(take((size_t)tokens * 4));
     p.count = reinterpret_cast<int*>(take(4));
     p.lse = reinterpret_cast<float*>(take((size_t)tokens * 4));
+    p.held = reinterpret_cast<float*>(take((size_t)tokens * 4));
     p.target = reinterpret_cast<int*>(take((size_t)tokens * 4));
     p.place = reinterpret_cast<int*>(take((size_t)tokens * 4));
     p.Hc = take((size_t)tokens * in_eights(k) * 2);
@@ -620,7 +638,7 @@ template <int TYPE>
 hipError_t grad_typed(const LossArgs& a, int64_t piece, uint8_t* ws, hipStream_t st) {
     const GradPlaces p = grad_places(ws, a.tokens, a.vocab, a.k, piece);
     const int64_t ldhs = in_eights(a.k), each = div_up(a.tokens, 512);
-    const GradTokens tokens{a.targets, a.lse_in, a.dloss, a.tokens, a.vocab, a.ignore, a.k, each, p.count, p.place, p.target, p.lse, p.row_factor, p.dw_factor, a.flags};
+    const GradTokens tokens{a.targets, a.lse_in, a.dloss, a.tokens, a.vocab, a.ignore, a.k, each, p.count, p.place, p.target, p.lse, p.row_factor, p.held, p.dw_factor, a.flags};
     hipLaunchKernelGGL((loss_tokens_kernel<TYPE>), dim3((unsigned)div_up(a.tokens, each)), dim3(TOKEN_THREADS), 0, st, tokens, a.H, a.ldh, p.Hc,
                        a.dW != nullptr ? p.Hs : nullptr, ldhs, a.dH, a.lddh);
     OZAKI_LOSS_TRY(hipGetLastError());
@@ -637,7 +655,7 @@ hipError_t grad_typed(const LossArgs& a, int64_t piece, uint8_t* ws, hipStream_t
         w.tokens = a.tokens;
         w.first_word = first;
         w.count = p.count;
-        w.token = TokenState{p.lse, p.target};
+        w.token = TokenState{p.lse, p.target, p.held};
         w.G = p.G;
         w.ldg = padded(words);
         const LogitPlan plan = logit_plan(a.tokens, words);

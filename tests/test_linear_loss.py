@@ -425,3 +425,33 @@ def test_outputs_at_plus_infinity(tokens, vocab, type, workspace):
     counts[0] = False
     assert bool(torch.isnan(loss[0])) and bool(torch.all(loss.cpu()[up & counts] == float("inf"))) and bool(torch.all(loss.cpu()[x.targets == x.ignore] == 0.0))
     assert bool(torch.all((loss.cpu().double() - want).abs()[~up & counts] <= (2 * bound + 2.0 ** -23 * want.abs())[~up & counts]))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("weight", [2.0 ** -10 * 1.37, 2.0 ** -14 * 1.9, 1e-5, 2.0 ** -19 * 1.01])
+@pytest.mark.parametrize("tokens,vocab,k", [(14, 60, 96), (200, 600, 96), (1030, 9001, 1000)])
+def test_tokens_of_little_weight_in_16_bit_floats(tokens, vocab, k, weight, workspace):
+    """Half of the tokens count a small share of the others, and have words of their own: what the gradient of these words is made of is the
+    small shares alone.  Down to 2^-19 of the largest weight the elements of H may be off by a rounding to 11 bits or, where they are small,
+    by 2^-14."""
+    x = Problem(tokens, vocab, k, "f16", 23, ignored=0.1)
+    light, own = torch.arange(tokens) % 2 == 1, torch.arange(vocab) >= vocab // 2
+    x.h[:, 0] = torch.where(light, 6.0, -6.0)
+    x.w[:, 0] = torch.where(own, 6.0, -6.0)                         # outputs of the others' words: lower by 72
+    x.targets[light & (x.targets != x.ignore)] = vocab - 1 - torch.arange(int((light & (x.targets != x.ignore)).sum())) % (vocab - vocab // 2)
+    x.targets[~light & (x.targets != x.ignore)] %= vocab // 2
+    x.dloss = torch.where(light, 64.0 * weight, 64.0)
+    x.upload()
+    _, lse = x.forward()
+    dh, dw = x.gradient(lse)
+    want_h, want_w, g, p, h = plain.loss_gradient(x.h, x.w, x.targets, x.ignore, lse.cpu(), x.dloss)
+    u, tiny = plain.ROUNDING["f16"]
+    factor = torch.where(x.targets == x.ignore, 0.0, x.dloss.double()).unsqueeze(1)
+    # g: its rounding, z's and the exponential's errors, and half of FP16's smallest step: g is held times 2^12, for small weights times 2^4 at least
+    dg = u * g.abs() + p * ((plain.logit_error(x.h, x.w) + EXP).unsqueeze(1) * (1 + u)) + 2.0 ** -22 * g.abs() + 2.0 ** -29 * factor
+    out = dg @ x.w.double().abs()
+    out = out + 2 * (vocab + 40) * 2.0 ** -24 * ((g.abs() + dg) @ x.w.double().abs())
+    assert bool(torch.all((dh.cpu().double() - want_h).abs() <= out + u * (want_h.abs() + out) + tiny))
+    out = dg.t() @ (h.abs() * (1 + u) + 2.0 ** -14) + g.abs().t() @ (u * h.abs() + 2.0 ** -14)
+    out = out + 2 * (tokens + 4) * 2.0 ** -24 * ((g.abs() + dg).t() @ (h.abs() + 2.0 ** -14))
+    assert bool(torch.all((dw.cpu().double() - want_w).abs() <= out + u * (want_w.abs() + out) + tiny))
