@@ -255,3 +255,123 @@ def test_without_work_memory():
 def test_nothing_to_do():
     for m, n in ((0, 100), (100, 0)):
         assert lib.ozaki_gemm_fp8(m, n, 128, None, 0, None, 0, None, 0, None, 0, lib.SCALE_BLOCKS, None, 0, lib.TYPE_BF16) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("blocks", [True, False])
+@pytest.mark.parametrize("m,n,k,type_d", [(300, 500, 4096, t) for t in ("bf16", "f32", "f16")] + [(1, 64, 65536, t) for t in ("bf16", "f32", "f16")] +
+                         [(5, 131, 20000, "bf16"), (3600, 3600, 128, "bf16"), (3600, 3700, 656, "f16"), (4353, 3841, 264, "bf16"), (3841, 4353, 401, "f16")])
+def test_cut_and_large_products_on_top_of_what_is_there(m, n, k, type_d, blocks, workspace):
+    """An inner dimension in shares, tiles of 256 x 256, and those whose last ones are left to smaller tiles: inside larger results, aligned and not."""
+    assert (lib.ozaki_gemm_fp8_workspace_bytes(m, n, k) > 0) == (m <= 300)
+    o = Operands(m, n, k, blocks, 15)
+    for offset, ldd in ((0, plain.ceil(n, 8) + 8), (1, n + 3)):
+        whole = torch.randn((m * ldd + 8,), device="cuda").to(plain.DTYPES[type_d])
+        kept = whole.clone()
+        view = lambda x: x[offset: offset + m * ldd].view(m, ldd)   # noqa: E731
+        o.multiply(whole[offset:], ldd, type_d, 1)
+        _check(o, view(whole)[:, :n], type_d, view(kept)[:, :n].double())
+        assert torch.equal(view(whole)[:, n:], view(kept)[:, n:])
+        assert torch.equal(whole[:offset], kept[:offset]) and torch.equal(whole[offset + m * ldd:], kept[offset + m * ldd:])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,n,k", [(3600, 3700, 400), (4353, 3841, 264)])
+def test_large_products_of_scales_far_apart(m, n, k, workspace):
+    o = Operands(m, n, k, True, 16, wide=True)
+    D = torch.empty((m, n), dtype=torch.bfloat16, device="cuda")
+    o.multiply(D, n, "bf16")
+    _check(o, D, "bf16")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,n,k,type_d", [(3600, 3700, 400, "bf16"), (4353, 3841, 264, "f16"), (300, 500, 4096, "bf16"), (1, 64, 65536, "bf16")])
+def test_a_nan_code_spoils_its_row_or_column_only(m, n, k, type_d, workspace):
+    for side in "AB":
+        o = Operands(m, n, k, True, 17)
+        D = torch.empty((m, n), dtype=plain.DTYPES[type_d], device="cuda")
+        if side == "A":
+            o.A[m // 2, 17] = 0x7F
+        else:
+            o.B[n - 1, k - 1] = 0xFF
+        o.multiply(D, n, type_d)
+        nan = torch.isnan(D)
+        assert bool(nan[m // 2].all() if side == "A" else nan[:, n - 1].all()) and int(nan.sum()) == (n if side == "A" else m)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("blocks", [True, False])
+@pytest.mark.parametrize("m,n,k", [(3600, 3700, 400), (4353, 3841, 264), (1, 64, 65536)])
+def test_large_and_cut_products_have_the_same_bits_in_graphs(m, n, k, blocks, workspace):
+    o = Operands(m, n, k, blocks, 18)
+    D, E = (torch.empty((m, n), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        lib.ozaki_set_stream(torch.cuda.current_stream().cuda_stream)
+        o.multiply(E, n, "bf16")
+    lib.ozaki_set_stream(torch.cuda.current_stream().cuda_stream)
+    for i in range(3):
+        E.fill_(float("nan"))
+        o.A[:, :k] = torch.roll(o.A[:, :k], 1, 1)                   # new inputs for every replay
+        graph.replay()
+        torch.cuda.synchronize()
+        for _ in range(2):
+            D.fill_(float("nan"))
+            o.multiply(D, n, "bf16")
+            assert torch.equal(D, E)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,n,k", [(300, 500, 4096), (1, 64, 65536)])
+def test_two_contexts_with_work_memory_of_their_own(m, n, k):
+    """An inner dimension in shares: calls that run at the same time meet in their own context's memory."""
+    o = [Operands(m, n, k, True, s) for s in (19, 20)]
+    D = [torch.zeros((m, n), device="cuda") for _ in o]
+    contexts, kept = [], []
+    try:
+        for x in o:
+            contexts.append(lib.ozaki_context_create())
+            lib.ozaki_context_use(contexts[-1])
+            need = lib.ozaki_gemm_fp8_workspace_bytes(m, n, k)
+            assert need > 256
+            kept.append((torch.empty(need, dtype=torch.uint8, device="cuda"), torch.cuda.Stream()))
+            torch.cuda.synchronize()
+            lib.ozaki_set_stream(kept[-1][1].cuda_stream)
+            lib.ozaki_set_workspace(kept[-1][0], need)
+        for _ in range(20):
+            for c, x, d in zip(contexts, o, D):
+                lib.ozaki_context_use(c)
+                x.multiply(d, n, "f32")
+        torch.cuda.synchronize()
+        for x, d in zip(o, D):
+            _check(x, d, "f32")
+    finally:
+        lib.ozaki_context_use(None)
+        for c in contexts:
+            lib.ozaki_context_destroy(c)
+
+
+@pytest.mark.gpu
+def test_offsets_beyond_2_32_in_large_tiles():
+    """Many vectors whose last ones start beyond 4 GiB, on either side and in the result."""
+    k, ld, n = 130, 1 << 17, 1300
+    m = (1 << 15) + 300
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    big = torch.full((m, ld), 0x7F, dtype=torch.uint8, device="cuda")
+    q = (torch.randn((m, k), device="cuda", generator=gen) * 100).clamp(-448, 448).to(torch.float8_e4m3fn)
+    big[:, :k] = q.view(torch.uint8)
+    small = (torch.randn((n, k), device="cuda", generator=gen) * 100).clamp(-448, 448).to(torch.float8_e4m3fn)
+    B = torch.zeros((n, 144), dtype=torch.uint8, device="cuda")
+    B[:, :k] = small.view(torch.uint8)
+    ones = torch.ones((2, m), device="cuda")
+    want = torch.mm(q.double(), small.double().t().contiguous())
+    magnitudes = torch.mm(q.double().abs(), small.double().abs().t().contiguous())
+    cut = torch.mm(plain.cut_products(q, ones, False), plain.cut_products(small, ones[:, :n], False).t().contiguous())
+    lib.ozaki_set_stream(torch.cuda.current_stream().cuda_stream)
+    assert lib.ozaki_gemm_fp8_workspace_bytes(m, n, k) == 0
+    D = torch.empty((m, ld), dtype=torch.bfloat16, device="cuda")
+    lib.ozaki_gemm_fp8(m, n, k, big, ld, ones, m, B, 144, ones, m, lib.SCALE_VECTORS, D, ld, lib.TYPE_BF16)
+    assert bool(torch.all((D[:, :n].double() - want).abs() <= plain.gemm_bound(k, magnitudes, "bf16", want, cut)))
+    lib.ozaki_gemm_fp8(n, m, k, B, 144, ones, m, big, ld, ones, m, lib.SCALE_VECTORS, D, ld, lib.TYPE_BF16)
+    assert bool(torch.all((D[:n, :m].double().t() - want).abs() <= plain.gemm_bound(k, magnitudes, "bf16", want, cut)))
