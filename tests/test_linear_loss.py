@@ -455,3 +455,55 @@ def test_tokens_of_little_weight_in_16_bit_floats(tokens, vocab, k, weight, work
     out = dg.t() @ (h.abs() * (1 + u) + 2.0 ** -14) + g.abs().t() @ (u * h.abs() + 2.0 ** -14)
     out = out + 2 * (tokens + 4) * 2.0 ** -24 * ((g.abs() + dg).t() @ (h.abs() + 2.0 ** -14))
     assert bool(torch.all((dw.cpu().double() - want_w).abs() <= out + u * (want_w.abs() + out) + tiny))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ignored", [0.0, 0.7])
+@pytest.mark.parametrize("tokens,vocab,k,type,memory", [(1101, 20001, 1000, "bf16", 0.84), (1030, 30001, 603, "f16", 0.84)])
+def test_gradient_in_pieces_by_large_tiles(tokens, vocab, k, type, memory, ignored):
+    """Work memory for two or three pieces of the vocabulary that are each large enough for tiles of 256 x 256 in z, dH (in shares) and dW; the
+    last piece is shorter and takes other tiles and other numbers of shares."""
+    x = Problem(tokens, vocab, k, type, 24, ignored=ignored)
+    least, best = (lib.ozaki_linear_loss_workspace_bytes(tokens, vocab, k, True, m) for m in (True, False))
+    assert least < memory * best
+    ws = device.Workspace(int(memory * best))
+    _, lse = x.forward()
+    dh, dw = x.gradient(lse)
+    x.check_gradient(dh, dw, lse)
+    assert bool(torch.all(dh[(x.T == x.ignore)] == 0.0))
+    for dh_again, dw_again in (x.gradient(lse), (x.gradient(lse, want=("dh",))[0], x.gradient(lse, want=("dw",))[1])):
+        assert torch.equal(dh, dh_again) and torch.equal(dw, dw_again)
+    ws.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens,vocab,k", [(20, 3000, 136), (700, 3001, 200), (1500, 9001, 1000), (2900, 4001, 72)])
+def test_replays_of_a_graph_follow_the_tokens_that_count(tokens, vocab, k, workspace):
+    """What a captured call does is decided on the card: other tokens count in every replay, from none to all."""
+    x = Problem(tokens, vocab, k, "bf16", 25)
+    all_targets = torch.randint(0, vocab, (tokens,), device="cuda", generator=torch.Generator(device="cuda").manual_seed(26))
+    dloss = x.dloss.cuda()
+    loss, lse = x.forward()
+    dh, dw = x.gradient(lse)
+    out = [torch.empty_like(t) for t in (loss, lse, dh, dw)]
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        lib.ozaki_set_stream(torch.cuda.current_stream().cuda_stream)
+        lib.ozaki_linear_loss(*x.arguments(), out[0], out[1])
+        lib.ozaki_linear_loss_grad(*x.arguments(), out[1], dloss, out[2], k, out[3], k)
+    lib.ozaki_set_stream(torch.cuda.current_stream().cuda_stream)
+    for i, share in enumerate((0.6, 0.0, 0.97, 1.1, 0.3)):
+        gen = torch.Generator(device="cuda").manual_seed(i)
+        x.T.copy_(torch.where(torch.rand((tokens,), device="cuda", generator=gen) < share, x.ignore, all_targets))
+        for t in out:
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        loss, lse = x.forward()
+        dh, dw = x.gradient(lse)
+        for got, want in zip(out, (loss, lse, dh, dw)):
+            assert torch.equal(got, want)
+        assert bool(torch.all(dh[x.T == x.ignore] == 0.0)) and (share < 1.0 or bool(torch.all(dw == 0.0)))
+    x.targets = x.T.cpu()
+    x.check_gradient(dh, dw, lse)
