@@ -373,8 +373,11 @@ int ozaki_quantise_fp8(int64_t rows, int64_t k, const void* X, int64_t ldx, int 
                        int64_t lds, void* Qt, int64_t ldqt, float* St, int64_t ldst);
 
 /* D[i * ldd + j] = sum over b of Sa[b * ldsa + i] * Sb[..] * (sum over e of block b of A[i * lda + e] * B[j * ldb + e]), i < m, j < n:
- * A's vectors with OZAKI_SCALE_VECTORS, B's with `scaling_b`, as ozaki_quantise_fp8 leaves them.  Products and sums in FP32, D of
- * `type_d`, rounded once; with `accumulate` the sum is added to what D holds.  k == 0 gives zeros.
+ * A's vectors with OZAKI_SCALE_VECTORS, B's with `scaling_b`, as ozaki_quantise_fp8 leaves them.  Sums, and the products of two scales
+ * (which have to lie in its range), in FP32; D of `type_d`, rounded once; with `accumulate` the sum is added to what D holds.  k == 0 gives zeros.
+ * For a D of 32 bits every product A[i][e] * B[j][e] is exact.  For a D of 16 bits they are formed by the matrix unit's FP8 instructions, which
+ * align the products of eight neighbouring elements to the largest of them and cut them 13 bits below its power of two: on normally distributed
+ * codes 1.4e-5 of the result's norm, a hundredth of D's own rounding, but more than that where a sum nearly cancels.
  * Where few results leave compute units without work the inner dimension is cut and the shares meet in the context's
  * workspace: ozaki_gemm_fp8_workspace_bytes, 0 where none is needed.  The cut depends on m, n and k only. */
 int ozaki_gemm_fp8(int64_t m, int64_t n, int64_t k, const void* A, int64_t lda, const float* Sa, int64_t ldsa, const void* B, int64_t ldb,
@@ -393,7 +396,9 @@ int ozaki_linear_loss(int64_t tokens, int64_t vocab, int64_t k, const void* H, i
  *     g[t][v] = (exp(z[t][v] - lse[t]) - [v == targets[t]]) * dloss[t]      dH = g W      dW = g^T H
  * in the type of H and W; either result may be null.  Tokens with targets[t] == ignore (or an invalid target, which raises
  * OZAKI_STATUS_TARGET) have no share: their rows of dH are zeros, and what their rows of H hold does not matter.  g is formed a
- * piece of the vocabulary at a time, in 16 bits; the piece follows from the workspace, of
+ * piece of the vocabulary at a time, in 16 bits and without dloss; dW is formed with H times dloss[t] over the largest |dloss|, which is rounded to
+ * 16 bits where the dloss of the tokens that count differ (dW's error is then about 1.4 times what it is with equal ones; in FP16, tokens of less
+ * than 2^-19 of the largest lose more).  The piece follows from the workspace, of
  * ozaki_linear_loss_workspace_bytes(tokens, vocab, k, 1, minimum) bytes: minimum != 0 the least, 0 what is recommended.  With the
  * recommended size or more the result does not depend on the workspace. */
 int ozaki_linear_loss_grad(int64_t tokens, int64_t vocab, int64_t k, const void* H, int64_t ldh, const void* W, int64_t ldw, int type,
