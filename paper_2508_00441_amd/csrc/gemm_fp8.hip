@@ -2,8 +2,8 @@
 //     D[i][j] = sum over blocks b of  Sa[b][i] * Sb[b][j or j / 128] * (sum over e in b of A[i][e] * B[j][e])
 // A block's products are summed by the matrix unit in FP32, the blocks' sums by FP32 fused multiply-adds with the product of their two
 // scales; D is rounded once.  A D of 16 bits takes the FP8 instructions, a D of 32 bits the FP16 ones (Fragment in tile_product.hpp).
-// Few vectors of A are bound by the read of B, many by the matrix unit's issue (4096 x 4096 x 4096: 61 us, 2.2 PFLOP/s), 32-bit results by the vector
-// unit, which widens the codes (16384 x 4096 x 8192: 1.03 ms, 1.07 PFLOP/s).
+// Few vectors of A are bound by the read of B, many by the matrix unit's issue (4096 x 4096 x 4096: 61 - 63 us, 2.2 PFLOP/s), 32-bit results by the
+// vector unit, which widens the codes (16384 x 4096 x 8192: 1.03 - 1.07 ms, 1.03 - 1.07 PFLOP/s).
 #include "layout.hpp"
 #include "tile_product.hpp"
 
@@ -16,8 +16,6 @@ struct GemmFp8Work {
     int tiles_m, tiles_n;
     WorkOrder order;
 };
-
-__device__ __forceinline__ int split_begin(int steps, int splits, int s) { return (int)((int64_t)steps * s / splits); }
 
 template <typename P, int TYPE>
 __device__ __forceinline__ void gemm_fp8_body(const GemmFp8Work& w) {
@@ -187,8 +185,9 @@ struct Shape { int kind, tm, tn, splits; };
 // 32-bit results: no tiles of 256 x 256.  The widened fragments do not fit beside their accumulators, and two workgroups of 128 x 128, which pause
 // at different times, do better than one of 256 x 128 (16384 x 4096 x 8192: 1030 and 1080).
 // Where 64 x 64 tiles are too few, the inner dimension is cut, into shares of at least four steps (64 x 4096 x 16384: 17.3 for 256 shares in all,
-// 18.4 for 512; shares of eight steps: 64 x 2048 x 2048 9.5 against 8.5).  Where few vectors meet few of B: of at least 32 steps, from three shares on
-// (1 x 64 x 65536: 7.5, uncut 37.7; 1 x 1024 x 16384: 8.4, 11.9, in shares of 64 steps 10.0; but 1 x 2048 x 8192, two shares: 8.1, uncut 7.7).
+// 18.4 for 512; shares of eight steps: 64 x 2048 x 2048 9.5 against 8.5).  Where few vectors meet few of B: from 96 steps on, into shares
+// of at least 32 (1 x 64 x 65536: 7.5, uncut 37.7; 1 x 1024 x 16384: 8.4, 11.9, in shares of 64 steps 10.0; 1 x 2048 x 12288, two shares: 10.9, uncut 11.6;
+// but two shares of 1 x 2048 x 8192, 64 steps: 8.1, uncut 7.7).
 Shape shape_of(int64_t m, int64_t n, int64_t k) {
     const int64_t steps = div_up(k, SCALE_BLOCK);
     const auto shares = [](int64_t want, int64_t most) {
@@ -218,7 +217,7 @@ hipError_t launch_kind(const GemmFp8Args& a, int splits, Shape s, hipStream_t st
     w.tiles_m = (int)div_up(a.m, s.tm);
     w.tiles_n = (int)div_up(a.n, s.tn);
     const int64_t tiles = (int64_t)w.tiles_m * w.tiles_n;
-    w.order = WorkOrder{s.kind == LARGE ? 32 : 64, 8};             // 4096 x 4096 x 4096: 70 us, in plain order 75
+    w.order = WorkOrder{s.kind == LARGE ? 32 : 64, 8};             // 4096 x 4096 x 4096: 63.1 us, in plain order 63.7; 2048 x 4096 x 4096: 42.7, 43.4
     const unsigned blocks = (unsigned)(tiles * splits);
     if (s.kind == VECTORS) hipLaunchKernelGGL((gemm_fp8_few_kernel<SCALING, TYPE>), dim3(blocks), dim3(FEW_WAVES * 64), 0, st, a, splits);
     else if (s.kind == SMALL) hipLaunchKernelGGL((gemm_fp8_small_kernel<SCALING, TYPE>), dim3(blocks), dim3(256), 0, st, w);

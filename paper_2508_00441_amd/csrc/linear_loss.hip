@@ -13,8 +13,8 @@
 // and lose nothing to 16 bits; times dloss they all lose alike, which does not average out (1.7 times the error of the result's own
 // rounding in FP16).  2^12 keeps the words down to a probability of 2^-26 among FP16's normal numbers.  dloss comes in where it costs no
 // rounding: as a factor of the rows of dH, and for dW with a copy of H times dloss over the largest |dloss|, which is one for a mean.
-// Where the shares differ, that copy is rounded to 16 bits once more (on normally distributed numbers the error of dW's rows of tokens of small
-// shares grows from the result's own rounding to 1.4 times that).  In FP16, whose smallest normal number is 2^-14, H times a share below 2^-10 would
+// Where the shares differ, that copy is rounded to 16 bits once more (on normally distributed numbers dW's error grows from 1.8e-3 of its norm
+// to 2.5e-3 in BF16, from 2.5e-4 to 3.3e-4 in FP16; the result's own rounding is 1.7e-3 and 2.1e-4).  In FP16, whose smallest normal number is 2^-14, H times a share below 2^-10 would
 // run out of bits; there g takes up to 2^8 of the share, a power of two that costs it nothing but the words below a probability of 2^-18 of
 // that token, whose error stays below 2^-29 (share_exponent).  So shares down to 2^-19 are as good as others.
 // Only the tokens that count take part (tokens_body).
@@ -360,8 +360,6 @@ struct ProductWork {
     float* partial;          // not null: unscaled sums go there, [split][token that counts][n in fours]
 };
 
-__device__ __forceinline__ int split_begin(int steps, int splits, int s) { return (int)((int64_t)steps * s / splits); }
-
 template <typename P, typename T, bool DW>
 __device__ __forceinline__ void loss_product_body(const ProductWork& w) {
     __shared__ __attribute__((aligned(16))) uint8_t lds[P::LDS_BYTES];
@@ -484,12 +482,9 @@ int tile_n(int shape) { return shape == LARGE ? 256 : 128; }
 int tile_words(int shape) { return shape == FEW || shape == SMALL ? 64 : tile_n(shape); }      // of the kernels that form z
 // tiles that run on an XCD at a time share its L2: 4096 tokens, 65536 words of 4096, gradient 4.98 ms, in plain order 5.37
 WorkOrder order_for(int shape) { return WorkOrder{shape == LARGE ? 32 : 64, 8}; }
-// dH, whose inner dimension is the vocabulary: large tiles also where they are few, if that leaves every compute unit a share of it of
-// some length (1003 x 1024 over 50001 words: 16 tiles in 16 shares; the whole gradient 339 us, with middle tiles 383).  Shares of at least eight steps,
-// as many as run at a time (twice as many: 365).
 // Large tiles run in rounds of one for every compute unit.  Where the last round has few of them, the words that they hold are left to smaller
 // tiles in a launch of their own (1003 tokens and 50001 words, 784 tiles: of 1000 elements 129 us against 144, of 256 58 against 66, the gradient
-// 353 against 376 and 150 against 157; up to 64 tiles, 256 of 128 x 128).
+// 353 against 376 and 150 against 157).  Up to 64 tiles: of z 512 of 128 x 64, two to a compute unit, of dW 256 of 128 x 128.
 int64_t words_in_rounds(int64_t across, int64_t words) {
     const int64_t tiles = across * div_up(words, 256), over = tiles % 256, whole = (tiles - over) / across;
     return over == 0 || whole == 0 || tiles - whole * across > 64 ? words : whole * 256;
@@ -510,6 +505,9 @@ struct ProductShape {
         return joined || splits > 1 ? ProductRoom{tiles * splits, tile_m(shape), most} : ProductRoom{tiles, tile_m(shape), 1};
     }
 };
+// dH, whose inner dimension is the vocabulary: large tiles also where they are few, if that leaves every compute unit a share of it of
+// some length (1003 x 1024 over 50001 words: 16 tiles in 16 shares; the whole gradient 339 us, with middle tiles 383).  Shares of at least eight steps,
+// as many as run at a time (twice as many: 365).
 ProductShape dh_shape(int64_t m, int64_t n, int64_t steps) {
     int shape = shape_for(m, n);
     if (shape == MIDDLE && m > 128 && div_up(m, 256) * div_up(n, 256) * (steps / 16) >= 128) shape = LARGE;

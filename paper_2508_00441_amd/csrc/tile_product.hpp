@@ -119,6 +119,9 @@ __device__ __forceinline__ v8i32 turned_fragment(const uint8_t* panel, int p, in
     return out;
 }
 
+// where share s of the steps begins
+__device__ __forceinline__ int split_begin(int steps, int splits, int s) { return (int)((int64_t)steps * s / splits); }
+
 // four neighbouring elements of a row of D, the first `left` of them; `wide`: D's rows start at multiples of four elements
 template <typename T>
 __device__ __forceinline__ void put_four(T* at, v4f32 v, int64_t left, bool wide, bool accumulate) {
