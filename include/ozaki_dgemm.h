@@ -406,6 +406,99 @@ int ozaki_linear_loss_grad(int64_t tokens, int64_t vocab, int64_t k, const void*
                            int64_t lddw);
 size_t ozaki_linear_loss_workspace_bytes(int64_t tokens, int64_t vocab, int64_t k, int grad, int minimum);
 
+/* ------------------------------------------------------------------------------------------------
+ * A model's feed-forward block and its training step.  The same conventions as for the low-precision operators above: matrices of vectors,
+ * inputs' vectors at multiples of 16 bytes (the 16 bytes in which one ends may be read whole), results anywhere, all pointers DEVICE unless
+ * stated otherwise.  Inputs and results do not overlap unless it is said that they may.
+ * ---------------------------------------------------------------------------------------------- */
+
+/* act(z); GELU z * Phi(z) with the normal distribution's Phi, GELU_TANH z * (1 + tanh(sqrt(2/pi) * (z + 0.044715 z^3))) / 2, SILU z / (1 + exp(-z)) */
+enum {
+    OZAKI_ACTIVATION_NONE = 0, OZAKI_ACTIVATION_RELU = 1, OZAKI_ACTIVATION_GELU = 2, OZAKI_ACTIVATION_GELU_TANH = 3, OZAKI_ACTIVATION_SILU = 4
+};
+#define OZAKI_MAX_NORM 16384 /* elements of a row of ozaki_block_norm                                                 */
+
+/* A linear layer with what follows it:     z = X W^T + bias          Y = act(z) + R
+ * X: m vectors, W: n vectors of k >= 1 elements of `type` (BF16 or F16), of which everything else is too; m * n is at most OZAKI_MAX_LOGITS.
+ *   bias      n elements; may be null
+ *   R, ldr    m x n, may lie anywhere, may be Y with its ld; may be null
+ *   Z, ldz    where z goes, for the gradient; may be null
+ * Sums, activation and additions in FP32, from z that has not been rounded; one rounding of each result.  Where few results leave compute units without
+ * work the inner dimension is cut and the shares meet in the context's workspace, ozaki_linear_workspace_bytes(m, n, k, 0); 0 where none is
+ * needed.  The cut depends on m, n and k only. */
+int ozaki_linear(int64_t m, int64_t n, int64_t k, const void* X, int64_t ldx, const void* W, int64_t ldw, int type, const void* bias, int activation,
+                 const void* R, int64_t ldr, void* Y, int64_t ldy, void* Z, int64_t ldz);
+
+/* Its gradient, from the gradient dY of Y (which is R's):
+ *     dz = dY * act'(Z)          dX = dz W          dW = dz^T X          dbias[j] = sum over i of dz[i][j]
+ *   Z, ldz    what ozaki_linear left, or anything else that dz is to be formed with; not read without an activation
+ *   dX, dW    of `type`; dbias in 32 bits.  Each may be null, not all of them; X is read for dW, W for dX.
+ * dz is formed once and rounded to `type` for the two products (without an activation it is dY); dbias is summed in 32 bits from what has not been rounded.
+ * RELU's derivative at zero is zero.  m == 0 gives zeros in dW and dbias.  n is at most OZAKI_MAX_EXTENT / 2.
+ * Needs the context's workspace, ozaki_linear_workspace_bytes(m, n, k, 1). */
+int ozaki_linear_grad(int64_t m, int64_t n, int64_t k, const void* X, int64_t ldx, const void* W, int64_t ldw, int type, int activation, const void* Z,
+                      int64_t ldz, const void* dY, int64_t lddy, void* dX, int64_t lddx, void* dW, int64_t lddw, float* dbias);
+size_t ozaki_linear_workspace_bytes(int64_t m, int64_t n, int64_t k, int grad);
+
+/* A pair of linear layers whose results are multiplied:     g = X Wg^T          u = X Wu^T          Y = act(g) * u
+ * Wg and Wu: n vectors each, ldw apart (of one matrix that holds both: Wu = Wg + n * ldw elements).
+ *   G, U      where g and u go, for the gradient; both may be null
+ * Everything else as for ozaki_linear; workspace ozaki_gated_linear_workspace_bytes(m, n, k, 0). */
+int ozaki_gated_linear(int64_t m, int64_t n, int64_t k, const void* X, int64_t ldx, const void* Wg, const void* Wu, int64_t ldw, int type, int activation,
+                       void* Y, int64_t ldy, void* G, int64_t ldg, void* U, int64_t ldu);
+
+/* Its gradient:
+ *     dg = dY * U * act'(G)      du = dY * act(G)      dX = dg Wg + du Wu      dWg = dg^T X      dWu = du^T X
+ * dg and du are formed once and rounded to `type`; dX is one sum of both terms.  Each result may be null, not all of them (dWg and dWu share lddw).  Everything else as for
+ * ozaki_linear_grad; workspace ozaki_gated_linear_workspace_bytes(m, n, k, 1). */
+int ozaki_gated_linear_grad(int64_t m, int64_t n, int64_t k, const void* X, int64_t ldx, const void* Wg, const void* Wu, int64_t ldw, int type,
+                            int activation, const void* G, int64_t ldg, const void* U, int64_t ldu, const void* dY, int64_t lddy, void* dX,
+                            int64_t lddx, void* dWg, void* dWu, int64_t lddw);
+size_t ozaki_gated_linear_workspace_bytes(int64_t m, int64_t n, int64_t k, int grad);
+
+/* What lies between two blocks of a model, for each of `rows` rows of k elements, 1 <= k <= OZAKI_MAX_NORM, with rho(v) = 1 / sqrt(mean(v^2) + eps):
+ *     u = X * rho(X) * w_post   (w_post null: u = X)          the norm behind a block
+ *     r = R + scale * gate * u                                its gate and scale, the sum that runs through the model
+ *     H = r * rho(r) * w_pre                                  the norm in front of the next block
+ *   X, H      of `type` (F32, BF16, F16); X null: nothing is added (r is R; R_out, w_post and gate are then null too)
+ *   w_post, w_pre      k elements in 32 bits
+ *   gate, group        32 bits, rows i share row i / group of it: gate[(i / group) * k + e]; null: one
+ *   R, R_out  of `type_r`, which is `type` or F32; R null: zeros.  R_out is r; may be null, may be R with its ld.
+ *   H         may be null (then so may w_pre), not with R_out; may be X with its ld
+ * Rounded once each: H is formed from the r that has not been rounded.  Sums along a row are in 64 bits. */
+int ozaki_block_norm(int64_t rows, int64_t k, const void* X, int64_t ldx, int type, const float* w_post, const float* gate, int64_t group, float scale,
+                     float eps, const void* R, int64_t ldr, int type_r, void* R_out, int64_t ldro, const float* w_pre, void* H, int64_t ldh);
+
+/* Its gradient, from those of H (dH, of `type`; null: none) and of R_out (dR_out, of `type_r`; null: none), with R_out here the r that the call above left:
+ *     dR = dR_out + the gradient of r through H          dX = the gradient of X through scale * gate * u, from dR that has not been rounded
+ *     dw_pre, dw_post (k elements), dgate (as gate), in 32 bits: sums over rows, in an order that depends on rows, k and group only
+ * Each result may be null, not all of them; R_out and w_pre are read with dH (and only then); dw_pre asks for dH; dX, dw_post and dgate ask for X, dw_post for
+ * w_post, dgate for gate.  dR may be dR_out, dX may be X or dH, each with its ld.  rows == 0 gives zeros in dw_pre and dw_post.  For the sums over rows the
+ * call needs the context's workspace, ozaki_block_norm_workspace_bytes(rows, k, group) with group 0 without a gate. */
+int ozaki_block_norm_grad(int64_t rows, int64_t k, const void* X, int64_t ldx, int type, const float* w_post, const float* gate, int64_t group,
+                          float scale, float eps, const void* R_out, int64_t ldro, int type_r, const float* w_pre, const void* dH, int64_t lddh,
+                          const void* dR_out, int64_t lddro, void* dX, int64_t lddx, void* dR, int64_t lddr, float* dw_post, float* dgate,
+                          float* dw_pre);
+size_t ozaki_block_norm_workspace_bytes(int64_t rows, int64_t k, int64_t group);
+
+/* The norm of `count` tensors together:     *norm = |scale| * sqrt(sum over all elements of x^2)
+ *   tensors, sizes, types      HOST: where each lies (DEVICE; aligned to its elements, no more), how many elements it has (at most 2^38), their type.
+ *                              They are read before the call returns.
+ *   scale                      what the elements are to be multiplied by (one over what the loss was multiplied by)
+ *   norm                       DEVICE, one number in 32 bits; infinite or NaN where an element is
+ * Squares are summed in 64 bits, in an order that depends on the sizes and types only.  Needs the context's workspace,
+ * ozaki_gradient_norm_workspace_bytes(count). */
+int ozaki_gradient_norm(int count, const void* const* tensors, const int64_t* sizes, const int* types, float scale, float* norm);
+
+/* The same, and the elements scaled so that the norm is at most max_norm:     out = x * scale * min(1, max_norm / *norm), rounded once
+ *   out       HOST: where each tensor's results go (DEVICE, of its type); out[i] may be tensors[i]
+ *   given     1: *norm is there already (that of all shares of a model, say) and read; 0: it is formed and written
+ * A norm that is NaN makes every element NaN, one that is infinite makes finite ones zero: look at *norm before the results are used.
+ * Workspace as above, none with `given`. */
+int ozaki_clip_gradients(int count, const void* const* tensors, const int64_t* sizes, const int* types, float scale, float max_norm, void* const* out,
+                         float* norm, int given);
+size_t ozaki_gradient_norm_workspace_bytes(int64_t count);
+
 #ifdef __cplusplus
 }
 #endif

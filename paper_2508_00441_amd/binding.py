@@ -33,15 +33,18 @@ SCALE_VECTORS, SCALE_BLOCKS = 0, 1
 SCALE_BLOCK = 128
 MAX_EXTENT = 1 << 22
 MAX_QUANTISED, MAX_LOGITS = 1 << 34, 1 << 38
+ACTIVATION_NONE, ACTIVATION_RELU, ACTIVATION_GELU, ACTIVATION_GELU_TANH, ACTIVATION_SILU = 0, 1, 2, 3, 4
+MAX_NORM = 16384
 
 SLICE_FORMATS = {"fp8": SLICE_FP8_E4M3, "fp16": SLICE_FP16, "fp6": SLICE_FP6_E2M3, "fp6_e3m2": SLICE_FP6_E3M2, "int8": SLICE_INT8}
 ACCUM_MODES = {"hw": ACCUM_FP64_HW, "emu": ACCUM_FP64_INT_EMU, "exact": ACCUM_EXACT_FIXED}
 PAIR_SETS = {"triangle": PAIRS_TRIANGLE, "full": PAIRS_ALL}
 TYPES = {"f32": TYPE_F32, "bf16": TYPE_BF16, "f16": TYPE_F16}
+ACTIVATIONS = {"none": ACTIVATION_NONE, "relu": ACTIVATION_RELU, "gelu": ACTIVATION_GELU, "gelu_tanh": ACTIVATION_GELU_TANH, "silu": ACTIVATION_SILU}
 SUM_RULES = {"runs": SUM_RUNS, "plain": SUM_PLAIN}
 
 #: every symbol include/ozaki_dgemm.h declares: name -> (restype, argtypes)
-_i64, _int, _vp, _sz = ctypes.c_int64, ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t
+_i64, _int, _vp, _sz, _f32 = ctypes.c_int64, ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_float
 SIGNATURES = {
     "ozaki_plan": (_int, [_i64, _int, ctypes.POINTER(_int), ctypes.POINTER(_int)]),
     "ozaki_dgemm": (_int, [_i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _int, _int, _i64, _int]),
@@ -74,6 +77,19 @@ SIGNATURES = {
     "ozaki_linear_loss": (_int, [_i64, _i64, _i64, _vp, _i64, _vp, _i64, _int, _vp, _i64, _vp, _vp]),
     "ozaki_linear_loss_grad": (_int, [_i64, _i64, _i64, _vp, _i64, _vp, _i64, _int, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _i64]),
     "ozaki_linear_loss_workspace_bytes": (_sz, [_i64, _i64, _i64, _int, _int]),
+    "ozaki_linear": (_int, [_i64, _i64, _i64, _vp, _i64, _vp, _i64, _int, _vp, _int, _vp, _i64, _vp, _i64, _vp, _i64]),
+    "ozaki_linear_grad": (_int, [_i64, _i64, _i64, _vp, _i64, _vp, _i64, _int, _int, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp]),
+    "ozaki_linear_workspace_bytes": (_sz, [_i64, _i64, _i64, _int]),
+    "ozaki_gated_linear": (_int, [_i64, _i64, _i64, _vp, _i64, _vp, _vp, _i64, _int, _int, _vp, _i64, _vp, _i64, _vp, _i64]),
+    "ozaki_gated_linear_grad": (_int, [_i64, _i64, _i64, _vp, _i64, _vp, _vp, _i64, _int, _int, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64]),
+    "ozaki_gated_linear_workspace_bytes": (_sz, [_i64, _i64, _i64, _int]),
+    "ozaki_block_norm": (_int, [_i64, _i64, _vp, _i64, _int, _vp, _vp, _i64, _f32, _f32, _vp, _i64, _int, _vp, _i64, _vp, _vp, _i64]),
+    "ozaki_block_norm_grad": (_int, [_i64, _i64, _vp, _i64, _int, _vp, _vp, _i64, _f32, _f32, _vp, _i64, _int, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64,
+                                     _vp, _vp, _vp]),
+    "ozaki_block_norm_workspace_bytes": (_sz, [_i64, _i64, _i64]),
+    "ozaki_gradient_norm": (_int, [_int, ctypes.POINTER(_vp), ctypes.POINTER(_i64), ctypes.POINTER(_int), _f32, _vp]),
+    "ozaki_clip_gradients": (_int, [_int, ctypes.POINTER(_vp), ctypes.POINTER(_i64), ctypes.POINTER(_int), _f32, _f32, ctypes.POINTER(_vp), _vp, _int]),
+    "ozaki_gradient_norm_workspace_bytes": (_sz, [_i64]),
 }
 
 _lib = None
@@ -266,3 +282,71 @@ def ozaki_linear_loss_grad(tokens, vocab, k, H, ldh, W, ldw, type, targets, igno
     st = load().ozaki_linear_loss_grad(tokens, vocab, k, _ptr(H), ldh, _ptr(W), ldw, type, _ptr(targets), ignore, _ptr(lse), _ptr(dloss),
                                        _ptr(dH), lddh, _ptr(dW), lddw)
     return _check(st, "ozaki_linear_loss_grad") if check else st
+
+
+def ozaki_linear_workspace_bytes(m, n, k, grad) -> int:
+    return int(load().ozaki_linear_workspace_bytes(m, n, k, 1 if grad else 0))
+
+
+def ozaki_linear(m, n, k, X, ldx, W, ldw, type, bias, activation, R, ldr, Y, ldy, Z=None, ldz=0, check: bool = True) -> int:
+    st = load().ozaki_linear(m, n, k, _ptr(X), ldx, _ptr(W), ldw, type, _ptr(bias), activation, _ptr(R), ldr, _ptr(Y), ldy, _ptr(Z), ldz)
+    return _check(st, "ozaki_linear") if check else st
+
+
+def ozaki_linear_grad(m, n, k, X, ldx, W, ldw, type, activation, Z, ldz, dY, lddy, dX, lddx, dW, lddw, dbias=None, check: bool = True) -> int:
+    st = load().ozaki_linear_grad(m, n, k, _ptr(X), ldx, _ptr(W), ldw, type, activation, _ptr(Z), ldz, _ptr(dY), lddy, _ptr(dX), lddx, _ptr(dW), lddw,
+                                  _ptr(dbias))
+    return _check(st, "ozaki_linear_grad") if check else st
+
+
+def ozaki_gated_linear_workspace_bytes(m, n, k, grad) -> int:
+    return int(load().ozaki_gated_linear_workspace_bytes(m, n, k, 1 if grad else 0))
+
+
+def ozaki_gated_linear(m, n, k, X, ldx, Wg, Wu, ldw, type, activation, Y, ldy, G=None, ldg=0, U=None, ldu=0, check: bool = True) -> int:
+    st = load().ozaki_gated_linear(m, n, k, _ptr(X), ldx, _ptr(Wg), _ptr(Wu), ldw, type, activation, _ptr(Y), ldy, _ptr(G), ldg, _ptr(U), ldu)
+    return _check(st, "ozaki_gated_linear") if check else st
+
+
+def ozaki_gated_linear_grad(m, n, k, X, ldx, Wg, Wu, ldw, type, activation, G, ldg, U, ldu, dY, lddy, dX, lddx, dWg, dWu, lddw, check: bool = True) -> int:
+    st = load().ozaki_gated_linear_grad(m, n, k, _ptr(X), ldx, _ptr(Wg), _ptr(Wu), ldw, type, activation, _ptr(G), ldg, _ptr(U), ldu, _ptr(dY), lddy,
+                                        _ptr(dX), lddx, _ptr(dWg), _ptr(dWu), lddw)
+    return _check(st, "ozaki_gated_linear_grad") if check else st
+
+
+def ozaki_block_norm_workspace_bytes(rows, k, group) -> int:
+    return int(load().ozaki_block_norm_workspace_bytes(rows, k, group))
+
+
+def ozaki_block_norm(rows, k, X, ldx, type, w_post, gate, group, scale, eps, R, ldr, type_r, R_out, ldro, w_pre, H, ldh, check: bool = True) -> int:
+    st = load().ozaki_block_norm(rows, k, _ptr(X), ldx, type, _ptr(w_post), _ptr(gate), group, scale, eps, _ptr(R), ldr, type_r, _ptr(R_out), ldro,
+                                 _ptr(w_pre), _ptr(H), ldh)
+    return _check(st, "ozaki_block_norm") if check else st
+
+
+def ozaki_block_norm_grad(rows, k, X, ldx, type, w_post, gate, group, scale, eps, R_out, ldro, type_r, w_pre, dH, lddh, dR_out, lddro, dX, lddx, dR, lddr,
+                          dw_post=None, dgate=None, dw_pre=None, check: bool = True) -> int:
+    st = load().ozaki_block_norm_grad(rows, k, _ptr(X), ldx, type, _ptr(w_post), _ptr(gate), group, scale, eps, _ptr(R_out), ldro, type_r, _ptr(w_pre),
+                                      _ptr(dH), lddh, _ptr(dR_out), lddro, _ptr(dX), lddx, _ptr(dR), lddr, _ptr(dw_post), _ptr(dgate), _ptr(dw_pre))
+    return _check(st, "ozaki_block_norm_grad") if check else st
+
+
+def ozaki_gradient_norm_workspace_bytes(count) -> int:
+    return int(load().ozaki_gradient_norm_workspace_bytes(count))
+
+
+def _array(values, of):
+    """A ctypes array, as it is; a list of tensors or numbers, as one."""
+    if values is None or isinstance(values, ctypes.Array):
+        return values
+    return (of * len(values))(*[_ptr(v) if of is _vp else v for v in values])
+
+
+def ozaki_gradient_norm(count, tensors, sizes, types, scale, norm, check: bool = True) -> int:
+    st = load().ozaki_gradient_norm(count, _array(tensors, _vp), _array(sizes, _i64), _array(types, _int), scale, _ptr(norm))
+    return _check(st, "ozaki_gradient_norm") if check else st
+
+
+def ozaki_clip_gradients(count, tensors, sizes, types, scale, max_norm, out, norm, given=0, check: bool = True) -> int:
+    st = load().ozaki_clip_gradients(count, _array(tensors, _vp), _array(sizes, _i64), _array(types, _int), scale, max_norm, _array(out, _vp), _ptr(norm), given)
+    return _check(st, "ozaki_clip_gradients") if check else st

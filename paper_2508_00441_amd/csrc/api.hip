@@ -5,7 +5,7 @@
 #include <new>
 #include <vector>
 
-#include "low_precision.hpp"
+#include "block_operators.hpp"
 #include "plan.hpp"
 
 using namespace ozaki;
@@ -15,6 +15,8 @@ static_assert(OZAKI_SLICE_INT8 == FMT_INT8 && OZAKI_ACCUM_EXACT_FIXED == ACC_EXA
               "header and implementation disagree");
 static_assert(OZAKI_TYPE_F16 == TYPE_F16 && OZAKI_SCALE_BLOCKS == SCALE_BLOCKS && OZAKI_SCALE_BLOCK == SCALE_BLOCK && OZAKI_MAX_EXTENT == MAX_VECTOR_BYTES,
               "header and implementation disagree");
+
+static_assert(OZAKI_ACTIVATION_SILU == ACT_SILU && OZAKI_ACTIVATION_GELU == ACT_GELU && OZAKI_MAX_NORM == MAX_NORM, "header and implementation disagree");
 
 // A context: everything a call needs beyond its arguments.
 struct ozaki_context_s {
@@ -246,6 +248,65 @@ int check_loss_args(int64_t tokens, int64_t vocab, int64_t k, const void* H, int
     if (!targets) return -9;
     return 0;
 }
+
+// linear layers: sizes, and the two operands of the forward product by position; `first` is X's
+int check_linear_args(int64_t m, int64_t n, int64_t k, const void* X, int64_t ldx, const void* W, const void* W2, bool pair, int64_t ldw, int type, int activation,
+                      bool need_x, bool need_w) {
+    if (!extent_ok(m)) return -1;
+    if (n < 1 || !extent_ok(n) || m * n > OZAKI_MAX_LOGITS) return -2;
+    if (k < 1 || k > OZAKI_MAX_EXTENT / 2 || m * k > OZAKI_MAX_LOGITS || n * k > OZAKI_MAX_LOGITS) return -3;
+    const int more = pair ? 1 : 0;
+    if (type != OZAKI_TYPE_BF16 && type != OZAKI_TYPE_F16) return -8 - more;
+    if (!activation_ok(activation)) return pair ? -10 : -9;
+    if (m == 0) return 0;
+    if (need_x && (!X || !aligned16(X))) return -4;
+    if (need_x && !stride_ok(ldx, k, 2)) return -5;
+    if (need_w && (!W || !aligned16(W))) return -6;
+    if (need_w && pair && (!W2 || !aligned16(W2))) return -7;
+    if (need_w && !stride_ok(ldw, k, 2)) return -7 - more;
+    return 0;
+}
+bool aligned(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+// vectors of k elements of `type` at multiples of 16 bytes, any distance apart
+bool rows_ok(int64_t ld, int64_t k, int type) { return ld >= k && ld <= ((int64_t)1 << 40) && ld * type_bytes(type) % 16 == 0; }
+
+int check_norm_args(int64_t rows, int64_t k, const void* X, int64_t ldx, int type, const float* w_post, const float* gate, int64_t group, float scale, float eps,
+                    int type_r) {
+    if (!extent_ok(rows)) return -1;
+    if (k < 1 || k > OZAKI_MAX_NORM) return -2;
+    if (!aligned16(X)) return -3;
+    if (X && !rows_ok(ldx, k, type)) return -4;
+    if (!type_ok(type)) return -5;
+    if (!aligned(w_post, 4) || (w_post && !X)) return -6;
+    if (!aligned(gate, 4) || (gate && !X)) return -7;
+    if (gate && group < 1) return -8;
+    if (!(scale - scale == 0.0f)) return -9;
+    if (!(eps >= 0.0f) || !(eps - eps == 0.0f)) return -10;
+    if (type_r != type && type_r != OZAKI_TYPE_F32) return -13;
+    return 0;
+}
+
+int check_tensors(int count, const void* const* tensors, const int64_t* sizes, const int* types, float scale) {
+    if (count < 0) return -1;
+    if (count > 0 && !tensors) return -2;
+    if (count > 0 && !sizes) return -3;
+    if (count > 0 && !types) return -4;
+    for (int i = 0; i < count; ++i) {
+        if (sizes[i] < 0 || sizes[i] > OZAKI_MAX_LOGITS) return -3;
+        if (!type_ok(types[i])) return -4;
+        if (sizes[i] > 0 && (!tensors[i] || !aligned(tensors[i], type_bytes(types[i])))) return -2;
+    }
+    return scale - scale == 0.0f ? 0 : -5;
+}
+
+// the context's work memory behind the flags, if it has `bytes`; FLAG_BYTES stay in front of every call's
+bool work_memory(size_t bytes, uint8_t*& ws) {
+    if (bytes == 0) return true;
+    if (!ctx().ws || ctx().ws_bytes < FLAG_BYTES + bytes) return false;
+    ws = ctx().ws + FLAG_BYTES;
+    return true;
+}
+size_t with_flags(size_t bytes) { return bytes > 0 ? FLAG_BYTES + align_up(bytes) : 0; }
 
 int plan_for_query(int64_t m, int64_t n, int64_t k, int fmt, int s, int64_t k_block, int pair_set, Plan& pl) {
     if (pair_set != OZAKI_PAIRS_TRIANGLE && pair_set != OZAKI_PAIRS_ALL) return -14;
@@ -684,6 +745,214 @@ int ozaki_linear_loss_grad(int64_t tokens, int64_t vocab, int64_t k, const void*
     a.dH = dH; a.dW = dW; a.lddh = lddh; a.lddw = lddw;
     a.flags = reinterpret_cast<int*>(c.ws);
     HIP_TRY(launch_linear_loss_grad(a, type, piece, c.ws, c.stream));
+    return 0;
+}
+
+size_t ozaki_linear_workspace_bytes(int64_t m, int64_t n, int64_t k, int grad) {
+    if (m < 1 || check_linear_args(m, n, k, nullptr, 0, nullptr, nullptr, false, 0, OZAKI_TYPE_BF16, 0, false, false) != 0) return 0;
+    return with_flags(grad ? linear_grad_bytes(m, n, k, false) : linear_bytes(m, n, k, false));
+}
+size_t ozaki_gated_linear_workspace_bytes(int64_t m, int64_t n, int64_t k, int grad) {
+    if (m < 1 || check_linear_args(m, n, k, nullptr, 0, nullptr, nullptr, false, 0, OZAKI_TYPE_BF16, 0, false, false) != 0) return 0;
+    return with_flags(grad ? linear_grad_bytes(m, n, k, true) : linear_bytes(m, n, k, true));
+}
+
+int ozaki_linear(int64_t m, int64_t n, int64_t k, const void* X, int64_t ldx, const void* W, int64_t ldw, int type, const void* bias, int activation,
+                 const void* R, int64_t ldr, void* Y, int64_t ldy, void* Z, int64_t ldz) {
+    int st = check_linear_args(m, n, k, X, ldx, W, nullptr, false, ldw, type, activation, true, true);
+    if (st == -9) return -10;                        // (bias stands in front of the activation here)
+    if (st != 0 || m == 0) return st;
+    if (!aligned(bias, 2)) return -9;
+    if (!aligned(R, 2)) return -11;
+    if (R && ldr < n) return -12;
+    if (!Y || !aligned(Y, 2)) return -13;
+    if (ldy < n) return -14;
+    if (!aligned(Z, 2)) return -15;
+    if (Z && ldz < n) return -16;
+    LinearArgs a = {};
+    a.X = X; a.W = W; a.bias = bias; a.R = R; a.Y = Y; a.Z = Z;
+    a.m = m; a.n = n; a.k = k; a.ldx = ldx; a.ldw = ldw; a.ldr = ldr; a.ldy = ldy; a.ldz = ldz;
+    a.activation = activation;
+    uint8_t* ws = nullptr;
+    if (!work_memory(linear_bytes(m, n, k, false), ws)) return OZAKI_STATUS_WORKSPACE;
+    a.partial = reinterpret_cast<float*>(ws);
+    HIP_TRY(launch_linear(a, type, ctx().stream));
+    return 0;
+}
+
+int ozaki_gated_linear(int64_t m, int64_t n, int64_t k, const void* X, int64_t ldx, const void* Wg, const void* Wu, int64_t ldw, int type, int activation,
+                       void* Y, int64_t ldy, void* G, int64_t ldg, void* U, int64_t ldu) {
+    const int st = check_linear_args(m, n, k, X, ldx, Wg, Wu, true, ldw, type, activation, true, true);
+    if (st != 0 || m == 0) return st;
+    if (!Y || !aligned(Y, 2)) return -11;
+    if (ldy < n) return -12;
+    if (!aligned(G, 2)) return -13;
+    if (G && ldg < n) return -14;
+    if (!aligned(U, 2) || (G != nullptr) != (U != nullptr)) return -15;
+    if (U && ldu < n) return -16;
+    LinearArgs a = {};
+    a.X = X; a.W = Wg; a.W2 = Wu; a.Y = Y; a.Z = G; a.U = U;
+    a.m = m; a.n = n; a.k = k; a.ldx = ldx; a.ldw = ldw; a.ldy = ldy; a.ldz = ldg; a.ldu = ldu;
+    a.activation = activation;
+    uint8_t* ws = nullptr;
+    if (!work_memory(linear_bytes(m, n, k, true), ws)) return OZAKI_STATUS_WORKSPACE;
+    a.partial = reinterpret_cast<float*>(ws);
+    HIP_TRY(launch_linear(a, type, ctx().stream));
+    return 0;
+}
+
+int ozaki_linear_grad(int64_t m, int64_t n, int64_t k, const void* X, int64_t ldx, const void* W, int64_t ldw, int type, int activation, const void* Z,
+                      int64_t ldz, const void* dY, int64_t lddy, void* dX, int64_t lddx, void* dW, int64_t lddw, float* dbias) {
+    int st = check_linear_args(m, n, k, X, ldx, W, nullptr, false, ldw, type, activation, dW != nullptr, dX != nullptr);
+    if (st != 0) return st;
+    if (n > OZAKI_MAX_EXTENT / 2) return -2;
+    if (m > 0 && activation != OZAKI_ACTIVATION_NONE && (!Z || !aligned16(Z))) return -10;
+    if (m > 0 && activation != OZAKI_ACTIVATION_NONE && !stride_ok(ldz, n, 2)) return -11;
+    if (m > 0 && (!dY || !aligned16(dY))) return -12;
+    if (m > 0 && !stride_ok(lddy, n, 2)) return -13;
+    if ((!dX && !dW && !dbias) || !aligned(dX, 2)) return -14;
+    if (dX && lddx < k) return -15;
+    if (!aligned(dW, 2)) return -16;
+    if (dW && lddw < k) return -17;
+    if (!aligned(dbias, 4)) return -18;
+    const hipStream_t stream = ctx().stream;
+    if (m == 0) {
+        if (dW) HIP_TRY(launch_zero_rows(dW, n, k, lddw, stream));
+        if (dbias) HIP_TRY(launch_zero_rows(dbias, 1, 2 * n, 2 * n, stream));
+        return 0;
+    }
+    LinearGradArgs a = {};
+    a.X = X; a.W = W; a.Z = Z; a.dY = dY; a.dX = dX; a.dW = dW; a.dbias = dbias;
+    a.m = m; a.n = n; a.k = k; a.ldx = ldx; a.ldw = ldw; a.ldz = ldz; a.lddy = lddy; a.lddx = lddx; a.lddw = lddw;
+    a.activation = activation;
+    if (!work_memory(linear_grad_bytes(m, n, k, false), a.ws)) return OZAKI_STATUS_WORKSPACE;
+    HIP_TRY(launch_linear_grad(a, type, stream));
+    return 0;
+}
+
+int ozaki_gated_linear_grad(int64_t m, int64_t n, int64_t k, const void* X, int64_t ldx, const void* Wg, const void* Wu, int64_t ldw, int type,
+                            int activation, const void* G, int64_t ldg, const void* U, int64_t ldu, const void* dY, int64_t lddy, void* dX,
+                            int64_t lddx, void* dWg, void* dWu, int64_t lddw) {
+    const int st = check_linear_args(m, n, k, X, ldx, Wg, Wu, true, ldw, type, activation, dWg || dWu, dX != nullptr);
+    if (st != 0) return st;
+    if (n > OZAKI_MAX_EXTENT / 2) return -2;
+    if (m > 0 && (!G || !aligned16(G))) return -11;
+    if (m > 0 && !stride_ok(ldg, n, 2)) return -12;
+    if (m > 0 && (!U || !aligned16(U))) return -13;
+    if (m > 0 && !stride_ok(ldu, n, 2)) return -14;
+    if (m > 0 && (!dY || !aligned16(dY))) return -15;
+    if (m > 0 && !stride_ok(lddy, n, 2)) return -16;
+    if ((!dX && !dWg && !dWu) || !aligned(dX, 2)) return -17;
+    if (dX && lddx < k) return -18;
+    if (!aligned(dWg, 2)) return -19;
+    if (!aligned(dWu, 2)) return -20;
+    if ((dWg || dWu) && lddw < k) return -21;
+    const hipStream_t stream = ctx().stream;
+    if (m == 0) {
+        if (dWg) HIP_TRY(launch_zero_rows(dWg, n, k, lddw, stream));
+        if (dWu) HIP_TRY(launch_zero_rows(dWu, n, k, lddw, stream));
+        return 0;
+    }
+    LinearGradArgs a = {};
+    a.X = X; a.W = Wg; a.W2 = Wu; a.Z = G; a.U = U; a.dY = dY; a.dX = dX; a.dW = dWg; a.dW2 = dWu;
+    a.m = m; a.n = n; a.k = k; a.ldx = ldx; a.ldw = ldw; a.ldz = ldg; a.ldu = ldu; a.lddy = lddy; a.lddx = lddx; a.lddw = lddw;
+    a.activation = activation;
+    a.pair = true;
+    if (!work_memory(linear_grad_bytes(m, n, k, true), a.ws)) return OZAKI_STATUS_WORKSPACE;
+    HIP_TRY(launch_linear_grad(a, type, stream));
+    return 0;
+}
+
+size_t ozaki_block_norm_workspace_bytes(int64_t rows, int64_t k, int64_t group) {
+    if (rows < 1 || !extent_ok(rows) || k < 1 || k > OZAKI_MAX_NORM || group < 0) return 0;
+    return with_flags(block_norm_grad_bytes(rows, k, group));
+}
+
+int ozaki_block_norm(int64_t rows, int64_t k, const void* X, int64_t ldx, int type, const float* w_post, const float* gate, int64_t group, float scale,
+                     float eps, const void* R, int64_t ldr, int type_r, void* R_out, int64_t ldro, const float* w_pre, void* H, int64_t ldh) {
+    const int st = check_norm_args(rows, k, X, ldx, type, w_post, gate, group, scale, eps, type_r);
+    if (st != 0 || rows == 0) return st;
+    if (!X && !R) return -3;
+    if (!aligned16(R)) return -11;
+    if (R && !rows_ok(ldr, k, type_r)) return -12;
+    if (!aligned(R_out, type_bytes(type_r)) || (R_out && !X) || (!R_out && !H)) return -14;
+    if (R_out && ldro < k) return -15;
+    if (!aligned(w_pre, 4) || (H && !w_pre)) return -16;
+    if (!aligned(H, type_bytes(type))) return -17;
+    if (H && ldh < k) return -18;
+    BlockNormArgs a = {};
+    a.X = X; a.w_post = w_post; a.gate = gate; a.w_pre = w_pre; a.R = R; a.R_out = R_out; a.H = H;
+    a.rows = rows; a.k = k; a.ldx = ldx; a.ldr = ldr; a.group = group; a.scale = scale; a.eps = eps; a.ldro = ldro; a.ldh = ldh;
+    HIP_TRY(launch_block_norm(a, type, type_r, ctx().stream));
+    return 0;
+}
+
+int ozaki_block_norm_grad(int64_t rows, int64_t k, const void* X, int64_t ldx, int type, const float* w_post, const float* gate, int64_t group,
+                          float scale, float eps, const void* R_out, int64_t ldro, int type_r, const float* w_pre, const void* dH, int64_t lddh,
+                          const void* dR_out, int64_t lddro, void* dX, int64_t lddx, void* dR, int64_t lddr, float* dw_post, float* dgate,
+                          float* dw_pre) {
+    const int st = check_norm_args(rows, k, X, ldx, type, w_post, gate, group, scale, eps, type_r);
+    if (st != 0) return st;
+    if (!X && (dX || dw_post || dgate) && rows > 0) return -3;
+    if (!aligned16(R_out) || (rows > 0 && dH && !R_out)) return -11;
+    if (rows > 0 && dH && !rows_ok(ldro, k, type_r)) return -12;
+    if (!aligned(w_pre, 4) || (rows > 0 && dH && !w_pre)) return -14;
+    if (!aligned16(dH) || (rows > 0 && !dH && !dR_out)) return -15;
+    if (dH && !rows_ok(lddh, k, type)) return -16;
+    if (!aligned16(dR_out)) return -17;
+    if (dR_out && !rows_ok(lddro, k, type_r)) return -18;
+    if (!aligned(dX, type_bytes(type)) || (!dX && !dR && !dw_post && !dgate && !dw_pre)) return -19;
+    if (dX && lddx < k) return -20;
+    if (!aligned(dR, type_bytes(type_r))) return -21;
+    if (dR && lddr < k) return -22;
+    if (!aligned(dw_post, 4) || (rows > 0 && dw_post && !w_post)) return -23;
+    if (!aligned(dgate, 4) || (rows > 0 && dgate && !gate)) return -24;
+    if (!aligned(dw_pre, 4) || (rows > 0 && dw_pre && !dH)) return -25;
+    const hipStream_t stream = ctx().stream;
+    if (rows == 0) {
+        if (dw_post) HIP_TRY(launch_zero_rows(dw_post, 1, 2 * k, 2 * k, stream));
+        if (dw_pre) HIP_TRY(launch_zero_rows(dw_pre, 1, 2 * k, 2 * k, stream));
+        return 0;
+    }
+    BlockNormArgs a = {};
+    a.X = X; a.w_post = w_post; a.gate = gate; a.w_pre = w_pre; a.R = R_out; a.dH = dH; a.dR_out = dR_out; a.dX = dX; a.dR = dR;
+    a.dw_post = dw_post; a.dgate = dgate; a.dw_pre = dw_pre;
+    a.rows = rows; a.k = k; a.ldx = ldx; a.ldr = ldro; a.group = group; a.scale = scale; a.eps = eps;
+    a.lddh = lddh; a.lddro = lddro; a.lddx = lddx; a.lddr = lddr;
+    if ((dw_post || dgate || dw_pre) && !work_memory(block_norm_grad_bytes(rows, k, gate ? group : 0), a.ws)) return OZAKI_STATUS_WORKSPACE;
+    HIP_TRY(launch_block_norm_grad(a, type, type_r, stream));
+    return 0;
+}
+
+size_t ozaki_gradient_norm_workspace_bytes(int64_t count) { return count < 0 || count > 0x7FFFFFFF ? 0 : with_flags(gradient_norm_bytes(count > 0 ? count : 1)); }
+
+int ozaki_gradient_norm(int count, const void* const* tensors, const int64_t* sizes, const int* types, float scale, float* norm) {
+    const int st = check_tensors(count, tensors, sizes, types, scale);
+    if (st != 0) return st;
+    if (!norm || !aligned(norm, 4)) return -6;
+    ClipArgs a = {count, tensors, sizes, types, nullptr, scale, 0.0f, norm, false, nullptr};
+    uint8_t* ws = nullptr;
+    if (!work_memory(gradient_norm_bytes(count > 0 ? count : 1), ws)) return OZAKI_STATUS_WORKSPACE;
+    a.partial = reinterpret_cast<double*>(ws);
+    HIP_TRY(launch_clip(a, ctx().stream));
+    return 0;
+}
+
+int ozaki_clip_gradients(int count, const void* const* tensors, const int64_t* sizes, const int* types, float scale, float max_norm, void* const* out,
+                         float* norm, int given) {
+    const int st = check_tensors(count, tensors, sizes, types, scale);
+    if (st != 0) return st;
+    if (!(max_norm >= 0.0f)) return -6;
+    if (count > 0 && !out) return -7;
+    for (int i = 0; i < count; ++i)
+        if (sizes[i] > 0 && (!out[i] || !aligned(out[i], type_bytes(types[i])))) return -7;
+    if (!norm || !aligned(norm, 4)) return -8;
+    if (given != 0 && given != 1) return -9;
+    ClipArgs a = {count, tensors, sizes, types, out, scale, max_norm, norm, given != 0, nullptr};
+    uint8_t* ws = nullptr;
+    if (!given && !work_memory(gradient_norm_bytes(count > 0 ? count : 1), ws)) return OZAKI_STATUS_WORKSPACE;
+    a.partial = reinterpret_cast<double*>(ws);
+    HIP_TRY(launch_clip(a, ctx().stream));
     return 0;
 }
 

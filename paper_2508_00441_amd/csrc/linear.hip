@@ -1,0 +1,336 @@
+// A linear layer with what follows it, and a pair of linear layers whose results are multiplied:
+//     z = x W^T + bias,  y = act(z) + r            and            g = x Wg^T,  u = x Wu^T,  y = act(g) * u.
+//
+// One product of 16-bit elements in FP32 on the matrix unit (tile_product.hpp); everything behind it happens on a tile in LDS on its way to memory, in
+// FP32, with one rounding of each result.  Of a pair, half of a tile's vectors of weights are Wg's and half are Wu's, so that a lane holds both
+// factors of its elements and neither reaches memory unless it is asked for.
+#include "block_operators.hpp"
+#include "layout.hpp"
+#include "tile_product.hpp"
+
+namespace ozaki {
+namespace {
+
+constexpr int kind_of(int type) { return type == TYPE_F16 ? KIND_F16 : KIND_BF16; }
+
+template <typename T> struct Eight { typedef T type __attribute__((ext_vector_type(8))); };
+template <typename T> __device__ __forceinline__ v8f32 eight_at(const T* p) { return __builtin_convertvector(*reinterpret_cast<const typename Eight<T>::type*>(p), v8f32); }
+
+// What becomes of the sums of row m, column c (both of the whole matrices) and its seven neighbours, or of one alone.
+template <int TYPE, bool PAIR, bool STREAMED>
+struct Epilogue {
+    typedef typename Element<TYPE>::type T;
+    typedef typename Eight<T>::type eight;
+    const LinearArgs& a;
+    bool wide;                       // every matrix has rows that start at multiples of 16 bytes
+
+    __device__ __forceinline__ explicit Epilogue(const LinearArgs& args) : a(args) {
+        const auto fits = [](const void* p, int64_t ld) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0); };
+        wide = fits(a.Y, a.ldy) && fits(a.Z, a.ldz) && (PAIR ? fits(a.U, a.ldu) : fits(a.R, a.ldr) && fits(a.bias, 8));
+    }
+    static __device__ __forceinline__ void put(void* to, int64_t at, v8f32 v) {
+        eight* const p = reinterpret_cast<eight*>(static_cast<T*>(to) + at);
+        const eight w = __builtin_convertvector(v, eight);
+        if constexpr (STREAMED) __builtin_nontemporal_store(w, p);
+        else *p = w;
+    }
+    __device__ __forceinline__ void piece(int64_t m, int64_t c, v8f32 v, v8f32 u) const {
+        if constexpr (PAIR) {
+            if (a.Z != nullptr) {
+                put(a.Z, m * a.ldz + c, v);
+                put(a.U, m * a.ldu + c, u);
+            }
+        } else {
+            if (a.bias != nullptr) v += eight_at(static_cast<const T*>(a.bias) + c);
+            if (a.Z != nullptr) put(a.Z, m * a.ldz + c, v);
+        }
+        with_activation(a.activation, [&](auto act) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[q] = activated<decltype(act)::value>(v[q]);
+        });
+        if constexpr (PAIR) v *= u;
+        else if (a.R != nullptr) v += eight_at(static_cast<const T*>(a.R) + m * a.ldr + c);
+        put(a.Y, m * a.ldy + c, v);
+    }
+    __device__ __forceinline__ void one(int64_t m, int64_t c, float v, float u) const {
+        if constexpr (PAIR) {
+            if (a.Z != nullptr) {
+                static_cast<T*>(a.Z)[m * a.ldz + c] = (T)v;
+                static_cast<T*>(a.U)[m * a.ldu + c] = (T)u;
+            }
+        } else {
+            if (a.bias != nullptr) v += (float)static_cast<const T*>(a.bias)[c];
+            if (a.Z != nullptr) static_cast<T*>(a.Z)[m * a.ldz + c] = (T)v;
+        }
+        with_activation(a.activation, [&](auto act) { v = activated<decltype(act)::value>(v); });
+        if constexpr (PAIR) v *= u;
+        else if (a.R != nullptr) v += (float)static_cast<const T*>(a.R)[m * a.ldr + c];
+        static_cast<T*>(a.Y)[m * a.ldy + c] = (T)v;
+    }
+};
+
+// A share of the inner dimension: sums as they are, [share][m][n in fours], a pair's second factor behind all shares of the first.
+struct Partial {
+    float* to;
+    int64_t ld, second;
+    bool wide = true;
+    template <typename V> __device__ __forceinline__ void put(int64_t at, V v) const { *reinterpret_cast<V*>(to + at) = v; }
+    __device__ __forceinline__ void piece(int64_t m, int64_t c, v8f32 v, v8f32 u) const {
+        const int64_t at = m * ld + c;
+        put(at, __builtin_shufflevector(v, v, 0, 1, 2, 3));
+        put(at + 4, __builtin_shufflevector(v, v, 4, 5, 6, 7));
+        if (second == 0) return;
+        put(at + second, __builtin_shufflevector(u, u, 0, 1, 2, 3));
+        put(at + second + 4, __builtin_shufflevector(u, u, 4, 5, 6, 7));
+    }
+    __device__ __forceinline__ void one(int64_t m, int64_t c, float v, float u) const {
+        to[m * ld + c] = v;
+        if (second != 0) to[m * ld + c + second] = u;
+    }
+};
+
+// The tile that P::multiply has left goes through LDS, 16 rows of every wave at a time in 32 bits: from there eight neighbouring columns are a
+// thread's, so that rows are read and written in 16-byte pieces of neighbouring lanes.  Where matrices' rows are not aligned to that, a thread has a column.
+template <typename P, typename E>
+__device__ __forceinline__ void put_tile(uint8_t* lds, const v4f32 (&acc)[P::FN][P::FM], int64_t m0, int64_t n0, int64_t left_m, int64_t left_n, const E& e) {
+    constexpr int COLUMNS = P::PAIR ? P::TN / 2 : P::TN, STRIDE = P::TN * 4 + 16, PIECES = COLUMNS / 8, ROWS = P::WM * 16, HALF = P::PAIR ? P::FN / 2 : P::FN;
+    static_assert(ROWS * STRIDE <= P::LDS_BYTES && P::THREADS % PIECES == 0 && P::THREADS % COLUMNS == 0, "");
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wn = wave / P::WM, wm = wave % P::WM;
+    const int columns = left_n < COLUMNS ? (int)left_n : COLUMNS, whole = e.wide ? columns / 8 * 8 : 0;
+#pragma unroll
+    for (int j = 0; j < P::FM; ++j) {
+        uint8_t* const mine = lds + (wm * 16 + (lane & 15)) * STRIDE + (wn * HALF * 16 + 4 * (lane >> 4)) * 4;
+#pragma unroll
+        for (int i = 0; i < P::FN; ++i) *reinterpret_cast<v4f32*>(mine + (i < HALF ? i * 64 : COLUMNS * 4 + (i - HALF) * 64)) = acc[i][j];
+        __syncthreads();
+        const auto row_of = [&](int r) -> int64_t { return ((r >> 4) * P::FM + j) * 16 + (r & 15); };
+        const int column = threadIdx.x % PIECES * 8;
+        if (column < whole) {
+            for (int r = threadIdx.x / PIECES; r < ROWS; r += P::THREADS / PIECES) {
+                const int64_t m = row_of(r);
+                if (m >= left_m) continue;
+                const float* const from = reinterpret_cast<const float*>(lds + r * STRIDE) + column;
+                v8f32 v, u = {};
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    v[q] = from[q];
+                    if (P::PAIR) u[q] = from[COLUMNS + q];
+                }
+                e.piece(m0 + m, n0 + column, v, u);
+            }
+        }
+        const int c = whole + threadIdx.x % COLUMNS;
+        if (c < columns) {
+            for (int r = threadIdx.x / COLUMNS; r < ROWS; r += P::THREADS / COLUMNS) {
+                const int64_t m = row_of(r);
+                if (m >= left_m) continue;
+                const float* const from = reinterpret_cast<const float*>(lds + r * STRIDE) + c;
+                e.one(m0 + m, n0 + c, from[0], P::PAIR ? from[COLUMNS] : 0.0f);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+struct LinearWork {
+    LinearArgs a;
+    int steps, splits;
+    int tiles_m, tiles_n;
+    WorkOrder order;
+};
+
+template <typename P, int TYPE>
+__device__ __forceinline__ void linear_body(const LinearWork& w) {
+    constexpr bool PAIR = P::PAIR;
+    constexpr int COLUMNS = PAIR ? P::TN / 2 : P::TN;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[P::LDS_BYTES];
+    const LinearArgs& a = w.a;
+    const WorkItem item = work_item(blockIdx.x, gridDim.x, w.order, w.tiles_m, w.tiles_n);
+    const int64_t m0 = (int64_t)item.bm * P::TM, n0 = (int64_t)item.bn * COLUMNS, left_m = a.m - m0, left_n = a.n - n0;
+    TileOperand X{static_cast<const uint8_t*>(a.W) + n0 * a.ldw * 2, a.ldw * 2, (int)(left_n < COLUMNS ? left_n : COLUMNS), nullptr, 0};
+    if constexpr (PAIR) X.second = static_cast<const uint8_t*>(a.W2) + n0 * a.ldw * 2;
+    const TileOperand Y{static_cast<const uint8_t*>(a.X) + m0 * a.ldx * 2, a.ldx * 2, (int)(left_m < P::TM ? left_m : P::TM), nullptr, 0};
+    const int split = item.gi;
+    v4f32 acc[P::FN][P::FM] = {};
+    P::multiply(lds, X, Y, a.k * 2, split_begin(w.steps, w.splits, split), split_begin(w.steps, w.splits, split + 1), acc);
+    if (w.splits > 1) {
+        const int64_t ld = in_fours(a.n);
+        put_tile<P>(lds, acc, m0, n0, left_m, in_fours(left_n), Partial{a.partial + split * a.m * ld, ld, PAIR ? w.splits * a.m * ld : 0});
+    } else {
+        put_tile<P>(lds, acc, m0, n0, left_m, left_n, Epilogue<TYPE, PAIR, (P::THREADS > 256)>(a));
+    }
+}
+
+template <int TYPE, bool PAIR>
+__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) linear_large_kernel(const LinearWork w) {
+    linear_body<PairedTile<kind_of(TYPE), false, false, PAIR>, TYPE>(w);
+}
+template <int TYPE, bool PAIR>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) linear_middle_kernel(const LinearWork w) {
+    linear_body<Tile<kind_of(TYPE), 2, 2, 4, 4, 2, false, false, PAIR>, TYPE>(w);
+}
+template <int TYPE, bool PAIR>
+__global__ void __launch_bounds__(256) linear_small_kernel(const LinearWork w) {
+    linear_body<Tile<kind_of(TYPE), 2, 2, 2, 2, 4, false, false, PAIR>, TYPE>(w);
+}
+
+// Up to sixteen vectors of X: no tile in LDS.  A workgroup of FEW_WAVES waves takes sixteen vectors of W (of each, of a pair), a wave every
+// FEW_WAVES-th step of 64 elements, straight from memory into registers; the waves' sums are added in LDS, in their order.
+constexpr int FEW = 16, FEW_WAVES = 8, AHEAD = 4;
+
+template <int TYPE, bool PAIR>
+__global__ void __launch_bounds__(FEW_WAVES * 64) linear_few_kernel(const LinearArgs a, const int splits) {
+    constexpr int FACTORS = PAIR ? 2 : 1;
+    __shared__ __attribute__((aligned(16))) v4f32 sums[FACTORS][FEW_WAVES][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, row = lane & 15;
+    const int split = blockIdx.x % splits;
+    const int64_t n0 = (int64_t)(blockIdx.x / splits) * 16, bytes = a.k * 2;
+    const int left_n = a.n - n0 < 16 ? (int)(a.n - n0) : 16, steps = (int)div_up(bytes, STEP_BYTES);
+    const int begin = split_begin(steps, splits, split), end = split_begin(steps, splits, split + 1);
+    const uint8_t* at[FACTORS + 1];                  // this lane's vectors, from piece lane / 16 on: of W, of W2, of X
+    const int64_t w_row = (n0 + (row < left_n ? row : left_n - 1)) * a.ldw * 2 + g * 16;
+    at[0] = static_cast<const uint8_t*>(a.W) + w_row;
+    if constexpr (PAIR) at[1] = static_cast<const uint8_t*>(a.W2) + w_row;
+    at[FACTORS] = static_cast<const uint8_t*>(a.X) + (row < a.m ? row : a.m - 1) * a.ldx * 2 + g * 16;
+    v4i32 pieces[AHEAD][FACTORS + 1][2];
+    // (behind the end of the vectors something that is there is read and not used)
+    const auto load = [&](int u, int s) {
+        const int64_t from = (int64_t)(s < end ? s : end - 1) * STEP_BYTES;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t off = from + g * 16 + h * 64 < bytes ? from + h * 64 : -(int64_t)g * 16;
+#pragma unroll
+            for (int o = 0; o <= FACTORS; ++o) pieces[u][o][h] = *reinterpret_cast<const v4i32*>(at[o] + off);
+        }
+    };
+    v4f32 acc[FACTORS] = {};
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) load(u, begin + wave + u * FEW_WAVES);
+    for (int first = begin + wave; first < end; first += FEW_WAVES * AHEAD) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int s = first + u * FEW_WAVES;
+            if (s >= end) break;
+            const int64_t left = bytes - (int64_t)s * STEP_BYTES;
+            if (left < STEP_BYTES) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int o = 0; o <= FACTORS; ++o) {
+                        const int keep = (int)left - g * 16 - h * 64;
+                        pieces[u][o][h] = first_bytes(pieces[u][o][h], keep < 0 ? 0 : keep);
+                    }
+            }
+#pragma unroll
+            for (int o = 0; o < FACTORS; ++o)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if constexpr (TYPE == TYPE_BF16)
+                        acc[o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf16, pieces[u][o][h]), __builtin_bit_cast(v8bf16, pieces[u][FACTORS][h]), acc[o], 0, 0, 0);
+                    else
+                        acc[o] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8f16, pieces[u][o][h]), __builtin_bit_cast(v8f16, pieces[u][FACTORS][h]), acc[o], 0, 0, 0);
+                }
+            if (first + FEW_WAVES * AHEAD < end) load(u, s + FEW_WAVES * AHEAD);
+        }
+    }
+#pragma unroll
+    for (int o = 0; o < FACTORS; ++o) sums[o][wave][lane] = acc[o];
+    __syncthreads();
+    const int n = threadIdx.x & 15, m = threadIdx.x >> 4;
+    if (threadIdx.x >= 256 || m >= a.m || n >= left_n) return;
+    float total[2] = {};
+#pragma unroll
+    for (int w = 0; w < FEW_WAVES; ++w)
+#pragma unroll
+        for (int o = 0; o < FACTORS; ++o) total[o] += reinterpret_cast<const float*>(&sums[o][w][(n >> 2) * 16 + m])[n & 3];
+    if (splits > 1) {
+        const int64_t ld = in_fours(a.n);
+        Partial{a.partial + split * a.m * ld, ld, PAIR ? splits * a.m * ld : 0}.one(m, n0 + n, total[0], total[1]);
+    } else {
+        Epilogue<TYPE, PAIR, false>(a).one(m, n0 + n, total[0], total[1]);
+    }
+}
+
+// sums the shares of the inner dimension in their order, eight columns a thread
+template <int TYPE, bool PAIR>
+__global__ void __launch_bounds__(256) linear_join_kernel(const LinearArgs a, const int splits) {
+    const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8, ld = in_fours(a.n);
+    if (c >= a.n) return;
+    const Epilogue<TYPE, PAIR, false> e(a);
+    const bool more = c + 4 < ld;
+    for (int64_t m = blockIdx.y; m < a.m; m += gridDim.y) {
+        v8f32 v[2] = {};
+#pragma unroll
+        for (int o = 0; o < (PAIR ? 2 : 1); ++o) {
+            const float* from = a.partial + (o * splits * a.m + m) * ld + c;
+            v4f32 lo = {}, hi = {};
+#pragma unroll 4
+            for (int s = 0; s < splits; ++s, from += a.m * ld) {
+                lo += *reinterpret_cast<const v4f32*>(from);
+                if (more) hi += *reinterpret_cast<const v4f32*>(from + 4);
+            }
+            v[o] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+        if (e.wide && c + 8 <= a.n) {
+            e.piece(m, c, v[0], v[1]);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                if (c + q < a.n) e.one(m, c + q, v[0][q], v[1][q]);
+        }
+    }
+}
+
+enum { VECTORS, SMALL, MIDDLE, LARGE };
+struct Shape { int kind, tm, tn, splits; };
+// By how many tiles there are for 256 compute units; `columns` counts both factors of a pair.
+Shape shape_of(int64_t m, int64_t n, int64_t k, bool pair) {
+    const int64_t steps = div_up(k * 2, STEP_BYTES), columns = pair ? 2 * n : n;
+    const auto shares = [](int64_t want, int64_t most) {
+        const int64_t s = want < most ? want : most;
+        return (int)(s < 1 ? 1 : s > 16 ? 16 : s);
+    };
+    if (m <= FEW) return Shape{VECTORS, FEW, 16, steps < 96 ? 1 : shares(256 / div_up(n, 16), steps / 32)};
+    const int64_t middle = div_up(m, 128) * div_up(columns, 128), least = m < columns ? m : columns;
+    if (middle >= 256 && least > 64) return middle <= 512 || least <= 128 ? Shape{MIDDLE, 128, pair ? 64 : 128, 1} : Shape{LARGE, 256, pair ? 128 : 256, 1};
+    return Shape{SMALL, 64, pair ? 32 : 64, shares(256 / (div_up(m, 64) * div_up(columns, 64)), steps / 4)};
+}
+
+template <int TYPE, bool PAIR>
+hipError_t launch_kind(const LinearArgs& a, Shape s, hipStream_t st) {
+    LinearWork w;
+    w.a = a;
+    w.steps = (int)div_up(a.k * 2, STEP_BYTES);
+    w.splits = s.splits;
+    w.tiles_m = (int)div_up(a.m, s.tm);
+    w.tiles_n = (int)div_up(a.n, s.tn);
+    w.order = WorkOrder{s.kind == LARGE ? 32 : 64, 8};
+    const unsigned blocks = (unsigned)((int64_t)w.tiles_m * w.tiles_n * s.splits);
+    if (s.kind == VECTORS) hipLaunchKernelGGL((linear_few_kernel<TYPE, PAIR>), dim3(blocks), dim3(FEW_WAVES * 64), 0, st, a, s.splits);
+    else if (s.kind == SMALL) hipLaunchKernelGGL((linear_small_kernel<TYPE, PAIR>), dim3(blocks), dim3(256), 0, st, w);
+    else if (s.kind == MIDDLE) hipLaunchKernelGGL((linear_middle_kernel<TYPE, PAIR>), dim3(blocks), dim3(256), 0, st, w);
+    else hipLaunchKernelGGL((linear_large_kernel<TYPE, PAIR>), dim3(blocks), dim3(512), 0, st, w);
+    if (s.splits > 1) {
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL((linear_join_kernel<TYPE, PAIR>), dim3((unsigned)div_up(a.n, 2048), (unsigned)(a.m < 65535 ? a.m : 65535)), dim3(256), 0, st, a, s.splits);
+    }
+    return hipGetLastError();
+}
+
+template <int TYPE>
+hipError_t launch_typed(const LinearArgs& a, hipStream_t st) {
+    const bool pair = a.W2 != nullptr;
+    const Shape s = shape_of(a.m, a.n, a.k, pair);
+    return pair ? launch_kind<TYPE, true>(a, s, st) : launch_kind<TYPE, false>(a, s, st);
+}
+
+}  // namespace
+
+size_t linear_bytes(int64_t m, int64_t n, int64_t k, bool pair) {
+    const int splits = shape_of(m, n, k, pair).splits;
+    return splits > 1 ? (size_t)splits * m * in_fours(n) * sizeof(float) * (pair ? 2 : 1) : 0;
+}
+hipError_t launch_linear(const LinearArgs& a, int type, hipStream_t st) { return type == TYPE_F16 ? launch_typed<TYPE_F16>(a, st) : launch_typed<TYPE_BF16>(a, st); }
+
+}  // namespace ozaki

@@ -1,0 +1,329 @@
+// Gradients of a linear layer with its activation, and of a pair of linear layers whose results are multiplied (linear.hip):
+//     dz = dy act'(z),                         dx = dz W,               dW = dz^T x,   dbias = sum over rows of dz
+//     dg = dy u act'(g),  du = dy act(g),      dx = dg Wg + du Wu,      dWg = dg^T x,  dWu = du^T x.
+//
+// dz (dg, du) is formed once, in 16 bits: its rounding is of the size of the results' own.  dbias is summed in the same pass, of what has not been
+// rounded.  Without an activation dz is dy itself.  Both products are sums over 16-bit elements in FP32 on the matrix unit (tile_product.hpp); W in dx, and
+// dz and x in dW, lie across the inner dimension and are turned on the way from LDS to registers.  The two terms of a pair's dx are one sum.
+// Where there are few tiles the inner dimension is cut into shares whose sums meet in work memory, in their order.
+#include "block_operators.hpp"
+#include "layout.hpp"
+#include "tile_product.hpp"
+
+namespace ozaki {
+namespace {
+
+constexpr int kind_of(int type) { return type == TYPE_F16 ? KIND_F16 : KIND_BF16; }
+size_t up(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
+int64_t in_eights(int64_t n) { return div_up(n, 8) * 8; }
+
+// ---- dz and dbias ------------------------------------------------------------------------------------------------
+struct SlopeWork {
+    const void* Z;
+    const void* U;
+    const void* dY;
+    void* dZ;                // null: only dbias is wanted
+    void* dU;
+    float* sums;             // null: no dbias; [chunk][columns in eights], or dbias itself where there is one chunk
+    int64_t m, n, ldz, ldu, lddy, ld;        // ld: of dZ and dU
+    int64_t rows;            // of a chunk
+    int activation;
+    bool whole;              // `sums` is dbias
+};
+constexpr int SLOPE_WAVES = 4, SLOPE_COLUMNS = 512;
+
+// A wave has eight columns a lane and every fourth row of a chunk.
+template <int TYPE, bool PAIR>
+__global__ void __launch_bounds__(SLOPE_WAVES * 64) linear_slope_kernel(const SlopeWork w) {
+    typedef typename Element<TYPE>::type T;
+    typedef T eight __attribute__((ext_vector_type(8)));
+    __shared__ v8f32 shares[SLOPE_WAVES][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t c = ((int64_t)blockIdx.x * 64 + lane) * 8, first = (int64_t)blockIdx.y * w.rows, end = first + w.rows < w.m ? first + w.rows : w.m;
+    const int there = w.n - c < 8 ? (int)(w.n - c) : 8;          // columns; behind them the pieces hold anything
+    v8f32 sum = {};
+    if (there > 0) {
+        with_activation(w.activation, [&](auto act) {
+            constexpr int ACT = decltype(act)::value;
+            const auto read = [&](const void* p, int64_t ld, int64_t r) { return __builtin_convertvector(*reinterpret_cast<const eight*>(static_cast<const T*>(p) + r * ld + c), v8f32); };
+            const auto write = [&](void* p, int64_t r, v8f32 v) { *reinterpret_cast<eight*>(static_cast<T*>(p) + r * w.ld + c) = __builtin_convertvector(v, eight); };
+#pragma unroll 2
+            for (int64_t r = first + wave; r < end; r += SLOPE_WAVES) {
+                v8f32 d = read(w.dY, w.lddy, r), z = {}, u = {};
+                if constexpr (ACT != ACT_NONE || PAIR) z = read(w.Z, w.ldz, r);
+                if constexpr (PAIR) u = read(w.U, w.ldu, r);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const Activation a = activation_of<ACT>(z[q]);
+                    if constexpr (PAIR) {
+                        z[q] = q < there ? d[q] * u[q] * a.slope : 0.0f;
+                        u[q] = q < there ? d[q] * a.value : 0.0f;
+                    } else {
+                        z[q] = q < there ? d[q] * a.slope : 0.0f;
+                    }
+                }
+                if (w.dZ != nullptr) write(w.dZ, r, z);
+                if constexpr (PAIR) write(w.dU, r, u);
+                sum += z;
+            }
+        });
+    }
+    if (PAIR || w.sums == nullptr) return;
+    shares[wave][lane] = sum;
+    __syncthreads();
+    if (wave != 0 || there <= 0) return;
+#pragma unroll
+    for (int i = 1; i < SLOPE_WAVES; ++i) sum += shares[i][lane];
+    float* const to = w.sums + (w.whole ? 0 : blockIdx.y * w.ld) + c;
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+        if (q < there) to[q] = sum[q];
+}
+
+// the chunks' sums, in an order of their own that depends on sizes only: 64 columns a workgroup, four shares of the chunks
+__global__ void __launch_bounds__(256) linear_bias_join_kernel(const float* sums, int64_t chunks, int64_t n, int64_t ld, float* dbias) {
+    __shared__ float shares[4][64];
+    const int lane = threadIdx.x & 63, share = threadIdx.x >> 6;
+    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    float sum = 0.0f;
+    if (c < n) {
+#pragma unroll 8
+        for (int64_t i = share; i < chunks; i += 4) sum += sums[i * ld + c];
+    }
+    shares[share][lane] = sum;
+    __syncthreads();
+    if (share == 0 && c < n) dbias[c] = ((shares[0][lane] + shares[1][lane]) + shares[2][lane]) + shares[3][lane];
+}
+
+// ---- products ----------------------------------------------------------------------------------------------------
+// D = sum of the terms X Y^T; rows of Y are D's rows.  A pair's dX has two terms; a pair's dW is two results, one behind the other in `tiles_m`.
+struct ProductWork {
+    const uint8_t* X[2];
+    const uint8_t* Y[2];
+    void* D[2];
+    int64_t ldx, ldy, ldd;   // ldx, ldy in bytes
+    int64_t elements;        // of the inner dimension
+    int64_t m, n;
+    float* partial;          // splits > 1: [result][split][m][n in fours]
+    int terms, results;
+    int steps, splits;       // steps: of one term
+    int tiles_m, tiles_n;    // of one result
+    WorkOrder order;
+};
+
+template <typename P, typename T, bool YT>
+__device__ __forceinline__ void product_body(const ProductWork& w) {
+    __shared__ __attribute__((aligned(16))) uint8_t lds[P::LDS_BYTES];
+    const WorkItem item = work_item(blockIdx.x, gridDim.x, w.order, w.tiles_m * w.results, w.tiles_n);
+    const int result = item.bm >= (unsigned)w.tiles_m ? 1 : 0, split = item.gi;
+    const int64_t m0 = (int64_t)(item.bm - result * w.tiles_m) * P::TM, n0 = (int64_t)item.bn * P::TN, left_m = w.m - m0, left_n = w.n - n0;
+    const int begin = split_begin(w.steps * w.terms, w.splits, split), end = split_begin(w.steps * w.terms, w.splits, split + 1);
+    v4f32 acc[P::FN][P::FM] = {};
+    for (int t = 0; t < w.terms; ++t) {
+        const int from = begin - t * w.steps > 0 ? begin - t * w.steps : 0, to = end - t * w.steps < w.steps ? end - t * w.steps : w.steps;
+        if (from >= to) continue;
+        const TileOperand X{w.X[t] + n0 * 2, w.ldx, (int)(left_n < P::TN ? left_n : P::TN), nullptr, 0, w.elements};
+        const TileOperand Y{w.Y[YT ? result : t] + m0 * (YT ? 2 : w.ldy), w.ldy, (int)(left_m < P::TM ? left_m : P::TM), nullptr, 0, w.elements};
+        P::multiply(lds, X, Y, w.elements * 2, from, to, acc);
+    }
+    const auto one = [](int64_t) { return 1.0f; };
+    if (w.splits > 1) {
+        const int64_t ld = in_fours(w.n);
+        store_tile<P, false>(lds, acc, w.partial + (((int64_t)result * w.splits + split) * w.m + m0) * ld + n0, ld, left_m, in_fours(left_n), false, one);
+    } else {
+        store_tile<P, (P::THREADS > 256)>(lds, acc, static_cast<T*>(w.D[result]) + m0 * w.ldd + n0, w.ldd, left_m, left_n, false, one);
+    }
+}
+
+template <int TYPE>
+__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) linear_dx_large_kernel(const ProductWork w) {
+    product_body<PairedTile<kind_of(TYPE), true, false>, typename Element<TYPE>::type, false>(w);
+}
+template <int TYPE>
+__global__ void __launch_bounds__(256) linear_dx_middle_kernel(const ProductWork w) {
+    product_body<Tile<kind_of(TYPE), 2, 2, 4, 2, 3, true, false>, typename Element<TYPE>::type, false>(w);
+}
+template <int TYPE>
+__global__ void __launch_bounds__(256) linear_dx_few_kernel(const ProductWork w) {
+    product_body<Tile<kind_of(TYPE), 4, 1, 2, 1, 4, true, false>, typename Element<TYPE>::type, false>(w);
+}
+template <int TYPE>
+__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) linear_dw_large_kernel(const ProductWork w) {
+    product_body<PairedTile<kind_of(TYPE), true, true>, typename Element<TYPE>::type, true>(w);
+}
+template <int TYPE>
+__global__ void __launch_bounds__(256) linear_dw_middle_kernel(const ProductWork w) {
+    product_body<Tile<kind_of(TYPE), 2, 2, 4, 4, 2, true, true>, typename Element<TYPE>::type, true>(w);
+}
+
+// the shares' sums in their order; blockIdx.z: the result
+template <int TYPE>
+__global__ void __launch_bounds__(256) linear_product_join_kernel(const ProductWork w) {
+    typedef typename Element<TYPE>::type T;
+    const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, ld = in_fours(w.n);
+    if (c >= w.n) return;
+    T* const D = static_cast<T*>(w.D[blockIdx.z]);
+    const bool wide = w.ldd % 4 == 0 && reinterpret_cast<uintptr_t>(D) % (4 * sizeof(T)) == 0;
+    for (int64_t m = blockIdx.y; m < w.m; m += gridDim.y) {
+        const float* from = w.partial + ((int64_t)blockIdx.z * w.splits * w.m + m) * ld + c;
+        v4f32 sum = {};
+#pragma unroll 4
+        for (int s = 0; s < w.splits; ++s, from += w.m * ld) sum += *reinterpret_cast<const v4f32*>(from);
+        put_four(D + m * w.ldd + c, sum, w.n - c, wide, false);
+    }
+}
+
+enum { FEW, MIDDLE, LARGE };
+struct Shape { int kind, tm, tn, splits; };
+int shares_of(int64_t tiles, int64_t at_a_time, int64_t steps) {
+    const int64_t want = at_a_time / tiles, most = steps / 8;
+    const int64_t s = want < most ? want : most;
+    return (int)(s < 1 ? 1 : s > 32 ? 32 : s);
+}
+// dX: m x n over `steps` steps.  Large tiles also where they are few, if that leaves every compute unit a share of the inner dimension of some length.
+Shape dx_shape(int64_t m, int64_t n, int64_t steps) {
+    const int64_t large = div_up(m, 256) * div_up(n, 256);
+    Shape s = m <= 16 ? Shape{FEW, 16, 128, 1} : m > 128 && (large >= 128 || large * (steps / 16) >= 128) ? Shape{LARGE, 256, 256, 1} : Shape{MIDDLE, 64, 128, 1};
+    s.splits = shares_of(div_up(m, s.tm) * div_up(n, s.tn), s.kind == LARGE ? 256 : 512, steps);
+    return s;
+}
+// dW: `results` of m x n
+Shape dw_shape(int64_t m, int64_t n, int64_t steps, int results) {
+    const int64_t large = results * div_up(m, 256) * div_up(n, 256);
+    Shape s = m > 128 && n > 128 && (large >= 128 || large * (steps / 16) >= 128) ? Shape{LARGE, 256, 256, 1} : Shape{MIDDLE, 128, 128, 1};
+    s.splits = shares_of(results * div_up(m, s.tm) * div_up(n, s.tn), s.kind == LARGE ? 256 : 512, steps);
+    return s;
+}
+
+struct Places {
+    uint8_t* dZ;
+    uint8_t* dU;
+    float* sums;
+    float* partial;
+    size_t total;
+};
+constexpr int64_t MOST_CHUNKS = 128;
+int64_t chunk_rows(int64_t m, int64_t n) {
+    const int64_t strips = div_up(n, SLOPE_COLUMNS), want = 2048 / strips, chunks = want < 1 ? 1 : want > MOST_CHUNKS ? MOST_CHUNKS : want, rows = div_up(m, chunks);
+    return rows < 16 ? 16 : rows;
+}
+Places places_of(uint8_t* ws, int64_t m, int64_t n, int64_t k, bool pair) {
+    Places p;
+    size_t at = 0;
+    const auto take = [&](size_t bytes) { uint8_t* const here = ws + at; at += up(bytes); return here; };
+    const Shape dx = dx_shape(m, k, div_up(n, 64) * (pair ? 2 : 1)), dw = dw_shape(n, k, div_up(m, 64), pair ? 2 : 1);
+    const size_t for_dx = dx.splits > 1 ? (size_t)dx.splits * m * in_fours(k) * 4 : 0, for_dw = dw.splits > 1 ? (size_t)(pair ? 2 : 1) * dw.splits * n * in_fours(k) * 4 : 0;
+    p.dZ = take((size_t)m * in_eights(n) * 2);
+    p.dU = take(pair ? (size_t)m * in_eights(n) * 2 : 0);
+    p.sums = reinterpret_cast<float*>(take(pair ? 0 : (size_t)div_up(m, chunk_rows(m, n)) * in_eights(n) * 4));
+    p.partial = reinterpret_cast<float*>(take(for_dx > for_dw ? for_dx : for_dw));
+    p.total = at;
+    return p;
+}
+
+#define OZAKI_LINEAR_TRY(expr) do { const hipError_t e_ = (expr); if (e_ != hipSuccess) return e_; } while (0)
+
+template <int TYPE>
+hipError_t launch_product(ProductWork w, Shape s, bool dw, hipStream_t st) {
+    w.splits = s.splits;
+    w.tiles_m = (int)div_up(w.m, s.tm);
+    w.tiles_n = (int)div_up(w.n, s.tn);
+    w.order = WorkOrder{s.kind == LARGE ? 32 : 64, 8};
+    const dim3 blocks((unsigned)((int64_t)w.tiles_m * w.results * w.tiles_n * w.splits));
+    if (dw && s.kind == LARGE) hipLaunchKernelGGL((linear_dw_large_kernel<TYPE>), blocks, dim3(512), 0, st, w);
+    else if (dw) hipLaunchKernelGGL((linear_dw_middle_kernel<TYPE>), blocks, dim3(256), 0, st, w);
+    else if (s.kind == LARGE) hipLaunchKernelGGL((linear_dx_large_kernel<TYPE>), blocks, dim3(512), 0, st, w);
+    else if (s.kind == MIDDLE) hipLaunchKernelGGL((linear_dx_middle_kernel<TYPE>), blocks, dim3(256), 0, st, w);
+    else hipLaunchKernelGGL((linear_dx_few_kernel<TYPE>), blocks, dim3(256), 0, st, w);
+    OZAKI_LINEAR_TRY(hipGetLastError());
+    if (w.splits > 1) {
+        hipLaunchKernelGGL((linear_product_join_kernel<TYPE>), dim3((unsigned)div_up(w.n, 1024), (unsigned)(w.m < 65535 ? w.m : 65535), (unsigned)w.results), dim3(256), 0, st, w);
+        OZAKI_LINEAR_TRY(hipGetLastError());
+    }
+    return hipSuccess;
+}
+
+template <int TYPE>
+hipError_t grad_typed(const LinearGradArgs& a, hipStream_t st) {
+    const bool pair = a.pair, products = a.dX != nullptr || a.dW != nullptr || a.dW2 != nullptr;
+    const Places p = places_of(a.ws, a.m, a.n, a.k, pair);
+    // (dY's pieces behind the end of a row hold anything, which dX's product, only one of whose operands is turned, would take)
+    const bool formed = pair || a.activation != ACT_NONE || a.n % 8 != 0;
+    SlopeWork w = {};
+    w.Z = a.Z;
+    w.U = a.U;
+    w.dY = a.dY;
+    w.dZ = formed && products ? p.dZ : nullptr;
+    w.dU = p.dU;
+    w.m = a.m;
+    w.n = a.n;
+    w.ldz = a.ldz;
+    w.ldu = a.ldu;
+    w.lddy = a.lddy;
+    w.ld = in_eights(a.n);
+    w.activation = a.activation;
+    w.rows = chunk_rows(a.m, a.n);
+    const int64_t chunks = div_up(a.m, w.rows);
+    w.whole = chunks == 1;
+    w.sums = a.dbias == nullptr ? nullptr : w.whole ? a.dbias : p.sums;
+    if (w.dZ != nullptr || w.sums != nullptr) {
+        const dim3 blocks((unsigned)div_up(a.n, SLOPE_COLUMNS), (unsigned)chunks);
+        if (pair) hipLaunchKernelGGL((linear_slope_kernel<TYPE, true>), blocks, dim3(SLOPE_WAVES * 64), 0, st, w);
+        else hipLaunchKernelGGL((linear_slope_kernel<TYPE, false>), blocks, dim3(SLOPE_WAVES * 64), 0, st, w);
+        OZAKI_LINEAR_TRY(hipGetLastError());
+    }
+    if (w.sums != nullptr && !w.whole) {
+        hipLaunchKernelGGL(linear_bias_join_kernel, dim3((unsigned)div_up(a.n, 64)), dim3(256), 0, st, p.sums, chunks, a.n, w.ld, a.dbias);
+        OZAKI_LINEAR_TRY(hipGetLastError());
+    }
+    const uint8_t* const dz[2] = {formed ? p.dZ : static_cast<const uint8_t*>(a.dY), p.dU};
+    const int64_t lddz = (formed ? w.ld : a.lddy) * 2;
+    if (a.dX != nullptr) {
+        ProductWork d = {};
+        d.X[0] = static_cast<const uint8_t*>(a.W);
+        d.X[1] = static_cast<const uint8_t*>(a.W2);
+        d.Y[0] = dz[0];
+        d.Y[1] = dz[1];
+        d.D[0] = a.dX;
+        d.ldx = a.ldw * 2;
+        d.ldy = lddz;
+        d.ldd = a.lddx;
+        d.elements = a.n;
+        d.m = a.m;
+        d.n = a.k;
+        d.partial = p.partial;
+        d.terms = pair ? 2 : 1;
+        d.results = 1;
+        d.steps = (int)div_up(a.n, 64);
+        OZAKI_LINEAR_TRY(launch_product<TYPE>(d, dx_shape(d.m, d.n, (int64_t)d.steps * d.terms), false, st));
+    }
+    if (a.dW != nullptr || a.dW2 != nullptr) {
+        ProductWork d = {};
+        const bool both = a.dW != nullptr && a.dW2 != nullptr;
+        d.X[0] = static_cast<const uint8_t*>(a.X);
+        d.Y[0] = a.dW != nullptr ? dz[0] : dz[1];
+        d.Y[1] = dz[1];
+        d.D[0] = a.dW != nullptr ? a.dW : a.dW2;
+        d.D[1] = a.dW2;
+        d.ldx = a.ldx * 2;
+        d.ldy = lddz;
+        d.ldd = a.lddw;
+        d.elements = a.m;
+        d.m = a.n;
+        d.n = a.k;
+        d.partial = p.partial;
+        d.terms = 1;
+        d.results = both ? 2 : 1;
+        d.steps = (int)div_up(a.m, 64);
+        // (the shape of both, also for one of a pair: the same bits)
+        OZAKI_LINEAR_TRY(launch_product<TYPE>(d, dw_shape(d.m, d.n, d.steps, pair ? 2 : 1), true, st));
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+size_t linear_grad_bytes(int64_t m, int64_t n, int64_t k, bool pair) { return places_of(nullptr, m, n, k, pair).total; }
+hipError_t launch_linear_grad(const LinearGradArgs& a, int type, hipStream_t st) { return type == TYPE_F16 ? grad_typed<TYPE_F16>(a, st) : grad_typed<TYPE_BF16>(a, st); }
+
+}  // namespace ozaki

@@ -74,6 +74,8 @@ struct TileOperand {
     // Turned operands (16 bits): the matrix lies the other way, element e of all vectors in a row; `vectors` is element 0 of the tile's first
     // vector, `stride` the distance between rows, and `rows` the vectors from there on; there are `elements` rows.
     int64_t elements = 0;
+    // Pairs of matrices (XP): the second one's vectors of the tile, as far apart; `rows` is each one's.
+    const uint8_t* second = nullptr;
 };
 
 // A turned operand in LDS: 64 rows of 128 vectors, 256 bytes each, to a panel.  A fragment is read with ds_read_b64_tr_b16, which gives a lane four
@@ -160,8 +162,9 @@ __device__ __forceinline__ void tile_wait() {
     asm volatile("" ::: "memory");
 }
 
-// WN x WM waves, each FN x FM tiles of 16 x 16; XT, YT: the operand is turned
-template <int KIND, int WN_, int WM_, int FN_, int FM_, int NST_, bool XT = false, bool YT = false>
+// WN x WM waves, each FN x FM tiles of 16 x 16; XT, YT: the operand is turned; XP: X is a pair of matrices, TN / 2 vectors of each, and a lane that has
+// element r of acc[i][j] from the first has the same vector of the second in acc[i + FN / 2][j].
+template <int KIND, int WN_, int WM_, int FN_, int FM_, int NST_, bool XT = false, bool YT = false, bool XP = false>
 struct Tile {
     static constexpr bool FP8 = KIND < KIND_BF16, WIDE = KIND == KIND_WIDE_BLOCKS || KIND == KIND_WIDE_VECTORS;
     static constexpr bool BLOCKS = KIND == KIND_FP8_BLOCKS || KIND == KIND_WIDE_BLOCKS;
@@ -174,6 +177,8 @@ struct Tile {
     static constexpr int LPW = (PIECE_LOADS + WAVES - 1) / WAVES, SPW = (SCALE_LOADS + WAVES - 1) / WAVES;
     static_assert(!FP8 || (!XT && !YT), "");
     static_assert((!XT || TN % 128 == 0) && (!YT || TM % 128 == 0), "");
+    static_assert(!XP || (!FP8 && !XT && FN % 2 == 0), "");
+    static constexpr bool PAIR = XP;
 
     // acc[i][j][r] += X row wn * FN * 16 + 16 i + 4 (lane / 16) + r  times  Y row wm * FM * 16 + 16 j + lane % 16, over the steps
     // [step0, step1) of vectors of `bytes` bytes (if only one operand is turned, the other has zeros behind them to the end of the 16 bytes).  Ends
@@ -198,11 +203,13 @@ struct Tile {
                 int at = wave * LPW + i;
                 at = at < PIECE_LOADS ? at : PIECE_LOADS - 1;                           // (the same bytes to the same place twice)
                 const bool x = at * 8 < TN;
-                const int row = at * 8 + r, mine = x ? row : row - TN, rows = x ? X.rows : Y.rows;
+                const int row = at * 8 + r, rows = x ? X.rows : Y.rows;
+                const int mine = !x ? row - TN : XP ? row / (FN * 16) * (FN * 8) + row % (FN * 8) : row;
                 const unsigned piece = (lane & 7) ^ ((row >> 1) & 7);
                 voff[i] = (unsigned)(mine < rows ? mine : rows - 1) * (unsigned)(x ? X.stride : Y.stride) + piece * 16;
                 from[i] = (x ? X.vectors : Y.vectors) + (int64_t)step0 * STEP_BYTES;
                 to[i] = at * 1024;
+                if (XP && x && at * 8 % (FN * 16) >= FN * 8) from[i] = X.second + (int64_t)step0 * STEP_BYTES;
                 if ((x && XT) || (!x && YT)) {
                     // four rows of a panel
                     const int q = x ? at : at - TN / 8, e = (q & 15) * 4 + (lane >> 4);
@@ -429,9 +436,11 @@ struct Tile {
 // leave no registers for 64-bit ones.
 // FP8, 8192 x 8192 x 8192: 460 us, 2.39 PFLOP/s, the matrix unit busy 60 % of the cycles at 1.9 GHz; without loads and LDS reads it would be 3.2 PFLOP/s.
 // BF16, 4096 x 65536 x 4096: 1.43 PFLOP/s, busy 74 %; 2.07 without.  Bound by the two together: LDS reads and scales hold up the issue.
-template <int KIND, bool XT = false, bool YT = false>
+template <int KIND, bool XT = false, bool YT = false, bool XP = false>
 struct PairedTile {
-    typedef Tile<KIND, 2, 4, 8, 4, 2> Base;
+    typedef Tile<KIND, 2, 4, 8, 4, 2, false, false, XP> Base;
+    static constexpr bool PAIR = XP;
+    static_assert(!XP || !XT, "");
     static constexpr bool FP8 = Base::FP8, BLOCKS = Base::BLOCKS;
     static_assert(!Base::WIDE, "registers");
     static constexpr int WN = 2, WM = 4, FN = 8, FM = 4, WAVES = 8, THREADS = 512, TN = 256, TM = 256, ROWS = 512;
@@ -454,7 +463,8 @@ struct PairedTile {
     }
 
     __device__ static TileOperand offset(const TileOperand& o, int step) {
-        return TileOperand{o.vectors + (int64_t)step * STEP_BYTES, o.stride, o.rows, o.scales + (int64_t)step * o.scale_stride, o.scale_stride, 0};
+        return TileOperand{o.vectors + (int64_t)step * STEP_BYTES, o.stride, o.rows, o.scales + (int64_t)step * o.scale_stride, o.scale_stride, 0,
+                           XP ? o.second + (int64_t)step * STEP_BYTES : nullptr};
     }
 
     __device__ static void pipeline(uint8_t* lds, const TileOperand& X, const TileOperand& Y, int64_t bytes, int step0, int step1,
@@ -472,6 +482,8 @@ struct PairedTile {
         // (beyond `RECORDS` bytes these resources give zeros)
         constexpr unsigned RECORDS = 0x7FFFFFFFu;
         const __amdgpu_buffer_rsrc_t in_x = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(X.vectors), 0, RECORDS, 0x00027000);
+        // (a pair's second matrix is part 2 of X: rows 64 - 127 of each 128)
+        const __amdgpu_buffer_rsrc_t in_x2 = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(XP ? X.second : X.vectors), 0, RECORDS, 0x00027000);
         const __amdgpu_buffer_rsrc_t in_y = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(Y.vectors), 0, RECORDS, 0x00027000);
         // A turned operand's loads bring four rows of a panel of 128 vectors: of X, panel 0 is part 1 and panel 1 part 2.
         auto panel_load = [&](int i) { return i < 4 ? wave * 4 + i : (i < P1 ? wave * 2 + i - 4 : 16 + wave * 2 + i - P1); };
@@ -480,7 +492,7 @@ struct PairedTile {
 #pragma unroll
         for (int i = 0; i < P1 + P2; ++i) {
             const TileOperand& o = i < 4 ? Y : X;
-            const int row = row_of(i) + (lane >> 3), mine = i < 4 ? row - TN : row;
+            const int row = row_of(i) + (lane >> 3), mine = i < 4 ? row - TN : XP ? (row >> 7) * 64 + (row & 63) : row;
             voff[i] = (unsigned)(mine < o.rows ? mine : o.rows - 1) * (unsigned)o.stride + (((lane & 7) ^ ((row >> 1) & 7)) << 4);
             if (i < 4 ? YT : XT) {
                 const int e = element_of(i), panel = panel_load(i) >> 4, c = (((lane & 15) >> 1) ^ turned_place(e)) * 16 + (lane & 1) * 8;
@@ -513,7 +525,7 @@ struct PairedTile {
             } else if (XT || YT) {
                 direct_load(resource_of(o.vectors, RECORDS), at, (step0 + s) * STEP_BYTES, to);
             } else {
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(i < 4 ? in_y : in_x, OZAKI_TILE_LPTR(to), 16, at, (step0 + s) * STEP_BYTES, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(i < 4 ? in_y : XP && i >= P1 ? in_x2 : in_x, OZAKI_TILE_LPTR(to), 16, at, (step0 + s) * STEP_BYTES, 0, 0);
             }
         };
         int scale_to = 0, scale_at = 0;                               // places in the ring of scales

@@ -1,0 +1,160 @@
+"""ozaki_gradient_norm and ozaki_clip_gradients against their definitions in 64 bits."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from low_precision import DTYPES, ROUNDING  # noqa: E402
+from paper_2508_00441_amd import binding as lib, device  # noqa: E402
+
+NAMES = list(DTYPES)
+
+
+def _tensors(sizes, seed=0, spread=1.0, shift=0):
+    """Tensors of alternating types; `shift` elements into a larger allocation."""
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    out = []
+    for i, n in enumerate(sizes):
+        whole = (spread * torch.randn((n + shift,), device="cuda", generator=gen)).to(DTYPES[NAMES[i % 3]])
+        out.append(whole[shift:])
+    return out
+
+
+def _types(tensors):
+    return [lib.TYPES[next(name for name in NAMES if DTYPES[name] == x.dtype)] for x in tensors]
+
+
+def _norm(tensors, scale):
+    return abs(scale) * math.sqrt(math.fsum(float(x.double().square().sum()) for x in tensors))
+
+
+def _clip(tensors, scale, max_norm, out=None, norm=None, given=0):
+    out = [torch.full_like(x, float("nan")) for x in tensors] if out is None else out
+    norm = torch.full((1,), float("nan"), device="cuda") if norm is None else norm
+    lib.ozaki_clip_gradients(len(tensors), tensors, [x.numel() for x in tensors], _types(tensors), scale, max_norm, out, norm, given)
+    return out, norm
+
+
+def _check(tensors, scale, max_norm, out, norm):
+    want = _norm(tensors, scale)
+    # one rounding to 32 bits, and the 64-bit sums' own, which are nothing beside it
+    assert abs(float(norm) - want) <= 2.0 ** -23 * want
+    factor = scale * (min(1.0, max_norm / want) if want > 0 else 1.0)
+    for x, y in zip(tensors, out):
+        rel, tiny = ROUNDING[NAMES[_types([x])[0]]]
+        exact = x.double() * factor
+        # the norm, the quotient, its product with the scale, the product with the element
+        off = 5 * 2.0 ** -24 * exact.abs() + 2.0 ** -149
+        assert bool(torch.all((y.double() - exact).abs() <= off + rel * (exact.abs() + off) + tiny))
+
+
+@pytest.fixture()
+def workspace():
+    ws = device.Workspace(8 << 20)
+    yield ws
+    ws.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shift", [0, 1, 3])
+@pytest.mark.parametrize("sizes", [[1], [3, 1, 2], [32768, 32769, 32767], [100003, 5, 4096, 0, 1000], [7] * 95, [130] * 96, [1001] * 97, [9, 40000] * 150, [3_000_001, 2_000_003, 64]])
+def test_norm_and_clip(sizes, shift, workspace):
+    x = _tensors(sizes, seed=len(sizes) + shift, shift=shift)
+    norm = torch.full((1,), float("nan"), device="cuda")
+    for scale, max_norm in ((1.0, 0.5), (1.0, 1e9), (0.25, 2.0), (-0.5, 1.0)):
+        lib.ozaki_gradient_norm(len(x), x, [v.numel() for v in x], _types(x), scale, norm)
+        out, again = _clip(x, scale, max_norm)
+        assert torch.equal(norm, again)
+        _check(x, scale, max_norm, out, again)
+
+
+@pytest.mark.gpu
+def test_in_place_and_given(workspace):
+    x = _tensors([50000, 33, 1000], seed=4)
+    copies = [v.clone() for v in x]
+    out, norm = _clip(x, 1.0, 3.0)
+    _clip(copies, 1.0, 3.0, out=copies)
+    assert all(torch.equal(a, b) for a, b in zip(out, copies))
+    # a norm that the caller has, of more than these tensors; without work memory
+    lib.ozaki_set_workspace(None, 0)
+    other = torch.full((1,), 1000.0, device="cuda")
+    out, norm = _clip(x, 1.0, 3.0, norm=other, given=1)
+    assert float(norm) == 1000.0
+    for a, b in zip(x, out):
+        assert torch.equal((a.float() * (torch.tensor(3.0) / torch.tensor(1000.0)).cuda()).to(a.dtype), b)
+    # within bounds nothing is written where results go to where the elements are
+    same = [v.clone() for v in x]
+    _clip(same, 1.0, 3.0, out=same, norm=torch.full((1,), 2.0, device="cuda"), given=1)
+    assert all(torch.equal(a, b) for a, b in zip(x, same))
+
+
+@pytest.mark.gpu
+def test_large_small_and_not_finite(workspace):
+    big = torch.full((70000,), 2.0 ** 100, device="cuda")
+    out, norm = _clip([big], 1.0, 1.0)
+    _check([big], 1.0, 1.0, out, norm)
+    small = torch.full((70000,), 2.0 ** -120, device="cuda")
+    _, norm = _clip([small], 1.0, 1.0)
+    assert abs(float(norm) - _norm([small], 1.0)) <= 2.0 ** -23 * _norm([small], 1.0)
+    zeros = torch.zeros((5000,), device="cuda")
+    out, norm = _clip([zeros], 1.0, 0.0)
+    assert float(norm) == 0.0 and bool(torch.all(out[0] == 0))
+    for bad, check in ((float("inf"), lambda y: bool(torch.all(y[1:] == 0)) and bool(torch.isnan(y[0]))), (float("nan"), lambda y: bool(torch.isnan(y).all()))):
+        x = torch.ones((40000,), device="cuda")
+        x[0] = bad
+        out, norm = _clip([x], 1.0, 1.0)
+        assert check(out[0]) and (math.isinf(float(norm)) if math.isinf(bad) else math.isnan(float(norm)))
+
+
+@pytest.mark.gpu
+def test_nothing(workspace):
+    norm = torch.full((1,), 7.0, device="cuda")
+    lib.ozaki_gradient_norm(0, None, None, None, 1.0, norm)
+    assert float(norm) == 0.0
+    norm.fill_(7.0)
+    lib.ozaki_clip_gradients(2, [0, 0], [0, 0], [0, 1], 1.0, 1.0, [0, 0], norm)
+    assert float(norm) == 0.0
+
+
+@pytest.mark.gpu
+def test_in_a_graph(workspace):
+    x = _tensors([200000, 77, 5000] * 40, seed=6)
+    sizes, types = [v.numel() for v in x], _types(x)
+    out, norm = [torch.zeros_like(v) for v in x], torch.zeros((1,), device="cuda")
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=stream):
+        lib.ozaki_set_stream(torch.cuda.current_stream().cuda_stream)
+        lib.ozaki_clip_gradients(len(x), x, sizes, types, 1.0, 1.0, out, norm)
+    lib.ozaki_set_stream(torch.cuda.current_stream().cuda_stream)
+    for step in range(3):
+        for v in x:
+            v.mul_(0.5)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        want, want_norm = _clip(x, 1.0, 1.0)
+        torch.cuda.synchronize()
+        assert torch.equal(norm, want_norm) and all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+FAKE = 1 << 20
+
+
+def test_refusals():
+    norm = [2, [FAKE, FAKE], [4, 4], [0, 1], 1.0, FAKE]
+    for at, value in ((1, -1), (2, None), (2, [FAKE, None]), (2, [FAKE + 2, FAKE]), (2, [FAKE, FAKE + 1]), (3, None), (3, [4, -1]), (3, [4, 2 ** 38 + 1]), (4, None), (4, [0, 3]), (5, float("nan")),
+                      (5, float("inf")), (6, None), (6, FAKE + 2)):
+        args = list(norm)
+        args[at - 1] = value
+        assert lib.ozaki_gradient_norm(*args, check=False) == -at, (at, value)
+    clip = [2, [FAKE, FAKE], [4, 4], [0, 1], 1.0, 1.0, [FAKE, FAKE], FAKE, 0]
+    for at, value in ((1, -1), (2, [FAKE, None]), (3, [-1, 4]), (4, [3, 0]), (5, float("nan")), (6, float("nan")), (6, -1.0), (7, None), (7, [FAKE, None]), (7, [FAKE + 2, FAKE]), (8, None),
+                      (8, FAKE + 1), (9, 2)):
+        args = list(clip)
+        args[at - 1] = value
+        assert lib.ozaki_clip_gradients(*args, check=False) == -at, (at, value)
+    lib.ozaki_set_workspace(None, 0)
+    assert lib.ozaki_gradient_norm(*norm, check=False) == lib.STATUS_WORKSPACE
+    assert lib.ozaki_gradient_norm_workspace_bytes(-1) == 0 and lib.ozaki_gradient_norm_workspace_bytes(0) > 0
