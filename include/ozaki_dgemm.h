@@ -465,7 +465,8 @@ size_t ozaki_gated_linear_workspace_bytes(int64_t m, int64_t n, int64_t k, int g
  *   gate, group        32 bits, rows i share row i / group of it: gate[(i / group) * k + e]; null: one
  *   R, R_out  of `type_r`, which is `type` or F32; R null: zeros.  R_out is r; may be null, may be R with its ld.
  *   H         may be null (then so may w_pre), not with R_out; may be X with its ld
- * Rounded once each: H is formed from the r that has not been rounded.  Sums along a row are in 64 bits. */
+ * Rounded once each: H is formed from the r that has not been rounded.  Sums in 32 bits; rows whose squares leave their range are normed all the same, as long as rho
+ * itself is a number that 32 bits hold. */
 int ozaki_block_norm(int64_t rows, int64_t k, const void* X, int64_t ldx, int type, const float* w_post, const float* gate, int64_t group, float scale,
                      float eps, const void* R, int64_t ldr, int type_r, void* R_out, int64_t ldro, const float* w_pre, void* H, int64_t ldh);
 
@@ -486,7 +487,8 @@ size_t ozaki_block_norm_workspace_bytes(int64_t rows, int64_t k, int64_t group);
  *                              They are read before the call returns.
  *   scale                      what the elements are to be multiplied by (one over what the loss was multiplied by)
  *   norm                       DEVICE, one number in 32 bits; infinite or NaN where an element is
- * Squares are summed in 64 bits, in an order that depends on the sizes and types only.  Needs the context's workspace,
+ * Squares of at most 128 elements are summed in 32 bits, those sums in twice as many; elements whose squares leave the range are no exception.  The order depends
+ * on sizes, types and alignment only.  Needs the context's workspace,
  * ozaki_gradient_norm_workspace_bytes(count). */
 int ozaki_gradient_norm(int count, const void* const* tensors, const int64_t* sizes, const int* types, float scale, float* norm);
 

@@ -931,9 +931,7 @@ int ozaki_gradient_norm(int count, const void* const* tensors, const int64_t* si
     if (st != 0) return st;
     if (!norm || !aligned(norm, 4)) return -6;
     ClipArgs a = {count, tensors, sizes, types, nullptr, scale, 0.0f, norm, false, nullptr};
-    uint8_t* ws = nullptr;
-    if (!work_memory(gradient_norm_bytes(count > 0 ? count : 1), ws)) return OZAKI_STATUS_WORKSPACE;
-    a.partial = reinterpret_cast<double*>(ws);
+    if (!work_memory(gradient_norm_bytes(count > 0 ? count : 1), a.ws)) return OZAKI_STATUS_WORKSPACE;
     HIP_TRY(launch_clip(a, ctx().stream));
     return 0;
 }
@@ -949,9 +947,7 @@ int ozaki_clip_gradients(int count, const void* const* tensors, const int64_t* s
     if (!norm || !aligned(norm, 4)) return -8;
     if (given != 0 && given != 1) return -9;
     ClipArgs a = {count, tensors, sizes, types, out, scale, max_norm, norm, given != 0, nullptr};
-    uint8_t* ws = nullptr;
-    if (!given && !work_memory(gradient_norm_bytes(count > 0 ? count : 1), ws)) return OZAKI_STATUS_WORKSPACE;
-    a.partial = reinterpret_cast<double*>(ws);
+    if (!given && !work_memory(gradient_norm_bytes(count > 0 ? count : 1), a.ws)) return OZAKI_STATUS_WORKSPACE;
     HIP_TRY(launch_clip(a, ctx().stream));
     return 0;
 }

@@ -5,9 +5,10 @@
 //     dn = dh w_pre          dr = dr' + rho(r') (dn - n mean(dn n))          dw_pre = sum over rows of dh n
 //     dm = scale gate dr w_post      dx = rho(x) (dm - m mean(dm m))         s = sum over rows of dr m,  dw_post = scale gate s,  dgate = scale w_post s.
 //
-// Every element is read and written once: a workgroup keeps a row in registers from the loads to the stores.  Sums along a row are in 64 bits, so that
-// neither large nor small numbers' squares leave the range.  Sums over rows are kept in registers, in 32 bits, over the rows that a workgroup has one after
-// another, and meet in work memory; a second launch adds them up, in an order that depends on sizes only.
+// Every element is read and written once: a workgroup keeps a row in registers from the loads to the stores.  Sums are in
+// 32 bits; where a row's squares leave their range, above or below, its sums are formed again with the row times a power of two.  Sums over rows
+// are kept in registers over the rows that a workgroup has one after another, and meet in work memory; a second launch adds them up, in an order that
+// depends on sizes only.
 #include "block_operators.hpp"
 
 namespace ozaki {
@@ -59,7 +60,7 @@ template <typename T> __device__ __forceinline__ void store_eight(T* p, v8f32 v,
 template <typename T> __device__ __forceinline__ bool rows_wide(const T* p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * sizeof(T) % 16 == 0; }
 
 // The sums of N numbers over a workgroup, for all its threads; `lds` has room for N numbers a wave and is free again when the next call's first barrier is passed.
-template <int THREADS, int N> __device__ __forceinline__ void row_sums(double (&v)[N], double* lds) {
+template <int THREADS, int N> __device__ __forceinline__ void row_sums(float (&v)[N], float* lds) {
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1)
 #pragma unroll
@@ -80,19 +81,55 @@ template <int THREADS, int N> __device__ __forceinline__ void row_sums(double (&
         }
     }
 }
-__device__ __forceinline__ double dot(v8f32 a, v8f32 b) {
-    double s = 0.0;
+__device__ __forceinline__ float dot(v8f32 a, v8f32 b, float s) {
 #pragma unroll
-    for (int q = 0; q < 8; ++q) s = __builtin_fma((double)a[q], (double)b[q], s);
+    for (int q = 0; q < 8; ++q) s = __builtin_fmaf(a[q], b[q], s);
     return s;
 }
-__device__ __forceinline__ double rho_of(double squares, int64_t k, float eps) { return 1.0 / sqrt(squares / (double)k + (double)eps); }
+
+// rho of a row and (ALONG) mean(d n) with n = row * rho; through(p): piece p of d
+struct RowNorm { float rho, along; };
+template <int THREADS, bool ALONG, int PIECES, typename F>
+__device__ __forceinline__ RowNorm row_norm(const v8f32 (&x)[PIECES], F through, float k, float eps, float* lds) {
+    float s[ALONG ? 2 : 1] = {};
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+        s[0] = dot(x[p], x[p], s[0]);
+        if constexpr (ALONG) s[1] = dot(through(p), x[p], s[1]);
+    }
+    row_sums<THREADS>(s, lds);
+    RowNorm r = {__builtin_amdgcn_rsqf(s[0] / k + eps), 0.0f};
+    const bool above = !(s[0] < 0x1p126f), below = s[0] < 0x1p-90f && eps < 0x1p-80f;
+    bool again = above || below;
+    if constexpr (ALONG) {
+        r.along = s[1] * r.rho / k;
+        again = again || !(fabsf(s[1]) < __builtin_inff());
+    }
+    if (again) {                                     // (the same for all threads)
+        // times 2^-72 no row's squares are too large, times 2^100 no row's that came to so little too small
+        const float f = above ? 0x1p-72f : below ? 0x1p100f : 1.0f;
+        float q[1] = {0.0f};
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) q[0] = dot(x[p] * f, x[p] * f, q[0]);
+        row_sums<THREADS>(q, lds);
+        r.rho = f * __builtin_amdgcn_rsqf(q[0] / k + eps * f * f);
+        if constexpr (ALONG) {
+            q[0] = 0.0f;
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) q[0] = dot(through(p), x[p] * r.rho, q[0]);
+            row_sums<THREADS>(q, lds);
+            r.along = q[0] / k;
+        }
+    }
+    return r;
+}
 
 template <int TYPE, int TYPE_R, int THREADS, int PIECES>
 __global__ void __launch_bounds__(THREADS) block_norm_kernel(const BlockNormArgs a) {
     typedef typename Element<TYPE>::type T;
     typedef typename Element<TYPE_R>::type TR;
-    __shared__ double lds[THREADS / 64];
+    __shared__ float lds[THREADS / 64];
+    const auto none = [](int) { return v8f32{}; };
     const T* const X = static_cast<const T*>(a.X);
     const TR* const R = static_cast<const TR*>(a.R);
     TR* const R_out = static_cast<TR*>(a.R_out);
@@ -113,14 +150,7 @@ __global__ void __launch_bounds__(THREADS) block_norm_kernel(const BlockNormArgs
             r[p] = R != nullptr ? load_eight(R + row * a.ldr + c[p], there[p]) : v8f32{};
         }
         if (X != nullptr) {
-            float rho = 1.0f;
-            if (a.w_post != nullptr) {
-                double s[1] = {0.0};
-#pragma unroll
-                for (int p = 0; p < PIECES; ++p) s[0] += dot(x[p], x[p]);
-                row_sums<THREADS, 1>(s, lds);
-                rho = (float)rho_of(s[0], a.k, a.eps);
-            }
+            const float rho = a.w_post != nullptr ? row_norm<THREADS, false>(x, none, (float)a.k, a.eps, lds).rho : 1.0f;
             const float* const gate = a.gate != nullptr ? a.gate + row / a.group * a.k : nullptr;
 #pragma unroll
             for (int p = 0; p < PIECES; ++p) {
@@ -132,11 +162,7 @@ __global__ void __launch_bounds__(THREADS) block_norm_kernel(const BlockNormArgs
             }
         }
         if (H == nullptr) continue;
-        double s[1] = {0.0};
-#pragma unroll
-        for (int p = 0; p < PIECES; ++p) s[0] += dot(r[p], r[p]);
-        row_sums<THREADS, 1>(s, lds);
-        const float rho = (float)rho_of(s[0], a.k, a.eps);
+        const float rho = row_norm<THREADS, false>(r, none, (float)a.k, a.eps, lds).rho;
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) store_eight(H + row * a.ldh + c[p], r[p] * rho * load_weights(a.w_pre + c[p], there[p], wide_pre), there[p], wide_h);
     }
@@ -161,7 +187,7 @@ template <int TYPE, int TYPE_R, int THREADS, int PIECES>
 __global__ void __launch_bounds__(THREADS) block_norm_grad_kernel(const NormGradWork w) {
     typedef typename Element<TYPE>::type T;
     typedef typename Element<TYPE_R>::type TR;
-    __shared__ double lds[2 * (THREADS / 64)];
+    __shared__ float lds[2 * (THREADS / 64)];
     // The sums over rows, t and s: in registers, or (the longest rows, which leave no registers) a thread's own places in LDS.
     constexpr bool HELD = THREADS == 1024 && PIECES == 2;
     __shared__ v4f32 held[HELD ? 4 * PIECES : 1][HELD ? THREADS : 1];
@@ -224,7 +250,7 @@ __global__ void __launch_bounds__(THREADS) block_norm_grad_kernel(const NormGrad
         unit = blockIdx.x * (n.rows / n.group);
     }
     for (; row < end; ++row) {
-        v8f32 x[PIECES], r[PIECES], dn[PIECES], dr[PIECES];
+        v8f32 x[PIECES], r[PIECES], dh[PIECES], dr[PIECES];
         const auto load_x = [&]() {
 #pragma unroll
             for (int p = 0; p < PIECES; ++p) x[p] = branch ? load_eight(X + row * a.ldx + c[p], there[p]) : v8f32{};
@@ -232,24 +258,17 @@ __global__ void __launch_bounds__(THREADS) block_norm_grad_kernel(const NormGrad
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) {
             dr[p] = dR_out != nullptr ? load_eight(dR_out + row * a.lddro + c[p], there[p]) : v8f32{};
-            dn[p] = dH != nullptr ? load_eight(dH + row * a.lddh + c[p], there[p]) : v8f32{};
+            dh[p] = dH != nullptr ? load_eight(dH + row * a.lddh + c[p], there[p]) : v8f32{};
             r[p] = dH != nullptr ? load_eight(R + row * a.ldr + c[p], there[p]) : v8f32{};
         }
         if constexpr (!HELD) load_x();
         if (dH != nullptr) {
-            double sums[2] = {};
+            const RowNorm rn = row_norm<THREADS, true>(r, [&](int p) { return dh[p] * load_weights(a.w_pre + c[p], there[p], wide_pre); }, (float)a.k, a.eps, lds);
 #pragma unroll
             for (int p = 0; p < PIECES; ++p) {
-                sums[0] += dot(r[p], r[p]);
-                sums[1] += dot(dn[p] * load_weights(a.w_pre + c[p], there[p], wide_pre), r[p]);
-            }
-            row_sums<THREADS, 2>(sums, lds);
-            const double rho = rho_of(sums[0], a.k, a.eps);
-            const float rho_r = (float)rho, back = (float)(rho * rho * rho * sums[1] / (double)a.k);
-#pragma unroll
-            for (int p = 0; p < PIECES; ++p) {
-                dr[p] += dn[p] * load_weights(a.w_pre + c[p], there[p], wide_pre) * rho_r - r[p] * back;
-                add(0, p, dn[p] * (r[p] * rho_r));
+                const v8f32 n = r[p] * rn.rho;
+                dr[p] += (dh[p] * load_weights(a.w_pre + c[p], there[p], wide_pre) - n * rn.along) * rn.rho;
+                add(0, p, dh[p] * n);
             }
         }
         if (dR != nullptr) {
@@ -258,30 +277,20 @@ __global__ void __launch_bounds__(THREADS) block_norm_grad_kernel(const NormGrad
         }
         if (branch) {
             if constexpr (HELD) load_x();
-            // d: what the gradient of m is, or of x without a norm; dr is needed for s once more
+            // what the gradient of m is, or of x without a norm
             const float* const gate = a.gate != nullptr ? a.gate + row / a.group * a.k : nullptr;
             const auto through = [&](int p) {
                 v8f32 d = dr[p] * a.scale;
                 if (gate != nullptr) d *= load_weights(gate + c[p], there[p], wide_gate);
                 return post ? d * load_weights(a.w_post + c[p], there[p], wide_post) : d;
             };
-            float rho_x = 1.0f, back = 0.0f;
-            if (post) {
-                double sums[2] = {};
-#pragma unroll
-                for (int p = 0; p < PIECES; ++p) {
-                    sums[0] += dot(x[p], x[p]);
-                    sums[1] += dot(through(p), x[p]);
-                }
-                row_sums<THREADS, 2>(sums, lds);
-                const double rho = rho_of(sums[0], a.k, a.eps);
-                rho_x = (float)rho;
-                back = (float)(rho * rho * rho * sums[1] / (double)a.k);
-            }
+            RowNorm xn = {1.0f, 0.0f};
+            if (post) xn = row_norm<THREADS, true>(x, through, (float)a.k, a.eps, lds);
 #pragma unroll
             for (int p = 0; p < PIECES; ++p) {
-                add(1, p, dr[p] * (x[p] * rho_x));
-                if (dX != nullptr) store_eight(dX + row * a.lddx + c[p], post ? through(p) * rho_x - x[p] * back : through(p), there[p], wide_x);
+                const v8f32 m = x[p] * xn.rho;
+                add(1, p, dr[p] * m);
+                if (dX != nullptr) store_eight(dX + row * a.lddx + c[p], post ? (through(p) - m * xn.along) * xn.rho : through(p), there[p], wide_x);
             }
         }
         if (--left == 0 && n.per_group == 0) {

@@ -87,9 +87,9 @@ struct ClipArgs {
     float scale, max_norm;
     float* norm;
     bool given;                      // the norm is there already
-    double* partial;
+    uint8_t* ws;
 };
-size_t gradient_norm_bytes(int64_t count);       // of `partial`
+size_t gradient_norm_bytes(int64_t count);
 hipError_t launch_clip(const ClipArgs& a, hipStream_t st);
 
 #if defined(__HIPCC__)

@@ -106,7 +106,8 @@ def gated_grad(x, wg, wu, act, g, u, dy, type):
 
 
 def block_norm(x, r, w_post, gate, group, scale, eps, w_pre):
-    """r' and h in 64 bits with what they may be off before they are rounded; x and r may be None."""
+    """r' and h in 64 bits with what they may be off before they are rounded; x and r may be None.  A row's squares: sixteen added one after another, then ten
+    exchanges at most, 26 roundings of which rho has half; three of its own, and the products around it: 24."""
     if x is None:
         total, off = r, 0 * r
     else:
@@ -114,19 +115,20 @@ def block_norm(x, r, w_post, gate, group, scale, eps, w_pre):
         if gate is not None:
             u = u * gate[torch.arange(len(x), device=x.device) // group]
         total = scale * u + (0 if r is None else r)
-        off = 8 * ULP * ((scale * u).abs() + (0 if r is None else r.abs()))
+        off = 24 * ULP * ((scale * u).abs() + (0 if r is None else r.abs()))
     if w_pre is None:
         return total, off, None, None
     rho = torch.rsqrt((total * total).mean(1, keepdim=True) + eps)
     h = total * rho * w_pre
-    return total, off, h, rho * w_pre.abs() * off + h.abs() * (8 * ULP + off.norm(dim=1, keepdim=True) / total.norm(dim=1, keepdim=True).clamp(min=1e-300))
+    return total, off, h, rho * w_pre.abs() * off + h.abs() * (24 * ULP + off.norm(dim=1, keepdim=True) / total.norm(dim=1, keepdim=True).clamp(min=1e-300))
 
 
 def block_norm_grad(x, r, w_post, gate, group, scale, eps, w_pre, dh, dr_out):
-    """name -> (gradient, what it may be off before it is rounded): dr, dx, dw_pre, dw_post, dgate.  32 roundings of every term and, for a sum over rows, one a row."""
+    """name -> (gradient, what it may be off before it is rounded): dr, dx, dw_pre, dw_post, dgate.  96 roundings of every term (of n 17, rho's with it, of the
+    mean along a row 26 and rho's 17 again, of the factor rho 16, and the products) and, for a sum over rows, one a row."""
     rows, k = (dh if dh is not None else dr_out).shape
     device = (dh if dh is not None else dr_out).device
-    few, many = 32 * ULP, 2 * (rows + 48) * ULP
+    few, many = 96 * ULP, 2 * (rows + 48) * ULP
     out = {}
     dr = torch.zeros((rows, k), dtype=torch.float64, device=device) if dr_out is None else dr_out
     terms = dr.abs()
