@@ -16,18 +16,25 @@ namespace {
 
 template <typename T> struct Eight { typedef T type __attribute__((ext_vector_type(8))); };
 
-// eight elements of a vector, of which `there` exist (zeros for the others); the 16 bytes in which a vector ends may be read whole
-template <typename T> __device__ __forceinline__ v8f32 load_eight(const T* p, int there) {
-    v8f32 v = {};
-    if (there <= 0) return v;
-    if constexpr (sizeof(T) == 4) {
-        const v4f32 lo = *reinterpret_cast<const v4f32*>(p);
-        v4f32 hi = {};
-        if (there > 4) hi = *reinterpret_cast<const v4f32*>(p + 4);
-        v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    } else {
-        v = __builtin_convertvector(*reinterpret_cast<const typename Eight<T>::type*>(p), v8f32);
-    }
+// Eight elements of a vector as they are in memory, and as numbers: `there` of them exist (zeros for the others); the 16 bytes in which a vector ends
+// may be read whole.
+template <typename T> struct Raw { v4i32 part[sizeof(T) / 2]; };
+// (a row's address is the same for all lanes and stays in scalar registers; a lane adds 32 bits to it)
+template <typename T> __device__ __forceinline__ const T* place(const T* row, unsigned c) {
+    return reinterpret_cast<const T*>(reinterpret_cast<const uint8_t*>(row) + c * (unsigned)sizeof(T));
+}
+template <typename T> __device__ __forceinline__ T* place(T* row, unsigned c) { return const_cast<T*>(place(const_cast<const T*>(row), c)); }
+template <typename T> __device__ __forceinline__ Raw<T> load_raw(const T* row, unsigned c, int there) {
+    Raw<T> r = {};
+    if (there > 0) r.part[0] = *reinterpret_cast<const v4i32*>(place(row, c));
+    if constexpr (sizeof(T) == 4)
+        if (there > 4) r.part[1] = *reinterpret_cast<const v4i32*>(place(row, c + 4));
+    return r;
+}
+template <typename T> __device__ __forceinline__ v8f32 numbers(const Raw<T>& r, int there) {
+    v8f32 v;
+    if constexpr (sizeof(T) == 4) v = __builtin_bit_cast(v8f32, r);
+    else v = __builtin_convertvector(__builtin_bit_cast(typename Eight<T>::type, r), v8f32);
     if (there < 8) {
 #pragma unroll
         for (int q = 0; q < 8; ++q) v[q] = q < there ? v[q] : 0.0f;
@@ -36,7 +43,7 @@ template <typename T> __device__ __forceinline__ v8f32 load_eight(const T* p, in
 }
 // of weights, which lie anywhere
 __device__ __forceinline__ v8f32 load_weights(const float* p, int there, bool wide) {
-    if (wide && there >= 8) return load_eight(p, 8);
+    if (wide && there >= 8) return __builtin_shufflevector(*reinterpret_cast<const v4f32*>(p), *reinterpret_cast<const v4f32*>(p + 4), 0, 1, 2, 3, 4, 5, 6, 7);
     v8f32 v = {};
 #pragma unroll
     for (int q = 0; q < 8; ++q)
@@ -59,45 +66,66 @@ template <typename T> __device__ __forceinline__ void store_eight(T* p, v8f32 v,
 }
 template <typename T> __device__ __forceinline__ bool rows_wide(const T* p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * sizeof(T) % 16 == 0; }
 
-// The sums of N numbers over a workgroup, for all its threads; `lds` has room for N numbers a wave and is free again when the next call's first barrier is passed.
-template <int THREADS, int N> __device__ __forceinline__ void row_sums(float (&v)[N], float* lds) {
+// Sums over a wave, without LDS: rows of sixteen lanes, then across them.
+template <int CONTROL, int ROWS> __device__ __forceinline__ float moved(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CONTROL, ROWS, 0xF, false));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+    v += moved<0x111, 0xF>(v);           // from 1, 2, 4, 8 lanes below
+    v += moved<0x112, 0xF>(v);
+    v += moved<0x114, 0xF>(v);
+    v += moved<0x118, 0xF>(v);
+    v += moved<0x142, 0xA>(v);           // the last lane of a row to the next one
+    v += moved<0x143, 0xC>(v);           // lane 31 to the upper half
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+// The sums of N numbers over a workgroup, for all its threads.  Calls take the two halves of `places` in turn, so that one meeting is enough.
+template <int THREADS> struct Meeting {
+    static constexpr int WAVES = THREADS / 64;
+    float (*places)[2][WAVES];           // [half][number][wave]
+    int half = 0;
+    template <int N> __device__ __forceinline__ void sums(float (&v)[N]) {
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1)
+        for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+        if constexpr (WAVES > 1) {
+            if ((threadIdx.x & 63) == 0) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], d);
-    if constexpr (THREADS > 64) {
-        constexpr int WAVES = THREADS / 64;
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) {
+                for (int i = 0; i < N; ++i) places[half][i][threadIdx.x >> 6] = v[i];
+            }
+            __syncthreads();
 #pragma unroll
-            for (int i = 0; i < N; ++i) lds[(threadIdx.x >> 6) * N + i] = v[i];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            v[i] = lds[(threadIdx.x & (WAVES - 1)) * N + i];
-#pragma unroll
-            for (int d = 1; d < WAVES; d <<= 1) v[i] += __shfl_xor(v[i], d);
+            for (int i = 0; i < N; ++i) {
+                // a lane has a wave's
+                float all = places[half][i][threadIdx.x & (WAVES - 1)];
+                all += moved<0x111, 0xF>(all);
+                if constexpr (WAVES > 2) all += moved<0x112, 0xF>(all);
+                if constexpr (WAVES > 4) all += moved<0x114, 0xF>(all);
+                if constexpr (WAVES > 8) all += moved<0x118, 0xF>(all);
+                v[i] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, all), WAVES - 1));
+            }
+            half ^= 1;
         }
     }
-}
+};
+__device__ __forceinline__ v8f32 multiply_add(v8f32 a, v8f32 b, v8f32 c) { return __builtin_elementwise_fma(a, b, c); }
 __device__ __forceinline__ float dot(v8f32 a, v8f32 b, float s) {
 #pragma unroll
     for (int q = 0; q < 8; ++q) s = __builtin_fmaf(a[q], b[q], s);
     return s;
 }
 
-// rho of a row and (ALONG) mean(d n) with n = row * rho; through(p): piece p of d
+// rho of a row x and (ALONG) mean(d n) with n = x * rho; x(p), d(p): piece p
 struct RowNorm { float rho, along; };
-template <int THREADS, bool ALONG, int PIECES, typename F>
-__device__ __forceinline__ RowNorm row_norm(const v8f32 (&x)[PIECES], F through, float k, float eps, float* lds) {
+template <bool ALONG, int PIECES, int THREADS, typename X, typename F>
+__device__ __forceinline__ RowNorm row_norm(X x, F d, float k, float eps, Meeting<THREADS>& meeting) {
     float s[ALONG ? 2 : 1] = {};
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
-        s[0] = dot(x[p], x[p], s[0]);
-        if constexpr (ALONG) s[1] = dot(through(p), x[p], s[1]);
+        const v8f32 xp = x(p);
+        s[0] = dot(xp, xp, s[0]);
+        if constexpr (ALONG) s[1] = dot(d(p), xp, s[1]);
     }
-    row_sums<THREADS>(s, lds);
+    meeting.sums(s);
     RowNorm r = {__builtin_amdgcn_rsqf(s[0] / k + eps), 0.0f};
     const bool above = !(s[0] < 0x1p126f), below = s[0] < 0x1p-90f && eps < 0x1p-80f;
     bool again = above || below;
@@ -110,61 +138,96 @@ __device__ __forceinline__ RowNorm row_norm(const v8f32 (&x)[PIECES], F through,
         const float f = above ? 0x1p-72f : below ? 0x1p100f : 1.0f;
         float q[1] = {0.0f};
 #pragma unroll
-        for (int p = 0; p < PIECES; ++p) q[0] = dot(x[p] * f, x[p] * f, q[0]);
-        row_sums<THREADS>(q, lds);
+        for (int p = 0; p < PIECES; ++p) q[0] = dot(x(p) * f, x(p) * f, q[0]);
+        meeting.sums(q);
         r.rho = f * __builtin_amdgcn_rsqf(q[0] / k + eps * f * f);
         if constexpr (ALONG) {
             q[0] = 0.0f;
 #pragma unroll
-            for (int p = 0; p < PIECES; ++p) q[0] = dot(through(p), x[p] * r.rho, q[0]);
-            row_sums<THREADS>(q, lds);
+            for (int p = 0; p < PIECES; ++p) q[0] = dot(d(p), x(p) * r.rho, q[0]);
+            meeting.sums(q);
             r.along = q[0] / k;
         }
     }
     return r;
 }
 
+// A thread's columns, and their weights: w_pre, and what of w_post, gate and scale goes with x.
+template <int PIECES> struct Columns {
+    unsigned c[PIECES];
+    int there[PIECES];
+    bool wide_post, wide_pre, wide_gate;
+    __device__ __forceinline__ Columns(const BlockNormArgs& a, int threads) {
+        wide_post = rows_wide(a.w_post, 0);
+        wide_pre = rows_wide(a.w_pre, 0);
+        wide_gate = rows_wide(a.gate, a.k);
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) {
+            c[p] = (p * threads + threadIdx.x) * 8;
+            there[p] = (int)a.k - (int)c[p];
+        }
+    }
+    __device__ __forceinline__ v8f32 pre(const BlockNormArgs& a, int p) const { return load_weights(place(a.w_pre, c[p]), there[p], wide_pre); }
+    // scale * gate * w_post for the rows of a gate
+    __device__ __forceinline__ v8f32 behind(const BlockNormArgs& a, int64_t gate, int p) const {
+        v8f32 f = v8f32{} + a.scale;
+        if (a.gate != nullptr) f *= load_weights(place(a.gate + gate * a.k, c[p]), there[p], wide_gate);
+        if (a.w_post != nullptr) f *= load_weights(place(a.w_post, c[p]), there[p], wide_post);
+        return f;
+    }
+};
+
 template <int TYPE, int TYPE_R, int THREADS, int PIECES>
 __global__ void __launch_bounds__(THREADS) block_norm_kernel(const BlockNormArgs a) {
     typedef typename Element<TYPE>::type T;
     typedef typename Element<TYPE_R>::type TR;
-    __shared__ float lds[THREADS / 64];
+    __shared__ float places[2][2][THREADS / 64];
+    Meeting<THREADS> meeting{places};
+    constexpr bool AHEAD = THREADS < 1024;           // the next row is asked for in front of this one's sums; the longest rows leave no registers for it
     const auto none = [](int) { return v8f32{}; };
     const T* const X = static_cast<const T*>(a.X);
     const TR* const R = static_cast<const TR*>(a.R);
     TR* const R_out = static_cast<TR*>(a.R_out);
     T* const H = static_cast<T*>(a.H);
     const bool wide_r = rows_wide(R_out, a.ldro), wide_h = rows_wide(H, a.ldh);
-    const bool wide_post = rows_wide(a.w_post, 0), wide_pre = rows_wide(a.w_pre, 0), wide_gate = rows_wide(a.gate, a.k);
-    int c[PIECES], there[PIECES];
-#pragma unroll
-    for (int p = 0; p < PIECES; ++p) {
-        c[p] = (p * THREADS + threadIdx.x) * 8;
-        there[p] = (int)a.k - c[p];
-    }
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        v8f32 x[PIECES], r[PIECES];
+    const Columns<PIECES> at(a, THREADS);
+    // weights stay in registers from row to row; those of the longest rows are read again for each
+    constexpr bool KEPT = PIECES == 1;
+    v8f32 pre = KEPT && H != nullptr ? at.pre(a, 0) : v8f32{}, behind = {};
+    int64_t gate = -1;
+    Raw<T> next_x[PIECES];
+    Raw<TR> next_r[PIECES];
+    const auto load = [&](int64_t row) {
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) {
-            x[p] = X != nullptr ? load_eight(X + row * a.ldx + c[p], there[p]) : v8f32{};
-            r[p] = R != nullptr ? load_eight(R + row * a.ldr + c[p], there[p]) : v8f32{};
+            if (X != nullptr) next_x[p] = load_raw(X + row * a.ldx, at.c[p], at.there[p]);
+            if (R != nullptr) next_r[p] = load_raw(R + row * a.ldr, at.c[p], at.there[p]);
         }
+    };
+    if (AHEAD) load(blockIdx.x);
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        v8f32 x[PIECES], r[PIECES];
+        if (!AHEAD) load(row);
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) {
+            x[p] = X != nullptr ? numbers<T>(next_x[p], at.there[p]) : v8f32{};
+            r[p] = R != nullptr ? numbers<TR>(next_r[p], at.there[p]) : v8f32{};
+        }
+        if (AHEAD && row + gridDim.x < a.rows) load(row + gridDim.x);
         if (X != nullptr) {
-            const float rho = a.w_post != nullptr ? row_norm<THREADS, false>(x, none, (float)a.k, a.eps, lds).rho : 1.0f;
-            const float* const gate = a.gate != nullptr ? a.gate + row / a.group * a.k : nullptr;
+            const int64_t g = a.gate != nullptr ? row / a.group : 0;
+            if (KEPT && g != gate) behind = at.behind(a, gate = g, 0);
+            const float rho = a.w_post != nullptr ? row_norm<false, PIECES>([&](int p) { return x[p]; }, none, (float)a.k, a.eps, meeting).rho : 1.0f;
 #pragma unroll
             for (int p = 0; p < PIECES; ++p) {
-                v8f32 u = x[p];
-                if (a.w_post != nullptr) u = u * rho * load_weights(a.w_post + c[p], there[p], wide_post);
-                if (gate != nullptr) u *= load_weights(gate + c[p], there[p], wide_gate);
-                r[p] += u * a.scale;
-                if (R_out != nullptr) store_eight(R_out + row * a.ldro + c[p], r[p], there[p], wide_r);
+                r[p] = multiply_add(x[p] * rho, KEPT ? behind : at.behind(a, g, p), r[p]);
+                if (R_out != nullptr) store_eight(place(R_out + row * a.ldro, at.c[p]), r[p], at.there[p], wide_r);
             }
         }
         if (H == nullptr) continue;
-        const float rho = row_norm<THREADS, false>(r, none, (float)a.k, a.eps, lds).rho;
+        const float rho = row_norm<false, PIECES>([&](int p) { return r[p]; }, none, (float)a.k, a.eps, meeting).rho;
 #pragma unroll
-        for (int p = 0; p < PIECES; ++p) store_eight(H + row * a.ldh + c[p], r[p] * rho * load_weights(a.w_pre + c[p], there[p], wide_pre), there[p], wide_h);
+        for (int p = 0; p < PIECES; ++p) store_eight(place(H + row * a.ldh, at.c[p]), r[p] * rho * (KEPT ? pre : at.pre(a, p)), at.there[p], wide_h);
     }
 }
 
@@ -187,23 +250,19 @@ template <int TYPE, int TYPE_R, int THREADS, int PIECES>
 __global__ void __launch_bounds__(THREADS) block_norm_grad_kernel(const NormGradWork w) {
     typedef typename Element<TYPE>::type T;
     typedef typename Element<TYPE_R>::type TR;
-    __shared__ float lds[2 * (THREADS / 64)];
-    // The sums over rows, t and s: in registers, or (the longest rows, which leave no registers) a thread's own places in LDS.
-    constexpr bool HELD = THREADS == 1024 && PIECES == 2;
-    __shared__ v4f32 held[HELD ? 4 * PIECES : 1][HELD ? THREADS : 1];
-    v8f32 kept[2][HELD ? 1 : PIECES] = {};
-    const auto add = [&](int which, int p, v8f32 v) {
-        if constexpr (HELD) {
-            held[which * 4 + 2 * p][threadIdx.x] += __builtin_shufflevector(v, v, 0, 1, 2, 3);
-            held[which * 4 + 2 * p + 1][threadIdx.x] += __builtin_shufflevector(v, v, 4, 5, 6, 7);
-        } else {
-            kept[which][p] += v;
-        }
+    __shared__ float places[2][2][THREADS / 64];
+    Meeting<THREADS> meeting{places};
+    // What goes with columns lies in LDS, each thread's in places of its own: the sums over rows, t and s, and the weights (those of the longest rows are read again
+    // for each).  In registers they would leave room for half as many waves.
+    enum { SUM_T, SUM_S, PRE, BEHIND };
+    constexpr bool LONG = PIECES > 1 || (TYPE == TYPE_F32 && THREADS == 1024), AHEAD = THREADS < 1024;
+    __shared__ v4f32 held[LONG ? 2 : 4][2 * PIECES][THREADS];
+    const auto get = [&](int which, int p) { return __builtin_shufflevector(held[which][2 * p][threadIdx.x], held[which][2 * p + 1][threadIdx.x], 0, 1, 2, 3, 4, 5, 6, 7); };
+    const auto put = [&](int which, int p, v8f32 v) {
+        held[which][2 * p][threadIdx.x] = __builtin_shufflevector(v, v, 0, 1, 2, 3);
+        held[which][2 * p + 1][threadIdx.x] = __builtin_shufflevector(v, v, 4, 5, 6, 7);
     };
-    if constexpr (HELD) {
-#pragma unroll
-        for (int i = 0; i < 4 * PIECES; ++i) held[i][threadIdx.x] = v4f32{};
-    }
+    const auto add = [&](int which, int p, v8f32 a, v8f32 b) { put(which, p, multiply_add(a, b, get(which, p))); };
     const BlockNormArgs& a = w.a;
     const T* const X = static_cast<const T*>(a.X);
     const T* const dH = static_cast<const T*>(a.dH);
@@ -212,31 +271,23 @@ __global__ void __launch_bounds__(THREADS) block_norm_grad_kernel(const NormGrad
     T* const dX = static_cast<T*>(a.dX);
     TR* const dR = static_cast<TR*>(a.dR);
     const bool wide_x = rows_wide(dX, a.lddx), wide_r = rows_wide(dR, a.lddr);
-    const bool wide_post = rows_wide(a.w_post, 0), wide_pre = rows_wide(a.w_pre, 0), wide_gate = rows_wide(a.gate, a.k);
-    const bool post = X != nullptr && a.w_post != nullptr, branch = X != nullptr && (dX != nullptr || w.s != nullptr);
-    int c[PIECES], there[PIECES];
-#pragma unroll
-    for (int p = 0; p < PIECES; ++p) {
-        c[p] = (p * THREADS + threadIdx.x) * 8;
-        there[p] = (int)a.k - c[p];
-    }
+    const bool post = a.w_post != nullptr, branch = X != nullptr && (dX != nullptr || w.s != nullptr);
+    const Columns<PIECES> at(a, THREADS);
     const auto leave = [&](float* to, int which) {
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) {
-            v8f32 v;
-            if constexpr (HELD) {
-                v = __builtin_shufflevector(held[which * 4 + 2 * p][threadIdx.x], held[which * 4 + 2 * p + 1][threadIdx.x], 0, 1, 2, 3, 4, 5, 6, 7);
-                held[which * 4 + 2 * p][threadIdx.x] = held[which * 4 + 2 * p + 1][threadIdx.x] = v4f32{};
-            } else {
-                v = kept[which][p];
-                kept[which][p] = v8f32{};
-            }
-            store_eight(to + c[p], v, there[p], a.k % 4 == 0);
+            store_eight(place(to, at.c[p]), get(which, p), at.there[p], a.k % 4 == 0);
+            put(which, p, v8f32{});
         }
     };
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+        put(SUM_T, p, v8f32{});
+        put(SUM_S, p, v8f32{});
+    }
+    if (!LONG && dH != nullptr) put(PRE, 0, at.pre(a, 0));
     const NormChunks& n = w.n;
-    int64_t row, end, left;                          // left: rows to the end of the unit
-    int64_t unit;
+    int64_t row, end, left, unit;                    // left: rows to the end of the unit
     if (n.per_group > 0) {
         const int64_t g = blockIdx.x / n.per_group, j = blockIdx.x - g * n.per_group, last = (g + 1) * n.group < a.rows ? (g + 1) * n.group : a.rows;
         row = g * n.group + j * n.rows;
@@ -249,58 +300,69 @@ __global__ void __launch_bounds__(THREADS) block_norm_grad_kernel(const NormGrad
         left = n.group;
         unit = blockIdx.x * (n.rows / n.group);
     }
+    int64_t gate = -1;
+    // A row's pieces: in registers, the next row's on their way; of the longest rows read again whenever they are needed, which the caches serve.
+    Raw<T> next_x, next_dh;
+    Raw<TR> next_r, next_dr;
+    const auto load = [&](int64_t i) {
+        if (dH != nullptr) {
+            next_r = load_raw(R + i * a.ldr, at.c[0], at.there[0]);
+            next_dh = load_raw(dH + i * a.lddh, at.c[0], at.there[0]);
+        }
+        if (dR_out != nullptr) next_dr = load_raw(dR_out + i * a.lddro, at.c[0], at.there[0]);
+        if (branch) next_x = load_raw(X + i * a.ldx, at.c[0], at.there[0]);
+    };
+    if (AHEAD && row < end) load(row);
     for (; row < end; ++row) {
-        v8f32 x[PIECES], r[PIECES], dh[PIECES], dr[PIECES];
-        const auto load_x = [&]() {
-#pragma unroll
-            for (int p = 0; p < PIECES; ++p) x[p] = branch ? load_eight(X + row * a.ldx + c[p], there[p]) : v8f32{};
-        };
+        v8f32 x0, r0, dh0, dr[PIECES];
+        asm volatile("" ::: "memory");               // (nothing of LDS is kept in registers from row to row)
+        if constexpr (!LONG) {
+            if (!AHEAD) load(row);
+            dr[0] = dR_out != nullptr ? numbers<TR>(next_dr, at.there[0]) : v8f32{};
+            if (dH != nullptr) {
+                r0 = numbers<TR>(next_r, at.there[0]);
+                dh0 = numbers<T>(next_dh, at.there[0]);
+            }
+            if (branch) x0 = numbers<T>(next_x, at.there[0]);
+            if (AHEAD && row + 1 < end) load(row + 1);
+        }
+        const auto x = [&](int p) { return LONG ? numbers<T>(load_raw(X + row * a.ldx, at.c[p], at.there[p]), at.there[p]) : x0; };
+        const auto r = [&](int p) { return LONG ? numbers<TR>(load_raw(R + row * a.ldr, at.c[p], at.there[p]), at.there[p]) : r0; };
+        const auto dh = [&](int p) { return LONG ? numbers<T>(load_raw(dH + row * a.lddh, at.c[p], at.there[p]), at.there[p]) : dh0; };
+        const auto dn = [&](int p) { return dh(p) * (LONG ? at.pre(a, p) : get(PRE, p)); };
+        RowNorm rn = {0.0f, 0.0f};
+        if (dH != nullptr) rn = row_norm<true, PIECES>(r, dn, (float)a.k, a.eps, meeting);
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) {
-            dr[p] = dR_out != nullptr ? load_eight(dR_out + row * a.lddro + c[p], there[p]) : v8f32{};
-            dh[p] = dH != nullptr ? load_eight(dH + row * a.lddh + c[p], there[p]) : v8f32{};
-            r[p] = dH != nullptr ? load_eight(R + row * a.ldr + c[p], there[p]) : v8f32{};
-        }
-        if constexpr (!HELD) load_x();
-        if (dH != nullptr) {
-            const RowNorm rn = row_norm<THREADS, true>(r, [&](int p) { return dh[p] * load_weights(a.w_pre + c[p], there[p], wide_pre); }, (float)a.k, a.eps, lds);
-#pragma unroll
-            for (int p = 0; p < PIECES; ++p) {
-                const v8f32 n = r[p] * rn.rho;
-                dr[p] += (dh[p] * load_weights(a.w_pre + c[p], there[p], wide_pre) - n * rn.along) * rn.rho;
-                add(0, p, dh[p] * n);
+            if (LONG) dr[p] = dR_out != nullptr ? numbers<TR>(load_raw(dR_out + row * a.lddro, at.c[p], at.there[p]), at.there[p]) : v8f32{};
+            if (dH != nullptr) {
+                const v8f32 m = r(p) * rn.rho;
+                dr[p] = multiply_add(multiply_add(-m, v8f32{} + rn.along, dn(p)), v8f32{} + rn.rho, dr[p]);
+                add(SUM_T, p, dh(p), m);
             }
-        }
-        if (dR != nullptr) {
-#pragma unroll
-            for (int p = 0; p < PIECES; ++p) store_eight(dR + row * a.lddr + c[p], dr[p], there[p], wide_r);
+            if (dR != nullptr) store_eight(place(dR + row * a.lddr, at.c[p]), dr[p], at.there[p], wide_r);
         }
         if (branch) {
-            if constexpr (HELD) load_x();
-            // what the gradient of m is, or of x without a norm
-            const float* const gate = a.gate != nullptr ? a.gate + row / a.group * a.k : nullptr;
-            const auto through = [&](int p) {
-                v8f32 d = dr[p] * a.scale;
-                if (gate != nullptr) d *= load_weights(gate + c[p], there[p], wide_gate);
-                return post ? d * load_weights(a.w_post + c[p], there[p], wide_post) : d;
-            };
+            const int64_t g = a.gate != nullptr ? row / a.group : 0;
+            if (!LONG && g != gate) put(BEHIND, 0, at.behind(a, gate = g, 0));
+            const auto dm = [&](int p) { return dr[p] * (LONG ? at.behind(a, g, p) : get(BEHIND, p)); };       // the gradient of m, or of x where that has no norm
             RowNorm xn = {1.0f, 0.0f};
-            if (post) xn = row_norm<THREADS, true>(x, through, (float)a.k, a.eps, lds);
+            if (post) xn = row_norm<true, PIECES>(x, dm, (float)a.k, a.eps, meeting);
 #pragma unroll
             for (int p = 0; p < PIECES; ++p) {
-                const v8f32 m = x[p] * xn.rho;
-                add(1, p, dr[p] * m);
-                if (dX != nullptr) store_eight(dX + row * a.lddx + c[p], post ? (through(p) - m * xn.along) * xn.rho : through(p), there[p], wide_x);
+                const v8f32 m = x(p) * xn.rho;
+                add(SUM_S, p, dr[p], m);
+                if (dX != nullptr) store_eight(place(dX + row * a.lddx, at.c[p]), multiply_add(-m, v8f32{} + xn.along, dm(p)) * xn.rho, at.there[p], wide_x);
             }
         }
         if (--left == 0 && n.per_group == 0) {
-            if (w.s != nullptr) leave(w.s + unit * a.k, 1);
+            if (w.s != nullptr) leave(w.s + unit * a.k, SUM_S);
             ++unit;
             left = n.group;
         }
     }
-    if (w.s != nullptr && (n.per_group > 0 || left < n.group)) leave(w.s + unit * a.k, 1);
-    if (w.t != nullptr) leave(w.t + blockIdx.x * a.k, 0);
+    if (w.s != nullptr && (n.per_group > 0 || left < n.group)) leave(w.s + unit * a.k, SUM_S);
+    if (w.t != nullptr) leave(w.t + blockIdx.x * a.k, SUM_T);
 }
 
 // Sums over chunks and units: 32 columns a workgroup, in 32 shares.  blockIdx.y: 0 dw_pre, 1 dw_post, from 2 on a gate's gradient.
@@ -353,11 +415,13 @@ __global__ void __launch_bounds__(256) block_norm_gate_kernel(const NormGradWork
 // threads and pieces of eight elements a thread that hold a row
 struct RowShape { int threads, pieces; };
 RowShape row_shape(int64_t k) {
-    return k <= 512 ? RowShape{64, 1} : k <= 1024 ? RowShape{64, 2} : k <= 2048 ? RowShape{256, 1} : k <= 4096 ? RowShape{256, 2} : k <= 8192 ? RowShape{1024, 1} : RowShape{1024, 2};
+    int threads = 64;
+    while (threads < 1024 && threads * 8 < k) threads *= 2;
+    return RowShape{threads, threads * 8 < k ? 2 : 1};
 }
 NormChunks norm_chunks(int64_t rows, int64_t k, int64_t group) {
     const int threads = row_shape(k).threads;
-    const int64_t most = threads == 64 ? 2048 : threads == 256 ? 768 : 256;
+    const int64_t most = threads <= 128 ? 2048 : 262144 / threads;
     NormChunks n;
     n.group = group > 0 && group < rows ? group : rows;
     n.groups = div_up(rows, n.group);
@@ -377,9 +441,14 @@ size_t up(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 
 template <typename F> hipError_t with_shape(int64_t k, F f) {
     const RowShape s = row_shape(k);
-    if (s.threads == 64) return s.pieces == 1 ? f(std::integral_constant<int, 64>(), std::integral_constant<int, 1>()) : f(std::integral_constant<int, 64>(), std::integral_constant<int, 2>());
-    if (s.threads == 256) return s.pieces == 1 ? f(std::integral_constant<int, 256>(), std::integral_constant<int, 1>()) : f(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
-    return s.pieces == 1 ? f(std::integral_constant<int, 1024>(), std::integral_constant<int, 1>()) : f(std::integral_constant<int, 1024>(), std::integral_constant<int, 2>());
+    const std::integral_constant<int, 1> one;
+    switch (s.threads) {
+        case 64: return f(std::integral_constant<int, 64>(), one);
+        case 128: return f(std::integral_constant<int, 128>(), one);
+        case 256: return f(std::integral_constant<int, 256>(), one);
+        case 512: return f(std::integral_constant<int, 512>(), one);
+        default: return s.pieces == 1 ? f(std::integral_constant<int, 1024>(), one) : f(std::integral_constant<int, 1024>(), std::integral_constant<int, 2>());
+    }
 }
 template <typename F> hipError_t with_types(int type, int type_r, F f) {
     if (type == TYPE_F32) return f(std::integral_constant<int, TYPE_F32>(), std::integral_constant<int, TYPE_F32>());
