@@ -11,36 +11,70 @@
 namespace ozaki {
 namespace {
 
-constexpr int64_t CHUNK = 32768;         // elements
-constexpr int TABLE = 96;                // tensors in a launch's arguments, which hold 4 KiB
+constexpr int64_t MOST_CHUNK = 32768, LEAST_CHUNK = 4096;     // elements
+constexpr int TABLE = 144;               // tensors in a launch's arguments, which hold 4 KiB
 constexpr unsigned MOST_BLOCKS = 2048;   // of a launch, and partial sums that it leaves
-constexpr int THREADS = 256;
+constexpr int THREADS = 256, MOST_JOINED = 512;
 
 struct ClipTable {
     const void* x[TABLE];
     void* out[TABLE];
-    int64_t size[TABLE];
-    uint32_t first[TABLE + 1];           // chunk
-    uint8_t type[TABLE];
-    int count;
+    uint64_t size[TABLE];                // and the type, in the two highest bits
+    uint32_t first[TABLE];               // chunk; behind the last tensor the number of all chunks
+    uint32_t chunks, chunk;              // elements of a chunk
 };
-static_assert(sizeof(ClipTable) < 3840, "kernel arguments");
+static_assert(sizeof(ClipTable) + 24 <= 4096, "kernel arguments");
 
-// f(x, first element, elements, type's constant) for chunk `at`
-template <typename F> __device__ __forceinline__ void with_chunk(const ClipTable& t, uint32_t at, F f) {
-    int lo = 0, hi = t.count - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (t.first[mid] <= at) lo = mid;
-        else hi = mid - 1;
+// The table in a wave's registers, a tensor a lane, read in one go: a search in memory would wait for each of its steps, since arguments come from far away.
+struct ClipLanes {
+    static constexpr int ROUNDS = (TABLE + 63) / 64;
+    const void* x[ROUNDS];
+    void* out[ROUNDS];
+    uint64_t size[ROUNDS];
+    uint32_t first[ROUNDS];
+    __device__ __forceinline__ explicit ClipLanes(const ClipTable& t, bool results) {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            const int i = r * 64 + lane < TABLE ? r * 64 + lane : TABLE - 1;
+            x[r] = t.x[i];
+            out[r] = results ? t.out[i] : nullptr;
+            size[r] = t.size[i];
+            first[r] = t.first[i];
+        }
     }
-    const int64_t from = (int64_t)(at - t.first[lo]) * CHUNK, left = t.size[lo] - from, n = left < CHUNK ? left : CHUNK;
-    switch (t.type[lo]) {
-        case TYPE_BF16: f(lo, from, n, std::integral_constant<int, TYPE_BF16>()); break;
-        case TYPE_F16: f(lo, from, n, std::integral_constant<int, TYPE_F16>()); break;
-        default: f(lo, from, n, std::integral_constant<int, TYPE_F32>()); break;
+    // f(x, out, elements, type's constant) for chunk `at`
+    template <typename F> __device__ __forceinline__ void with_chunk(uint32_t at, uint32_t chunk, F f) const {
+        int i = -1;                      // tensors that begin there or before it (the places behind the last hold the number of all chunks)
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) i += __popcll(__ballot(first[r] <= at && r * 64 + (threadIdx.x & 63) < TABLE));
+        const int lane = i & 63, round = i >> 6;
+        const auto lanes = [&](uint64_t v) {
+            return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane) << 32;
+        };
+        uint64_t p = 0, q = 0, n = 0;
+        uint32_t begin = 0;
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r)
+            if (r == round) {
+                p = lanes(reinterpret_cast<uint64_t>(x[r]));
+                q = lanes(reinterpret_cast<uint64_t>(out[r]));
+                n = lanes(size[r]);
+                begin = (uint32_t)__builtin_amdgcn_readlane((int)first[r], lane);
+            }
+        const int type = (int)(n >> 62);
+        n &= ((uint64_t)1 << 62) - 1;
+        const uint64_t from = (uint64_t)(at - begin) * chunk, left = n - from;
+        const int elements = (int)(left < chunk ? left : chunk);
+        const auto of = [&](auto c) {
+            typedef typename Element<decltype(c)::value>::type T;
+            f(reinterpret_cast<const T*>(p) + from, reinterpret_cast<T*>(q) + from, elements);
+        };
+        if (type == TYPE_BF16) of(std::integral_constant<int, TYPE_BF16>());
+        else if (type == TYPE_F16) of(std::integral_constant<int, TYPE_F16>());
+        else of(std::integral_constant<int, TYPE_F32>());
     }
-}
+};
 
 // hi + lo, with lo less than hi's last place
 struct Sum { float hi, lo; };
@@ -66,16 +100,16 @@ __device__ __forceinline__ Squares block_sum(Squares v) {
     return all;
 }
 
-// A thread's squares of the n elements of a chunk, each times `factor` first: eight sums, of CHUNK / THREADS / 8 = 16 elements each at most.
-template <typename T> __device__ __forceinline__ float chunk_squares(const T* x, int64_t n, float factor) {
+// A thread's squares of the n elements of a chunk, each times `factor` first: eight sums, of MOST_CHUNK / THREADS / 8 = 16 elements each at most.
+template <typename T> __device__ __forceinline__ float chunk_squares(const T* x, int n, float factor) {
     typedef T eight __attribute__((ext_vector_type(8), aligned(16)));
     float sum[8] = {};
     const auto add = [&](int q, T v) { sum[q] = __builtin_fmaf((float)v * factor, (float)v * factor, sum[q]); };
-    int64_t e = 0;
+    int e = 0;
     if (reinterpret_cast<uintptr_t>(x) % 16 == 0) {
-        const int64_t pieces = n / 8;
+        const int pieces = n / 8;
 #pragma unroll 4
-        for (int64_t p = threadIdx.x; p < pieces; p += THREADS) {
+        for (int p = threadIdx.x; p < pieces; p += THREADS) {
             const eight v = reinterpret_cast<const eight*>(x)[p];
 #pragma unroll
             for (int q = 0; q < 8; ++q) add(q, v[q]);
@@ -88,18 +122,17 @@ template <typename T> __device__ __forceinline__ float chunk_squares(const T* x,
     }
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
-        const int64_t at = e + q * THREADS + threadIdx.x;
+        const int at = e + q * THREADS + threadIdx.x;
         if (at < n) add(q, x[at]);
     }
     return ((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7]));
 }
 
 __global__ void __launch_bounds__(THREADS) gradient_squares_kernel(const ClipTable t, Squares* partial) {
+    const ClipLanes lanes(t, false);
     Squares all = {};
-    for (uint32_t at = blockIdx.x; at < t.first[t.count]; at += gridDim.x)
-        with_chunk(t, at, [&](int i, int64_t from, int64_t n, auto type) {
-            typedef typename Element<decltype(type)::value>::type T;
-            const T* const x = static_cast<const T*>(t.x[i]) + from;
+    for (uint32_t at = blockIdx.x; at < t.chunks; at += gridDim.x)
+        lanes.with_chunk(at, t.chunk, [&](auto x, auto, int n) {
             const float sum = chunk_squares(x, n, 1.0f);
             if (sum >= 0x1p-80f && sum < 0x1p90f) {
                 all.level[PLAIN] = all.level[PLAIN] + Sum{sum, 0.0f};
@@ -113,15 +146,16 @@ __global__ void __launch_bounds__(THREADS) gradient_squares_kernel(const ClipTab
     if (threadIdx.x == 0) partial[blockIdx.x] = all;
 }
 
-__global__ void __launch_bounds__(THREADS) gradient_norm_kernel(const Squares* partial, int64_t count, float scale, float* norm) {
+// the norm from `count` partial sums, for all threads of a workgroup
+__device__ __forceinline__ float norm_of(const Squares* partial, int count, float scale) {
     Squares all = {};
-    for (int64_t i = threadIdx.x; i < count; i += THREADS) {
+#pragma unroll 4
+    for (int i = threadIdx.x; i < count; i += THREADS) {
         const Squares p = partial[i];
 #pragma unroll
         for (int l = 0; l < LEVELS; ++l) all.level[l] = all.level[l] + p.level[l];
     }
     all = block_sum(all);
-    if (threadIdx.x != 0) return;
     // the highest level that is there, with the next one's share of it (the one below that is less than its last place)
     const auto scaled = [](Sum s, float f) { return Sum{s.hi * f, s.lo * f}; };
     const bool large = all.level[LARGE].hi != 0.0f, plain = all.level[PLAIN].hi != 0.0f;
@@ -132,25 +166,37 @@ __global__ void __launch_bounds__(THREADS) gradient_norm_kernel(const Squares* p
     // the root with what it lacks, times the scale: one rounding
     const float root = sqrtf(sum.hi), lacks = root > 0.0f && root < __builtin_inff() ? (__builtin_fmaf(-root, root, sum.hi) + sum.lo) / (2.0f * root) : 0.0f;
     const float n = root * by, rest = root < __builtin_inff() ? __builtin_fmaf(root, by, -n) + lacks * by : 0.0f;
-    *norm = (n + rest) * back;
+    return (n + rest) * back;
 }
 
-__global__ void __launch_bounds__(THREADS) gradient_clip_kernel(const ClipTable t, const float* norm_at, float scale, float max_norm) {
+__global__ void __launch_bounds__(THREADS) gradient_norm_kernel(const Squares* partial, int count, float scale, float* norm) {
+    const float n = norm_of(partial, count, scale);
+    if (threadIdx.x == 0) *norm = n;
+}
+
+// `count` partial sums, each workgroup adding them up itself; 0: the norm is there.
+__global__ void __launch_bounds__(THREADS) gradient_clip_kernel(const ClipTable t, float* norm_at, const Squares* partial, int count, float scale, float max_norm) {
+    const ClipLanes lanes(t, true);
+    float norm;
+    if (count > 0) {
+        norm = norm_of(partial, count, scale);
+        if (blockIdx.x == 0 && threadIdx.x == 0) *norm_at = norm;
+    } else {
+        norm = *norm_at;
+    }
     // (a norm that is no number makes the factor none, one that is infinite makes it zero)
-    const float norm = *norm_at, factor = norm <= max_norm ? scale : scale * (max_norm / norm);
-    for (uint32_t at = blockIdx.x; at < t.first[t.count]; at += gridDim.x)
-        with_chunk(t, at, [&](int i, int64_t from, int64_t n, auto type) {
-            typedef typename Element<decltype(type)::value>::type T;
+    const float factor = norm <= max_norm ? scale : scale * (max_norm / norm);
+    for (uint32_t i = blockIdx.x; i < t.chunks; i += gridDim.x)
+        lanes.with_chunk(t.chunks - 1 - i, t.chunk, [&](auto x, auto out, int n) {
+            typedef std::remove_pointer_t<decltype(out)> T;
             constexpr int PER = 16 / sizeof(T);
             typedef T piece __attribute__((ext_vector_type(PER)));
-            const T* const x = static_cast<const T*>(t.x[i]) + from;
-            T* const out = static_cast<T*>(t.out[i]) + from;
             if (factor == 1.0f && x == out) return;
-            int64_t e = threadIdx.x;
+            int e = threadIdx.x;
             if (reinterpret_cast<uintptr_t>(x) % 16 == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0) {
-                const int64_t pieces = n / PER;
+                const int pieces = n / PER;
 #pragma unroll 4
-                for (int64_t p = threadIdx.x; p < pieces; p += THREADS) {
+                for (int p = threadIdx.x; p < pieces; p += THREADS) {
                     piece v = reinterpret_cast<const piece*>(x)[p];
 #pragma unroll
                     for (int q = 0; q < PER; ++q) v[q] = (T)((float)v[q] * factor);
@@ -163,57 +209,62 @@ __global__ void __launch_bounds__(THREADS) gradient_clip_kernel(const ClipTable 
         });
 }
 
-// f(table, blocks, index of the launch) for each launch
-template <typename F> hipError_t with_tables(const ClipArgs& a, F f) {
-    ClipTable t;
-    t.count = 0;
-    t.first[0] = 0;
-    int launch = 0;
-    const auto flush = [&]() -> hipError_t {
-        if (t.count == 0) return hipSuccess;
-        const uint32_t chunks = t.first[t.count];
-        f(t, chunks < MOST_BLOCKS ? chunks : MOST_BLOCKS, launch++);
-        t.count = 0;
-        return hipGetLastError();
-    };
-    for (int i = 0; i < a.count; ++i) {
-        if (a.sizes[i] == 0) continue;
-        const int64_t chunks = div_up(a.sizes[i], CHUNK);
-        if (t.count == TABLE) {      // (no tensor has more than 2^38 elements: their chunks' numbers stay inside 32 bits)
-            const hipError_t e = flush();
-            if (e != hipSuccess) return e;
+// A launch's tensors: from `begin` on, as many as fit; returns where the next one begins.
+int fill_table(const ClipArgs& a, int begin, ClipTable& t) {
+    int at[TABLE], count = 0, i = begin;
+    uint64_t total = 0;
+    for (; i < a.count && count < TABLE; ++i)
+        if (a.sizes[i] > 0) {
+            at[count++] = i;
+            total += a.sizes[i];
         }
-        t.x[t.count] = a.tensors[i];
-        t.out[t.count] = a.out != nullptr ? a.out[i] : nullptr;
-        t.size[t.count] = a.sizes[i];
-        t.type[t.count] = (uint8_t)a.types[i];
-        t.first[t.count + 1] = t.first[t.count] + (uint32_t)chunks;
-        ++t.count;
+    // chunks of a size that gives every compute unit eight, where that is inside the bounds (no tensor has more than 2^38 elements: their numbers stay inside 32 bits)
+    t.chunk = LEAST_CHUNK;
+    while (t.chunk < MOST_CHUNK && total / t.chunk > MOST_BLOCKS) t.chunk *= 2;
+    t.chunks = 0;
+    for (int j = 0; j < TABLE; ++j) {
+        t.first[j] = t.chunks;
+        t.x[j] = j < count ? a.tensors[at[j]] : nullptr;
+        t.out[j] = j < count && a.out != nullptr ? a.out[at[j]] : nullptr;
+        t.size[j] = j < count ? (uint64_t)a.sizes[at[j]] | (uint64_t)a.types[at[j]] << 62 : 0;
+        if (j < count) t.chunks += (uint32_t)div_up(a.sizes[at[j]], t.chunk);
     }
-    return flush();
+    return i;
 }
+unsigned blocks_of(const ClipTable& t) { return t.chunks < MOST_BLOCKS ? t.chunks : MOST_BLOCKS; }
 
 }  // namespace
 
 size_t gradient_norm_bytes(int64_t count) { return (size_t)div_up(count, TABLE) * MOST_BLOCKS * sizeof(Squares); }
 
 hipError_t launch_clip(const ClipArgs& a, hipStream_t st) {
-    if (!a.given) {
-        int64_t partials = 0;
-        Squares* const partial = reinterpret_cast<Squares*>(a.ws);
-        hipError_t e = with_tables(a, [&](const ClipTable& t, unsigned blocks, int) {
-            hipLaunchKernelGGL(gradient_squares_kernel, dim3(blocks), dim3(THREADS), 0, st, t, partial + partials);
-            partials += blocks;
-        });
+    Squares* const partial = reinterpret_cast<Squares*>(a.ws);
+    int partials = 0, launches = 0;
+    ClipTable t;
+    for (int i = 0; i < a.count && !a.given;) {
+        i = fill_table(a, i, t);
+        if (t.chunks == 0) break;
+        hipLaunchKernelGGL(gradient_squares_kernel, dim3(blocks_of(t)), dim3(THREADS), 0, st, t, partial + partials);
+        const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
+        partials += blocks_of(t);
+        ++launches;
+    }
+    // Few partial sums are added up by every workgroup of the second reading, without a launch in between.
+    const bool apart = !a.given && (a.out == nullptr || launches != 1 || partials > MOST_JOINED);
+    if (apart) {
         hipLaunchKernelGGL(gradient_norm_kernel, dim3(1), dim3(THREADS), 0, st, partial, partials, a.scale, a.norm);
-        e = hipGetLastError();
+        const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (a.out == nullptr) return hipSuccess;
-    return with_tables(a, [&](const ClipTable& t, unsigned blocks, int) {
-        hipLaunchKernelGGL(gradient_clip_kernel, dim3(blocks), dim3(THREADS), 0, st, t, a.norm, a.scale, a.max_norm);
-    });
+    for (int i = 0; i < a.count && a.out != nullptr;) {
+        i = fill_table(a, i, t);
+        if (t.chunks == 0) break;
+        hipLaunchKernelGGL(gradient_clip_kernel, dim3(blocks_of(t)), dim3(THREADS), 0, st, t, a.norm, partial, a.given || apart ? 0 : partials, a.scale, a.max_norm);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace ozaki
