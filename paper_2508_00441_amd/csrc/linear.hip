@@ -169,9 +169,10 @@ template <int TYPE, bool PAIR>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) linear_middle_kernel(const LinearWork w) {
     linear_body<Tile<kind_of(TYPE), 2, 2, 4, 4, 2, false, false, PAIR>, TYPE>(w);
 }
-template <int TYPE, bool PAIR>
+// DEEP: one workgroup to a compute unit, with seven steps under way instead of three
+template <int TYPE, bool PAIR, bool DEEP>
 __global__ void __launch_bounds__(256) linear_small_kernel(const LinearWork w) {
-    linear_body<Tile<kind_of(TYPE), 2, 2, 2, 2, 4, false, false, PAIR>, TYPE>(w);
+    linear_body<Tile<kind_of(TYPE), 2, 2, 2, 2, DEEP ? 8 : 4, false, false, PAIR>, TYPE>(w);
 }
 
 // Up to sixteen vectors of X: no tile in LDS.  A workgroup of FEW_WAVES waves takes sixteen vectors of W (of each, of a pair), a wave every
@@ -307,7 +308,8 @@ hipError_t launch_kind(const LinearArgs& a, Shape s, hipStream_t st) {
     w.order = WorkOrder{s.kind == LARGE ? 32 : 64, 8};
     const unsigned blocks = (unsigned)((int64_t)w.tiles_m * w.tiles_n * s.splits);
     if (s.kind == VECTORS) hipLaunchKernelGGL((linear_few_kernel<TYPE, PAIR>), dim3(blocks), dim3(FEW_WAVES * 64), 0, st, a, s.splits);
-    else if (s.kind == SMALL) hipLaunchKernelGGL((linear_small_kernel<TYPE, PAIR>), dim3(blocks), dim3(256), 0, st, w);
+    else if (s.kind == SMALL && blocks <= 256) hipLaunchKernelGGL((linear_small_kernel<TYPE, PAIR, true>), dim3(blocks), dim3(256), 0, st, w);
+    else if (s.kind == SMALL) hipLaunchKernelGGL((linear_small_kernel<TYPE, PAIR, false>), dim3(blocks), dim3(256), 0, st, w);
     else if (s.kind == MIDDLE) hipLaunchKernelGGL((linear_middle_kernel<TYPE, PAIR>), dim3(blocks), dim3(256), 0, st, w);
     else hipLaunchKernelGGL((linear_large_kernel<TYPE, PAIR>), dim3(blocks), dim3(512), 0, st, w);
     if (s.splits > 1) {

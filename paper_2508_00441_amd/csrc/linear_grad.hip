@@ -5,7 +5,8 @@
 // dz (dg, du) is formed once, in 16 bits: its rounding is of the size of the results' own.  dbias is summed in the same pass, of what has not been
 // rounded.  Without an activation dz is dy itself.  Both products are sums over 16-bit elements in FP32 on the matrix unit (tile_product.hpp); W in dx, and
 // dz and x in dW, lie across the inner dimension and are turned on the way from LDS to registers.  The two terms of a pair's dx are one sum.
-// Where there are few tiles the inner dimension is cut into shares whose sums meet in work memory, in their order.
+// Both products go in one launch, so that the tiles of one fill up what the other leaves of the compute units.  Where there are few tiles all the same, the inner
+// dimension is cut into shares whose sums meet in work memory, in their order.
 #include "block_operators.hpp"
 #include "layout.hpp"
 #include "tile_product.hpp"
@@ -111,10 +112,10 @@ struct ProductWork {
     WorkOrder order;
 };
 
+// `b` of `blocks` workgroups
 template <typename P, typename T, bool YT>
-__device__ __forceinline__ void product_body(const ProductWork& w) {
-    __shared__ __attribute__((aligned(16))) uint8_t lds[P::LDS_BYTES];
-    const WorkItem item = work_item(blockIdx.x, gridDim.x, w.order, w.tiles_m * w.results, w.tiles_n);
+__device__ __forceinline__ void product_body(const ProductWork& w, uint8_t* lds, unsigned b, unsigned blocks) {
+    const WorkItem item = work_item(b, blocks, w.order, w.tiles_m * w.results, w.tiles_n);
     const int result = item.bm >= (unsigned)w.tiles_m ? 1 : 0, split = item.gi;
     const int64_t m0 = (int64_t)(item.bm - result * w.tiles_m) * P::TM, n0 = (int64_t)item.bn * P::TN, left_m = w.m - m0, left_n = w.n - n0;
     const int begin = split_begin(w.steps * w.terms, w.splits, split), end = split_begin(w.steps * w.terms, w.splits, split + 1);
@@ -135,25 +136,32 @@ __device__ __forceinline__ void product_body(const ProductWork& w) {
     }
 }
 
-template <int TYPE>
-__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) linear_dx_large_kernel(const ProductWork w) {
-    product_body<PairedTile<kind_of(TYPE), true, false>, typename Element<TYPE>::type, false>(w);
+// Both products, or one: `dx_blocks` workgroups have tiles of dX, the others of dW; `dx_first` says whose go out first.
+struct BothWork {
+    ProductWork dx, dw;
+    unsigned dx_blocks, dw_blocks;
+    bool dx_first;
+};
+template <typename PX, typename PW, typename T>
+__device__ __forceinline__ void both_body(const BothWork& w) {
+    static_assert(PX::THREADS == PW::THREADS, "");
+    __shared__ __attribute__((aligned(16))) uint8_t lds[PX::LDS_BYTES > PW::LDS_BYTES ? PX::LDS_BYTES : PW::LDS_BYTES];
+    const unsigned front = w.dx_first ? w.dx_blocks : w.dw_blocks, b = blockIdx.x < front ? blockIdx.x : blockIdx.x - front;
+    if ((blockIdx.x < front) == w.dx_first) product_body<PX, T, false>(w.dx, lds, b, w.dx_blocks);
+    else product_body<PW, T, true>(w.dw, lds, b, w.dw_blocks);
 }
+
 template <int TYPE>
-__global__ void __launch_bounds__(256) linear_dx_middle_kernel(const ProductWork w) {
-    product_body<Tile<kind_of(TYPE), 2, 2, 4, 2, 3, true, false>, typename Element<TYPE>::type, false>(w);
+__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) linear_grad_large_kernel(const BothWork w) {
+    both_body<PairedTile<kind_of(TYPE), true, false>, PairedTile<kind_of(TYPE), true, true>, typename Element<TYPE>::type>(w);
 }
-template <int TYPE>
-__global__ void __launch_bounds__(256) linear_dx_few_kernel(const ProductWork w) {
-    product_body<Tile<kind_of(TYPE), 4, 1, 2, 1, 4, true, false>, typename Element<TYPE>::type, false>(w);
-}
-template <int TYPE>
-__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) linear_dw_large_kernel(const ProductWork w) {
-    product_body<PairedTile<kind_of(TYPE), true, true>, typename Element<TYPE>::type, true>(w);
-}
-template <int TYPE>
-__global__ void __launch_bounds__(256) linear_dw_middle_kernel(const ProductWork w) {
-    product_body<Tile<kind_of(TYPE), 2, 2, 4, 4, 2, true, true>, typename Element<TYPE>::type, true>(w);
+// of dX 64 x 128 elements or (FEW) 16 x 128, of dW 128 x 128; DEEP: one workgroup to a compute unit, with twice the steps under way
+template <int TYPE, bool FEW, bool DEEP>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 2))) linear_grad_middle_kernel(const BothWork w) {
+    typedef Tile<kind_of(TYPE), 2, 2, 4, 4, DEEP ? 4 : 2, true, true> DW;
+    typedef typename Element<TYPE>::type T;
+    if constexpr (FEW) both_body<Tile<kind_of(TYPE), 4, 1, 2, 1, DEEP ? 8 : 4, true, false>, DW, T>(w);
+    else both_body<Tile<kind_of(TYPE), 2, 2, 4, 2, DEEP ? 6 : 3, true, false>, DW, T>(w);
 }
 
 // the shares' sums in their order; blockIdx.z: the result
@@ -175,23 +183,33 @@ __global__ void __launch_bounds__(256) linear_product_join_kernel(const ProductW
 
 enum { FEW, MIDDLE, LARGE };
 struct Shape { int kind, tm, tn, splits; };
-int shares_of(int64_t tiles, int64_t at_a_time, int64_t steps) {
-    const int64_t want = at_a_time / tiles, most = steps / 8;
-    const int64_t s = want < most ? want : most;
-    return (int)(s < 1 ? 1 : s > 32 ? 32 : s);
-}
-// dX: m x n over `steps` steps.  Large tiles also where they are few, if that leaves every compute unit a share of the inner dimension of some length.
-Shape dx_shape(int64_t m, int64_t n, int64_t steps) {
-    const int64_t large = div_up(m, 256) * div_up(n, 256);
-    Shape s = m <= 16 ? Shape{FEW, 16, 128, 1} : m > 128 && (large >= 128 || large * (steps / 16) >= 128) ? Shape{LARGE, 256, 256, 1} : Shape{MIDDLE, 64, 128, 1};
-    s.splits = shares_of(div_up(m, s.tm) * div_up(n, s.tn), s.kind == LARGE ? 256 : 512, steps);
-    return s;
-}
-// dW: `results` of m x n
-Shape dw_shape(int64_t m, int64_t n, int64_t steps, int results) {
-    const int64_t large = results * div_up(m, 256) * div_up(n, 256);
-    Shape s = m > 128 && n > 128 && (large >= 128 || large * (steps / 16) >= 128) ? Shape{LARGE, 256, 256, 1} : Shape{MIDDLE, 128, 128, 1};
-    s.splits = shares_of(results * div_up(m, s.tm) * div_up(n, s.tn), s.kind == LARGE ? 256 : 512, steps);
+// Of dX, which is m x k, and of dW, `results` of n x k; `dx`, `dw`: which are wanted.  A size that has none: 0 tiles.
+struct Shapes {
+    Shape dx, dw;
+    int64_t dx_tiles, dw_tiles, dx_steps, dw_steps;
+};
+Shapes shapes_of(int64_t m, int64_t n, int64_t k, bool pair, bool dx, bool dw) {
+    const int results = pair ? 2 : 1;
+    Shapes s = {};
+    s.dx_steps = div_up(n, 64) * results;
+    s.dw_steps = div_up(m, 64);
+    const auto tiles = [](int64_t rows, int64_t columns, int64_t tm, int64_t tn) { return div_up(rows, tm) * div_up(columns, tn); };
+    const int64_t dx_large = tiles(m, k, 256, 256), dw_large = results * tiles(n, k, 256, 256);
+    // Large tiles where both results together have as much for them to do as eight steps of every second compute unit; also where they are few.
+    const int64_t work = (dx ? dx_large * s.dx_steps : 0) + (dw ? dw_large * s.dw_steps : 0);
+    const bool large = m > 128 && k > 128 && n > 128 && work >= 128 * 16;
+    s.dx = m <= 16 ? Shape{FEW, 16, 128, 1} : large ? Shape{LARGE, 256, 256, 1} : Shape{MIDDLE, 64, 128, 1};
+    s.dw = large ? Shape{LARGE, 256, 256, 1} : Shape{MIDDLE, 128, 128, 1};
+    s.dx_tiles = dx ? tiles(m, k, s.dx.tm, s.dx.tn) : 0;
+    s.dw_tiles = dw ? results * tiles(n, k, s.dw.tm, s.dw.tn) : 0;
+    // Shares as long as a compute unit has steps to do in all, in which a step of dW's smaller tiles counts twice
+    const int64_t weight = large ? 1 : 2, all = s.dx_tiles * s.dx_steps + s.dw_tiles * s.dw_steps * weight, each = div_up(all, large ? 256 : 512);
+    const auto shares = [&](int64_t steps, int64_t weighted) {
+        const int64_t want = (2 * weighted + each) / (2 * each), most = steps / (large ? 8 : 4), splits = want < most ? want : most;
+        return (int)(splits < 1 ? 1 : splits > 32 ? 32 : splits);
+    };
+    s.dx.splits = shares(s.dx_steps, s.dx_steps);
+    s.dw.splits = shares(s.dw_steps, s.dw_steps * weight);
     return s;
 }
 
@@ -199,24 +217,32 @@ struct Places {
     uint8_t* dZ;
     uint8_t* dU;
     float* sums;
-    float* partial;
+    uint8_t* partial;
     size_t total;
 };
-constexpr int64_t MOST_CHUNKS = 128;
-int64_t chunk_rows(int64_t m, int64_t n) {
-    const int64_t strips = div_up(n, SLOPE_COLUMNS), want = 2048 / strips, chunks = want < 1 ? 1 : want > MOST_CHUNKS ? MOST_CHUNKS : want, rows = div_up(m, chunks);
-    return rows < 16 ? 16 : rows;
+// Rows of a chunk.  With dbias: at most 128 chunks, whose sums the join reads.
+int64_t chunk_rows(int64_t m, int64_t n, bool pair) {
+    const int64_t strips = div_up(n, SLOPE_COLUMNS), want = 2048 / strips, most = pair ? 65535 : 128, chunks = want < 1 ? 1 : want > most ? most : want, rows = div_up(m, chunks);
+    return rows < SLOPE_WAVES ? SLOPE_WAVES : rows;
+}
+size_t partial_bytes(const Shapes& s, int64_t m, int64_t n, int64_t k, int results, size_t& for_dx) {
+    for_dx = s.dx.splits > 1 && s.dx_tiles > 0 ? up((size_t)s.dx.splits * m * in_fours(k) * 4) : 0;
+    return for_dx + (s.dw.splits > 1 && s.dw_tiles > 0 ? up((size_t)results * s.dw.splits * n * in_fours(k) * 4) : 0);
 }
 Places places_of(uint8_t* ws, int64_t m, int64_t n, int64_t k, bool pair) {
     Places p;
-    size_t at = 0;
+    size_t at = 0, unused;
     const auto take = [&](size_t bytes) { uint8_t* const here = ws + at; at += up(bytes); return here; };
-    const Shape dx = dx_shape(m, k, div_up(n, 64) * (pair ? 2 : 1)), dw = dw_shape(n, k, div_up(m, 64), pair ? 2 : 1);
-    const size_t for_dx = dx.splits > 1 ? (size_t)dx.splits * m * in_fours(k) * 4 : 0, for_dw = dw.splits > 1 ? (size_t)(pair ? 2 : 1) * dw.splits * n * in_fours(k) * 4 : 0;
     p.dZ = take((size_t)m * in_eights(n) * 2);
     p.dU = take(pair ? (size_t)m * in_eights(n) * 2 : 0);
-    p.sums = reinterpret_cast<float*>(take(pair ? 0 : (size_t)div_up(m, chunk_rows(m, n)) * in_eights(n) * 4));
-    p.partial = reinterpret_cast<float*>(take(for_dx > for_dw ? for_dx : for_dw));
+    p.sums = reinterpret_cast<float*>(take(pair ? 0 : (size_t)div_up(m, chunk_rows(m, n, pair)) * in_eights(n) * 4));
+    // the shares' sums, of whatever results a call asks for
+    size_t most = 0;
+    for (int which = 1; which < 4; ++which) {
+        const size_t need = partial_bytes(shapes_of(m, n, k, pair, which & 1, which & 2), m, n, k, pair ? 2 : 1, unused);
+        most = need > most ? need : most;
+    }
+    p.partial = take(most);
     p.total = at;
     return p;
 }
@@ -224,23 +250,33 @@ Places places_of(uint8_t* ws, int64_t m, int64_t n, int64_t k, bool pair) {
 #define OZAKI_LINEAR_TRY(expr) do { const hipError_t e_ = (expr); if (e_ != hipSuccess) return e_; } while (0)
 
 template <int TYPE>
-hipError_t launch_product(ProductWork w, Shape s, bool dw, hipStream_t st) {
+hipError_t launch_join(const ProductWork& w, hipStream_t st) {
+    if (w.splits == 1) return hipSuccess;
+    hipLaunchKernelGGL((linear_product_join_kernel<TYPE>), dim3((unsigned)div_up(w.n, 1024), (unsigned)(w.m < 65535 ? w.m : 65535), (unsigned)w.results), dim3(256), 0, st, w);
+    return hipGetLastError();
+}
+unsigned set_tiles(ProductWork& w, const Shape& s) {
     w.splits = s.splits;
     w.tiles_m = (int)div_up(w.m, s.tm);
     w.tiles_n = (int)div_up(w.n, s.tn);
     w.order = WorkOrder{s.kind == LARGE ? 32 : 64, 8};
-    const dim3 blocks((unsigned)((int64_t)w.tiles_m * w.results * w.tiles_n * w.splits));
-    if (dw && s.kind == LARGE) hipLaunchKernelGGL((linear_dw_large_kernel<TYPE>), blocks, dim3(512), 0, st, w);
-    else if (dw) hipLaunchKernelGGL((linear_dw_middle_kernel<TYPE>), blocks, dim3(256), 0, st, w);
-    else if (s.kind == LARGE) hipLaunchKernelGGL((linear_dx_large_kernel<TYPE>), blocks, dim3(512), 0, st, w);
-    else if (s.kind == MIDDLE) hipLaunchKernelGGL((linear_dx_middle_kernel<TYPE>), blocks, dim3(256), 0, st, w);
-    else hipLaunchKernelGGL((linear_dx_few_kernel<TYPE>), blocks, dim3(256), 0, st, w);
+    return (unsigned)((int64_t)w.tiles_m * w.results * w.tiles_n * w.splits);
+}
+template <int TYPE>
+hipError_t launch_both(BothWork w, const Shapes& s, bool dx, bool dw, hipStream_t st) {
+    w.dx_blocks = dx ? set_tiles(w.dx, s.dx) : 0;
+    w.dw_blocks = dw ? set_tiles(w.dw, s.dw) : 0;
+    w.dx_first = s.dx_steps / s.dx.splits >= s.dw_steps / s.dw.splits;
+    const dim3 blocks(w.dx_blocks + w.dw_blocks);
+    const bool deep = blocks.x <= 256;
+    if (s.dw.kind == LARGE) hipLaunchKernelGGL((linear_grad_large_kernel<TYPE>), blocks, dim3(512), 0, st, w);
+    else if (s.dx.kind == FEW && deep) hipLaunchKernelGGL((linear_grad_middle_kernel<TYPE, true, true>), blocks, dim3(256), 0, st, w);
+    else if (s.dx.kind == FEW) hipLaunchKernelGGL((linear_grad_middle_kernel<TYPE, true, false>), blocks, dim3(256), 0, st, w);
+    else if (deep) hipLaunchKernelGGL((linear_grad_middle_kernel<TYPE, false, true>), blocks, dim3(256), 0, st, w);
+    else hipLaunchKernelGGL((linear_grad_middle_kernel<TYPE, false, false>), blocks, dim3(256), 0, st, w);
     OZAKI_LINEAR_TRY(hipGetLastError());
-    if (w.splits > 1) {
-        hipLaunchKernelGGL((linear_product_join_kernel<TYPE>), dim3((unsigned)div_up(w.n, 1024), (unsigned)(w.m < 65535 ? w.m : 65535), (unsigned)w.results), dim3(256), 0, st, w);
-        OZAKI_LINEAR_TRY(hipGetLastError());
-    }
-    return hipSuccess;
+    if (dx) OZAKI_LINEAR_TRY(launch_join<TYPE>(w.dx, st));
+    return dw ? launch_join<TYPE>(w.dw, st) : hipSuccess;
 }
 
 template <int TYPE>
@@ -262,7 +298,7 @@ hipError_t grad_typed(const LinearGradArgs& a, hipStream_t st) {
     w.lddy = a.lddy;
     w.ld = in_eights(a.n);
     w.activation = a.activation;
-    w.rows = chunk_rows(a.m, a.n);
+    w.rows = chunk_rows(a.m, a.n, pair);
     const int64_t chunks = div_up(a.m, w.rows);
     w.whole = chunks == 1;
     w.sums = a.dbias == nullptr ? nullptr : w.whole ? a.dbias : p.sums;
@@ -278,47 +314,48 @@ hipError_t grad_typed(const LinearGradArgs& a, hipStream_t st) {
     }
     const uint8_t* const dz[2] = {formed ? p.dZ : static_cast<const uint8_t*>(a.dY), p.dU};
     const int64_t lddz = (formed ? w.ld : a.lddy) * 2;
-    if (a.dX != nullptr) {
-        ProductWork d = {};
-        d.X[0] = static_cast<const uint8_t*>(a.W);
-        d.X[1] = static_cast<const uint8_t*>(a.W2);
-        d.Y[0] = dz[0];
-        d.Y[1] = dz[1];
-        d.D[0] = a.dX;
-        d.ldx = a.ldw * 2;
-        d.ldy = lddz;
-        d.ldd = a.lddx;
-        d.elements = a.n;
-        d.m = a.m;
-        d.n = a.k;
-        d.partial = p.partial;
-        d.terms = pair ? 2 : 1;
-        d.results = 1;
-        d.steps = (int)div_up(a.n, 64);
-        OZAKI_LINEAR_TRY(launch_product<TYPE>(d, dx_shape(d.m, d.n, (int64_t)d.steps * d.terms), false, st));
+    const bool dx = a.dX != nullptr, both = a.dW != nullptr && a.dW2 != nullptr, dw = a.dW != nullptr || a.dW2 != nullptr;
+    if (!dx && !dw) return hipSuccess;
+    // (of a pair one dW is cut as both are, so that it has the same bits)
+    const Shapes s = shapes_of(a.m, a.n, a.k, pair, dx, dw);
+    size_t for_dx;
+    partial_bytes(s, a.m, a.n, a.k, pair ? 2 : 1, for_dx);
+    BothWork d = {};
+    if (dx) {
+        d.dx.X[0] = static_cast<const uint8_t*>(a.W);
+        d.dx.X[1] = static_cast<const uint8_t*>(a.W2);
+        d.dx.Y[0] = dz[0];
+        d.dx.Y[1] = dz[1];
+        d.dx.D[0] = a.dX;
+        d.dx.ldx = a.ldw * 2;
+        d.dx.ldy = lddz;
+        d.dx.ldd = a.lddx;
+        d.dx.elements = a.n;
+        d.dx.m = a.m;
+        d.dx.n = a.k;
+        d.dx.partial = reinterpret_cast<float*>(p.partial);
+        d.dx.terms = pair ? 2 : 1;
+        d.dx.results = 1;
+        d.dx.steps = (int)div_up(a.n, 64);
     }
-    if (a.dW != nullptr || a.dW2 != nullptr) {
-        ProductWork d = {};
-        const bool both = a.dW != nullptr && a.dW2 != nullptr;
-        d.X[0] = static_cast<const uint8_t*>(a.X);
-        d.Y[0] = a.dW != nullptr ? dz[0] : dz[1];
-        d.Y[1] = dz[1];
-        d.D[0] = a.dW != nullptr ? a.dW : a.dW2;
-        d.D[1] = a.dW2;
-        d.ldx = a.ldx * 2;
-        d.ldy = lddz;
-        d.ldd = a.lddw;
-        d.elements = a.m;
-        d.m = a.n;
-        d.n = a.k;
-        d.partial = p.partial;
-        d.terms = 1;
-        d.results = both ? 2 : 1;
-        d.steps = (int)div_up(a.m, 64);
-        // (the shape of both, also for one of a pair: the same bits)
-        OZAKI_LINEAR_TRY(launch_product<TYPE>(d, dw_shape(d.m, d.n, d.steps, pair ? 2 : 1), true, st));
+    if (dw) {
+        d.dw.X[0] = static_cast<const uint8_t*>(a.X);
+        d.dw.Y[0] = a.dW != nullptr ? dz[0] : dz[1];
+        d.dw.Y[1] = dz[1];
+        d.dw.D[0] = a.dW != nullptr ? a.dW : a.dW2;
+        d.dw.D[1] = a.dW2;
+        d.dw.ldx = a.ldx * 2;
+        d.dw.ldy = lddz;
+        d.dw.ldd = a.lddw;
+        d.dw.elements = a.m;
+        d.dw.m = a.n;
+        d.dw.n = a.k;
+        d.dw.partial = reinterpret_cast<float*>(p.partial + for_dx);
+        d.dw.terms = 1;
+        d.dw.results = both ? 2 : 1;
+        d.dw.steps = (int)div_up(a.m, 64);
     }
-    return hipSuccess;
+    return launch_both<TYPE>(d, s, dx, dw, st);
 }
 
 }  // namespace
