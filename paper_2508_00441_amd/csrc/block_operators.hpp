@@ -108,9 +108,27 @@ __device__ __forceinline__ float gelu_argument(float z) {
     const float c = fminf(fmaxf(z, -20.0f), 20.0f);
     return 2.0f * GELU_C * (c + GELU_CUBE * c * c * c);
 }
+// Phi(z) and exp(-z^2 / 2).  With x = |z| / sqrt(2) and r = 1 / (1 + 0.4 x), erfc(x) exp(x^2) / r is a polynomial of degree 8 in 2 r - 1 to within 1.3e-7 of itself for
+// all x (least squares, reweighted until the largest relative error is least); so the tail keeps its relative precision, and 20 instructions do what the library's erfc takes
+// several times as many for.
+struct Normal { float phi, e; };
+__device__ __forceinline__ Normal normal_of(float z) {
+    const float r = __builtin_amdgcn_rcpf(__builtin_fmaf(0.4f * 0.70710678118654752440f, fabsf(z), 1.0f)), t = __builtin_fmaf(2.0f, r, -1.0f);
+    float q = 1.963244576472789e-04f;
+    q = __builtin_fmaf(q, t, 1.4176529657561332e-04f);
+    q = __builtin_fmaf(q, t, -1.8630237318575382e-03f);
+    q = __builtin_fmaf(q, t, -3.3358947839587927e-03f);
+    q = __builtin_fmaf(q, t, 1.1324104852974415e-02f);
+    q = __builtin_fmaf(q, t, 6.849516183137894e-02f);
+    q = __builtin_fmaf(q, t, 1.8156789243221283e-01f);
+    q = __builtin_fmaf(q, t, 3.218610882759094e-01f);
+    q = __builtin_fmaf(q, t, 4.216126799583435e-01f);
+    const float e = __builtin_amdgcn_exp2f(-0.72134752044448170368f * z * z), half = 0.5f * q * r * e;
+    return Normal{z < 0.0f ? half : 1.0f - half, e};
+}
 template <int ACT> __device__ __forceinline__ float activated(float z) {
     if constexpr (ACT == ACT_RELU) return z < 0.0f ? 0.0f : z;
-    if constexpr (ACT == ACT_GELU) return z * (0.5f * erfcf(-0.70710678118654752440f * z));      // (1 + erf would cancel where z < 0)
+    if constexpr (ACT == ACT_GELU) return z * normal_of(z).phi;
     if constexpr (ACT == ACT_GELU_TANH) return z * sigmoid_of(gelu_argument(z)).p;                 // (1 + tanh y) / 2 = 1 / (1 + exp(-2 y))
     if constexpr (ACT == ACT_SILU) return z * sigmoid_of(z).p;
     return z;
@@ -120,8 +138,8 @@ struct Activation { float value, slope; };
 template <int ACT> __device__ __forceinline__ Activation activation_of(float z) {
     if constexpr (ACT == ACT_RELU) return Activation{z < 0.0f ? 0.0f : z, z > 0.0f ? 1.0f : z <= 0.0f ? 0.0f : z};
     if constexpr (ACT == ACT_GELU) {
-        const float p = 0.5f * erfcf(-0.70710678118654752440f * z), density = 0.39894228040143267794f * __builtin_amdgcn_exp2f(-0.72134752044448170368f * z * z);
-        return Activation{z * p, p + z * density};
+        const Normal n = normal_of(z);
+        return Activation{z * n.phi, n.phi + z * (0.39894228040143267794f * n.e)};
     }
     if constexpr (ACT == ACT_GELU_TANH) {
         const Sigmoid s = sigmoid_of(gelu_argument(z));

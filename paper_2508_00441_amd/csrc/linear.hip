@@ -34,33 +34,64 @@ struct Epilogue {
         if constexpr (STREAMED) __builtin_nontemporal_store(w, p);
         else *p = w;
     }
-    __device__ __forceinline__ void piece(int64_t m, int64_t c, v8f32 v, v8f32 u) const {
-        if constexpr (PAIR) {
-            if (a.Z != nullptr) {
-                put(a.Z, m * a.ldz + c, v);
-                put(a.U, m * a.ldu + c, u);
-            }
-        } else {
-            if (a.bias != nullptr) v += eight_at(static_cast<const T*>(a.bias) + c);
-            if (a.Z != nullptr) put(a.Z, m * a.ldz + c, v);
-        }
+    __device__ __forceinline__ v8f32 activate(v8f32 v) const {
         with_activation(a.activation, [&](auto act) {
 #pragma unroll
             for (int q = 0; q < 8; ++q) v[q] = activated<decltype(act)::value>(v[q]);
         });
+        return v;
+    }
+    // What eight columns, or one, need beside their sums, for every row: the bias.
+    __device__ __forceinline__ v8f32 columns(int64_t c) const { return !PAIR && a.bias != nullptr ? eight_at(static_cast<const T*>(a.bias) + c) : v8f32{}; }
+    __device__ __forceinline__ float column(int64_t c) const { return !PAIR && a.bias != nullptr ? (float)static_cast<const T*>(a.bias)[c] : 0.0f; }
+    // ... and for one row: the residual, asked for in front of the others' arithmetic
+    __device__ __forceinline__ eight ahead(int64_t m, int64_t c) const {
+        return !PAIR && a.R != nullptr ? *reinterpret_cast<const eight*>(static_cast<const T*>(a.R) + m * a.ldr + c) : eight{};
+    }
+    __device__ __forceinline__ void piece(int64_t m, int64_t c, v8f32 v, v8f32 u, v8f32 bias, eight r) const {
+        v += bias;
+        if (a.Z != nullptr) {
+            put(a.Z, m * a.ldz + c, v);
+            if constexpr (PAIR) put(a.U, m * a.ldu + c, u);
+        }
+        v = activate(v);
         if constexpr (PAIR) v *= u;
-        else if (a.R != nullptr) v += eight_at(static_cast<const T*>(a.R) + m * a.ldr + c);
+        else v += __builtin_convertvector(r, v8f32);
         put(a.Y, m * a.ldy + c, v);
     }
+    // the sums of one column of rows m0 + m[q]; `there`: bit q, that row exists
+    template <int N> __device__ __forceinline__ void rows(int64_t m0, const int (&m)[N], unsigned there, int64_t c, float (&v)[N], const float (&u)[N], float bias) const {
+        T r[N];
+        if constexpr (!PAIR) {
+#pragma unroll
+            for (int q = 0; q < N; ++q) r[q] = a.R != nullptr && (there >> q & 1) ? static_cast<const T*>(a.R)[(m0 + m[q]) * a.ldr + c] : (T)0.0f;
+        }
+#pragma unroll
+        for (int q = 0; q < N; ++q) v[q] += bias;
+        if (a.Z != nullptr) {
+#pragma unroll
+            for (int q = 0; q < N; ++q)
+                if (there >> q & 1) {
+                    static_cast<T*>(a.Z)[(m0 + m[q]) * a.ldz + c] = (T)v[q];
+                    if constexpr (PAIR) static_cast<T*>(a.U)[(m0 + m[q]) * a.ldu + c] = (T)u[q];
+                }
+        }
+        with_activation(a.activation, [&](auto act) {
+#pragma unroll
+            for (int q = 0; q < N; ++q) v[q] = activated<decltype(act)::value>(v[q]);
+        });
+#pragma unroll
+        for (int q = 0; q < N; ++q) {
+            if constexpr (PAIR) v[q] *= u[q];
+            else v[q] += (float)r[q];
+            if (there >> q & 1) static_cast<T*>(a.Y)[(m0 + m[q]) * a.ldy + c] = (T)v[q];
+        }
+    }
     __device__ __forceinline__ void one(int64_t m, int64_t c, float v, float u) const {
-        if constexpr (PAIR) {
-            if (a.Z != nullptr) {
-                static_cast<T*>(a.Z)[m * a.ldz + c] = (T)v;
-                static_cast<T*>(a.U)[m * a.ldu + c] = (T)u;
-            }
-        } else {
-            if (a.bias != nullptr) v += (float)static_cast<const T*>(a.bias)[c];
-            if (a.Z != nullptr) static_cast<T*>(a.Z)[m * a.ldz + c] = (T)v;
+        v += column(c);
+        if (a.Z != nullptr) {
+            static_cast<T*>(a.Z)[m * a.ldz + c] = (T)v;
+            if constexpr (PAIR) static_cast<T*>(a.U)[m * a.ldu + c] = (T)u;
         }
         with_activation(a.activation, [&](auto act) { v = activated<decltype(act)::value>(v); });
         if constexpr (PAIR) v *= u;
@@ -74,8 +105,12 @@ struct Partial {
     float* to;
     int64_t ld, second;
     bool wide = true;
+    typedef float eight;             // (nothing beside the sums)
+    __device__ __forceinline__ float columns(int64_t) const { return 0.0f; }
+    __device__ __forceinline__ float column(int64_t) const { return 0.0f; }
+    __device__ __forceinline__ float ahead(int64_t, int64_t) const { return 0.0f; }
     template <typename V> __device__ __forceinline__ void put(int64_t at, V v) const { *reinterpret_cast<V*>(to + at) = v; }
-    __device__ __forceinline__ void piece(int64_t m, int64_t c, v8f32 v, v8f32 u) const {
+    __device__ __forceinline__ void piece(int64_t m, int64_t c, v8f32 v, v8f32 u, float, float) const {
         const int64_t at = m * ld + c;
         put(at, __builtin_shufflevector(v, v, 0, 1, 2, 3));
         put(at + 4, __builtin_shufflevector(v, v, 4, 5, 6, 7));
@@ -86,6 +121,11 @@ struct Partial {
     __device__ __forceinline__ void one(int64_t m, int64_t c, float v, float u) const {
         to[m * ld + c] = v;
         if (second != 0) to[m * ld + c + second] = u;
+    }
+    template <int N> __device__ __forceinline__ void rows(int64_t m0, const int (&m)[N], unsigned there, int64_t c, float (&v)[N], const float (&u)[N], float) const {
+#pragma unroll
+        for (int q = 0; q < N; ++q)
+            if (there >> q & 1) one(m0 + m[q], c, v[q], u[q]);
     }
 };
 
@@ -103,29 +143,52 @@ __device__ __forceinline__ void put_tile(uint8_t* lds, const v4f32 (&acc)[P::FN]
 #pragma unroll
         for (int i = 0; i < P::FN; ++i) *reinterpret_cast<v4f32*>(mine + (i < HALF ? i * 64 : COLUMNS * 4 + (i - HALF) * 64)) = acc[i][j];
         __syncthreads();
-        const auto row_of = [&](int r) -> int64_t { return ((r >> 4) * P::FM + j) * 16 + (r & 15); };
+        const auto row_of = [&](int r) { return ((r >> 4) * P::FM + j) * 16 + (r & 15); };
         const int column = threadIdx.x % PIECES * 8;
         if (column < whole) {
-            for (int r = threadIdx.x / PIECES; r < ROWS; r += P::THREADS / PIECES) {
-                const int64_t m = row_of(r);
-                if (m >= left_m) continue;
-                const float* const from = reinterpret_cast<const float*>(lds + r * STRIDE) + column;
-                v8f32 v, u = {};
+            constexpr int APART = P::THREADS / PIECES, EACH = ROWS < APART ? 1 : ROWS / APART, AT_ONCE = P::PAIR ? 1 : EACH < 4 ? EACH : 4;
+            static_assert(EACH % AT_ONCE == 0, "");
+            const auto bias = e.columns(n0 + column);
+#pragma unroll 1
+            for (int first = threadIdx.x / PIECES; first < ROWS; first += AT_ONCE * APART) {
+                typename E::eight ahead[AT_ONCE];
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    v[q] = from[q];
-                    if (P::PAIR) u[q] = from[COLUMNS + q];
+                for (int q = 0; q < AT_ONCE; ++q) {
+                    const int m = row_of(first + q * APART);
+                    ahead[q] = e.ahead(m0 + (m < left_m ? m : 0), n0 + column);
                 }
-                e.piece(m0 + m, n0 + column, v, u);
+#pragma unroll
+                for (int q = 0; q < AT_ONCE; ++q) {
+                    const int r = first + q * APART;
+                    const int m = row_of(r);
+                    if (m >= left_m) continue;
+                    const v4f32* const from = reinterpret_cast<const v4f32*>(lds + r * STRIDE + column * 4);
+                    const v8f32 v = __builtin_shufflevector(from[0], from[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                    v8f32 u = {};
+                    if (P::PAIR) u = __builtin_shufflevector(from[COLUMNS / 4], from[COLUMNS / 4 + 1], 0, 1, 2, 3, 4, 5, 6, 7);
+                    e.piece(m0 + m, n0 + column, v, u, bias, ahead[q]);
+                }
             }
         }
         const int c = whole + threadIdx.x % COLUMNS;
         if (c < columns) {
-            for (int r = threadIdx.x / COLUMNS; r < ROWS; r += P::THREADS / COLUMNS) {
-                const int64_t m = row_of(r);
-                if (m >= left_m) continue;
-                const float* const from = reinterpret_cast<const float*>(lds + r * STRIDE) + c;
-                e.one(m0 + m, n0 + c, from[0], P::PAIR ? from[COLUMNS] : 0.0f);
+            constexpr int APART = P::THREADS / COLUMNS, N = P::PAIR && P::TM == 256 ? 4 : 8;       // (of registers for eight the largest tiles leave too few)
+            const float bias = e.column(n0 + c);
+#pragma unroll 1
+            for (int first = threadIdx.x / COLUMNS; first < ROWS; first += N * APART) {
+                int m[N];
+                unsigned there = 0;
+                float v[N], u[N];
+#pragma unroll
+                for (int q = 0; q < N; ++q) {
+                    const int r = first + q * APART < ROWS ? first + q * APART : 0;
+                    m[q] = row_of(r);
+                    there |= first + q * APART < ROWS && m[q] < left_m ? 1u << q : 0u;
+                    const float* const from = reinterpret_cast<const float*>(lds + r * STRIDE) + c;
+                    v[q] = from[0];
+                    u[q] = P::PAIR ? from[COLUMNS] : 0.0f;
+                }
+                e.rows(m0, m, there, n0 + c, v, u, bias);
             }
         }
         __syncthreads();
@@ -157,7 +220,7 @@ __device__ __forceinline__ void linear_body(const LinearWork& w) {
         const int64_t ld = in_fours(a.n);
         put_tile<P>(lds, acc, m0, n0, left_m, in_fours(left_n), Partial{a.partial + split * a.m * ld, ld, PAIR ? w.splits * a.m * ld : 0});
     } else {
-        put_tile<P>(lds, acc, m0, n0, left_m, left_n, Epilogue<TYPE, PAIR, (P::THREADS > 256)>(a));
+        put_tile<P>(lds, acc, m0, n0, left_m, left_n, Epilogue<TYPE, PAIR, (P::TM == 256)>(a));
     }
 }
 
@@ -169,10 +232,19 @@ template <int TYPE, bool PAIR>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) linear_middle_kernel(const LinearWork w) {
     linear_body<Tile<kind_of(TYPE), 2, 2, 4, 4, 2, false, false, PAIR>, TYPE>(w);
 }
-// DEEP: one workgroup to a compute unit, with seven steps under way instead of three
-template <int TYPE, bool PAIR, bool DEEP>
-__global__ void __launch_bounds__(256) linear_small_kernel(const LinearWork w) {
-    linear_body<Tile<kind_of(TYPE), 2, 2, 2, 2, DEEP ? 8 : 4, false, false, PAIR>, TYPE>(w);
+// Smaller tiles in eight waves, two to a SIMD: with one, a step's wait, LDS reads and products follow each other (100 x 5001 x 2048: 14.3 us against 15.8 in four waves)
+template <int TYPE, bool PAIR>
+__global__ void __launch_bounds__(512) linear_half_kernel(const LinearWork w) {
+    linear_body<Tile<kind_of(TYPE), 2, 4, 4, 1, 3, false, false, PAIR>, TYPE>(w);
+}
+template <int TYPE, bool PAIR>
+__global__ void __launch_bounds__(512) linear_small_kernel(const LinearWork w) {
+    linear_body<Tile<kind_of(TYPE), 2, 4, 2, 1, 4, false, false, PAIR>, TYPE>(w);
+}
+// (of a pair a wave has both factors' vectors: half as many waves)
+template <int TYPE, bool PAIR>
+__global__ void __launch_bounds__(PAIR ? 256 : 512) linear_narrow_kernel(const LinearWork w) {
+    linear_body<Tile<kind_of(TYPE), PAIR ? 1 : 2, 4, PAIR ? 2 : 1, 1, 4, false, false, PAIR>, TYPE>(w);
 }
 
 // Up to sixteen vectors of X: no tile in LDS.  A workgroup of FEW_WAVES waves takes sixteen vectors of W (of each, of a pair), a wave every
@@ -273,7 +345,7 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const LinearArgs a, co
             v[o] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         }
         if (e.wide && c + 8 <= a.n) {
-            e.piece(m, c, v[0], v[1]);
+            e.piece(m, c, v[0], v[1], e.columns(c), e.ahead(m, c));
         } else {
 #pragma unroll
             for (int q = 0; q < 8; ++q)
@@ -282,9 +354,16 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const LinearArgs a, co
     }
 }
 
-enum { VECTORS, SMALL, MIDDLE, LARGE };
+enum { VECTORS, NARROW, SMALL, HALF, MIDDLE, LARGE };
 struct Shape { int kind, tm, tn, splits; };
-// By how many tiles there are for 256 compute units; `columns` counts both factors of a pair.
+// By how many tiles there are for 256 compute units; `columns` counts both factors of a pair.  Times in us, with bias and GELU in BF16:
+//     tiles of 64 tokens and 64 columns, up to 128 of them: 32 columns     200 x 2048 x 2048: 11.4, by 64 x 64 13.2;  128 x 4096 x 4096: 17.2, 20.2
+//     fewer than 256 of 64 x 128: 64 x 64                                  1000 x 1000 x 1000: 10.3, by 32 columns 12.0, by 64 x 128 12.4
+//     up to 768 of 64 x 128                                                1024 x 4096 x 4096: 45, by 64 x 64 55, by 128 x 128 50;  300 x 11000 x 4096: 42, 53, 55
+//     up to 512 of 128 x 128                                               2048 x 4096 x 2048: 42.5, by 64 x 128 49, by 256 x 256 60
+//     more: 256 x 256                                                      2048 x 8192 x 512: 33.5, by 128 x 128 38
+// The narrowest tiles where they are fewer than compute units: in shares of the inner dimension of sixteen steps at least (20 x 1000 x 8192: 13.2 in eight, 27.8 uncut;
+// but 48 x 1000 x 500, eight steps: 7.0, in two shares 8.6).
 Shape shape_of(int64_t m, int64_t n, int64_t k, bool pair) {
     const int64_t steps = div_up(k * 2, STEP_BYTES), columns = pair ? 2 * n : n;
     const auto shares = [](int64_t want, int64_t most) {
@@ -292,9 +371,12 @@ Shape shape_of(int64_t m, int64_t n, int64_t k, bool pair) {
         return (int)(s < 1 ? 1 : s > 16 ? 16 : s);
     };
     if (m <= FEW) return Shape{VECTORS, FEW, 16, steps < 96 ? 1 : shares(256 / div_up(n, 16), steps / 32)};
-    const int64_t middle = div_up(m, 128) * div_up(columns, 128), least = m < columns ? m : columns;
-    if (middle >= 256 && least > 64) return middle <= 512 || least <= 128 ? Shape{MIDDLE, 128, pair ? 64 : 128, 1} : Shape{LARGE, 256, pair ? 128 : 256, 1};
-    return Shape{SMALL, 64, pair ? 32 : 64, shares(256 / (div_up(m, 64) * div_up(columns, 64)), steps / 4)};
+    const auto tiles = [&](int64_t tm, int64_t tn) { return div_up(m, tm) * div_up(columns, tn); };
+    const auto shape = [&](int kind, int tm, int tn, int splits) { return Shape{kind, tm, pair ? tn / 2 : tn, splits}; };
+    if (tiles(64, 64) <= 128) return shape(NARROW, 64, 32, shares(256 / tiles(64, 32), steps / 16));
+    if (tiles(64, 128) < 256) return shape(SMALL, 64, 64, 1);
+    if (tiles(64, 128) <= 768) return shape(HALF, 64, 128, 1);
+    return tiles(128, 128) <= 512 || m <= 128 || columns <= 128 ? shape(MIDDLE, 128, 128, 1) : shape(LARGE, 256, 256, 1);
 }
 
 template <int TYPE, bool PAIR>
@@ -308,8 +390,9 @@ hipError_t launch_kind(const LinearArgs& a, Shape s, hipStream_t st) {
     w.order = WorkOrder{s.kind == LARGE ? 32 : 64, 8};
     const unsigned blocks = (unsigned)((int64_t)w.tiles_m * w.tiles_n * s.splits);
     if (s.kind == VECTORS) hipLaunchKernelGGL((linear_few_kernel<TYPE, PAIR>), dim3(blocks), dim3(FEW_WAVES * 64), 0, st, a, s.splits);
-    else if (s.kind == SMALL && blocks <= 256) hipLaunchKernelGGL((linear_small_kernel<TYPE, PAIR, true>), dim3(blocks), dim3(256), 0, st, w);
-    else if (s.kind == SMALL) hipLaunchKernelGGL((linear_small_kernel<TYPE, PAIR, false>), dim3(blocks), dim3(256), 0, st, w);
+    else if (s.kind == NARROW) hipLaunchKernelGGL((linear_narrow_kernel<TYPE, PAIR>), dim3(blocks), dim3(PAIR ? 256 : 512), 0, st, w);
+    else if (s.kind == SMALL) hipLaunchKernelGGL((linear_small_kernel<TYPE, PAIR>), dim3(blocks), dim3(512), 0, st, w);
+    else if (s.kind == HALF) hipLaunchKernelGGL((linear_half_kernel<TYPE, PAIR>), dim3(blocks), dim3(512), 0, st, w);
     else if (s.kind == MIDDLE) hipLaunchKernelGGL((linear_middle_kernel<TYPE, PAIR>), dim3(blocks), dim3(256), 0, st, w);
     else hipLaunchKernelGGL((linear_large_kernel<TYPE, PAIR>), dim3(blocks), dim3(512), 0, st, w);
     if (s.splits > 1) {

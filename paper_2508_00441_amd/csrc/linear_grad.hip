@@ -81,19 +81,29 @@ __global__ void __launch_bounds__(SLOPE_WAVES * 64) linear_slope_kernel(const Sl
         if (q < there) to[q] = sum[q];
 }
 
-// the chunks' sums, in an order of their own that depends on sizes only: 64 columns a workgroup, four shares of the chunks
-__global__ void __launch_bounds__(256) linear_bias_join_kernel(const float* sums, int64_t chunks, int64_t n, int64_t ld, float* dbias) {
-    __shared__ float shares[4][64];
+// The chunks' sums, in an order that depends on sizes only: 64 columns a workgroup, its waves each with a share of the chunks.
+struct BiasJoin {
+    const float* sums;       // null: nothing to do
+    float* dbias;
+    int64_t chunks, n, ld;
+    unsigned blocks;
+};
+constexpr int BIAS_COLUMNS = 64, BIAS_WAVES = 4;
+__device__ __forceinline__ void bias_join(const BiasJoin& w, float* lds, unsigned block) {
     const int lane = threadIdx.x & 63, share = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    const int64_t c = (int64_t)block * BIAS_COLUMNS + lane;
     float sum = 0.0f;
-    if (c < n) {
+    if (c < w.n && share < BIAS_WAVES) {
 #pragma unroll 8
-        for (int64_t i = share; i < chunks; i += 4) sum += sums[i * ld + c];
+        for (int64_t i = share; i < w.chunks; i += BIAS_WAVES) sum += w.sums[i * w.ld + c];
     }
-    shares[share][lane] = sum;
+    if (share < BIAS_WAVES) lds[share * 64 + lane] = sum;
     __syncthreads();
-    if (share == 0 && c < n) dbias[c] = ((shares[0][lane] + shares[1][lane]) + shares[2][lane]) + shares[3][lane];
+    if (share == 0 && c < w.n) w.dbias[c] = ((lds[lane] + lds[64 + lane]) + lds[128 + lane]) + lds[192 + lane];
+}
+__global__ void __launch_bounds__(BIAS_WAVES * 64) linear_bias_join_kernel(const BiasJoin w) {
+    __shared__ float lds[BIAS_WAVES * 64];
+    bias_join(w, lds, blockIdx.x);
 }
 
 // ---- products ----------------------------------------------------------------------------------------------------
@@ -120,6 +130,7 @@ __device__ __forceinline__ void product_body(const ProductWork& w, uint8_t* lds,
     const int64_t m0 = (int64_t)(item.bm - result * w.tiles_m) * P::TM, n0 = (int64_t)item.bn * P::TN, left_m = w.m - m0, left_n = w.n - n0;
     const int begin = split_begin(w.steps * w.terms, w.splits, split), end = split_begin(w.steps * w.terms, w.splits, split + 1);
     v4f32 acc[P::FN][P::FM] = {};
+#pragma unroll 1
     for (int t = 0; t < w.terms; ++t) {
         const int from = begin - t * w.steps > 0 ? begin - t * w.steps : 0, to = end - t * w.steps < w.steps ? end - t * w.steps : w.steps;
         if (from >= to) continue;
@@ -132,13 +143,14 @@ __device__ __forceinline__ void product_body(const ProductWork& w, uint8_t* lds,
         const int64_t ld = in_fours(w.n);
         store_tile<P, false>(lds, acc, w.partial + (((int64_t)result * w.splits + split) * w.m + m0) * ld + n0, ld, left_m, in_fours(left_n), false, one);
     } else {
-        store_tile<P, (P::THREADS > 256)>(lds, acc, static_cast<T*>(w.D[result]) + m0 * w.ldd + n0, w.ldd, left_m, left_n, false, one);
+        store_tile<P, (P::TM == 256)>(lds, acc, static_cast<T*>(w.D[result]) + m0 * w.ldd + n0, w.ldd, left_m, left_n, false, one);
     }
 }
 
-// Both products, or one: `dx_blocks` workgroups have tiles of dX, the others of dW; `dx_first` says whose go out first.
+// Both products, or one: `dx_blocks` workgroups have tiles of dX, the others of dW; `dx_first` says whose go out first.  Behind them the join of dbias.
 struct BothWork {
     ProductWork dx, dw;
+    BiasJoin bias;
     unsigned dx_blocks, dw_blocks;
     bool dx_first;
 };
@@ -146,6 +158,10 @@ template <typename PX, typename PW, typename T>
 __device__ __forceinline__ void both_body(const BothWork& w) {
     static_assert(PX::THREADS == PW::THREADS, "");
     __shared__ __attribute__((aligned(16))) uint8_t lds[PX::LDS_BYTES > PW::LDS_BYTES ? PX::LDS_BYTES : PW::LDS_BYTES];
+    if (blockIdx.x >= w.dx_blocks + w.dw_blocks) {
+        bias_join(w.bias, reinterpret_cast<float*>(lds), blockIdx.x - w.dx_blocks - w.dw_blocks);
+        return;
+    }
     const unsigned front = w.dx_first ? w.dx_blocks : w.dw_blocks, b = blockIdx.x < front ? blockIdx.x : blockIdx.x - front;
     if ((blockIdx.x < front) == w.dx_first) product_body<PX, T, false>(w.dx, lds, b, w.dx_blocks);
     else product_body<PW, T, true>(w.dw, lds, b, w.dw_blocks);
@@ -155,13 +171,13 @@ template <int TYPE>
 __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) linear_grad_large_kernel(const BothWork w) {
     both_body<PairedTile<kind_of(TYPE), true, false>, PairedTile<kind_of(TYPE), true, true>, typename Element<TYPE>::type>(w);
 }
-// of dX 64 x 128 elements or (FEW) 16 x 128, of dW 128 x 128; DEEP: one workgroup to a compute unit, with twice the steps under way
-template <int TYPE, bool FEW, bool DEEP>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 2))) linear_grad_middle_kernel(const BothWork w) {
-    typedef Tile<kind_of(TYPE), 2, 2, 4, 4, DEEP ? 4 : 2, true, true> DW;
-    typedef typename Element<TYPE>::type T;
-    if constexpr (FEW) both_body<Tile<kind_of(TYPE), 4, 1, 2, 1, DEEP ? 8 : 4, true, false>, DW, T>(w);
-    else both_body<Tile<kind_of(TYPE), 2, 2, 4, 2, DEEP ? 6 : 3, true, false>, DW, T>(w);
+// Of dX 64 x 128 elements or (FEW) 16 x 128, of dW 128 x 128, in eight waves: with four a step's wait, LDS reads and products follow each other (512 x 1024 x 1024:
+// 14.7 us against 18); twice the steps under way in one workgroup to a compute unit are no faster.
+template <int TYPE, bool FEW>
+__global__ void __launch_bounds__(512) linear_grad_middle_kernel(const BothWork w) {
+    constexpr int KIND = kind_of(TYPE);
+    typedef std::conditional_t<FEW, Tile<KIND, 8, 1, 1, 1, 4, true, false>, Tile<KIND, 4, 2, 2, 2, 3, true, false>> DX;
+    both_body<DX, Tile<KIND, 4, 2, 2, 4, 2, true, true>, typename Element<TYPE>::type>(w);
 }
 
 // the shares' sums in their order; blockIdx.z: the result
@@ -195,17 +211,18 @@ Shapes shapes_of(int64_t m, int64_t n, int64_t k, bool pair, bool dx, bool dw) {
     s.dw_steps = div_up(m, 64);
     const auto tiles = [](int64_t rows, int64_t columns, int64_t tm, int64_t tn) { return div_up(rows, tm) * div_up(columns, tn); };
     const int64_t dx_large = tiles(m, k, 256, 256), dw_large = results * tiles(n, k, 256, 256);
-    // Large tiles where both results together have as much for them to do as eight steps of every second compute unit; also where they are few.
+    // Large tiles where they are sixteen steps of every compute unit (1024 x 4096 x 2048, just that: 48.7 us, by smaller ones 50; half of it, 2048 x 2048 x 1024: 47, 37).
     const int64_t work = (dx ? dx_large * s.dx_steps : 0) + (dw ? dw_large * s.dw_steps : 0);
-    const bool large = m > 128 && k > 128 && n > 128 && work >= 128 * 16;
-    s.dx = m <= 16 ? Shape{FEW, 16, 128, 1} : large ? Shape{LARGE, 256, 256, 1} : Shape{MIDDLE, 64, 128, 1};
+    const bool large = m > 128 && k > 128 && n > 128 && work >= 256 * 16;
+    s.dx = large ? Shape{LARGE, 256, 256, 1} : m <= 16 ? Shape{FEW, 16, 128, 1} : Shape{MIDDLE, 64, 128, 1};
     s.dw = large ? Shape{LARGE, 256, 256, 1} : Shape{MIDDLE, 128, 128, 1};
     s.dx_tiles = dx ? tiles(m, k, s.dx.tm, s.dx.tn) : 0;
     s.dw_tiles = dw ? results * tiles(n, k, s.dw.tm, s.dw.tn) : 0;
-    // Shares as long as a compute unit has steps to do in all, in which a step of dW's smaller tiles counts twice
-    const int64_t weight = large ? 1 : 2, all = s.dx_tiles * s.dx_steps + s.dw_tiles * s.dw_steps * weight, each = div_up(all, large ? 256 : 512);
+    // Shares as long as a compute unit has steps to do in all, in which a step of dW's smaller tiles counts twice, and of eight steps at least.  Up to sixteen steps stay
+    // uncut: the join costs more (333 x 1000 x 1001: 15.5, in shares of eight 18.1).
+    const int64_t weight = large ? 1 : 2, all = s.dx_tiles * s.dx_steps + s.dw_tiles * s.dw_steps * weight, each = div_up(all, 256);
     const auto shares = [&](int64_t steps, int64_t weighted) {
-        const int64_t want = (2 * weighted + each) / (2 * each), most = steps / (large ? 8 : 4), splits = want < most ? want : most;
+        const int64_t want = (2 * weighted + each) / (2 * each), most = steps > 16 ? steps / 8 : 1, splits = want < most ? want : most;
         return (int)(splits < 1 ? 1 : splits > 32 ? 32 : splits);
     };
     s.dx.splits = shares(s.dx_steps, s.dx_steps);
@@ -267,13 +284,10 @@ hipError_t launch_both(BothWork w, const Shapes& s, bool dx, bool dw, hipStream_
     w.dx_blocks = dx ? set_tiles(w.dx, s.dx) : 0;
     w.dw_blocks = dw ? set_tiles(w.dw, s.dw) : 0;
     w.dx_first = s.dx_steps / s.dx.splits >= s.dw_steps / s.dw.splits;
-    const dim3 blocks(w.dx_blocks + w.dw_blocks);
-    const bool deep = blocks.x <= 256;
+    const dim3 blocks(w.dx_blocks + w.dw_blocks + w.bias.blocks);
     if (s.dw.kind == LARGE) hipLaunchKernelGGL((linear_grad_large_kernel<TYPE>), blocks, dim3(512), 0, st, w);
-    else if (s.dx.kind == FEW && deep) hipLaunchKernelGGL((linear_grad_middle_kernel<TYPE, true, true>), blocks, dim3(256), 0, st, w);
-    else if (s.dx.kind == FEW) hipLaunchKernelGGL((linear_grad_middle_kernel<TYPE, true, false>), blocks, dim3(256), 0, st, w);
-    else if (deep) hipLaunchKernelGGL((linear_grad_middle_kernel<TYPE, false, true>), blocks, dim3(256), 0, st, w);
-    else hipLaunchKernelGGL((linear_grad_middle_kernel<TYPE, false, false>), blocks, dim3(256), 0, st, w);
+    else if (s.dx.kind == FEW) hipLaunchKernelGGL((linear_grad_middle_kernel<TYPE, true>), blocks, dim3(512), 0, st, w);
+    else hipLaunchKernelGGL((linear_grad_middle_kernel<TYPE, false>), blocks, dim3(512), 0, st, w);
     OZAKI_LINEAR_TRY(hipGetLastError());
     if (dx) OZAKI_LINEAR_TRY(launch_join<TYPE>(w.dx, st));
     return dw ? launch_join<TYPE>(w.dw, st) : hipSuccess;
@@ -308,19 +322,19 @@ hipError_t grad_typed(const LinearGradArgs& a, hipStream_t st) {
         else hipLaunchKernelGGL((linear_slope_kernel<TYPE, false>), blocks, dim3(SLOPE_WAVES * 64), 0, st, w);
         OZAKI_LINEAR_TRY(hipGetLastError());
     }
-    if (w.sums != nullptr && !w.whole) {
-        hipLaunchKernelGGL(linear_bias_join_kernel, dim3((unsigned)div_up(a.n, 64)), dim3(256), 0, st, p.sums, chunks, a.n, w.ld, a.dbias);
-        OZAKI_LINEAR_TRY(hipGetLastError());
-    }
     const uint8_t* const dz[2] = {formed ? p.dZ : static_cast<const uint8_t*>(a.dY), p.dU};
     const int64_t lddz = (formed ? w.ld : a.lddy) * 2;
     const bool dx = a.dX != nullptr, both = a.dW != nullptr && a.dW2 != nullptr, dw = a.dW != nullptr || a.dW2 != nullptr;
-    if (!dx && !dw) return hipSuccess;
+    BothWork d = {};
+    if (w.sums != nullptr && !w.whole) d.bias = BiasJoin{p.sums, a.dbias, chunks, a.n, w.ld, (unsigned)div_up(a.n, BIAS_COLUMNS)};
+    if (!dx && !dw) {
+        if (d.bias.blocks > 0) hipLaunchKernelGGL(linear_bias_join_kernel, dim3(d.bias.blocks), dim3(BIAS_WAVES * 64), 0, st, d.bias);
+        return hipGetLastError();
+    }
     // (of a pair one dW is cut as both are, so that it has the same bits)
     const Shapes s = shapes_of(a.m, a.n, a.k, pair, dx, dw);
     size_t for_dx;
     partial_bytes(s, a.m, a.n, a.k, pair ? 2 : 1, for_dx);
-    BothWork d = {};
     if (dx) {
         d.dx.X[0] = static_cast<const uint8_t*>(a.W);
         d.dx.X[1] = static_cast<const uint8_t*>(a.W2);
