@@ -247,13 +247,15 @@ __global__ void __launch_bounds__(PAIR ? 256 : 512) linear_narrow_kernel(const L
     linear_body<Tile<kind_of(TYPE), PAIR ? 1 : 2, 4, PAIR ? 2 : 1, 1, 4, false, false, PAIR>, TYPE>(w);
 }
 
-// Up to sixteen vectors of X: no tile in LDS.  A workgroup of FEW_WAVES waves takes sixteen vectors of W (of each, of a pair), a wave every
-// FEW_WAVES-th step of 64 elements, straight from memory into registers; the waves' sums are added in LDS, in their order.
-constexpr int FEW = 16, FEW_WAVES = 8, AHEAD = 4;
+// Up to sixteen vectors of X: no tile in LDS.  A workgroup takes sixteen vectors of W (of each, of a pair), its waves take steps of 64 elements in turn, straight
+// from memory into registers; the waves' sums are added in LDS, in their order.  W is read once, past the caches, and bounds it.  A wave has AHEAD steps under way.
+// 1 x 4096 x 8192: 13.9 us, 4.8 TB/s, in sixteen waves 15.3;  a pair of 4096 x 8192: 24.7, 5.4 TB/s, in eight waves with four steps under way 29.1.
+constexpr int FEW = 16;
+constexpr int few_waves(bool pair) { return pair ? 16 : 8; }
 
 template <int TYPE, bool PAIR>
-__global__ void __launch_bounds__(FEW_WAVES * 64) linear_few_kernel(const LinearArgs a, const int splits) {
-    constexpr int FACTORS = PAIR ? 2 : 1;
+__global__ void __launch_bounds__(few_waves(PAIR) * 64) linear_few_kernel(const LinearArgs a, const int splits) {
+    constexpr int FACTORS = PAIR ? 2 : 1, FEW_WAVES = few_waves(PAIR), AHEAD = PAIR ? 2 : 4;
     __shared__ __attribute__((aligned(16))) v4f32 sums[FACTORS][FEW_WAVES][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, row = lane & 15;
     const int split = blockIdx.x % splits;
@@ -273,7 +275,10 @@ __global__ void __launch_bounds__(FEW_WAVES * 64) linear_few_kernel(const Linear
         for (int h = 0; h < 2; ++h) {
             const int64_t off = from + g * 16 + h * 64 < bytes ? from + h * 64 : -(int64_t)g * 16;
 #pragma unroll
-            for (int o = 0; o <= FACTORS; ++o) pieces[u][o][h] = *reinterpret_cast<const v4i32*>(at[o] + off);
+            for (int o = 0; o <= FACTORS; ++o) {
+                const v4i32* const p = reinterpret_cast<const v4i32*>(at[o] + off);
+                pieces[u][o][h] = o < FACTORS ? __builtin_nontemporal_load(p) : *p;
+            }
         }
     };
     v4f32 acc[FACTORS] = {};
@@ -363,14 +368,15 @@ struct Shape { int kind, tm, tn, splits; };
 //     up to 512 of 128 x 128                                               2048 x 4096 x 2048: 42.5, by 64 x 128 49, by 256 x 256 60
 //     more: 256 x 256                                                      2048 x 8192 x 512: 33.5, by 128 x 128 38
 // The narrowest tiles where they are fewer than compute units: in shares of the inner dimension of sixteen steps at least (20 x 1000 x 8192: 13.2 in eight, 27.8 uncut;
-// but 48 x 1000 x 500, eight steps: 7.0, in two shares 8.6).
+// but 48 x 1000 x 500, eight steps: 7.0, in two shares 8.6).  Few vectors: from 96 steps on, in shares of at least 32 (1 x 1000 x 16384: 12.4, uncut 21.5); from 256 steps on
+// in two also where there are enough workgroups (1 x 16384 x 16384: 98, uncut 105; a pair of those 193, 226).
 Shape shape_of(int64_t m, int64_t n, int64_t k, bool pair) {
     const int64_t steps = div_up(k * 2, STEP_BYTES), columns = pair ? 2 * n : n;
     const auto shares = [](int64_t want, int64_t most) {
         const int64_t s = want < most ? want : most;
         return (int)(s < 1 ? 1 : s > 16 ? 16 : s);
     };
-    if (m <= FEW) return Shape{VECTORS, FEW, 16, steps < 96 ? 1 : shares(256 / div_up(n, 16), steps / 32)};
+    if (m <= FEW) return Shape{VECTORS, FEW, 16, steps < 96 ? 1 : shares(256 / div_up(n, 16) > 1 || steps < 256 ? 256 / div_up(n, 16) : 2, steps / 32)};
     const auto tiles = [&](int64_t tm, int64_t tn) { return div_up(m, tm) * div_up(columns, tn); };
     const auto shape = [&](int kind, int tm, int tn, int splits) { return Shape{kind, tm, pair ? tn / 2 : tn, splits}; };
     if (tiles(64, 64) <= 128) return shape(NARROW, 64, 32, shares(256 / tiles(64, 32), steps / 16));
@@ -389,7 +395,7 @@ hipError_t launch_kind(const LinearArgs& a, Shape s, hipStream_t st) {
     w.tiles_n = (int)div_up(a.n, s.tn);
     w.order = WorkOrder{s.kind == LARGE ? 32 : 64, 8};
     const unsigned blocks = (unsigned)((int64_t)w.tiles_m * w.tiles_n * s.splits);
-    if (s.kind == VECTORS) hipLaunchKernelGGL((linear_few_kernel<TYPE, PAIR>), dim3(blocks), dim3(FEW_WAVES * 64), 0, st, a, s.splits);
+    if (s.kind == VECTORS) hipLaunchKernelGGL((linear_few_kernel<TYPE, PAIR>), dim3(blocks), dim3(few_waves(PAIR) * 64), 0, st, a, s.splits);
     else if (s.kind == NARROW) hipLaunchKernelGGL((linear_narrow_kernel<TYPE, PAIR>), dim3(blocks), dim3(PAIR ? 256 : 512), 0, st, w);
     else if (s.kind == SMALL) hipLaunchKernelGGL((linear_small_kernel<TYPE, PAIR>), dim3(blocks), dim3(512), 0, st, w);
     else if (s.kind == HALF) hipLaunchKernelGGL((linear_half_kernel<TYPE, PAIR>), dim3(blocks), dim3(512), 0, st, w);
@@ -403,12 +409,49 @@ hipError_t launch_kind(const LinearArgs& a, Shape s, hipStream_t st) {
     return hipGetLastError();
 }
 
-template <int TYPE>
-hipError_t launch_typed(const LinearArgs& a, hipStream_t st) {
-    const bool pair = a.W2 != nullptr;
-    const Shape s = shape_of(a.m, a.n, a.k, pair);
-    return pair ? launch_kind<TYPE, true>(a, s, st) : launch_kind<TYPE, false>(a, s, st);
+// Large tiles run in rounds of one for every compute unit.  Where the last round has few of them, the rows or columns that they hold, of the longer
+// dimension, are left to smaller tiles in a launch of their own (4608 x 4096 x 4096, 288 tiles: 136 us against 190; 2304 x 8192 x 4096, the same: 148, 189).
+int64_t in_rounds(int64_t length, int64_t edge, int64_t across) {
+    const int64_t tiles = across * div_up(length, edge), over = tiles % 256, whole = (tiles - over) / across;
+    return over == 0 || whole == 0 || tiles - whole * across > 128 ? length : whole * edge;
 }
+
+template <int TYPE, bool PAIR>
+hipError_t launch_shaped(LinearArgs a, hipStream_t st) {
+    const Shape s = shape_of(a.m, a.n, a.k, PAIR);
+    if (s.kind != LARGE) return launch_kind<TYPE, PAIR>(a, s, st);
+    const int64_t m = a.m, n = a.n;
+    if (m >= (PAIR ? 2 * n : n)) a.m = in_rounds(m, s.tm, div_up(n, s.tn));
+    else a.n = in_rounds(n, s.tn, div_up(m, s.tm));
+    const hipError_t e = launch_kind<TYPE, PAIR>(a, s, st);
+    if (e != hipSuccess || (a.m == m && a.n == n)) return e;
+    const auto rows = [](auto*& p, int64_t elements) {
+        if (p != nullptr) p = reinterpret_cast<std::remove_reference_t<decltype(p)>>(reinterpret_cast<uintptr_t>(p) + elements * 2);
+    };
+    if (a.m < m) {
+        rows(a.X, a.m * a.ldx);
+        rows(a.R, a.m * a.ldr);
+        rows(a.Y, a.m * a.ldy);
+        rows(a.Z, a.m * a.ldz);
+        rows(a.U, a.m * a.ldu);
+        a.m = m - a.m;
+    } else {
+        rows(a.W, a.n * a.ldw);
+        rows(a.W2, a.n * a.ldw);
+        rows(a.bias, a.n);
+        rows(a.R, a.n);
+        rows(a.Y, a.n);
+        rows(a.Z, a.n);
+        rows(a.U, a.n);
+        a.n = n - a.n;
+    }
+    Shape rest = shape_of(a.m, a.n, a.k, PAIR);
+    rest.splits = 1;
+    return launch_kind<TYPE, PAIR>(a, rest, st);
+}
+
+template <int TYPE>
+hipError_t launch_typed(const LinearArgs& a, hipStream_t st) { return a.W2 != nullptr ? launch_shaped<TYPE, true>(a, st) : launch_shaped<TYPE, false>(a, st); }
 
 }  // namespace
 

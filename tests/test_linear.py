@@ -8,9 +8,11 @@ from low_precision import DTYPES  # noqa: E402
 from paper_2508_00441_amd import binding as lib, device  # noqa: E402
 
 ACTIVATIONS = ["none", "relu", "gelu", "gelu_tanh", "silu"]
-# few vectors (whole, and the inner dimension in shares), small tiles (the same), middle and large tiles; odd sizes; steps that end inside 16 bytes
+# few vectors (whole, and the inner dimension in shares), tiles from narrow (the same) to large ones, large ones whose last round is left to smaller ones, along either
+# dimension; odd sizes; steps that end inside 16 bytes
 SHAPES = [(1, 1, 1), (1, 16, 64), (1, 257, 100), (3, 5, 8), (2, 40, 6200), (16, 100, 6401), (7, 1000, 257), (17, 33, 72), (33, 129, 640), (64, 500, 1000), (65, 1000, 33),
-          (100, 300, 4096), (200, 1001, 200), (300, 511, 64), (1000, 4100, 100), (1030, 4104, 264), (2100, 4200, 72), (2310, 4097, 129), (2304, 4352, 256)]
+          (100, 300, 4096), (200, 1001, 200), (300, 511, 64), (1000, 4100, 100), (1030, 4104, 264), (2100, 4200, 72), (2310, 4097, 129), (2304, 4352, 256),
+          (3000, 2800, 72), (4616, 4090, 40), (2100, 8461, 40), (9, 300, 16400)]
 GRAD_SHAPES = [(1, 1, 1), (1, 257, 100), (3, 5, 8), (16, 1000, 136), (17, 33, 72), (40, 3000, 64), (65, 1000, 33), (200, 1001, 200), (300, 511, 64), (513, 264, 1031), (1000, 72, 72),
                (5000, 100, 130), (1030, 2100, 264), (2100, 1100, 4200), (2100, 4200, 300), (4100, 300, 280)]
 
