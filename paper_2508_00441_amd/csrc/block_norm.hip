@@ -14,8 +14,6 @@
 namespace ozaki {
 namespace {
 
-template <typename T> struct Eight { typedef T type __attribute__((ext_vector_type(8))); };
-
 // Eight elements of a vector as they are in memory, and as numbers: `there` of them exist (zeros for the others); the 16 bytes in which a vector ends
 // may be read whole.
 template <typename T> struct Raw { v4i32 part[sizeof(T) / 2]; };
@@ -34,37 +32,31 @@ template <typename T> __device__ __forceinline__ Raw<T> load_raw(const T* row, u
 template <typename T> __device__ __forceinline__ v8f32 numbers(const Raw<T>& r, int there) {
     v8f32 v;
     if constexpr (sizeof(T) == 4) v = __builtin_bit_cast(v8f32, r);
-    else v = __builtin_convertvector(__builtin_bit_cast(typename Eight<T>::type, r), v8f32);
+    else v = __builtin_convertvector(__builtin_bit_cast(Eight<T>, r), v8f32);
     if (there < 8) {
 #pragma unroll
         for (int q = 0; q < 8; ++q) v[q] = q < there ? v[q] : 0.0f;
     }
     return v;
 }
-// of weights, which lie anywhere
-__device__ __forceinline__ v8f32 load_weights(const float* p, int there, bool wide) {
-    if (wide && there >= 8) return __builtin_shufflevector(*reinterpret_cast<const v4f32*>(p), *reinterpret_cast<const v4f32*>(p + 4), 0, 1, 2, 3, 4, 5, 6, 7);
+// of weights and results, which lie anywhere
+__device__ __forceinline__ v8f32 load_weights(const float* p, int there) {
+    if (there >= 8) return get_eight(p);
     v8f32 v = {};
 #pragma unroll
     for (int q = 0; q < 8; ++q)
         if (q < there) v[q] = p[q];
     return v;
 }
-template <typename T> __device__ __forceinline__ void store_eight(T* p, v8f32 v, int there, bool wide) {
-    if (wide && there >= 8) {
-        if constexpr (sizeof(T) == 4) {
-            *reinterpret_cast<v4f32*>(p) = __builtin_shufflevector(v, v, 0, 1, 2, 3);
-            *reinterpret_cast<v4f32*>(p + 4) = __builtin_shufflevector(v, v, 4, 5, 6, 7);
-        } else {
-            *reinterpret_cast<typename Eight<T>::type*>(p) = __builtin_convertvector(v, typename Eight<T>::type);
-        }
+template <typename T> __device__ __forceinline__ void store_eight(T* p, v8f32 v, int there) {
+    if (there >= 8) {
+        put_eight<false>(p, v);
     } else {
 #pragma unroll
         for (int q = 0; q < 8; ++q)
             if (q < there) p[q] = (T)v[q];
     }
 }
-template <typename T> __device__ __forceinline__ bool rows_wide(const T* p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * sizeof(T) % 16 == 0; }
 
 // Sums over a wave, without LDS: rows of sixteen lanes, then across them.
 template <int CONTROL, int ROWS> __device__ __forceinline__ float moved(float v) {
@@ -156,23 +148,19 @@ __device__ __forceinline__ RowNorm row_norm(X x, F d, float k, float eps, Meetin
 template <int PIECES> struct Columns {
     unsigned c[PIECES];
     int there[PIECES];
-    bool wide_post, wide_pre, wide_gate;
     __device__ __forceinline__ Columns(const BlockNormArgs& a, int threads) {
-        wide_post = rows_wide(a.w_post, 0);
-        wide_pre = rows_wide(a.w_pre, 0);
-        wide_gate = rows_wide(a.gate, a.k);
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) {
             c[p] = (p * threads + threadIdx.x) * 8;
             there[p] = (int)a.k - (int)c[p];
         }
     }
-    __device__ __forceinline__ v8f32 pre(const BlockNormArgs& a, int p) const { return load_weights(place(a.w_pre, c[p]), there[p], wide_pre); }
+    __device__ __forceinline__ v8f32 pre(const BlockNormArgs& a, int p) const { return load_weights(place(a.w_pre, c[p]), there[p]); }
     // scale * gate * w_post for the rows of a gate
     __device__ __forceinline__ v8f32 behind(const BlockNormArgs& a, int64_t gate, int p) const {
         v8f32 f = v8f32{} + a.scale;
-        if (a.gate != nullptr) f *= load_weights(place(a.gate + gate * a.k, c[p]), there[p], wide_gate);
-        if (a.w_post != nullptr) f *= load_weights(place(a.w_post, c[p]), there[p], wide_post);
+        if (a.gate != nullptr) f *= load_weights(place(a.gate + gate * a.k, c[p]), there[p]);
+        if (a.w_post != nullptr) f *= load_weights(place(a.w_post, c[p]), there[p]);
         return f;
     }
 };
@@ -189,7 +177,6 @@ __global__ void __launch_bounds__(THREADS) block_norm_kernel(const BlockNormArgs
     const TR* const R = static_cast<const TR*>(a.R);
     TR* const R_out = static_cast<TR*>(a.R_out);
     T* const H = static_cast<T*>(a.H);
-    const bool wide_r = rows_wide(R_out, a.ldro), wide_h = rows_wide(H, a.ldh);
     const Columns<PIECES> at(a, THREADS);
     // weights stay in registers from row to row; those of the longest rows are read again for each
     constexpr bool KEPT = PIECES == 1;
@@ -221,13 +208,13 @@ __global__ void __launch_bounds__(THREADS) block_norm_kernel(const BlockNormArgs
 #pragma unroll
             for (int p = 0; p < PIECES; ++p) {
                 r[p] = multiply_add(x[p] * rho, KEPT ? behind : at.behind(a, g, p), r[p]);
-                if (R_out != nullptr) store_eight(place(R_out + row * a.ldro, at.c[p]), r[p], at.there[p], wide_r);
+                if (R_out != nullptr) store_eight(place(R_out + row * a.ldro, at.c[p]), r[p], at.there[p]);
             }
         }
         if (H == nullptr) continue;
         const float rho = row_norm<false, PIECES>([&](int p) { return r[p]; }, none, (float)a.k, a.eps, meeting).rho;
 #pragma unroll
-        for (int p = 0; p < PIECES; ++p) store_eight(place(H + row * a.ldh, at.c[p]), r[p] * rho * (KEPT ? pre : at.pre(a, p)), at.there[p], wide_h);
+        for (int p = 0; p < PIECES; ++p) store_eight(place(H + row * a.ldh, at.c[p]), r[p] * rho * (KEPT ? pre : at.pre(a, p)), at.there[p]);
     }
 }
 
@@ -270,13 +257,12 @@ __global__ void __launch_bounds__(THREADS) block_norm_grad_kernel(const NormGrad
     const TR* const dR_out = static_cast<const TR*>(a.dR_out);
     T* const dX = static_cast<T*>(a.dX);
     TR* const dR = static_cast<TR*>(a.dR);
-    const bool wide_x = rows_wide(dX, a.lddx), wide_r = rows_wide(dR, a.lddr);
     const bool post = a.w_post != nullptr, branch = X != nullptr && (dX != nullptr || w.s != nullptr);
     const Columns<PIECES> at(a, THREADS);
     const auto leave = [&](float* to, int which) {
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) {
-            store_eight(place(to, at.c[p]), get(which, p), at.there[p], a.k % 4 == 0);
+            store_eight(place(to, at.c[p]), get(which, p), at.there[p]);
             put(which, p, v8f32{});
         }
     };
@@ -340,7 +326,7 @@ __global__ void __launch_bounds__(THREADS) block_norm_grad_kernel(const NormGrad
                 dr[p] = multiply_add(multiply_add(-m, v8f32{} + rn.along, dn(p)), v8f32{} + rn.rho, dr[p]);
                 add(SUM_T, p, dh(p), m);
             }
-            if (dR != nullptr) store_eight(place(dR + row * a.lddr, at.c[p]), dr[p], at.there[p], wide_r);
+            if (dR != nullptr) store_eight(place(dR + row * a.lddr, at.c[p]), dr[p], at.there[p]);
         }
         if (branch) {
             const int64_t g = a.gate != nullptr ? row / a.group : 0;
@@ -352,7 +338,7 @@ __global__ void __launch_bounds__(THREADS) block_norm_grad_kernel(const NormGrad
             for (int p = 0; p < PIECES; ++p) {
                 const v8f32 m = x(p) * xn.rho;
                 add(SUM_S, p, dr[p], m);
-                if (dX != nullptr) store_eight(place(dX + row * a.lddx, at.c[p]), multiply_add(-m, v8f32{} + xn.along, dm(p)) * xn.rho, at.there[p], wide_x);
+                if (dX != nullptr) store_eight(place(dX + row * a.lddx, at.c[p]), multiply_add(-m, v8f32{} + xn.along, dm(p)) * xn.rho, at.there[p]);
             }
         }
         if (--left == 0 && n.per_group == 0) {

@@ -95,6 +95,15 @@ hipError_t launch_clip(const ClipArgs& a, hipStream_t st);
 #if defined(__HIPCC__)
 
 typedef float v8f32 __attribute__((ext_vector_type(8)));
+// Eight neighbouring elements, wherever they lie: the memory takes 16-byte accesses at any element.
+template <typename T> using Eight = T __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+template <typename T> __device__ __forceinline__ v8f32 get_eight(const T* p) { return __builtin_convertvector(*reinterpret_cast<const Eight<T>*>(p), v8f32); }
+template <bool STREAMED, typename T> __device__ __forceinline__ void put_eight(T* to, v8f32 v) {
+    const Eight<T> w = __builtin_convertvector(v, Eight<T>);
+    if constexpr (STREAMED) __builtin_nontemporal_store(w, reinterpret_cast<Eight<T>*>(to));
+    else *reinterpret_cast<Eight<T>*>(to) = w;
+}
+template <typename T> __device__ __forceinline__ bool rows_aligned(const T* p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * sizeof(T) % 16 == 0; }
 
 // 1 / (1 + exp(-x)) and what it lacks of one, each with its own few roundings: the exponential is of -|x|, so that it neither overflows nor cancels.
 struct Sigmoid { float p, rest; };

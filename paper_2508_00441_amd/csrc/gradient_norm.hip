@@ -16,7 +16,7 @@ namespace {
 constexpr uint32_t MOST_CHUNK = 8192, LEAST_CHUNK = 2048;
 constexpr unsigned MOST_BLOCKS = 1024;
 constexpr int TABLE = 144;               // tensors in a launch's arguments, which hold 4 KiB
-constexpr int THREADS = 256, MOST_JOINED = 512;      // partial sums that every workgroup of the second reading adds up itself: 3 us, a launch of its own 5
+constexpr int THREADS = 256, MOST_JOINED = 1024;     // partial sums that every workgroup of the second reading adds up itself: 3 us, a launch of its own 5
 
 struct ClipTable {
     const void* x[TABLE];
@@ -106,29 +106,16 @@ __device__ __forceinline__ Squares block_sum(Squares v) {
 
 // A thread's squares of the n elements of a chunk, each times `factor` first: eight sums, of MOST_CHUNK / THREADS / 8 = 4 elements each.
 template <typename T> __device__ __forceinline__ float chunk_squares(const T* x, int n, float factor) {
-    typedef T eight __attribute__((ext_vector_type(8), aligned(16)));
     float sum[8] = {};
     const auto add = [&](int q, T v) { sum[q] = __builtin_fmaf((float)v * factor, (float)v * factor, sum[q]); };
-    int e = 0;
-    if (reinterpret_cast<uintptr_t>(x) % 16 == 0) {
-        const int pieces = n / 8;
+    const int pieces = n / 8, e = pieces * 8;
 #pragma unroll 4
-        for (int p = threadIdx.x; p < pieces; p += THREADS) {
-            const eight v = reinterpret_cast<const eight*>(x)[p];
+    for (int p = threadIdx.x; p < pieces; p += THREADS) {
+        const Eight<T> v = *reinterpret_cast<const Eight<T>*>(x + 8 * p);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) add(q, v[q]);
-        }
-        e = pieces * 8;
-    } else {
-        for (; e + 8 * THREADS <= n; e += 8 * THREADS)
-#pragma unroll
-            for (int q = 0; q < 8; ++q) add(q, x[e + q * THREADS + threadIdx.x]);
+        for (int q = 0; q < 8; ++q) add(q, v[q]);
     }
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-        const int at = e + q * THREADS + threadIdx.x;
-        if (at < n) add(q, x[at]);
-    }
+    if (e + (int)threadIdx.x < n) add(0, x[e + threadIdx.x]);
     return ((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7]));
 }
 
@@ -194,22 +181,17 @@ __global__ void __launch_bounds__(THREADS) gradient_clip_kernel(const ClipTable 
         lanes.with_chunk(t.chunks - 1 - i, t.chunk, [&](auto x, auto out, int n) {
             typedef std::remove_pointer_t<decltype(out)> T;
             constexpr int PER = 16 / sizeof(T);
-            typedef T piece __attribute__((ext_vector_type(PER)));
+            typedef T piece __attribute__((ext_vector_type(PER), aligned(sizeof(T))));
             if (factor == 1.0f && x == out) return;
-            int e = threadIdx.x;
-            if (reinterpret_cast<uintptr_t>(x) % 16 == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0) {
-                const int pieces = n / PER;
+            const int pieces = n / PER, e = pieces * PER + threadIdx.x;
 #pragma unroll 4
-                for (int p = threadIdx.x; p < pieces; p += THREADS) {
-                    piece v = reinterpret_cast<const piece*>(x)[p];
+            for (int p = threadIdx.x; p < pieces; p += THREADS) {
+                piece v = *reinterpret_cast<const piece*>(x + PER * p);
 #pragma unroll
-                    for (int q = 0; q < PER; ++q) v[q] = (T)((float)v[q] * factor);
-                    reinterpret_cast<piece*>(out)[p] = v;
-                }
-                e += pieces * PER;
+                for (int q = 0; q < PER; ++q) v[q] = (T)((float)v[q] * factor);
+                *reinterpret_cast<piece*>(out + PER * p) = v;
             }
-#pragma unroll 8
-            for (; e < n; e += THREADS) out[e] = (T)((float)x[e] * factor);
+            if (e < n) out[e] = (T)((float)x[e] * factor);
         });
 }
 
@@ -222,9 +204,9 @@ int fill_table(const ClipArgs& a, int begin, ClipTable& t) {
             at[count++] = i;
             total += a.sizes[i];
         }
-    // as short as leaves a chunk to a workgroup, within the bounds (no tensor has more than 2^38 elements: the chunks' numbers stay inside 32 bits)
+    // as short as makes 512 of them, within the bounds (no tensor has more than 2^38 elements: the chunks' numbers stay inside 32 bits)
     t.chunk = LEAST_CHUNK;
-    while (t.chunk < MOST_CHUNK && total / t.chunk > MOST_BLOCKS) t.chunk *= 2;
+    while (t.chunk < MOST_CHUNK && total / t.chunk > MOST_JOINED / 2) t.chunk *= 2;
     t.chunks = 0;
     for (int j = 0; j < TABLE; ++j) {
         t.first[j] = t.chunks;
@@ -255,7 +237,7 @@ hipError_t launch_clip(const ClipArgs& a, hipStream_t st) {
         ++launches;
     }
     // Few partial sums are added up by every workgroup of the second reading, without a launch in between.
-    const bool apart = !a.given && (a.out == nullptr || launches != 1 || partials > MOST_JOINED);
+    const bool apart = !a.given && (a.out == nullptr || launches == 0 || partials > MOST_JOINED);
     if (apart) {
         hipLaunchKernelGGL(gradient_norm_kernel, dim3(1), dim3(THREADS), 0, st, partial, partials, a.scale, a.norm);
         const hipError_t e = hipGetLastError();

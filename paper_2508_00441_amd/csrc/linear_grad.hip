@@ -9,7 +9,7 @@
 // dimension is cut into shares whose sums meet in work memory, in their order.
 #include "block_operators.hpp"
 #include "layout.hpp"
-#include "tile_product.hpp"
+#include "tile_epilogue.hpp"
 
 namespace ozaki {
 namespace {
@@ -138,12 +138,11 @@ __device__ __forceinline__ void product_body(const ProductWork& w, uint8_t* lds,
         const TileOperand Y{w.Y[YT ? result : t] + m0 * (YT ? 2 : w.ldy), w.ldy, (int)(left_m < P::TM ? left_m : P::TM), nullptr, 0, w.elements};
         P::multiply(lds, X, Y, w.elements * 2, from, to, acc);
     }
-    const auto one = [](int64_t) { return 1.0f; };
     if (w.splits > 1) {
         const int64_t ld = in_fours(w.n);
-        store_tile<P, false>(lds, acc, w.partial + (((int64_t)result * w.splits + split) * w.m + m0) * ld + n0, ld, left_m, in_fours(left_n), false, one);
+        put_tile<P>(lds, acc, m0, n0, left_m, in_fours(left_n), Partial{w.partial + ((int64_t)result * w.splits + split) * w.m * ld, ld, 0});
     } else {
-        store_tile<P, (P::TM == 256)>(lds, acc, static_cast<T*>(w.D[result]) + m0 * w.ldd + n0, w.ldd, left_m, left_n, false, one);
+        put_tile<P>(lds, acc, m0, n0, left_m, left_n, Plain<T, (P::TM == 256)>(static_cast<T*>(w.D[result]), w.ldd));
     }
 }
 
