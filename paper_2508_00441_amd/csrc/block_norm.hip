@@ -351,7 +351,8 @@ __global__ void __launch_bounds__(THREADS) block_norm_grad_kernel(const NormGrad
     if (w.t != nullptr) leave(w.t + blockIdx.x * a.k, SUM_T);
 }
 
-// Sums over chunks and units: 32 columns a workgroup, in 32 shares.  blockIdx.y: 0 dw_pre, 1 dw_post, from 2 on a gate's gradient.
+// Sums over chunks and units: 32 columns a workgroup, in 32 shares.  blockIdx.y: 0 dw_pre, 1 dw_post, from 2 on a gate's gradient; a single gate's
+// comes from the same sum as dw_post.
 constexpr int JOIN_COLUMNS = 32, JOIN_SHARES = 32;
 __global__ void __launch_bounds__(JOIN_COLUMNS * JOIN_SHARES) block_norm_join_kernel(const NormGradWork w) {
     __shared__ float shares[JOIN_SHARES][JOIN_COLUMNS + 1];
@@ -359,7 +360,8 @@ __global__ void __launch_bounds__(JOIN_COLUMNS * JOIN_SHARES) block_norm_join_ke
     const NormChunks& n = w.n;
     const int in = threadIdx.x % JOIN_COLUMNS, share = threadIdx.x / JOIN_COLUMNS;
     const int64_t c = (int64_t)blockIdx.x * JOIN_COLUMNS + in, what = blockIdx.y;
-    if (what == 0 ? a.dw_pre == nullptr : what == 1 ? a.dw_post == nullptr : false) return;
+    const bool single = a.gate != nullptr && n.groups == 1;
+    if (what == 0 ? a.dw_pre == nullptr : what == 1 ? a.dw_post == nullptr && !(single && a.dgate != nullptr) : false) return;
     float sum = 0.0f;
     if (c < a.k) {
         if (what == 0) {
@@ -368,7 +370,7 @@ __global__ void __launch_bounds__(JOIN_COLUMNS * JOIN_SHARES) block_norm_join_ke
         } else if (what == 1) {
 #pragma unroll 8
             for (int64_t i = share; i < n.units; i += JOIN_SHARES)
-                sum += w.s[i * a.k + c] * (a.gate != nullptr ? a.gate[(n.per_group > 0 ? i / n.per_group : i) * a.k + c] : 1.0f);
+                sum += w.s[i * a.k + c] * (a.gate != nullptr && !single ? a.gate[(n.per_group > 0 ? i / n.per_group : i) * a.k + c] : 1.0f);
         } else {
             const float* const from = w.s + (what - 2) * n.per_group * a.k + c;
 #pragma unroll 8
@@ -385,8 +387,10 @@ __global__ void __launch_bounds__(JOIN_COLUMNS * JOIN_SHARES) block_norm_join_ke
     const int64_t to = (int64_t)blockIdx.x * JOIN_COLUMNS + column;
     if (from != 0 || to >= a.k) return;
     if (what == 0) a.dw_pre[to] = sum;
-    else if (what == 1) a.dw_post[to] = sum * a.scale;
-    else a.dgate[(what - 2) * a.k + to] = sum * a.scale * (a.w_post != nullptr ? a.w_post[to] : 1.0f);
+    else if (what == 1) {
+        if (a.dw_post != nullptr) a.dw_post[to] = sum * (single ? a.gate[to] * a.scale : a.scale);
+        if (single && a.dgate != nullptr) a.dgate[to] = sum * a.scale * (a.w_post != nullptr ? a.w_post[to] : 1.0f);
+    } else a.dgate[(what - 2) * a.k + to] = sum * a.scale * (a.w_post != nullptr ? a.w_post[to] : 1.0f);
 }
 // a gate's gradient where its rows are one unit
 __global__ void __launch_bounds__(256) block_norm_gate_kernel(const NormGradWork w) {
@@ -478,9 +482,9 @@ hipError_t launch_block_norm_grad(const BlockNormArgs& a, int type, int type_r, 
         });
     });
     if (e != hipSuccess || (w.t == nullptr && w.s == nullptr)) return e;
-    const bool gates = a.dgate != nullptr && w.n.per_group > 0;
+    const bool gates = a.dgate != nullptr && w.n.per_group > 0, single = w.n.groups == 1;
     if (a.dw_pre != nullptr || a.dw_post != nullptr || gates) {
-        hipLaunchKernelGGL(block_norm_join_kernel, dim3((unsigned)div_up(a.k, JOIN_COLUMNS), (unsigned)(gates ? 2 + w.n.groups : 2)), dim3(JOIN_COLUMNS * JOIN_SHARES), 0, st, w);
+        hipLaunchKernelGGL(block_norm_join_kernel, dim3((unsigned)div_up(a.k, JOIN_COLUMNS), (unsigned)(gates && !single ? 2 + w.n.groups : 2)), dim3(JOIN_COLUMNS * JOIN_SHARES), 0, st, w);
         const hipError_t j = hipGetLastError();
         if (j != hipSuccess) return j;
     }
