@@ -263,3 +263,23 @@ def test_no_rows():
     lib.ozaki_set_stream(torch.cuda.current_stream().cuda_stream)
     lib.ozaki_block_norm_grad(0, 20, None, 0, lib.TYPE_BF16, None, None, 0, 1.0, EPS, None, 0, lib.TYPE_BF16, None, None, 0, None, 0, None, 0, None, 0, a, None, b)
     assert bool(torch.all(a == 0)) and bool(torch.all(b == 0))
+
+
+@pytest.mark.gpu
+def test_beyond_32_bits(workspace):
+    """More than 2^31 elements: the last rows are as they are alone."""
+    rows, k = 270000, 8192
+    few = Problem(5, k, ("bf16", "bf16"), group=None)
+    few.check_gradient(few.gradient(want=("dx", "dr")))
+    X, R, dH = (torch.zeros((rows, k), dtype=torch.bfloat16, device="cuda") for _ in range(3))
+    X[-5:], R[-5:], dH[-5:] = few.x, few.r, few.dh
+    H = torch.zeros_like(X)
+    args = (rows, k, X, k, lib.TYPE_BF16, few.w_post, None, 0, few.scale, EPS)
+    dw_pre = torch.zeros((k,), device="cuda")
+    lib.ozaki_block_norm_grad(*args, R, k, lib.TYPE_BF16, few.w_pre, dH, k, None, 0, H, k, None, 0, None, None, dw_pre)
+    want = few.gradient(True, False, ("dx", "dw_pre"))
+    assert torch.equal(H[-5:], want["dx"]) and bool(torch.all(H[:-5] == 0))
+    assert bool(torch.all((dw_pre - want["dw_pre"]).abs() <= 2.0 ** -20 * (few.dh.float() * few.r.float()).abs().sum(0)))
+    lib.ozaki_block_norm(*args, R, k, lib.TYPE_BF16, R, k, few.w_pre, H, k)
+    r, h = few.forward()
+    assert torch.equal(H[-5:], h) and torch.equal(R[-5:], r) and bool(torch.all(H[:-5] == 0))

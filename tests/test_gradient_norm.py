@@ -159,3 +159,15 @@ def test_refusals():
     lib.ozaki_set_workspace(None, 0)
     assert lib.ozaki_gradient_norm(*norm, check=False) == lib.STATUS_WORKSPACE
     assert lib.ozaki_gradient_norm_workspace_bytes(-1) == 0 and lib.ozaki_gradient_norm_workspace_bytes(0) > 0
+
+
+@pytest.mark.gpu
+def test_beyond_32_bits(workspace):
+    x = torch.zeros(((1 << 31) + 70001,), dtype=torch.bfloat16, device="cuda")
+    x[-3:] = torch.tensor([3.0, -4.0, 12.0])
+    x[5] = 84.0
+    out, norm = _clip([x], 1.0, 17.0)
+    assert float(norm) == 85.0                                      # (5, 12, 13 and 13, 84, 85)
+    factor = torch.tensor(17.0) / torch.tensor(85.0)
+    assert torch.equal(out[0][-3:].cpu(), (torch.tensor([3.0, -4.0, 12.0]) * factor).bfloat16()) and float(out[0][5]) == float((84.0 * factor).bfloat16())
+    assert int((out[0] != 0).sum()) == 4

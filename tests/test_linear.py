@@ -329,3 +329,33 @@ def test_refusals():
     assert lib.ozaki_linear_workspace_bytes(0, 4, 4, True) == lib.ozaki_linear_workspace_bytes(4, 4, 0, True) == lib.ozaki_linear_workspace_bytes(4, 0, 4, True) == 0
     assert lib.ozaki_linear_workspace_bytes(64, 64, 65536, False) > 0
     assert lib.ozaki_linear(64, 64, 65536, FAKE, 65536, FAKE, 65536, lib.TYPE_BF16, None, 0, None, 0, FAKE, 64, check=False) == lib.STATUS_WORKSPACE
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("pair", [False, True])
+def test_beyond_32_bits(pair):
+    """Matrices of more than 2^32 bytes and 2^31 elements: the last rows and columns, of the results and of the sums over all tokens."""
+    m, n, k = 40000, 60000, 64
+    x = Problem(m, 8, k, "bf16", "silu", pair=pair, bias=False, residual=False)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x.n, x.w = n, [(torch.randn((n, k), device="cuda", generator=gen) / 8).bfloat16() for _ in x.w]
+    x.W = x.w
+    ws = _need(x, False)
+    Y, Z = x.forward()
+    ws.close()
+    rows, columns = torch.tensor([0, 777, m - 300, m - 1], device="cuda"), torch.tensor([0, 1, n - 200, n - 1], device="cuda")
+    part = Problem(4, 4, k, "bf16", "silu", pair=pair, bias=False, residual=False)
+    part.x, part.w, part.n = x.x[rows], [w[columns] for w in x.w], 4
+    part.check_forward(Y[rows][:, columns], [z[rows][:, columns] for z in Z])
+    # the gradient, of a dY that is zero but in some rows and columns
+    x.Z, x.dY = Z, Y.zero_()
+    picked = torch.randn((4, 4), device="cuda", generator=gen).bfloat16()
+    x.dY[rows.unsqueeze(1), columns] = picked
+    ws = _need(x, True)
+    dX, dW, _ = x.gradient("xwu")
+    ws.close()
+    part.z, part.dy = [z[rows][:, columns] for z in Z], picked
+    part.check_gradient(dX[rows], [w[columns] for w in dW], None)
+    others = torch.ones((m,), dtype=torch.bool, device="cuda")
+    others[rows] = False
+    assert bool(torch.all(dX[others] == 0)) and all(int((w != 0).any(1).sum()) == 4 for w in dW)
