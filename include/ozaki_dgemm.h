@@ -433,8 +433,9 @@ int ozaki_linear(int64_t m, int64_t n, int64_t k, const void* X, int64_t ldx, co
  *     dz = dY * act'(Z)          dX = dz W          dW = dz^T X          dbias[j] = sum over i of dz[i][j]
  *   Z, ldz    what ozaki_linear left, or anything else that dz is to be formed with; not read without an activation
  *   dX, dW    of `type`; dbias in 32 bits.  Each may be null, not all of them; X is read for dW, W for dX.
- * dz is formed once and rounded to `type` for the two products (without an activation it is dY); dbias is summed in 32 bits from what has not been rounded.
- * RELU's derivative at zero is zero.  m == 0 gives zeros in dW and dbias.  n is at most OZAKI_MAX_EXTENT / 2.
+ * dz is formed once and rounded to `type` for the two products (without an activation it is dY; in FP16 magnitudes from 65520 on become infinite there); dbias is
+ * summed in 32 bits from what has not been rounded.  Where few tiles leave compute units without work the sums over n or m are cut into shares; the cut depends on the sizes
+ * and on which of dX and dW are asked for.  RELU's derivative at zero is zero.  m == 0 gives zeros in dW and dbias.  n is at most OZAKI_MAX_EXTENT / 2.
  * Needs the context's workspace, ozaki_linear_workspace_bytes(m, n, k, 1). */
 int ozaki_linear_grad(int64_t m, int64_t n, int64_t k, const void* X, int64_t ldx, const void* W, int64_t ldw, int type, int activation, const void* Z,
                       int64_t ldz, const void* dY, int64_t lddy, void* dX, int64_t lddx, void* dW, int64_t lddw, float* dbias);

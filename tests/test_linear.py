@@ -231,6 +231,25 @@ def test_large_and_infinite_arguments(pair):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("m", [1, 40])
+def test_numbers_below_fp16s_normal_ones(m):
+    """2^-20 and 2^-24 have one significant bit in FP16 and are no normal numbers there; their sums are exact."""
+    n, k = 24, 64
+    X, W = torch.full((m, k), 2.0 ** -20, dtype=torch.float16, device="cuda"), torch.full((n, k), 0.5, dtype=torch.float16, device="cuda")
+    Y, dX, dW = (torch.full(shape, float("nan"), dtype=torch.float16, device="cuda") for shape in ((m, n), (m, k), (n, k)))
+    ws = device.Workspace(max(lib.ozaki_linear_workspace_bytes(m, n, k, grad) for grad in (False, True)))
+    lib.ozaki_linear(m, n, k, X, k, W, k, lib.TYPE_F16, None, 0, None, 0, Y, n)
+    assert bool(torch.all(Y == 2.0 ** -15))
+    Z, dY = torch.ones((m, n), dtype=torch.float16, device="cuda"), torch.full((m, n), 2.0 ** -24, dtype=torch.float16, device="cuda")
+    lib.ozaki_linear_grad(m, n, k, X, k, W, k, lib.TYPE_F16, lib.ACTIVATION_RELU, Z, n, dY, n, dX, k, dW, k)
+    assert bool(torch.all(dX == 12 * 2.0 ** -24)) and bool(torch.all(dW == 0))
+    X.fill_(1.0)
+    lib.ozaki_linear_grad(m, n, k, X, k, W, k, lib.TYPE_F16, lib.ACTIVATION_RELU, Z, n, dY, n, dX, k, dW, k)
+    assert bool(torch.all(dW == m * 2.0 ** -24))
+    ws.close()
+
+
+@pytest.mark.gpu
 def test_no_tokens():
     x = Problem(1, 24, 40, "bf16", "silu")
     dW, dbias = x.result(24, 40, 2), torch.full((24,), 7.0, device="cuda")
