@@ -1,8 +1,9 @@
 // The norm of many tensors together, and the tensors scaled so that it stays within bounds:
 //     norm = |scale| sqrt(sum over all elements of x^2),        out = x * scale * min(1, max_norm / norm).
 //
-// Bound by memory: every element is read for the norm and once more to be scaled.  Tensors are named in the kernel's arguments, as many to a launch as fit there;
-// elements go to workgroups in chunks, whatever the tensors' sizes.  
+// Bound by memory: every element is read for the norm and once more to be scaled, from the end, which the last-level cache still has (268 million BF16 elements: 121 us
+// for the squares, 4.4 TB/s, 175 - 181 for the second reading, 5.9 - 6.1 TB/s read and written).  Tensors are named in the kernel's arguments, as many to a launch as fit there;
+// elements go to workgroups in chunks, whatever the tensors' sizes.
 // Squares are summed in 32 bits by a thread over its elements of a chunk, and from there on in pairs of 32-bit numbers, a sum and what it lacks, in an order that
 // depends on the sizes only.  Where a thread's squares leave the range of 32 bits, it reads its elements again and squares them times 2^-90 or 2^90; such sums are kept apart
 // and join at the end.
@@ -16,6 +17,7 @@ namespace {
 constexpr uint32_t MOST_CHUNK = 8192, LEAST_CHUNK = 2048;
 constexpr unsigned MOST_BLOCKS = 1024;
 constexpr int TABLE = 144;               // tensors in a launch's arguments, which hold 4 KiB
+constexpr int MOST_REVERSED = 64;        // launches that the second reading takes from the last one on
 constexpr int THREADS = 256, MOST_JOINED = 1024;     // partial sums that every workgroup of the second reading adds up itself: 3 us, a launch of its own 5
 
 struct ClipTable {
@@ -226,8 +228,10 @@ size_t gradient_norm_bytes(int64_t count) { return (size_t)div_up(count, TABLE) 
 hipError_t launch_clip(const ClipArgs& a, hipStream_t st) {
     Squares* const partial = reinterpret_cast<Squares*>(a.ws);
     int partials = 0, launches = 0;
+    int begins[MOST_REVERSED];           // of the launches' tensors
     ClipTable t;
     for (int i = 0; i < a.count && !a.given;) {
+        if (launches < MOST_REVERSED) begins[launches] = i;
         i = fill_table(a, i, t);
         if (t.chunks == 0) break;
         hipLaunchKernelGGL(gradient_squares_kernel, dim3(blocks_of(t)), dim3(THREADS), 0, st, t, partial + partials);
@@ -243,12 +247,24 @@ hipError_t launch_clip(const ClipArgs& a, hipStream_t st) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    for (int i = 0; i < a.count && a.out != nullptr;) {
-        i = fill_table(a, i, t);
-        if (t.chunks == 0) break;
+    const auto clip = [&](int begin, int& next) {
+        next = fill_table(a, begin, t);
+        if (t.chunks == 0) return hipSuccess;
         hipLaunchKernelGGL(gradient_clip_kernel, dim3(blocks_of(t)), dim3(THREADS), 0, st, t, a.norm, partial, a.given || apart ? 0 : partials, a.scale, a.max_norm);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
+        return hipGetLastError();
+    };
+    if (a.out == nullptr) return hipSuccess;
+    int next = 0;
+    if (launches > 0 && launches <= MOST_REVERSED) {                   // what was read last comes first
+        for (int l = launches - 1; l >= 0; --l) {
+            const hipError_t e = clip(begins[l], next);
+            if (e != hipSuccess) return e;
+        }
+    } else {
+        while (next < a.count) {
+            const hipError_t e = clip(next, next);
+            if (e != hipSuccess) return e;
+        }
     }
     return hipSuccess;
 }

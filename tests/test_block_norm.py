@@ -172,6 +172,17 @@ def test_zeros_large_and_small_numbers(types, workspace):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("k", [520, 9000])
+def test_gradient_without_a_norm_does_not_look_at_x(k, workspace):
+    """Without w_post the gradient of X is scale * gate * dR, whatever X holds."""
+    x = Problem(6, k, ("bf16", "bf16"), post=False, group=2)
+    want = x.gradient(want=("dx", "dr"))
+    x.X[1, 3], x.X[4, k - 1] = float("inf"), float("nan")
+    got = x.gradient(want=("dx", "dr"))
+    assert torch.equal(got["dx"], want["dx"]) and torch.equal(got["dr"], want["dr"])
+
+
+@pytest.mark.gpu
 def test_gradient_against_differences(workspace):
     """Along a direction, in 32 bits: a central difference over t is off by the third derivative's t^2 / 6, for which the step of half t, a quarter as far off, is the measure."""
     rows, k = 6, 72
