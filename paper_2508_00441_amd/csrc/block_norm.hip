@@ -412,6 +412,7 @@ RowShape row_shape(int64_t k) {
 }
 NormChunks norm_chunks(int64_t rows, int64_t k, int64_t group) {
     const int threads = row_shape(k).threads;
+    // as many as run at a time: 8192 x 4096 in 512 chunks 95 us, in 256 111, in 768 102;  16384 x 512 in 2048 32, in 1024 40, in 4096 34
     const int64_t most = threads <= 128 ? 2048 : 262144 / threads;
     NormChunks n;
     n.group = group > 0 && group < rows ? group : rows;

@@ -12,9 +12,9 @@ ACTIVATIONS = ["none", "relu", "gelu", "gelu_tanh", "silu"]
 # dimension; odd sizes; steps that end inside 16 bytes
 SHAPES = [(1, 1, 1), (1, 16, 64), (1, 257, 100), (3, 5, 8), (2, 40, 6200), (16, 100, 6401), (7, 1000, 257), (17, 33, 72), (33, 129, 640), (64, 500, 1000), (65, 1000, 33),
           (100, 300, 4096), (200, 1001, 200), (300, 511, 64), (1000, 4100, 100), (1030, 4104, 264), (2100, 4200, 72), (2310, 4097, 129), (2304, 4352, 256),
-          (3000, 2800, 72), (4616, 4090, 40), (2100, 8461, 40), (9, 300, 16400)]
+          (3000, 2800, 72), (4616, 4090, 40), (2100, 8461, 40), (9, 300, 16400), (700, 1300, 100), (700, 700, 333), (2000, 3201, 136), (1000, 3204, 72), (70, 70000, 40), (500, 2600, 72), (4104, 4096, 40)]
 GRAD_SHAPES = [(1, 1, 1), (1, 257, 100), (3, 5, 8), (16, 1000, 136), (17, 33, 72), (40, 3000, 64), (65, 1000, 33), (200, 1001, 200), (300, 511, 64), (513, 264, 1031), (1000, 72, 72),
-               (5000, 100, 130), (1030, 2100, 264), (2100, 1100, 4200), (2100, 4200, 300), (4100, 300, 280)]
+               (5000, 100, 130), (1030, 2100, 264), (2100, 1100, 4200), (2100, 4200, 300), (4100, 300, 280), (8, 3000, 300), (1030, 8000, 1030), (10000, 600, 1100)]
 
 
 class Problem:
