@@ -419,7 +419,8 @@ enum {
 #define OZAKI_MAX_NORM 16384 /* elements of a row of ozaki_block_norm                                                 */
 
 /* A linear layer with what follows it:     z = X W^T + bias          Y = act(z) + R
- * X: m vectors, W: n vectors of k >= 1 elements of `type` (BF16 or F16), of which everything else is too; m * n is at most OZAKI_MAX_LOGITS.
+ * X: m vectors, W: n >= 1 vectors of k >= 1 elements of `type` (BF16 or F16), of which everything else is too; m * n, m * k and n * k are at most
+ * OZAKI_MAX_LOGITS.
  *   bias      n elements; may be null
  *   R, ldr    m x n, may lie anywhere, may be Y with its ld; may be null
  *   Z, ldz    where z goes, for the gradient; may be null
