@@ -108,6 +108,47 @@ def test_gates(rows, k, group, workspace):
 
 
 @pytest.mark.gpu
+# gates that end inside the chunk of a workgroup, beside one another and one after another, and that have one, some and many chunks
+@pytest.mark.parametrize("rows,k,group", [(16400, 24, 1), (16400, 24, 5), (16384, 128, 16), (9000, 130, 15), (9000, 130, 17), (5000, 250, 2), (7003, 500, 4), (7003, 500, 7), (40, 100, 1),
+                                          (2500, 513, 1), (1100, 2048, 3), (1100, 4100, 1), (600, 9000, 1), (1300, 9000, 4), (3000, 1000, 64), (5000, 90, 1700), (4097, 300, 4096)])
+@pytest.mark.parametrize("types", [("bf16", "f32"), ("f32", "f32")])
+def test_gates_of_few_and_many_rows(rows, k, group, types, workspace):
+    p = Problem(rows, k, types, group=group)
+    p.check_gradient(p.gradient())
+    for want in (("dgate",), ("dw_post",), ("dx", "dgate"), ("dw_pre", "dw_post")):
+        p.check_gradient(p.gradient(want=want))
+    p = Problem(rows, k, types, post=False, group=group)
+    p.check_gradient(p.gradient(want=("dx", "dgate")))
+
+
+@pytest.mark.parametrize("types", [("bf16", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("k", [40, 128, 200, 500, 520])
+def test_rows_side_by_side_are_rows_of_their_own(k, types, workspace):
+    """Each row's results have the bits of a call for it alone, also beside rows that are normed again with a scale, zeros, infinities and NaN."""
+    rows = 41
+    p = Problem(rows, k, types, group=4)
+    for v in (p.X, p.R) if types[0] == "f32" else (p.R,):
+        v[1], v[6], v[11], v[18] = v[1] * 1e25, v[6] * 1e-25, 0.0, float("nan")
+        v[23, k // 2] = float("inf")
+    if types[0] == "f32":
+        p.dH[7] *= 1e30
+
+    def call(i, n):
+        x, r, dh, dr_out = (v[i : i + n] for v in (p.X, p.R, p.dH, p.dR_out))
+        gate = p.gate[i // 4 : (i + n + 3) // 4]
+        R_out, H, dR, dX = torch.empty_like(r), torch.empty_like(x), torch.empty_like(r), torch.empty_like(x)
+        common = (n, k, x, x.shape[1], lib.TYPES[p.type], p.w_post, gate, 4, p.scale, EPS)
+        lib.ozaki_block_norm(*common, r, r.shape[1], lib.TYPES[p.type_r], R_out, k, p.w_pre, H, k)
+        lib.ozaki_block_norm_grad(*common, r, r.shape[1], lib.TYPES[p.type_r], p.w_pre, dh, dh.shape[1], dr_out, dr_out.shape[1], dX, k, dR, k, None, None, None)
+        bits = torch.int32 if p.type == "f32" else torch.int16
+        return [v.reshape(-1)[: n * k].reshape(n, k).view(bits) for v in (R_out, H, dR, dX)]
+
+    together = call(0, rows)
+    for i in range(rows):
+        for all, one in zip(together, call(i, 1)):
+            assert torch.equal(all[i : i + 1], one), i
+
+
 @pytest.mark.parametrize("post", [True, False])
 def test_parts(post, workspace):
     x = Problem(40, 600, ("f16", "f32"), post=post, group=40)
