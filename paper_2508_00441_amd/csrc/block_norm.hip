@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(workgroup_threads(ROW)) block_norm_kernel(cons
 
 // ---- gradient ----------------------------------------------------------------------------------------------------
 // A workgroup has a chunk of neighbouring rows.  Where a gate's rows are more than a chunk, a chunk lies inside them and leaves its s for the join.  Where they are
-// fewer, a chunk is some gates' rows: the workgroup writes their gradients itself and leaves the sum of gate s (16384 x 2048 with a gate for each row 371 us where
+// fewer, a chunk is some gates' rows: the workgroup writes their gradients itself and leaves the sum of gate s (16384 x 2048 with a gate for each row 187 us, 371 where
 // every s went through memory).
 struct NormChunks {
     int64_t group, groups;   // rows of a gate (or all, without one), and how many gates
@@ -475,12 +475,16 @@ RowShape row_shape(int64_t k) {
 }
 NormChunks norm_chunks(int64_t rows, int64_t k, int64_t group) {
     const int threads = row_shape(k).threads, at_once = workgroup_threads(threads) / threads;
-    // as many as run at a time: 8192 x 4096 in 512 chunks 95 us, in 256 111, in 768 102
-    const int64_t most = threads == 128 ? 2048 : 262144 / workgroup_threads(threads);
+    // as many as run at a time, of short rows fewer, whose join counts: 8192 x 4096 in 512 chunks 95 us, in 256 111, in 768 102;  16384 x 1024 in 1024 70, in 2048 71;
+    // 16384 x 255 in 512 21, in 256 23, in 1024 25;  16384 x 32 in 512 11.6, in 256 13.2, in 1024 13.6
+    const int64_t most = threads <= 64 ? 512 : threads == 128 ? 1024 : 262144 / threads;
     NormChunks n;
     n.group = group > 0 && group < rows ? group : rows;
     n.groups = div_up(rows, n.group);
     n.rows = div_up(div_up(rows, most), at_once) * at_once;
+    // gates of fewer rows whose rows fill a workgroup are a chunk each, if they are not too many: one after another they would take longer than more chunks to join
+    // (16384 x 128 with a gate for 16 rows 21 us, inside chunks 34)
+    if (at_once > 1 && n.group < n.rows && n.group >= at_once && n.groups <= 4 * most) n.rows = n.group;
     if (n.group >= n.rows || n.groups == 1) {
         n.per_group = div_up(n.group, n.rows);
         n.chunks = n.groups * n.per_group;
