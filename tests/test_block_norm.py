@@ -107,11 +107,11 @@ def test_gates(rows, k, group, workspace):
         x.check_gradient(x.gradient(want=("dw_post", "dx") if post else ("dgate",)))
 
 
-@pytest.mark.gpu
 # gates that end inside the chunk of a workgroup, beside one another and one after another, and that have one, some and many chunks
 @pytest.mark.parametrize("rows,k,group", [(16400, 24, 1), (16400, 24, 5), (16384, 128, 16), (9000, 130, 15), (9000, 130, 17), (5000, 250, 2), (7003, 500, 4), (7003, 500, 7), (40, 100, 1),
                                           (2500, 513, 1), (1100, 2048, 3), (1100, 4100, 1), (600, 9000, 1), (1300, 9000, 4), (3000, 1000, 64), (5000, 90, 1700), (4097, 300, 4096)])
 @pytest.mark.parametrize("types", [("bf16", "f32"), ("f32", "f32")])
+@pytest.mark.gpu
 def test_gates_of_few_and_many_rows(rows, k, group, types, workspace):
     p = Problem(rows, k, types, group=group)
     p.check_gradient(p.gradient())
@@ -121,6 +121,7 @@ def test_gates_of_few_and_many_rows(rows, k, group, types, workspace):
     p.check_gradient(p.gradient(want=("dx", "dgate")))
 
 
+@pytest.mark.gpu
 @pytest.mark.parametrize("types", [("bf16", "bf16"), ("f32", "f32")])
 @pytest.mark.parametrize("k", [40, 128, 200, 500, 520])
 def test_rows_side_by_side_are_rows_of_their_own(k, types, workspace):
@@ -149,6 +150,7 @@ def test_rows_side_by_side_are_rows_of_their_own(k, types, workspace):
             assert torch.equal(all[i : i + 1], one), i
 
 
+@pytest.mark.gpu
 @pytest.mark.parametrize("post", [True, False])
 def test_parts(post, workspace):
     x = Problem(40, 600, ("f16", "f32"), post=post, group=40)
