@@ -462,7 +462,8 @@ size_t ozaki_gated_linear_workspace_bytes(int64_t m, int64_t n, int64_t k, int g
  *     u = X * rho(X) * w_post   (w_post null: u = X)          the norm behind a block
  *     r = R + scale * gate * u                                its gate and scale, the sum that runs through the model
  *     H = r * rho(r) * w_pre                                  the norm in front of the next block
- *   X, H      of `type` (F32, BF16, F16); X null: nothing is added (r is R; R_out, w_post and gate are then null too)
+ *   X, H      of `type` (F32, BF16, F16); X null: nothing is added (r is R; R_out, w_post and gate are then null too, unless rows is 0: then
+ *             nothing is done, and any address of rows may be null)
  *   w_post, w_pre      k elements in 32 bits
  *   gate, group        32 bits, rows i share row i / group of it: gate[(i / group) * k + e]; null: one
  *   R, R_out  of `type_r`, which is `type` or F32; R null: zeros.  R_out is r; may be null, may be R with its ld.

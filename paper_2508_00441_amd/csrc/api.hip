@@ -277,8 +277,8 @@ int check_norm_args(int64_t rows, int64_t k, const void* X, int64_t ldx, int typ
     if (!aligned16(X)) return -3;
     if (X && !rows_ok(ldx, k, type)) return -4;
     if (!type_ok(type)) return -5;
-    if (!aligned(w_post, 4) || (w_post && !X)) return -6;
-    if (!aligned(gate, 4) || (gate && !X)) return -7;
+    if (!aligned(w_post, 4) || (rows > 0 && w_post && !X)) return -6;         // (the address of no rows may be null)
+    if (!aligned(gate, 4) || (rows > 0 && gate && !X)) return -7;
     if (gate && group < 1) return -8;
     if (!(scale - scale == 0.0f)) return -9;
     if (!(eps >= 0.0f) || !(eps - eps == 0.0f)) return -10;

@@ -319,6 +319,30 @@ def test_no_rows():
     assert bool(torch.all(a == 0)) and bool(torch.all(b == 0))
 
 
+def test_no_rows_with_weights():
+    """A batch of no rows lies at a null address; the weights and gates that go with every batch are there all the same."""
+    norm = (0, 20, None, 0, lib.TYPE_BF16, FAKE, FAKE, 2, 1.0, EPS, None, 0, lib.TYPE_BF16)
+    assert lib.ozaki_block_norm(*norm, None, 0, FAKE, None, 0, check=False) == 0
+    assert lib.ozaki_block_norm(*norm[:6], None, 0, *norm[8:], None, 0, FAKE, None, 0, check=False) == 0
+    assert lib.ozaki_block_norm_grad(*norm, FAKE, None, 0, None, 0, None, 0, None, 0, None, FAKE, None, check=False) == 0
+    # what is wrong with any number of rows is refused with none, too
+    assert lib.ozaki_block_norm(*norm[:5], FAKE + 2, *norm[6:], None, 0, FAKE, None, 0, check=False) == -6
+    assert lib.ozaki_block_norm(*norm[:7], 0, *norm[8:], None, 0, FAKE, None, 0, check=False) == -8
+
+
+@pytest.mark.gpu
+def test_no_rows_with_weights_gives_zeros():
+    rand = lambda *shape: torch.randn(shape, device="cuda")    # noqa: E731
+    x, w_post, w_pre, gate = rand(0, 20).bfloat16(), rand(20), rand(20), rand(3, 20)
+    dw_post, dw_pre = (torch.full((20,), 7.0, device="cuda") for _ in range(2))
+    lib.ozaki_set_stream(torch.cuda.current_stream().cuda_stream)
+    for g, group in ((gate, 2), (None, 0)):
+        common = (0, 20, x, 24, lib.TYPE_BF16, w_post, g, group, 1.0, EPS)
+        lib.ozaki_block_norm(*common, x, 24, lib.TYPE_BF16, x, 20, w_pre, x, 20)
+        lib.ozaki_block_norm_grad(*common, x, 24, lib.TYPE_BF16, w_pre, x, 24, x, 24, x, 20, x, 20, dw_post.fill_(7.0), None, dw_pre.fill_(7.0))
+        assert bool(torch.all(dw_post == 0)) and bool(torch.all(dw_pre == 0))
+
+
 @pytest.mark.gpu
 def test_beyond_32_bits(workspace):
     """More than 2^31 elements: the last rows are as they are alone."""
