@@ -436,8 +436,8 @@ int ozaki_linear(int64_t m, int64_t n, int64_t k, const void* X, int64_t ldx, co
  *   dX, dW    of `type`; dbias in 32 bits.  Each may be null, not all of them; X is read for dW, W for dX.
  * dz is formed once and rounded to `type` for the two products (without an activation it is dY; in FP16 magnitudes from 65520 on become infinite there); dbias is
  * summed in 32 bits from what has not been rounded.  Where few tiles leave compute units without work the sums over n or m are cut into shares; the cut depends on the sizes
- * and on which of dX and dW are asked for.  RELU's derivative at zero is zero.  m == 0 gives zeros in dW and dbias.  n is at most OZAKI_MAX_EXTENT / 2.
- * Needs the context's workspace, ozaki_linear_workspace_bytes(m, n, k, 1). */
+ * and on which of dX and dW are asked for.  RELU's derivative at zero is zero.  m == 0 gives zeros in dW and dbias, and all results may be null then
+ * (an empty dX is).  n is at most OZAKI_MAX_EXTENT / 2.  Needs the context's workspace, ozaki_linear_workspace_bytes(m, n, k, 1). */
 int ozaki_linear_grad(int64_t m, int64_t n, int64_t k, const void* X, int64_t ldx, const void* W, int64_t ldw, int type, int activation, const void* Z,
                       int64_t ldz, const void* dY, int64_t lddy, void* dX, int64_t lddx, void* dW, int64_t lddw, float* dbias);
 size_t ozaki_linear_workspace_bytes(int64_t m, int64_t n, int64_t k, int grad);
@@ -477,8 +477,8 @@ int ozaki_block_norm(int64_t rows, int64_t k, const void* X, int64_t ldx, int ty
  *     dR = dR_out + the gradient of r through H          dX = the gradient of X through scale * gate * u, from dR that has not been rounded
  *     dw_pre, dw_post (k elements), dgate (as gate), in 32 bits: sums over rows, in an order that depends on rows, k and group only
  * Each result may be null, not all of them; R_out and w_pre are read with dH (and only then); dw_pre asks for dH; dX, dw_post and dgate ask for X, dw_post for
- * w_post, dgate for gate.  dR may be dR_out, dX may be X or dH, each with its ld.  rows == 0 gives zeros in dw_pre and dw_post.  For the sums over rows the
- * call needs the context's workspace, ozaki_block_norm_workspace_bytes(rows, k, group) with group 0 without a gate. */
+ * w_post, dgate for gate.  dR may be dR_out, dX may be X or dH, each with its ld.  rows == 0 gives zeros in dw_pre and dw_post, and all
+ * results may be null then.  For the sums over rows the call needs the context's workspace, ozaki_block_norm_workspace_bytes(rows, k, group) with group 0 without a gate. */
 int ozaki_block_norm_grad(int64_t rows, int64_t k, const void* X, int64_t ldx, int type, const float* w_post, const float* gate, int64_t group,
                           float scale, float eps, const void* R_out, int64_t ldro, int type_r, const float* w_pre, const void* dH, int64_t lddh,
                           const void* dR_out, int64_t lddro, void* dX, int64_t lddx, void* dR, int64_t lddr, float* dw_post, float* dgate,

@@ -810,7 +810,7 @@ int ozaki_linear_grad(int64_t m, int64_t n, int64_t k, const void* X, int64_t ld
     if (m > 0 && activation != OZAKI_ACTIVATION_NONE && !stride_ok(ldz, n, 2)) return -11;
     if (m > 0 && (!dY || !aligned16(dY))) return -12;
     if (m > 0 && !stride_ok(lddy, n, 2)) return -13;
-    if ((!dX && !dW && !dbias) || !aligned(dX, 2)) return -14;
+    if ((m > 0 && !dX && !dW && !dbias) || !aligned(dX, 2)) return -14;      // (of no rows dX is null)
     if (dX && lddx < k) return -15;
     if (!aligned(dW, 2)) return -16;
     if (dW && lddw < k) return -17;
@@ -842,7 +842,7 @@ int ozaki_gated_linear_grad(int64_t m, int64_t n, int64_t k, const void* X, int6
     if (m > 0 && !stride_ok(ldu, n, 2)) return -14;
     if (m > 0 && (!dY || !aligned16(dY))) return -15;
     if (m > 0 && !stride_ok(lddy, n, 2)) return -16;
-    if ((!dX && !dWg && !dWu) || !aligned(dX, 2)) return -17;
+    if ((m > 0 && !dX && !dWg && !dWu) || !aligned(dX, 2)) return -17;       // (of no rows dX is null)
     if (dX && lddx < k) return -18;
     if (!aligned(dWg, 2)) return -19;
     if (!aligned(dWu, 2)) return -20;
@@ -901,7 +901,7 @@ int ozaki_block_norm_grad(int64_t rows, int64_t k, const void* X, int64_t ldx, i
     if (dH && !rows_ok(lddh, k, type)) return -16;
     if (!aligned16(dR_out)) return -17;
     if (dR_out && !rows_ok(lddro, k, type_r)) return -18;
-    if (!aligned(dX, type_bytes(type)) || (!dX && !dR && !dw_post && !dgate && !dw_pre)) return -19;
+    if (!aligned(dX, type_bytes(type)) || (rows > 0 && !dX && !dR && !dw_post && !dgate && !dw_pre)) return -19;
     if (dX && lddx < k) return -20;
     if (!aligned(dR, type_bytes(type_r))) return -21;
     if (dR && lddr < k) return -22;

@@ -330,6 +330,11 @@ def test_no_rows_with_weights():
     assert lib.ozaki_block_norm(*norm[:7], 0, *norm[8:], None, 0, FAKE, None, 0, check=False) == -8
 
 
+def test_no_rows_and_nothing_but_their_gradients():
+    norm = (0, 20, None, 0, lib.TYPE_BF16, None, None, 0, 1.0, EPS, None, 0, lib.TYPE_BF16, FAKE, None, 0, None, 0)
+    assert lib.ozaki_block_norm_grad(*norm, None, 20, None, 20, None, None, None, check=False) == 0
+
+
 @pytest.mark.gpu
 def test_no_rows_with_weights_gives_zeros():
     rand = lambda *shape: torch.randn(shape, device="cuda")    # noqa: E731

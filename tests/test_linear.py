@@ -264,6 +264,12 @@ def test_no_tokens():
     assert bool(torch.all(dW[:, :40] == 0)) and bool(torch.isnan(dW[:, 40:]).all())
 
 
+def test_no_tokens_and_nothing_but_their_gradient():
+    """A frozen layer's gradient asks for dX alone, which of no tokens lies at a null address."""
+    assert lib.ozaki_linear_grad(0, 24, 40, None, 0, FAKE, 40, lib.TYPE_BF16, 4, None, 0, None, 0, None, 40, None, 0, None, check=False) == 0
+    assert lib.ozaki_gated_linear_grad(0, 24, 40, None, 0, FAKE, FAKE, 40, lib.TYPE_BF16, 4, None, 0, None, 0, None, 0, None, 40, None, None, 0, check=False) == 0
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("m,n,k", [(40, 200, 4096), (600, 1031, 328)])
 def test_same_bits_every_time_on_another_stream_and_in_a_graph(m, n, k):
