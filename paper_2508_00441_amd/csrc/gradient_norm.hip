@@ -155,10 +155,15 @@ __device__ __forceinline__ float norm_of(const Squares* partial, int count, floa
     const Sum sum = large ? all.level[LARGE] + scaled(scaled(all.level[PLAIN], LEVEL_FACTOR[LARGE]), LEVEL_FACTOR[LARGE])
                   : plain ? all.level[PLAIN] + scaled(scaled(all.level[SMALL], LEVEL_FACTOR[LARGE]), LEVEL_FACTOR[LARGE])
                           : all.level[SMALL];
-    const float by = fabsf(scale), back = large ? LEVEL_FACTOR[SMALL] : plain ? 1.0f : LEVEL_FACTOR[LARGE];
+    float by = fabsf(scale), back = large ? LEVEL_FACTOR[SMALL] : plain ? 1.0f : LEVEL_FACTOR[LARGE];
+    // a scale on the other side of one takes the level's power of two with it: no product on the way leaves the range unless the norm does
+    if (large ? by < 1.0f : by > 1.0f) {
+        by *= back;
+        back = 1.0f;
+    }
     // the root with what it lacks, times the scale: one rounding
     const float root = sqrtf(sum.hi), lacks = root > 0.0f && root < __builtin_inff() ? (__builtin_fmaf(-root, root, sum.hi) + sum.lo) / (2.0f * root) : 0.0f;
-    const float n = root * by, rest = root < __builtin_inff() ? __builtin_fmaf(root, by, -n) + lacks * by : 0.0f;
+    const float n = root * by, rest = n < __builtin_inff() ? __builtin_fmaf(root, by, -n) + lacks * by : 0.0f;
     return (n + rest) * back;
 }
 

@@ -109,6 +109,28 @@ def test_large_small_and_not_finite(workspace):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("element,scale", [(2.0 ** 60, 2.0 ** -110), (2.0 ** 60, -1.5 * 2.0 ** -140), (2.0 ** 100, 2.0 ** -40), (2.0 ** 50, 3.0 * 2.0 ** 60), (2.0 ** -50, 2.0 ** 100),
+                                           (2.0 ** -60, 2.0 ** 127), (2.0 ** -100, -1.25 * 2.0 ** 90), (2.0 ** -60, 2.0 ** -50), (1.0, 2.0 ** -120), (1.0, 2.0 ** 110)])
+def test_scales_far_from_one(element, scale, workspace):
+    """Norms in 32 bits' range of elements whose squares are not, with scales that leave it on the way: 2^60 times 2^-110 as well as 2^-50 times 2^100."""
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    x = [element * torch.randn((n,), device="cuda", generator=gen) for n in (70001, 3)]
+    norm, want = torch.zeros((1,), device="cuda"), _norm(x, scale)
+    assert 2.0 ** -126 < want < 2.0 ** 128
+    lib.ozaki_gradient_norm(len(x), x, [v.numel() for v in x], _types(x), scale, norm)
+    assert abs(float(norm) - want) <= OFF * want
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("element,scale", [(1.0, 2.0 ** 127), (2.0 ** 100, 2.0 ** 60), (-(2.0 ** 127), 1.5)])
+def test_norms_beyond_32_bits_are_infinite(element, scale, workspace):
+    """... of finite elements too, which become zero."""
+    x = torch.full((70000,), element, device="cuda")
+    (out,), norm = _clip([x], scale, 1.0)
+    assert math.isinf(float(norm)) and float(norm) > 0 and bool(torch.all(out == 0))
+
+
+@pytest.mark.gpu
 def test_nothing(workspace):
     norm = torch.full((1,), 7.0, device="cuda")
     lib.ozaki_gradient_norm(0, None, None, None, 1.0, norm)
