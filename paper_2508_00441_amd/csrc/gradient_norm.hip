@@ -183,22 +183,30 @@ __global__ void __launch_bounds__(THREADS) gradient_clip_kernel(const ClipTable 
         norm = *norm_at;
     }
     // (a norm that is no number makes the factor none, one that is infinite makes it zero)
-    const float factor = norm <= max_norm ? scale : scale * (max_norm / norm);
+    const float ratio = max_norm / norm, factor = norm <= max_norm ? scale : scale * ratio;
+    // A factor below the normal numbers would lose its bits: then elements meet the scale first, which keeps them within the norm, and the ratio after that; a ratio
+    // as small is formed times 2^100, which the elements give back in between.
+    const bool far = norm > max_norm && norm < __builtin_inff() && (ratio < 0x1p-126f || fabsf(factor) < 0x1p-126f);
+    const float back = ratio < 0x1p-126f ? 0x1p-100f : 1.0f, rest = ratio < 0x1p-126f ? 0x1p100f * max_norm / norm : ratio;
     for (uint32_t i = blockIdx.x; i < t.chunks; i += gridDim.x)
         lanes.with_chunk(t.chunks - 1 - i, t.chunk, [&](auto x, auto out, int n) {
             typedef std::remove_pointer_t<decltype(out)> T;
             constexpr int PER = 16 / sizeof(T);
             typedef T piece __attribute__((ext_vector_type(PER), aligned(sizeof(T))));
             if (factor == 1.0f && x == out) return;
-            const int pieces = n / PER, e = pieces * PER + threadIdx.x;
+            const auto write = [&](auto times) {
+                const int pieces = n / PER, e = pieces * PER + threadIdx.x;
 #pragma unroll 4
-            for (int p = threadIdx.x; p < pieces; p += THREADS) {
-                piece v = *reinterpret_cast<const piece*>(x + PER * p);
+                for (int p = threadIdx.x; p < pieces; p += THREADS) {
+                    piece v = *reinterpret_cast<const piece*>(x + PER * p);
 #pragma unroll
-                for (int q = 0; q < PER; ++q) v[q] = (T)((float)v[q] * factor);
-                *reinterpret_cast<piece*>(out + PER * p) = v;
-            }
-            if (e < n) out[e] = (T)((float)x[e] * factor);
+                    for (int q = 0; q < PER; ++q) v[q] = (T)times((float)v[q]);
+                    *reinterpret_cast<piece*>(out + PER * p) = v;
+                }
+                if (e < n) out[e] = (T)times((float)x[e]);
+            };
+            if (far) write([&](float v) { return v * scale * back * rest; });
+            else write([&](float v) { return v * factor; });
         });
 }
 

@@ -131,6 +131,21 @@ def test_norms_beyond_32_bits_are_infinite(element, scale, workspace):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("element,scale,max_norm", [(2.0 ** 100, 1.0, 2.0 ** -40), (2.0 ** 100, 1.0, 3 * 2.0 ** -60), (2.0 ** 110, 0.75, 2.0 ** -100), (2.0 ** 100, -(2.0 ** -100), 2.0 ** -60),
+                                                    (2.0 ** 90, 2.0 ** -90, 2.0 ** -50), (2.0 ** 60, 2.0 ** 50, 2.0 ** -70), (1.0, 1.0, 0.0)])
+def test_factors_below_the_normal_numbers(element, scale, max_norm, workspace):
+    """max_norm / norm, or its product with the scale, has few bits in 32 bits or none; the results, of a norm of max_norm, have all of theirs."""
+    gen = torch.Generator(device="cuda").manual_seed(13)
+    x = [(element * torch.randn((n,), device="cuda", generator=gen)).to(dtype) for n, dtype in ((5001, torch.float32), (3, torch.float32), (4099, torch.bfloat16))]
+    out, norm = _clip(x, scale, max_norm)
+    assert math.isfinite(float(norm))
+    _check(x, scale, max_norm, out, norm)
+    in_place = [v.clone() for v in x]
+    _clip(in_place, scale, max_norm, out=in_place)
+    assert all(torch.equal(a, b) for a, b in zip(in_place, out))
+
+
+@pytest.mark.gpu
 def test_nothing(workspace):
     norm = torch.full((1,), 7.0, device="cuda")
     lib.ozaki_gradient_norm(0, None, None, None, 1.0, norm)
