@@ -486,8 +486,8 @@ int ozaki_block_norm_grad(int64_t rows, int64_t k, const void* X, int64_t ldx, i
 size_t ozaki_block_norm_workspace_bytes(int64_t rows, int64_t k, int64_t group);
 
 /* The norm of `count` tensors together:     *norm = |scale| * sqrt(sum over all elements of x^2)
- *   tensors, sizes, types      HOST: where each lies (DEVICE; aligned to its elements, no more), how many elements it has (at most 2^38), their type.
- *                              They are read before the call returns.
+ *   tensors, sizes, types      HOST: where each lies (DEVICE; aligned to its elements, no more), how many elements it has (at most 2^38, all of
+ *                              them together at most 2^43), their type.  They are read before the call returns.  At most 2^27 tensors.
  *   scale                      what the elements are to be multiplied by (one over what the loss was multiplied by)
  *   norm                       DEVICE, one number in 32 bits; infinite or NaN where an element is
  * Squares of at most 32 elements are summed in 32 bits, those sums in twice as many; elements whose squares leave the range are no exception.  The order depends

@@ -287,12 +287,13 @@ int check_norm_args(int64_t rows, int64_t k, const void* X, int64_t ldx, int typ
 }
 
 int check_tensors(int count, const void* const* tensors, const int64_t* sizes, const int* types, float scale) {
-    if (count < 0) return -1;
+    if (count < 0 || count > MAX_TENSORS) return -1;
     if (count > 0 && !tensors) return -2;
     if (count > 0 && !sizes) return -3;
     if (count > 0 && !types) return -4;
+    int64_t elements = 0;
     for (int i = 0; i < count; ++i) {
-        if (sizes[i] < 0 || sizes[i] > OZAKI_MAX_LOGITS) return -3;
+        if (sizes[i] < 0 || sizes[i] > OZAKI_MAX_LOGITS || (elements += sizes[i]) > MAX_CLIPPED) return -3;
         if (!type_ok(types[i])) return -4;
         if (sizes[i] > 0 && (!tensors[i] || !aligned(tensors[i], type_bytes(types[i])))) return -2;
     }
@@ -924,7 +925,7 @@ int ozaki_block_norm_grad(int64_t rows, int64_t k, const void* X, int64_t ldx, i
     return 0;
 }
 
-size_t ozaki_gradient_norm_workspace_bytes(int64_t count) { return count < 0 || count > 0x7FFFFFFF ? 0 : with_flags(gradient_norm_bytes(count > 0 ? count : 1)); }
+size_t ozaki_gradient_norm_workspace_bytes(int64_t count) { return count < 0 || count > MAX_TENSORS ? 0 : with_flags(gradient_norm_bytes(count > 0 ? count : 1)); }
 
 int ozaki_gradient_norm(int count, const void* const* tensors, const int64_t* sizes, const int* types, float scale, float* norm) {
     const int st = check_tensors(count, tensors, sizes, types, scale);

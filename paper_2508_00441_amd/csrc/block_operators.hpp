@@ -78,6 +78,7 @@ hipError_t launch_block_norm(const BlockNormArgs& a, int type, int type_r, hipSt
 hipError_t launch_block_norm_grad(const BlockNormArgs& a, int type, int type_r, hipStream_t st);
 
 // ---- gradient_norm.hip ---------------------------------------------------------------------------------------
+constexpr int64_t MAX_TENSORS = (int64_t)1 << 27, MAX_CLIPPED = (int64_t)1 << 43;       // of a call; elements of all of them
 struct ClipArgs {
     int count;
     const void* const* tensors;      // HOST

@@ -27,7 +27,9 @@ struct ClipTable {
     uint32_t first[TABLE];               // chunk; behind the last tensor the number of all chunks
     uint32_t chunks, chunk;              // elements of a chunk
 };
-static_assert(sizeof(ClipTable) + 24 <= 4096, "kernel arguments");
+static_assert(sizeof(ClipTable) + 2 * sizeof(void*) + sizeof(int) + 2 * sizeof(float) <= 4096, "kernel arguments");
+static_assert(MAX_CLIPPED / MOST_CHUNK + TABLE + MOST_BLOCKS <= 0x7FFFFFFF, "chunks of a launch, counted in 32 bits");
+static_assert((MAX_TENSORS / TABLE + 1) * MOST_BLOCKS <= 0x7FFFFFFF, "partial sums, counted in 32 bits");
 
 // The table in a wave's registers, a tensor a lane, read in one go: a search in memory would wait for each of its steps, since arguments come from far away.
 struct ClipLanes {
@@ -219,7 +221,7 @@ int fill_table(const ClipArgs& a, int begin, ClipTable& t) {
             at[count++] = i;
             total += a.sizes[i];
         }
-    // as short as makes 512 of them, within the bounds (no tensor has more than 2^38 elements: the chunks' numbers stay inside 32 bits)
+    // as short as makes 512 of them, within the bounds
     t.chunk = LEAST_CHUNK;
     while (t.chunk < MOST_CHUNK && total / t.chunk > MOST_JOINED / 2) t.chunk *= 2;
     t.chunks = 0;

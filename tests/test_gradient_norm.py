@@ -198,6 +198,17 @@ def test_refusals():
     assert lib.ozaki_gradient_norm_workspace_bytes(-1) == 0 and lib.ozaki_gradient_norm_workspace_bytes(0) > 0
 
 
+def test_more_than_a_call_counts():
+    """Chunks and partial sums are counted in 32 bits: 144 tensors of 2^38 elements would be more than 2^32 chunks."""
+    lib.ozaki_set_workspace(None, 0)
+    most = 2 ** 38
+    for count, answer in ((32, lib.STATUS_WORKSPACE), (33, -3), (144, -3)):
+        assert lib.ozaki_gradient_norm(count, [FAKE] * count, [most] * count, [1] * count, 1.0, FAKE, check=False) == answer
+        assert lib.ozaki_clip_gradients(count, [FAKE] * count, [most] * count, [1] * count, 1.0, 1.0, [FAKE] * count, FAKE, check=False) == answer
+    assert lib.ozaki_gradient_norm((1 << 27) + 1, [FAKE], [4], [1], 1.0, FAKE, check=False) == -1
+    assert lib.ozaki_gradient_norm_workspace_bytes((1 << 27) + 1) == 0 < lib.ozaki_gradient_norm_workspace_bytes(1 << 27)
+
+
 @pytest.mark.gpu
 def test_beyond_32_bits(workspace):
     x = torch.zeros(((1 << 31) + 70001,), dtype=torch.bfloat16, device="cuda")
