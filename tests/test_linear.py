@@ -170,6 +170,81 @@ def test_gradient_against_differences(act):
     ws.close()
 
 
+def _slope(value, leaves, i, direction):
+    """The derivative of value(leaves) along a direction of leaf i by central differences over t and t / 2, and what it may be off: the second one's error is a quarter of the first
+    one's, of which their difference is three quarters."""
+    out = []
+    for t in (2.0 ** -8, 2.0 ** -9):
+        ends = [value([v + sign * t * direction if j == i else v for j, v in enumerate(leaves)]) for sign in (1, -1)]
+        out.append(float((ends[0] - ends[1]) / (2 * t)))
+    return out[1], 2 * abs(out[0] - out[1])
+
+
+def _directions(grad, gen):
+    """Along the gradient's signs the derivative is as large as it can be: everywhere, and on halves of the elements."""
+    sign = torch.where(grad >= 0, 0.125, -0.125).double()
+    return [sign] + [sign * torch.randint(0, 2, grad.shape, device="cuda", generator=gen) for _ in range(3)]
+
+
+HALF = 2.0 ** -11                                                   # what rounding to FP16 may change, relative
+
+
+def _check_slopes(value, leaves, grads, changes):
+    """changes[i](direction): for every number that is rounded on its way to gradient i, what a relative change of it comes to in that gradient's slope.  Roundings are at most HALF each
+    and independent of one another, with a spread of 0.58 of that: four times the root of the sum of squares is seven times the spread."""
+    gen = torch.Generator(device="cuda").manual_seed(21)
+    for i, grad in enumerate(grads):
+        for direction in _directions(grad, gen):
+            want, off = _slope(value, leaves, i, direction)
+            along = grad.double() * direction
+            terms = ([along] if grad.dtype != torch.float32 else []) + changes[i](direction)
+            tolerance = off + 4 * HALF * float(sum(v.square().sum() for v in terms)) ** 0.5 + 2.0 ** -18 * float(along.abs().sum())
+            assert tolerance < 0.02 * abs(want), (i, tolerance, want)          # (so that a gradient which is missing, another one's or of the other sign does not pass)
+            assert abs(float(along.sum()) - want) <= tolerance, i
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", ["none", "gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("m,n,k", [(24, 40, 48), (130, 264, 96)])
+def test_slopes_of_a_pair(m, n, k, act):
+    """The gradient against differences of sum(dy * act(x wg^T) * (x wu^T)) in 64 bits.  g and u are held in FP16, then dg and du are; g's change is act'(g) g of du and act''(g) g, of
+    magnitude 1 at most, times dy u of dg."""
+    x = Problem(m, n, k, "f16", act, pair=True, seed=5)
+    ws = _need(x, True)
+    Y, Z = x.forward()
+    x.Z = [plain.padded(z, "f16") for z in Z]
+    dX, dW, _ = x.gradient()
+    ws.close()
+    across = lambda v, w: v @ w.t().contiguous()    # noqa: E731
+    xs, wg, wu = leaves = [v.double() for v in [x.x] + x.w]
+    dy, g, u = x.dy.double(), across(xs, wg), across(xs, wu)
+    a, slope, _, _ = plain.activation(g, act)
+    dg, du, g_of_dg, g_of_du = dy * u * slope, dy * a, (dy * u).abs(), (dy * slope * g).abs()
+    changes = [lambda d: [g_of_dg * across(d, wg).abs() + g_of_du * across(d, wu).abs(), dg * across(d, wg), dg * across(d, wg), du * across(d, wu)],
+               lambda d: [v * across(xs, d) for v in (g_of_dg, dg, dg)],
+               lambda d: [v * across(xs, d) for v in (g_of_du, du)]]
+    _check_slopes(lambda at: (dy * plain.gated(*at, act)[4]).sum(), leaves, [dX] + dW, changes)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", ["none", "gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("m,n,k", [(24, 40, 48), (130, 264, 96)])
+def test_slopes_of_a_layer(m, n, k, act):
+    """The same of sum(dy * (act(x w^T + bias) + r)): z is held in FP16, dz is for the two products."""
+    x = Problem(m, n, k, "f16", act, seed=6)
+    ws = _need(x, True)
+    Y, Z = x.forward()
+    x.Z = [plain.padded(z, "f16") for z in Z]
+    dX, (dW,), dbias = x.gradient()
+    ws.close()
+    across = lambda v, w: v @ w.t().contiguous()    # noqa: E731
+    xs, w, bias = leaves = [x.x.double(), x.w[0].double(), x.bias.double()]
+    dy = x.dy.double()
+    dz = dy * plain.activation(across(xs, w) + bias, act)[1]
+    changes = [lambda d: [v * across(d, w) for v in (dy, dz)], lambda d: [v * across(xs, d) for v in (dy, dz)], lambda d: [dy * d]]
+    _check_slopes(lambda at: (dy * plain.linear(*at, act, x.r.double())[2]).sum(), leaves, [dX, dW, dbias], changes)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("m,n", [(5, 264), (70, 264), (70, 261), (1100, 4200)])
 def test_residual_in_place(m, n):
@@ -228,6 +303,32 @@ def test_large_and_infinite_arguments(pair):
     z = x.X[1, :8].float() @ x.W[0][:, :8].float().t()
     assert bool(torch.all(Y[1].float() == z.clamp(min=0.0)))
     ws.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m", [3, 40])
+@pytest.mark.parametrize("act", ACTIVATIONS)
+def test_large_and_infinite_arguments_of_a_pairs_gradient(act, m):
+    """What the pair's gradient is formed with far from zero; and numbers that are none or infinite stay in their rows of dX and their columns' rows of dWg and dWu."""
+    values = [0.0, -0.0, 1e-4, -1e-4, 3.0, -3.0, 11.0, -11.0, 60.0, -60.0, 88.0, -88.0, 110.0, -110.0, 1e4, -1e4, 6e4, -6e4, 1e30, -1e30]
+    n, k = 64, 16
+    x = Problem(m, n, k, "bf16", act, pair=True)
+    x.z[0][0, : len(values)] = torch.tensor(values, device="cuda").bfloat16()
+    x.z[1][0, : len(values)] = 1.0
+    x.z[1][1, : len(values)] = torch.tensor(values, device="cuda").bfloat16()
+    x.Z = [plain.padded(z, "bf16") for z in x.z]
+    ws = _need(x, True)
+    finite = x.gradient()
+    x.check_gradient(*finite)
+    x.Z[0][2, 7], x.Z[1][2, 9] = float("nan"), float("inf")
+    got = x.gradient()
+    ws.close()
+    assert bool(torch.isnan(got[0][2]).all())
+    rows, columns = torch.arange(m, device="cuda") != 2, torch.arange(n, device="cuda")
+    assert torch.equal(got[0][rows], finite[0][rows])
+    # (without an activation dg does not look at g)
+    for after, before, kept in zip(got[1], finite[1], (columns != 9 if act == "none" else (columns != 7) & (columns != 9), columns != 7)):
+        assert torch.equal(after[kept], before[kept]) and not bool(torch.isfinite(after[~kept]).any())
 
 
 @pytest.mark.gpu
