@@ -177,6 +177,49 @@ def test_in_a_graph(workspace):
         assert torch.equal(norm, want_norm) and all(torch.equal(a, b) for a, b in zip(out, want))
 
 
+#: of one tensor and of many: five squares of a thread one after another and three additions of such sums, each half a unit in the last place, of which the root halves what they come to;
+#: its own rounding; pairs of numbers from there on (2^-40 is more than all of theirs)
+NEAR = (0.5 * (5 + 3) + 1) * 2.0 ** -24 + 2.0 ** -40
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("sizes", [[1], [2047], [2048], [2049], [8191], [8191 + 8192], [4_200_000 - 1], [8192 * 600 - 1], [8_400_001], [7] * 143, [130] * 144, [1001] * 145, [9, 0, 4000] * 96, [3] * 287, [5] * 288,
+                                   [2049, 1] * 144 + [77]])
+def test_tables_and_chunks(sizes, workspace):
+    """Tensors as many as a launch's table holds, one fewer and one more, of one table and of two; chunks that end before, at and behind a piece's end."""
+    x = _tensors(sizes, seed=sum(sizes))
+    for scale, max_norm in ((1.0, 0.5), (-0.375, 1e9)):
+        out, norm = _clip(x, scale, max_norm)
+        _check(x, scale, max_norm, out, norm)
+        want = _norm(x, scale)
+        assert abs(float(norm) - want) <= NEAR * want
+        again = [v.clone() for v in x]
+        _, norm_again = _clip(again, scale, max_norm, out=again)
+        assert torch.equal(norm, norm_again) and all(torch.equal(a, b) for a, b in zip(out, again))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("count", [9215, 9216, 9217, 9500])
+def test_thousands_of_tensors(count):
+    """64 launches, behind which the second reading goes forwards, and more; whole numbers, whose squares are added without a rounding."""
+    ws = device.Workspace(lib.ozaki_gradient_norm_workspace_bytes(count))
+    gen = torch.Generator(device="cuda").manual_seed(count)
+    whole = torch.randint(-3, 4, (count * 6,), device="cuda", generator=gen).float()
+    sizes = [1 + i % 5 for i in range(count)]
+    x = [whole[6 * i: 6 * i + n] for i, n in enumerate(sizes)]
+    held = torch.full_like(whole, float("nan"))
+    out = [held[6 * i: 6 * i + n] for i, n in enumerate(sizes)]
+    _, norm = _clip(x, 1.0, 1.0, out=out)
+    inside = torch.arange(6, device="cuda").repeat(count) < torch.tensor(sizes, device="cuda").repeat_interleave(6)
+    square = float((whole.double() ** 2)[inside].sum())
+    assert abs(float(norm) - square ** 0.5) <= 2.0 ** -24 * square ** 0.5
+    want = whole * (torch.ones((1,), device="cuda") / norm)
+    assert torch.equal(held[inside], want[inside]) and bool(torch.isnan(held[~inside]).all())
+    _clip(x, 1.0, 1.0, out=x)
+    assert torch.equal(whole[inside], want[inside])
+    ws.close()
+
+
 FAKE = 1 << 20
 
 
