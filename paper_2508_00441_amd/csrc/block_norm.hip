@@ -138,7 +138,7 @@ __device__ __forceinline__ RowNorm row_norm(X x, F d, float k, float eps, Meetin
     bool again = above || below;
     if constexpr (ALONG) {
         r.along = s[1] * r.rho / k;
-        again = again || !(fabsf(s[1]) < __builtin_inff());
+        again = again || !(fabsf(r.along) < __builtin_inff());
     }
     if (again) {                                     // (the same for all of a row's threads)
         // times 2^-72 no row's squares are too large, times 2^100 no row's that came to so little too small
@@ -149,11 +149,12 @@ __device__ __forceinline__ RowNorm row_norm(X x, F d, float k, float eps, Meetin
         meeting.sums(q);
         r.rho = f * __builtin_amdgcn_rsqf(q[0] / k + eps * f * f);
         if constexpr (ALONG) {
+            // (divided before it is summed: the mean may be a number where the sum is none)
             q[0] = 0.0f;
 #pragma unroll
-            for (int p = 0; p < PIECES; ++p) q[0] = dot(d(p), x(p) * r.rho, q[0]);
+            for (int p = 0; p < PIECES; ++p) q[0] = dot(d(p), x(p) * r.rho / k, q[0]);
             meeting.sums(q);
-            r.along = q[0] / k;
+            r.along = q[0];
         }
     }
     return r;

@@ -215,6 +215,24 @@ def test_zeros_large_and_small_numbers(types, workspace):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("types", [("bf16", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("k", [100, 2000, 16384])
+def test_means_whose_sums_leave_the_range(k, types, workspace):
+    """Gradients of 2^121 and 3 * 2^121: their mean along the row is 2^122, the sum of thousands of them is beyond 2^128."""
+    x = Problem(3, k, types, post=False, seed=4)
+    d = 2.0 ** 121 * (2 + (-1.0) ** torch.arange(k, device="cuda"))
+    x.r[:], x.dh[:], x.w_pre[:] = 1.0, d.to(x.dh.dtype), 1.0
+    x.R, x.dH = plain.padded(x.r, types[1]), plain.padded(x.dh, types[0])
+    out = x.gradient(True, False, ("dr", "dw_pre"))
+    x.check_gradient(out, True, False)
+    # the same through the norm behind the block
+    x = Problem(3, k, types, seed=4, scale=1.0)
+    x.x[:], x.dr_out[:], x.w_post[:] = 1.0, d.to(x.dr_out.dtype), 1.0
+    x.X, x.dR_out = plain.padded(x.x, types[0]), plain.padded(x.dr_out, types[1])
+    x.check_gradient(x.gradient(False, True, ("dx", "dr")), False, True)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("k", [520, 9000])
 def test_gradient_without_a_norm_does_not_look_at_x(k, workspace):
     """Without w_post the gradient of X is scale * gate * dR, whatever X holds."""
