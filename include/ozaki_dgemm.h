@@ -490,7 +490,7 @@ size_t ozaki_block_norm_workspace_bytes(int64_t rows, int64_t k, int64_t group);
  *                              them together at most 2^43), their type.  They are read before the call returns.  At most 2^27 tensors.
  *   scale                      what the elements are to be multiplied by (one over what the loss was multiplied by)
  *   norm                       DEVICE, one number in 32 bits; infinite or NaN where an element is
- * Squares of at most 32 elements are summed in 32 bits, those sums in twice as many; elements whose squares leave the range are no exception.  The order depends
+ * Squares of at most 33 elements are summed in 32 bits, those sums in twice as many; elements whose squares leave the range are no exception.  The order depends
  * on sizes, types and alignment only.  Needs the context's workspace,
  * ozaki_gradient_norm_workspace_bytes(count). */
 int ozaki_gradient_norm(int count, const void* const* tensors, const int64_t* sizes, const int* types, float scale, float* norm);

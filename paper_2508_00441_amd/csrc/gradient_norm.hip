@@ -16,7 +16,9 @@ namespace {
 // 32768 129 and 183, of 4096 148 and 184; 2048 workgroups add 2 us to the join.
 constexpr uint32_t MOST_CHUNK = 8192, LEAST_CHUNK = 2048;
 constexpr unsigned MOST_BLOCKS = 1024;
-constexpr int TABLE = 144;               // tensors in a launch's arguments, which hold 4 KiB
+// Tensors in a launch's arguments: what 4 KiB hold, but for one.  One more is two more launches: 144 tensors of 2.6 million BF16 elements 13 us, 153 of 2.8 million 24; 144 of 42 million 55, 153 of 45
+// million 67.
+constexpr int TABLE = 144;
 constexpr int MOST_REVERSED = 64;        // launches that the second reading takes from the last one on
 constexpr int THREADS = 256, MOST_JOINED = 1024;     // partial sums that every workgroup of the second reading adds up itself: 3 us, a launch of its own 5
 
@@ -108,7 +110,8 @@ __device__ __forceinline__ Squares block_sum(Squares v) {
     return all;
 }
 
-// A thread's squares of the n elements of a chunk, each times `factor` first: eight sums, of MOST_CHUNK / THREADS / 8 = 4 elements each.
+// A thread's squares of the n elements of a chunk, each times `factor` first: eight sums, of MOST_CHUNK / THREADS / 8 = 4 elements each at most; a chunk that
+// ends inside a piece has up to seven more, one for each of the first threads.
 template <typename T> __device__ __forceinline__ float chunk_squares(const T* x, int n, float factor) {
     float sum[8] = {};
     const auto add = [&](int q, T v) { sum[q] = __builtin_fmaf((float)v * factor, (float)v * factor, sum[q]); };

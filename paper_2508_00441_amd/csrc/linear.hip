@@ -5,7 +5,7 @@
 // FP32, with one rounding of each result.  Of a pair, half of a tile's vectors of weights are Wg's and half are Wu's, so that a lane holds both
 // factors of its elements and neither reaches memory unless it is asked for.
 // Few vectors of X are bound by the read of the weights (below), many by the matrix unit and power (pair of 4096 x 8192 x 4096, both factors kept: 394 - 416 us, 1.32 - 1.40 PFLOP/s;
-// GELU's 134 million elements of 8192 x 16384 x 2048 take 100 of 490 us, which no product covers), in between by a step's latency.
+// 8192 x 16384 x 2048 426 - 440 us, with bias and GELU, which no product covers, 483), in between by a step's latency.
 #include "block_operators.hpp"
 #include "layout.hpp"
 #include "tile_epilogue.hpp"
@@ -131,7 +131,7 @@ template <int TYPE, bool PAIR>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) linear_middle_kernel(const LinearWork w) {
     linear_body<Tile<kind_of(TYPE), 2, 2, 4, 4, 2, false, false, PAIR>, TYPE>(w);
 }
-// Smaller tiles in eight waves, two to a SIMD: with one, a step's wait, LDS reads and products follow each other (100 x 5001 x 2048: 14.3 us against 15.8 in four waves)
+// Smaller tiles in eight waves, two to a SIMD: with one, a step's wait, LDS reads and products follow each other (100 x 5001 x 2048: 13.1 us against 14.2 in four waves)
 template <int TYPE, bool PAIR>
 __global__ void __launch_bounds__(512) linear_half_kernel(const LinearWork w) {
     linear_body<Tile<kind_of(TYPE), 2, 4, 4, 1, 3, false, false, PAIR>, TYPE>(w);
@@ -148,7 +148,8 @@ __global__ void __launch_bounds__(PAIR ? 256 : 512) linear_narrow_kernel(const L
 
 // Up to sixteen vectors of X: no tile in LDS.  A workgroup takes sixteen vectors of W (of each, of a pair), its waves take steps of 64 elements in turn, straight
 // from memory into registers; the waves' sums are added in LDS, in their order.  W is read once, past the caches, and bounds it.  A wave has AHEAD steps under way.
-// 1 x 4096 x 8192: 13.9 us, 4.8 TB/s, in sixteen waves 15.3;  a pair of 4096 x 8192: 24.7, 5.4 TB/s, in eight waves with four steps under way 29.1.
+// 1 x 4096 x 8192: 15.5 us, 4.3 TB/s.  Eight waves without a pair: 1 x 16384 x 2048 13.7, in sixteen 23.7;  4 x 4096 x 1024 6.3, 8.1;  16 x 11001 x 4096 26.6, 29.1;  longer vectors are
+// about even, 16 x 16384 x 16384 144, 152, but 1 x 4096 x 8192 13.5 in sixteen, 1 x 16384 x 16384 106, 100.  A pair of 8192 x 4096: 25.3, 5.3 TB/s, in eight waves with four steps under way 29.1.
 constexpr int FEW = 16;
 constexpr int few_waves(bool pair) { return pair ? 16 : 8; }
 
@@ -260,15 +261,17 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const LinearArgs a, co
 
 enum { VECTORS, NARROW, SMALL, HALF, MIDDLE, LARGE };
 struct Shape { int kind, tm, tn, splits; };
-// By how many tiles there are for 256 compute units; `columns` counts both factors of a pair.  Times in us, with bias and GELU in BF16:
-//     tiles of 64 tokens and 64 columns, up to 128 of them: 32 columns     200 x 2048 x 2048: 11.4, by 64 x 64 13.2;  128 x 4096 x 4096: 17.2, 20.2
-//     fewer than 256 of 64 x 128: 64 x 64                                  1000 x 1000 x 1000: 10.3, by 32 columns 12.0, by 64 x 128 12.4
-//     up to 768 of 64 x 128                                                1024 x 4096 x 4096: 45, by 64 x 64 55, by 128 x 128 50;  300 x 11000 x 4096: 42, 53, 55
-//     up to 512 of 128 x 128                                               2048 x 4096 x 2048: 42.5, by 64 x 128 49, by 256 x 256 60
-//     more: 256 x 256                                                      2048 x 8192 x 512: 33.5, by 128 x 128 38
-// The narrowest tiles where they are fewer than compute units: in shares of the inner dimension of sixteen steps at least (20 x 1000 x 8192: 13.2 in eight, 27.8 uncut;
-// but 48 x 1000 x 500, eight steps: 7.0, in two shares 8.6).  Few vectors: from 96 steps on, in shares of at least 32 (1 x 1000 x 16384: 12.4, uncut 21.5); from 256 steps on
-// in two also where there are enough workgroups (1 x 16384 x 16384: 98, uncut 105; a pair of those 193, 226).
+// By how many tiles there are for 256 compute units; `columns` counts both factors of a pair.  Times in us, with bias and GELU in BF16, W in the last-level cache (from memory the
+// order is the same: 300 x 11000 x 4096 56, 67, 65;  1024 x 4096 x 4096 54, 68, 64):
+//     tiles of 64 tokens and 64 columns, up to 128 of them: 32 columns     200 x 2048 x 2048: 11.2, by 64 x 64 12.9;  128 x 4096 x 4096: 17.2, 19.6
+//     fewer than 256 of 64 x 128: 64 x 64                                  1000 x 1000 x 1000: 9.7, by 32 columns 12.0, by 64 x 128 11.8
+//     up to 768 of 64 x 128                                                1024 x 4096 x 4096: 49, by 64 x 64 62, by 128 x 128 51;  300 x 11000 x 4096: 42, 53, 54
+//     up to 512 of 128 x 128                                               2048 x 4096 x 2048: 42.4, by 64 x 128 52.5, by 256 x 256 57
+//     more: 256 x 256                                                      2048 x 8192 x 512: 31, by 128 x 128 36
+// The narrowest tiles where they are fewer than compute units: in shares of the inner dimension of sixteen steps at least (20 x 1000 x 8192: 13.1 in eight, 26.8 uncut;
+// but 48 x 1000 x 500, eight steps: 7.0, in two shares 8.6).  64 x 64 tiles are not cut, however long the inner dimension is (128 x 4160 x 16384, 130 of them: 75, where W's read is 30).  Few
+// vectors: from 96 steps on, in shares of at least 32 (1 x 1000 x 16384: 12.5, uncut 20.4); from 256 steps on in two also where there are enough workgroups (1 x 5000 x 16384: 37.5, uncut 45; a pair
+// of 16384 x 16384: 192, 204; not so without a pair, 1 x 16384 x 16384: 106, uncut 100).
 Shape shape_of(int64_t m, int64_t n, int64_t k, bool pair) {
     const int64_t steps = div_up(k * 2, STEP_BYTES), columns = pair ? 2 * n : n;
     const auto shares = [](int64_t want, int64_t most) {
