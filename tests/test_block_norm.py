@@ -191,6 +191,19 @@ def test_in_place(rows, k, workspace):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("post,group", [(True, 0), (False, 3), (True, 1)])
+@pytest.mark.parametrize("rows,k", [(700, 40), (700, 264), (3, 4096), (900, 2056), (300, 16384)])
+def test_gradient_in_the_place_of_x(rows, k, post, group, workspace):
+    x = Problem(rows, k, ("bf16", "f32"), post=post, group=group or None)
+    out = x.gradient()
+    x.check_gradient(out)
+    X, sums = x.X, {name: torch.full_like(out[name], float("nan")) for name in ("dw_post", "dgate", "dw_pre") if name in out}
+    lib.ozaki_block_norm_grad(*x.common(), x.R, x.R.shape[1], lib.TYPE_F32, x.w_pre, x.dH, x.dH.shape[1], x.dR_out, x.dR_out.shape[1], X, X.shape[1], None, 0, sums.get("dw_post"),
+                              sums.get("dgate"), sums["dw_pre"])
+    assert torch.equal(X[:, :k], out["dx"]) and all(torch.equal(sums[name], out[name]) for name in sums)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("types", TYPES)
 def test_zeros_large_and_small_numbers(types, workspace):
     """Rows of zeros give zeros; rows whose squares leave 32 bits' range, above or below, are normed all the same (eps is nothing beside 2^-40 squared only where it is smaller)."""
